@@ -513,6 +513,70 @@ int resonator_epilogue_bwd(const void* y, const void* gate, const void* v, const
                            float* dlambda_c, float* dw, float* ds, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Rows of a [B][L] set of D consecutive elements each: row (b, t) starts at element
+ * b sb + t st of p (strides in elements, >= 0).  A contiguous [B][L][D] tensor has
+ * sb = L D, st = D; one of three columns of a fused projection [B][L][3 D] has st = 3 D.
+ */
+typedef struct {
+  const void* p;
+  int64_t sb, st;
+} res_rows_t;
+typedef struct {
+  void* p;
+  int64_t sb, st;
+} res_rows_out_t;
+
+/*
+ * Gated scan: a causal mixer whose damping depends on the data.  Per channel d
+ *   s = gamma[d] sigmoid(r_t),  a = exp(-s),  beta = sqrt(1 - a^2),
+ *   h_t = a h_{t-1} + beta sigmoid(i_t) x_t,  y_t = h_t,  h_{-1} = h0.
+ * gamma is the damping of a fully open gate (gamma >= 0 is a precondition; at 0
+ * the state is kept and nothing is added).  The state h is float32 whatever dt.
+ *   x, r, i  rows of dt (drive, and the logits of the damping's and the drive's gate)
+ *   y        [B][L][D] of dt, or NULL
+ *   gamma    [D]; h0 [B][D] or NULL (zero); h_out [B][D] or NULL (may be h0 itself)
+ *   lengths  [B] int32 or NULL: row b has its first lengths[b] steps (clamped to
+ *            0..L); behind them nothing is read, y is 0 and the state stays
+ *   carry    [B][ceil(L / RES_GATED_CARRY)][D] or NULL: receives the state before
+ *            every RES_GATED_CARRY-th step, which the backward starts from
+ *   ws       resonator_gated_scan_workspace_bytes(dt, B, L, D) bytes, 256-byte aligned
+ * The workspace must be zero-filled before its first use; every call leaves it
+ * ready for the next call, forward or backward, of any sizes whose need it covers.
+ * Calls that share one must not overlap in time.  B, D >= 1, L >= 0.
+ * Outputs must not overlap inputs or each other.
+ */
+#define RES_GATED_CARRY 128
+size_t resonator_gated_scan_workspace_bytes(res_dtype_t dt, int64_t B, int64_t L, int64_t D);
+int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype_t dt, void* y, int64_t B, int64_t L,
+                             int64_t D, const float* gamma, const float* h0, const int32_t* lengths, float* h_out,
+                             float* carry, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of resonator_gated_scan_fwd for the loss sum(dy y) + sum(dh_out h_out):
+ * with q = sigmoid(i) and g_t the gradient of h_t (g_t = dy_t + a_{t+1} g_{t+1}),
+ *   dx = g beta q,  di = g beta q (1 - q) x,  w = g (a^2 / beta q x - a h_{t-1}),
+ *   dr = w s (1 - sigmoid(r)),  dgamma = sum over b, t of w sigmoid(r),  dh0 = a_0 g_0
+ * (the derivative of beta is taken as 0 where beta is 0).
+ *   dy           rows of dt; dx, dr, di rows of dt, overwritten (0 behind a row's length);
+ *                they may be columns of one tensor
+ *   carry        from the forward of the same inputs; dh_out [B][D] or NULL (zero)
+ *   dgamma [D], dh0 [B][D] (or NULL)  float32, overwritten
+ * Sums run in a fixed order: calls on the same inputs are bitwise reproducible.
+ */
+int resonator_gated_scan_bwd(res_rows_t x, res_rows_t r, res_rows_t i, res_rows_t dy, res_dtype_t dt,
+                             res_rows_out_t dx, res_rows_out_t dr, res_rows_out_t di, int64_t B, int64_t L, int64_t D,
+                             const float* gamma, const float* carry, const int32_t* lengths, const float* dh_out,
+                             float* dgamma, float* dh0, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One step of the gated scan for B sequences: rows x, r, i [B] (their st is not
+ * used), state h [B][D] float32; y [B][D] of dt and h_out [B][D] (may be h itself)
+ * are written.
+ */
+int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype_t dt, void* y, int64_t B, int64_t D,
+                              const float* gamma, const float* h, float* h_out, void* stream);
+
+/*
  * Measurement hook.  Arms a pair of HIP events (hipEvent_t passed as void*) on the
  * calling thread: the next resonator_mix_fwd or resonator_mix_bwd call on this
  * thread records start_event immediately before and stop_event immediately after

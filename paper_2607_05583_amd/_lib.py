@@ -16,6 +16,7 @@ RES_F32, RES_BF16 = 0, 1
 RES_OK, RES_ERR_INVALID_ARG, RES_ERR_UNSUPPORTED, RES_ERR_MISALIGNED, RES_ERR_WORKSPACE, RES_ERR_HIP = range(6)
 RES_OP_FWD, RES_OP_BWD, RES_OP_STATE_INIT = 0, 1, 2
 RES_M_MAX = 16
+RES_GATED_CARRY = 128
 
 SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd",
            "resonator_mix_bwd", "resonator_state_init", "resonator_decode_step",
@@ -31,7 +32,15 @@ SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd"
            "resonator_grouped_linear_bwd_weight_sum_workspace_bytes",
            "resonator_grouped_linear_bwd_weight_split", "resonator_grouped_linear_bwd_weight_split_workspace_bytes",
            "resonator_mix_fwd_noalloc", "resonator_mix_fwd_noalloc_max_bytes", "resonator_fwd_workspace_init", "resonator_fwd_status",
-           "resonator_fwd_status_noalloc")
+           "resonator_fwd_status_noalloc",
+           "resonator_gated_scan_workspace_bytes", "resonator_gated_scan_fwd", "resonator_gated_scan_bwd",
+           "resonator_gated_scan_step")
+
+class Rows(ctypes.Structure):
+    """res_rows_t / res_rows_out_t: rows of consecutive elements at p + b sb + t st."""
+
+    _fields_ = [("p", ctypes.c_void_p), ("sb", ctypes.c_int64), ("st", ctypes.c_int64)]
+
 
 _lib = None
 
@@ -132,6 +141,15 @@ def _declare(lib):
     lib.resonator_decode_constants.argtypes = [i64, i64, fp, fp, fp, fp, fp, vp]
     lib.resonator_decode_step_tab.restype = i32
     lib.resonator_decode_step_tab.argtypes = [vp, i32, vp, i32, i64, i64, i64, fp, fp, vp]
+    lib.resonator_gated_scan_workspace_bytes.restype = sz
+    lib.resonator_gated_scan_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.resonator_gated_scan_fwd.restype = i32
+    lib.resonator_gated_scan_fwd.argtypes = [Rows, Rows, Rows, i32, vp, i64, i64, i64, fp, fp, vp, fp, fp, vp, sz, vp]
+    lib.resonator_gated_scan_bwd.restype = i32
+    lib.resonator_gated_scan_bwd.argtypes = [Rows, Rows, Rows, Rows, i32, Rows, Rows, Rows, i64, i64, i64, fp, fp, vp,
+                                             fp, fp, fp, vp, sz, vp]
+    lib.resonator_gated_scan_step.restype = i32
+    lib.resonator_gated_scan_step.argtypes = [Rows, Rows, Rows, i32, vp, i64, i64, fp, fp, fp, vp]
 
 
 def lib():

@@ -12,6 +12,7 @@
 #include "../../include/resonator.h"
 #include "common.h"
 #include "kernels.h"
+#include "layer.h"
 
 using namespace res;
 
@@ -36,6 +37,20 @@ int fail(int code, const char* fmt, ...) {
   g_err = buf;
   return code;
 }
+
+}  // namespace
+
+int res::api_error(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  g_err = buf;
+  return code;
+}
+
+namespace {
 
 int hip_fail(hipError_t e, const char* what) {
   return fail(RES_ERR_HIP, "%s: %s", what, hipGetErrorString(e));

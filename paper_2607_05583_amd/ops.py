@@ -1005,3 +1005,171 @@ def resonator_epilogue_bwd(y, gate, v, dz, Ct, lambda_c, w, s, H, ws=None):
         H, D // H, K, _ptr(Ct), float(lambda_c), _ptr(w) if K else None, _ptr(s) if K else None, _ptr(dCt),
         _ptr(dlam), _ptr(dw), _ptr(ds), _ptr(ws), ws.numel(), _stream(y.device)))
     return dy, dgate, dv, dCt, dlam, dw, ds
+
+
+# ---------------------------------------------------------------------------
+# Gated recurrent layer: gated scan
+# ---------------------------------------------------------------------------
+def _rows(t, name, dtype, shape):
+    """A GPU tensor of ``shape`` whose last dimension is consecutive, as rows of the library."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {t.device})")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {list(shape)} (got {t.dtype} {list(t.shape)})")
+    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be consecutive in memory")
+    return _lib.Rows(t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0)
+
+
+def _f32(t, name, shape):
+    if t is None:
+        return None
+    _dev(t, name)
+    if t.dtype != torch.float32 or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be float32 {list(shape)}")
+    return t
+
+
+def _gated_inputs(x, r, i, gamma, dims):
+    if not isinstance(x, torch.Tensor) or x.dim() != dims:
+        raise ValueError(f"x must be a [{'B, L, D' if dims == 3 else 'B, D'}] tensor")
+    _code(x)
+    rows = [_rows(t, name, x.dtype, x.shape) for name, t in (("x", x), ("r", r), ("i", i))]
+    if gamma is None:
+        raise TypeError("gamma must be a torch.Tensor")
+    _f32(gamma, "gamma", x.shape[-1:])
+    return rows
+
+
+def _gated_lengths(lengths, B):
+    if lengths is None:
+        return None
+    _dev(lengths, "lengths")
+    if lengths.dtype != torch.int32 or tuple(lengths.shape) != (B,):
+        raise ValueError("lengths must be int32 [B]")
+    return lengths
+
+
+def gated_scan_workspace(act_dtype, B, L, D, device):
+    """A zero-filled workspace of the gated scan for sizes up to (B, L, D), reusable across its calls on one stream."""
+    n = _lib.lib().resonator_gated_scan_workspace_bytes(_DT[act_dtype], B, L, D)
+    return torch.zeros(max(int(n), 256), dtype=torch.uint8, device=device)
+
+
+def _gated_ws(ws, act_dtype, B, L, D, device):
+    if ws is None:
+        return gated_scan_workspace(act_dtype, B, L, D, device)
+    _dev(ws, "ws")
+    return ws
+
+
+def resonator_gated_scan_fwd(x, r, i, gamma, h0=None, lengths=None, return_state=False, save=False, out=None, ws=None,
+                             h_out=None):
+    """Gated scan: s = gamma sigmoid(r_t), a = exp(-s), h_t = a h_{t-1} + sqrt(1 - a^2) sigmoid(i_t) x_t, y_t = h_t.
+
+    x, r, i: [B, L, D] of one type, the last dimension consecutive (columns of a
+    fused projection are taken as they are); gamma [D], h0 [B, D] float32;
+    ``lengths`` [B] int32: row b has its first lengths[b] steps (y is 0 behind
+    them and nothing there is read).  Returns y; with ``return_state`` also the
+    last state [B, D] float32 (written to ``h_out`` where given, which may be h0
+    itself); with ``save`` also the states that resonator_gated_scan_bwd starts
+    from.  ``ws``: a gated_scan_workspace, else one is made for the call."""
+    rows = _gated_inputs(x, r, i, gamma, 3)
+    B, L, D = x.shape
+    _f32(h0, "h0", (B, D))
+    _gated_lengths(lengths, B)
+    y = torch.empty((B, L, D), dtype=x.dtype, device=x.device) if out is None else _given(out, "out", B * L * D, x.dtype)
+    if h_out is not None:
+        _f32(h_out, "h_out", (B, D))
+    elif return_state:
+        h_out = torch.empty((B, D), dtype=torch.float32, device=x.device)
+    carry = _gated_carry(B, L, D, x.device) if save else None
+    ws = _gated_ws(ws, x.dtype, B, L, D, x.device)
+    check(_lib.lib().resonator_gated_scan_fwd(
+        *rows, _code(x), _ptr(y), B, L, D, _ptr(gamma), _ptr(h0), _ptr(lengths), _ptr(h_out), _ptr(carry), _ptr(ws),
+        ws.numel() * ws.element_size(), _stream(x.device)))
+    r_ = (y,) + ((h_out,) if return_state else ()) + ((carry,) if save else ())
+    return r_ if len(r_) > 1 else y
+
+
+def _gated_carry(B, L, D, device):
+    return torch.empty((B, -(-L // _lib.RES_GATED_CARRY), D), dtype=torch.float32, device=device)
+
+
+def resonator_gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh_out=None, carry=None, want_dh0=False,
+                             out=None, ws=None):
+    """Gradients of sum(dy y) + sum(dh_out h_out): dict with dx, dr, di, dgamma (, dh0).
+
+    ``carry``: the states of a forward with ``save`` on the same inputs, else
+    they are computed again from ``h0``.  ``out`` = (dx, dr, di) receives the
+    gradients (they may be columns of one tensor)."""
+    rows = _gated_inputs(x, r, i, gamma, 3)
+    B, L, D = x.shape
+    rows.append(_rows(dy, "dy", x.dtype, x.shape))
+    _f32(h0, "h0", (B, D))
+    _f32(dh_out, "dh_out", (B, D))
+    _gated_lengths(lengths, B)
+    if out is None:
+        out = [torch.empty((B, L, D), dtype=x.dtype, device=x.device) for _ in range(3)]
+    dx, dr, di = out
+    orows = [_rows(t, name, x.dtype, x.shape) for name, t in (("dx", dx), ("dr", dr), ("di", di))]
+    ws = _gated_ws(ws, x.dtype, B, L, D, x.device)
+    wsb = ws.numel() * ws.element_size()
+    if carry is None:
+        carry = _gated_carry(B, L, D, x.device)
+        if L > 0:
+            check(_lib.lib().resonator_gated_scan_fwd(*rows[:3], _code(x), None, B, L, D, _ptr(gamma), _ptr(h0),
+                                                      _ptr(lengths), None, _ptr(carry), _ptr(ws), wsb,
+                                                      _stream(x.device)))
+    else:
+        _f32(carry, "carry", (B, -(-L // _lib.RES_GATED_CARRY), D))
+    dgamma = torch.empty((D,), dtype=torch.float32, device=x.device)
+    dh0 = torch.empty((B, D), dtype=torch.float32, device=x.device) if want_dh0 else None
+    check(_lib.lib().resonator_gated_scan_bwd(
+        *rows, _code(x), *orows, B, L, D, _ptr(gamma), _ptr(carry), _ptr(lengths), _ptr(dh_out), _ptr(dgamma),
+        _ptr(dh0), _ptr(ws), wsb, _stream(x.device)))
+    g = {"dx": dx, "dr": dr, "di": di, "dgamma": dgamma}
+    if want_dh0:
+        g["dh0"] = dh0
+    return g
+
+
+def resonator_gated_scan_step(x_t, r_t, i_t, gamma, h, h_out=None, out=None):
+    """One step of the gated scan: x_t, r_t, i_t [B, D], state h [B, D] float32, advanced in place unless ``h_out``
+    receives the new one; returns y_t [B, D]."""
+    rows = _gated_inputs(x_t, r_t, i_t, gamma, 2)
+    B, D = x_t.shape
+    if h is None:
+        raise TypeError("h must be a torch.Tensor")
+    _f32(h, "h", (B, D))
+    h_out = h if h_out is None else _f32(h_out, "h_out", (B, D))
+    y = torch.empty((B, D), dtype=x_t.dtype, device=x_t.device) if out is None else _given(out, "out", B * D, x_t.dtype)
+    check(_lib.lib().resonator_gated_scan_step(*rows, _code(x_t), _ptr(y), B, D, _ptr(gamma), _ptr(h), _ptr(h_out),
+                                               _stream(x_t.device)))
+    return y
+
+
+class GatedScanFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_gated_scan_fwd (y and the last state) and resonator_gated_scan_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, r, i, gamma, h0=None, lengths=None):
+        y, h, carry = resonator_gated_scan_fwd(x, r, i, gamma, h0=h0, lengths=lengths, return_state=True, save=True)
+        ctx.save_for_backward(x, r, i, gamma, carry, lengths)
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    def backward(ctx, dy, dh):
+        x, r, i, gamma, carry, lengths = ctx.saved_tensors
+        dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None else dy.contiguous()
+        g = resonator_gated_scan_bwd(x, r, i, gamma, dy, lengths=lengths, dh_out=None if dh is None else dh.contiguous(),
+                                     carry=carry, want_dh0=ctx.needs_input_grad[4])
+        return g["dx"], g["dr"], g["di"], g["dgamma"], g.get("dh0"), None
+
+
+def resonator_gated_scan(x, r, i, gamma, h0=None, lengths=None):
+    """Differentiable gated scan: (y, last state); x, r, i, gamma and h0 receive gradients."""
+    return GatedScanFunction.apply(x, r, i, gamma, h0, lengths)
