@@ -577,6 +577,86 @@ int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtyp
                               const float* gamma, const float* h, float* h_out, void* stream);
 
 /*
+ * Linear product with bias, activation and residual:
+ *   pre = x W + bias,  y = act(pre) + residual
+ *   x         R rows of K consecutive elements of dt, ldx >= K elements apart
+ *   W         [K][N] of dt; bias [N] float32 or NULL
+ *   residual  [R][N] of dt or NULL; y [R][N] of dt (may be the residual itself)
+ *   pre       [R][N] float32 or NULL: receives pre, which the backward needs unless act is none
+ *             (float32, since db sums what its rounding would be: with a bf16 pre the bias
+ *             gradient is off by 2.6e-3 of its size)
+ *   act       RES_ACT_*: none; relu; silu = v sigmoid(v);
+ *             gelu_tanh = v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3)))
+ * Sums, bias, activation and residual are float32, rounded once to dt.  Sums run in
+ * an order that depends on the sizes alone.  K, N >= 1, R >= 0.
+ *   ws        resonator_linear_workspace_bytes(0, ...) bytes (may be none), 256-byte
+ *             aligned; contents need not be initialised
+ * Outputs must not overlap inputs or each other otherwise.
+ */
+enum { RES_ACT_NONE = 0, RES_ACT_RELU = 1, RES_ACT_SILU = 2, RES_ACT_GELU_TANH = 3 };
+size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N);
+int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, int act,
+                         const void* residual, void* y, float* pre, int64_t R, int64_t K, int64_t N, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/*
+ * Backward of resonator_linear_fwd for the loss sum(dy y): with dpre = dy act'(pre)
+ *   dx = dpre W^T + residual   [R][K] of dt, or NULL (residual [R][K] of dt or NULL, or dx itself:
+ *                              the gradient that reaches x on another path)
+ *   dW = x^T dpre              [K][N] of dt, or NULL
+ *   db = sum over rows of dpre [N] float32, or NULL
+ * (the forward's own residual has the gradient dy).  pre is the forward's (not read
+ * when act is none); x may be NULL without dW, W without dx.  For bf16 the products
+ * take dpre rounded to bf16; db sums it unrounded.  With R = 0, dW and db are zero.
+ * ws: resonator_linear_workspace_bytes(1, ...).
+ */
+int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const void* dy, const float* pre,
+                         int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K, int64_t N,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * AdamW step over many tensors (one launch for up to 64 of them):
+ *   g' = grad_scale g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ *   tensors     HOST array: parameters p of p_dt, gradients g of g_dt, where the new parameters go
+ *               (p_out, may be p itself), elements n (0 is taken), and the element of the state buffers
+ *               at which the tensor's own begin (a multiple of RES_ADAMW_BLOCK)
+ *   state       read, state_out written (HOST structs of device pointers; may be the same buffers)
+ *     bits 32   m, v float32
+ *     bits 8    m int8, v uint8 codes in blocks of RES_ADAMW_BLOCK elements, with one scale S each
+ *               (scale_m, scale_v, at the block's index): m = sgn(c) (c / 127)^2 S,
+ *               v = (c / 255)^4 S, S the block's largest |value| (below 1e-30 all codes are 0);
+ *               a v that is not 0 gets a code of at least 1.  The step uses the unrounded m and v.
+ *     master    float32 parameters laid out as the states (bf16 parameters only; NULL for none):
+ *               the step reads and writes them, and p_out receives their rounding
+ *   grad_scale  [1] float32 on the device, or NULL for 1 (a clipping factor, a loss scale)
+ * lr, eps, weight_decay >= 0, betas in [0, 1), step >= 1 counts from one; all are host values.
+ * m, v and master must be 16-byte aligned, and a buffer written must not overlap one
+ * read except as the same buffer.  A gradient that is not finite makes its block's state
+ * (8 bits) or its element's (32) not finite.
+ */
+#define RES_ADAMW_BLOCK 256
+typedef struct {
+  const void* p;
+  const void* g;
+  void* p_out;
+  int64_t n;
+  int64_t state;
+} res_adamw_tensor_t;
+typedef struct {
+  int bits;
+  void *m, *v;
+  float *scale_m, *scale_v, *master;
+} res_adamw_state_t;
+int resonator_adamw_step(const res_adamw_tensor_t* tensors, int64_t count, res_dtype_t p_dt, res_dtype_t g_dt,
+                         const res_adamw_state_t* state, const res_adamw_state_t* state_out, double lr, double beta1,
+                         double beta2, double eps, double weight_decay, int64_t step, const float* grad_scale,
+                         void* stream);
+
+/* The values m, v [n] float32 that a state of 8 bits stands for (n a multiple of RES_ADAMW_BLOCK). */
+int resonator_adamw_values(const res_adamw_state_t* state, int64_t n, float* m, float* v, void* stream);
+
+/*
  * Measurement hook.  Arms a pair of HIP events (hipEvent_t passed as void*) on the
  * calling thread: the next resonator_mix_fwd or resonator_mix_bwd call on this
  * thread records start_event immediately before and stop_event immediately after

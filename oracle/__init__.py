@@ -7,4 +7,5 @@ from .resonator_oracle import *  # noqa: F401,F403
 from .epilogue_oracle import coupling_matrix, epilogue_fwd, epilogue_bwd  # noqa: F401
 from .params_oracle import params_map, params_map_bwd, params_init, half_lives, energy_decay, spectrum  # noqa: F401
 from .block_oracle import grouped_linear, grouped_linear_bwd, block_fwd, block_bwd  # noqa: F401
-from .layer_oracle import gated_scan_bwd, gated_scan_fwd  # noqa: F401
+from .layer_oracle import (act_slope, act_value, adamw, adamw_decode, adamw_encode, gated_scan_bwd,  # noqa: F401
+                           gated_scan_fwd, linear_bwd, linear_fwd)

@@ -54,3 +54,72 @@ def gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh=None):
             dg += w * sr
             g[b] = a * gt
     return dict(dx=dx, dr=dr, di=di, dgamma=dg, dh0=g)
+
+
+# ---------------------------------------------------------------------------
+# linear product: y = act(x W + b) + residual
+# ---------------------------------------------------------------------------
+def act_value(v, act):
+    if act == "relu":
+        return np.maximum(v, 0.0)
+    if act == "silu":
+        return v * _sigmoid(v)
+    if act == "gelu_tanh":
+        return 0.5 * v * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (v + 0.044715 * v ** 3)))
+    return v
+
+
+def act_slope(v, act):
+    if act == "relu":
+        return (v > 0).astype(np.float64)
+    if act == "silu":
+        q = _sigmoid(v)
+        return q * (1.0 + v * (1.0 - q))
+    if act == "gelu_tanh":
+        c = np.sqrt(2.0 / np.pi)
+        th = np.tanh(c * (v + 0.044715 * v ** 3))
+        return 0.5 * (1.0 + th) + 0.5 * v * (1.0 - th * th) * c * (1.0 + 3 * 0.044715 * v * v)
+    return np.ones_like(v)
+
+
+def linear_fwd(x, W, b=None, act="none", residual=None):
+    """(y, pre)"""
+    pre = x @ W + (0.0 if b is None else b)
+    return act_value(pre, act) + (0.0 if residual is None else residual), pre
+
+
+def linear_bwd(x, W, dy, b=None, act="none", residual=None, pre=None):
+    """dict dx (plus residual), dW, db; pre is computed unless given"""
+    pre = linear_fwd(x, W, b)[1] if pre is None else pre
+    d = dy * act_slope(pre, act)
+    return dict(dx=d @ W.T + (0.0 if residual is None else residual), dW=x.T @ d, db=d.sum(0))
+
+
+# ---------------------------------------------------------------------------
+# AdamW and its states in 8 bits (blocks of 256 elements with one scale)
+# ---------------------------------------------------------------------------
+def adamw(p, g, m, v, step, lr, betas, eps, weight_decay, scale=1.0):
+    """(p, m, v) after one step"""
+    g = g * scale
+    m = betas[0] * m + (1 - betas[0]) * g
+    v = betas[1] * v + (1 - betas[1]) * g * g
+    up = m / (1 - betas[0] ** step) / (np.sqrt(v / (1 - betas[1] ** step)) + eps)
+    return p - lr * weight_decay * p - lr * up, m, v
+
+
+def adamw_encode(v, positive):
+    """(place of every value on its block's grid before rounding, scales): codes are the places rounded"""
+    top, root = (255, 4) if positive else (127, 2)
+    b = v.reshape(-1, 256)
+    scale = np.abs(b).max(1)
+    share = np.divide(np.abs(b), scale[:, None], out=np.zeros_like(b), where=scale[:, None] >= 1e-30)
+    place = top * share ** (1.0 / root)
+    if positive:
+        place = np.where((place > 0) & (place < 1), 1.0, place)
+    return (place * np.sign(b)).reshape(-1), scale
+
+
+def adamw_decode(code, scale, positive):
+    top, root = (255, 4) if positive else (127, 2)
+    c = code.astype(np.float64).reshape(-1, 256) / top
+    return (np.sign(c) * np.abs(c) ** root * scale[:, None]).reshape(-1)

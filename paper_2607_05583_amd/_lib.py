@@ -17,6 +17,7 @@ RES_OK, RES_ERR_INVALID_ARG, RES_ERR_UNSUPPORTED, RES_ERR_MISALIGNED, RES_ERR_WO
 RES_OP_FWD, RES_OP_BWD, RES_OP_STATE_INIT = 0, 1, 2
 RES_M_MAX = 16
 RES_GATED_CARRY = 128
+RES_ADAMW_BLOCK = 256
 
 SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd",
            "resonator_mix_bwd", "resonator_state_init", "resonator_decode_step",
@@ -34,12 +35,28 @@ SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd"
            "resonator_mix_fwd_noalloc", "resonator_mix_fwd_noalloc_max_bytes", "resonator_fwd_workspace_init", "resonator_fwd_status",
            "resonator_fwd_status_noalloc",
            "resonator_gated_scan_workspace_bytes", "resonator_gated_scan_fwd", "resonator_gated_scan_bwd",
-           "resonator_gated_scan_step")
+           "resonator_gated_scan_step",
+           "resonator_linear_workspace_bytes", "resonator_linear_fwd", "resonator_linear_bwd",
+           "resonator_adamw_step", "resonator_adamw_values")
 
 class Rows(ctypes.Structure):
     """res_rows_t / res_rows_out_t: rows of consecutive elements at p + b sb + t st."""
 
     _fields_ = [("p", ctypes.c_void_p), ("sb", ctypes.c_int64), ("st", ctypes.c_int64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    """res_adamw_tensor_t"""
+
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("p_out", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("state", ctypes.c_int64)]
+
+
+class AdamWState(ctypes.Structure):
+    """res_adamw_state_t"""
+
+    _fields_ = [("bits", ctypes.c_int), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scale_m", ctypes.c_void_p),
+                ("scale_v", ctypes.c_void_p), ("master", ctypes.c_void_p)]
 
 
 _lib = None
@@ -150,6 +167,18 @@ def _declare(lib):
                                              fp, fp, fp, vp, sz, vp]
     lib.resonator_gated_scan_step.restype = i32
     lib.resonator_gated_scan_step.argtypes = [Rows, Rows, Rows, i32, vp, i64, i64, fp, fp, fp, vp]
+    lib.resonator_linear_workspace_bytes.restype = sz
+    lib.resonator_linear_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i64]
+    lib.resonator_linear_fwd.restype = i32
+    lib.resonator_linear_fwd.argtypes = [vp, i64, vp, i32, fp, i32, vp, vp, vp, i64, i64, i64, vp, sz, vp]
+    lib.resonator_linear_bwd.restype = i32
+    lib.resonator_linear_bwd.argtypes = [vp, i64, vp, i32, vp, vp, i32, vp, vp, vp, fp, i64, i64, i64, vp, sz, vp]
+    f64 = ctypes.c_double
+    lib.resonator_adamw_step.restype = i32
+    lib.resonator_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, i32, i32, ctypes.POINTER(AdamWState),
+                                         ctypes.POINTER(AdamWState), f64, f64, f64, f64, f64, i64, fp, vp]
+    lib.resonator_adamw_values.restype = i32
+    lib.resonator_adamw_values.argtypes = [ctypes.POINTER(AdamWState), i64, fp, fp, vp]
 
 
 def lib():

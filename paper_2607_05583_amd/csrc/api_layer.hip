@@ -1,6 +1,7 @@
 // C ABI of the gated recurrent layer's operators: argument checks and dispatch.
 // Declared in include/resonator.h.
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "../../include/resonator.h"
@@ -223,6 +224,273 @@ int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtyp
   return launched(dt == RES_BF16 ? launch_gated_step<bf16_t>(rx, rr, ri, y, B, D, gamma, h, h_out, (hipStream_t)stream)
                                  : launch_gated_step<float>(rx, rr, ri, y, B, D, gamma, h, h_out, (hipStream_t)stream),
                   "gated scan step launch");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Linear product
+// ---------------------------------------------------------------------------
+namespace {
+
+int check_linear(int64_t R, int64_t K, int64_t N, res_dtype_t dt, int act) {
+  if (!known(dt)) return api_error(RES_ERR_INVALID_ARG, "unknown dtype code");
+  if (act < RES_ACT_NONE || act > RES_ACT_GELU_TANH) return api_error(RES_ERR_INVALID_ARG, "unknown activation code %d", act);
+  if (R < 0 || K < 1 || N < 1)
+    return api_error(RES_ERR_INVALID_ARG, "K and N must be >= 1 and R >= 0 (got R=%lld K=%lld N=%lld)", (long long)R,
+                     (long long)K, (long long)N);
+  // (work-groups of a launch, by tiles of 64 x 64 or 256 elements: below 2^31)
+  if (R > (1LL << 31) || K > (1 << 20) || N > (1 << 20) || R * std::max(K, N) > (1LL << 38))
+    return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (R=%lld K=%lld N=%lld)", (long long)R,
+                     (long long)K, (long long)N);
+  return RES_OK;
+}
+
+size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
+size_t split_bytes(int64_t M, int64_t N, int64_t K) {
+  const int64_t s = linear_splits(M, N, K);
+  return s > 1 ? (size_t)(s * M * N) * 4 : 0;
+}
+size_t linear_fwd_bytes(int64_t R, int64_t K, int64_t N) { return up256(split_bytes(R, N, K)); }
+struct LinearBwdLayout {
+  size_t dpre, part, split, total;
+};
+LinearBwdLayout linear_bwd_layout(res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N) {
+  LinearBwdLayout w{};
+  size_t off = 0;
+  w.dpre = off;
+  if (act != RES_ACT_NONE) off += up256((size_t)(R * N) * elt(dt));
+  w.part = off;
+  off += up256((size_t)(linear_row_blocks(R) * N) * 4);
+  w.split = off;
+  off += up256(std::max(split_bytes(R, K, N), split_bytes(K, N, R)));
+  w.total = off;
+  return w;
+}
+int check_ws(const void* ws, size_t have, size_t need) {
+  if (need == 0) return RES_OK;
+  if (ws == nullptr || have < need)
+    return api_error(RES_ERR_WORKSPACE, "workspace null or too small (%zu bytes, %zu needed)", have, need);
+  return aligned(ws, 256) ? RES_OK : api_error(RES_ERR_MISALIGNED, "the workspace must be 256-byte aligned");
+}
+int check_mat(const char* name, const void* p, size_t es, bool needed) {
+  if (p == nullptr) return needed ? api_error(RES_ERR_INVALID_ARG, "%s must be non-null", name) : RES_OK;
+  return aligned(p, es) ? RES_OK : api_error(RES_ERR_MISALIGNED, "%s must be aligned to its element", name);
+}
+hipError_t gemm(res_dtype_t dt, GemmArgs& g, float* part, hipStream_t st) {
+  g.splits = (int)linear_splits(g.M, g.N, g.K);
+  g.part = part;
+  return dt == RES_BF16 ? launch_gemm<bf16_t>(g, st) : launch_gemm<float>(g, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N) {
+  if (check_linear(R, K, N, dt, act)) return 0;
+  return backward ? linear_bwd_layout(dt, act, R, K, N).total : linear_fwd_bytes(R, K, N);
+}
+
+int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, int act,
+                         const void* residual, void* y, float* pre, int64_t R, int64_t K, int64_t N, void* ws,
+                         size_t ws_bytes, void* stream) {
+  int rc = check_linear(R, K, N, dt, act);
+  if (rc) return rc;
+  const size_t es = elt(dt);
+  if ((rc = check_mat("W", W, es, true)) || (rc = check_f32("bias", bias, false))) return rc;
+  if (R == 0) return RES_OK;
+  if (ldx < K || ldx > (1LL << 40)) return api_error(RES_ERR_INVALID_ARG, "ldx must be in [K, 2^40]");
+  if ((rc = check_mat("x", x, es, true)) || (rc = check_mat("y", y, es, true)) || (rc = check_f32("pre", pre, false)) ||
+      (rc = check_mat("residual", residual, es, false)))
+    return rc;
+  const size_t need = linear_fwd_bytes(R, K, N);
+  if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+  const Span in[] = {span(x, 0, ldx, 1, R, K, es), flat(W, es * K * N), flat(bias, 4 * N), flat(residual, es * R * N)};
+  const Span out[] = {flat(y, es * R * N), flat(pre, 4 * R * N), flat(need ? ws : nullptr, need)};
+  for (int o = 0; o < 3; ++o) {
+    for (int k = 0; k < 4; ++k)
+      if (touch(out[o], in[k]) && !(o == 0 && k == 3 && y == residual))
+        return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap inputs (y may be the residual itself)");
+    for (int k = 0; k < o; ++k)
+      if (touch(out[o], out[k])) return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap each other");
+  }
+  GemmArgs g{};
+  g.A = x;
+  g.B = W;
+  g.sam = ldx;
+  g.sak = 1;
+  g.sbk = N;
+  g.sbn = 1;
+  g.M = R;
+  g.N = N;
+  g.K = K;
+  g.bias = bias;
+  g.res = residual;
+  g.pre = pre;
+  g.out = y;
+  g.act = act;
+  return launched(gemm(dt, g, static_cast<float*>(ws), (hipStream_t)stream), "linear launch");
+}
+
+int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const void* dy, const float* pre,
+                         int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K, int64_t N,
+                         void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_linear(R, K, N, dt, act);
+  if (rc) return rc;
+  const size_t es = elt(dt);
+  if (dx == nullptr && dW == nullptr && db == nullptr)
+    return api_error(RES_ERR_INVALID_ARG, "one of dx, dW and db must be non-null");
+  if (R > 0 && ((rc = check_mat("dy", dy, es, true)) || (rc = check_f32("pre", pre, act != RES_ACT_NONE)) ||
+                (rc = check_mat("x", x, es, dW != nullptr)) || (rc = check_mat("W", W, es, dx != nullptr))))
+    return rc;
+  if ((rc = check_mat("residual", residual, es, false)) || (rc = check_mat("dx", dx, es, false)) ||
+      (rc = check_mat("dW", dW, es, false)) || (rc = check_f32("db", db, false)))
+    return rc;
+  if (R > 0 && dW != nullptr && (ldx < K || ldx > (1LL << 40)))
+    return api_error(RES_ERR_INVALID_ARG, "ldx must be in [K, 2^40]");
+  const LinearBwdLayout w = linear_bwd_layout(dt, act, R, K, N);
+  if ((rc = check_ws(ws, ws_bytes, w.total))) return rc;
+  const Span in[] = {span(dW ? x : nullptr, 0, ldx, 1, R, K, es), flat(W, es * K * N), flat(dy, es * R * N),
+                     flat(pre, 4 * R * N), flat(residual, es * R * K)};
+  const Span out[] = {flat(dx, es * R * K), flat(dW, es * K * N), flat(db, 4 * N), flat(w.total ? ws : nullptr, w.total)};
+  for (int o = 0; o < 4; ++o) {
+    for (int k = 0; k < 5; ++k)
+      if (touch(out[o], in[k]) && !(o == 0 && k == 4 && dx == residual))
+        return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap inputs (dx may be the residual itself)");
+    for (int k = 0; k < o; ++k)
+      if (touch(out[o], out[k])) return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap each other");
+  }
+  hipStream_t st = (hipStream_t)stream;
+  char* base = static_cast<char*>(ws);
+  const void* dpre = dy;
+  hipError_t e = hipSuccess;
+  if (act != RES_ACT_NONE || db != nullptr) {
+    void* o = act != RES_ACT_NONE ? base + w.dpre : nullptr;
+    float* part = db != nullptr ? reinterpret_cast<float*>(base + w.part) : nullptr;
+    const float* p = act != RES_ACT_NONE ? pre : nullptr;
+    e = dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, p, act, o, part, db, R, N, st)
+                       : launch_act_bwd<float>(dy, p, act, o, part, db, R, N, st);
+    if (o != nullptr) dpre = o;
+  }
+  if (e == hipSuccess && dx != nullptr && R > 0) {
+    GemmArgs g{};
+    g.A = dpre;
+    g.B = W;
+    g.sam = N;
+    g.sak = 1;
+    g.sbk = 1;
+    g.sbn = N;
+    g.M = R;
+    g.N = K;
+    g.K = N;
+    g.res = residual;
+    g.out = dx;
+    e = gemm(dt, g, reinterpret_cast<float*>(base + w.split), st);
+  }
+  if (e == hipSuccess && dW != nullptr) {
+    GemmArgs g{};
+    g.A = x;
+    g.B = dpre;
+    g.sam = 1;
+    g.sak = ldx;
+    g.sbk = N;
+    g.sbn = 1;
+    g.M = K;
+    g.N = N;
+    g.K = R;
+    g.out = dW;
+    e = gemm(dt, g, reinterpret_cast<float*>(base + w.split), st);
+  }
+  return launched(e, "linear backward launch");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// AdamW
+// ---------------------------------------------------------------------------
+extern "C" {
+
+int resonator_adamw_step(const res_adamw_tensor_t* tensors, int64_t count, res_dtype_t p_dt, res_dtype_t g_dt,
+                         const res_adamw_state_t* state, const res_adamw_state_t* state_out, double lr, double beta1,
+                         double beta2, double eps, double weight_decay, int64_t step, const float* grad_scale,
+                         void* stream) {
+  if (!known(p_dt) || !known(g_dt)) return api_error(RES_ERR_INVALID_ARG, "unknown dtype code");
+  if (count < 0 || (count > 0 && tensors == nullptr) || state == nullptr || state_out == nullptr)
+    return api_error(RES_ERR_INVALID_ARG, "tensors, state and state_out must be non-null");
+  if (state->bits != state_out->bits || (state->bits != 8 && state->bits != 32))
+    return api_error(RES_ERR_INVALID_ARG, "states must be of 8 or of 32 bits, both of the same");
+  if (!(lr >= 0) || !(beta1 >= 0 && beta1 < 1) || !(beta2 >= 0 && beta2 < 1) || !(eps >= 0) || !(weight_decay >= 0) || step < 1)
+    return api_error(RES_ERR_INVALID_ARG, "lr, eps and weight_decay must be >= 0, betas in [0, 1), step >= 1");
+  const bool master = state->master != nullptr;
+  if (master != (state_out->master != nullptr))
+    return api_error(RES_ERR_INVALID_ARG, "master must be given in both states or in none");
+  if (master && p_dt != RES_BF16)
+    return api_error(RES_ERR_INVALID_ARG, "float32 parameters need no master copy");
+  int64_t total = 0;
+  for (int64_t k = 0; k < count; ++k) {
+    const res_adamw_tensor_t& t = tensors[k];
+    if (t.n < 0 || t.n > (1LL << 40) || t.state < 0 || t.state % RES_ADAMW_BLOCK || t.state > (1LL << 40))
+      return api_error(RES_ERR_INVALID_ARG, "tensor %lld: n must be >= 0 and its state start at a multiple of %d",
+                       (long long)k, RES_ADAMW_BLOCK);
+    if (t.n == 0) continue;
+    if (t.p == nullptr || t.g == nullptr || t.p_out == nullptr)
+      return api_error(RES_ERR_INVALID_ARG, "tensor %lld: p, g and p_out must be non-null", (long long)k);
+    if (!aligned(t.p, elt(p_dt)) || !aligned(t.p_out, elt(p_dt)) || !aligned(t.g, elt(g_dt)))
+      return api_error(RES_ERR_MISALIGNED, "tensor %lld: pointers must be aligned to their element", (long long)k);
+    const Span p = flat(t.p, t.n * elt(p_dt)), o = flat(t.p_out, t.n * elt(p_dt)), g = flat(t.g, t.n * elt(g_dt));
+    if ((t.p != t.p_out && touch(p, o)) || touch(o, g))
+      return api_error(RES_ERR_INVALID_ARG, "tensor %lld: p_out must not overlap g, nor p unless it is p", (long long)k);
+    total += t.n;
+  }
+  if (total == 0) return RES_OK;
+  for (const res_adamw_state_t* s : {state, state_out}) {
+    if (s->m == nullptr || s->v == nullptr || (s->bits == 8 && (s->scale_m == nullptr || s->scale_v == nullptr)))
+      return api_error(RES_ERR_INVALID_ARG, "the states' tensors must be non-null");
+    if (!aligned(s->m, 16) || !aligned(s->v, 16) || !aligned(s->scale_m, 4) || !aligned(s->scale_v, 4) || !aligned(s->master, 16))
+      return api_error(RES_ERR_MISALIGNED, "m, v and master must be 16-byte aligned, scales 4-byte");
+  }
+  if (!aligned(grad_scale, 4)) return api_error(RES_ERR_MISALIGNED, "grad_scale must be 4-byte aligned");
+  AdamWArgs a{};
+  a.m = state->m;
+  a.v = state->v;
+  a.sm = state->scale_m;
+  a.sv = state->scale_v;
+  a.master = state->master;
+  a.m_out = state_out->m;
+  a.v_out = state_out->v;
+  a.sm_out = state_out->scale_m;
+  a.sv_out = state_out->scale_v;
+  a.master_out = state_out->master;
+  a.grad_scale = grad_scale;
+  a.b1 = (float)beta1;
+  a.b1c = (float)(1.0 - beta1);
+  a.b2 = (float)beta2;
+  a.b2c = (float)(1.0 - beta2);
+  a.eps = (float)eps;
+  a.decay = (float)(1.0 - lr * weight_decay);
+  a.step = (float)(lr / (1.0 - std::pow(beta1, (double)step)));
+  a.root = (float)(1.0 / std::sqrt(1.0 - std::pow(beta2, (double)step)));
+  return launched(launch_adamw(a, tensors, count, p_dt == RES_BF16, g_dt == RES_BF16, state->bits, (hipStream_t)stream),
+                  "AdamW launch");
+}
+
+int resonator_adamw_values(const res_adamw_state_t* state, int64_t n, float* m, float* v, void* stream) {
+  if (state == nullptr || state->bits != 8) return api_error(RES_ERR_INVALID_ARG, "state must be of 8 bits");
+  if (n < 0 || n % RES_ADAMW_BLOCK || n > (1LL << 40))
+    return api_error(RES_ERR_INVALID_ARG, "n must be a multiple of %d", RES_ADAMW_BLOCK);
+  if (n == 0) return RES_OK;
+  if (state->m == nullptr || state->v == nullptr || state->scale_m == nullptr || state->scale_v == nullptr ||
+      m == nullptr || v == nullptr)
+    return api_error(RES_ERR_INVALID_ARG, "the state's tensors, m and v must be non-null");
+  if (!aligned(state->m, 16) || !aligned(state->v, 16) || !aligned(m, 16) || !aligned(v, 16))
+    return api_error(RES_ERR_MISALIGNED, "the codes, m and v must be 16-byte aligned");
+  if (touch(flat(m, 4 * n), flat(v, 4 * n)) || touch(flat(m, 4 * n), flat(state->m, n)) || touch(flat(v, 4 * n), flat(state->v, n)) ||
+      touch(flat(m, 4 * n), flat(state->v, n)) || touch(flat(v, 4 * n), flat(state->m, n)))
+    return api_error(RES_ERR_INVALID_ARG, "m and v must not overlap each other or the codes");
+  return launched(launch_adamw_values(state->m, state->v, state->scale_m, state->scale_v, n, m, v, (hipStream_t)stream),
+                  "AdamW values launch");
 }
 
 }  // extern "C"

@@ -16,13 +16,6 @@
 namespace res {
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f;
-
-__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
-__device__ __forceinline__ float sigmoid_fast(float v) {
-  return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-LOG2E * v));  // exp2 = inf gives 0
-}
-
 // 1 - exp(-2 s), without the cancellation of 1 - a a for small s: the series of
 // 1 - exp(-t) up to t^7 below t = 0.3 (relative error 6e-9 there).
 __device__ __forceinline__ float one_minus_a2(float s, float a) {

@@ -3,6 +3,7 @@
 // step (adamw.hip), between their C entry points (api_layer.hip) and the kernels.
 #pragma once
 
+#include "../../include/resonator.h"
 #include "common.h"
 
 namespace res {
@@ -19,6 +20,42 @@ struct RowsOut {
   void* p;
   int64_t sb, st;
 };
+
+// ---------------------------------------------------------------------------
+// Device mathematics shared by the operators
+// ---------------------------------------------------------------------------
+constexpr float LOG2E = 1.44269504088896340736f;
+
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float sigmoid_fast(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-LOG2E * v));  // exp2 = inf gives 0
+}
+
+// Activations of the linear product (codes RES_ACT_*): none, relu, silu = v sigmoid(v),
+// gelu_tanh = v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))), which is v sigmoid(2 sqrt(2/pi) (...)).
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU_TANH = 3 };
+constexpr float GELU_2C = 1.59576912160573071176f;  // 2 sqrt(2 / pi)
+constexpr float GELU_K = 0.044715f;
+
+__device__ __forceinline__ float act_value(float v, int act) {
+  if (act == ACT_RELU) return v > 0.0f ? v : (v != v ? v : 0.0f);
+  if (act == ACT_SILU) return v * sigmoid_fast(v);
+  if (act == ACT_GELU_TANH) return v * sigmoid_fast(GELU_2C * v * fmaf(GELU_K * v, v, 1.0f));
+  return v;
+}
+__device__ __forceinline__ float act_slope(float v, int act) {
+  if (act == ACT_RELU) return v > 0.0f ? 1.0f : 0.0f;
+  if (act == ACT_SILU) {
+    const float q = sigmoid_fast(v);
+    return q * fmaf(v, 1.0f - q, 1.0f);
+  }
+  if (act == ACT_GELU_TANH) {
+    const float q = sigmoid_fast(GELU_2C * v * fmaf(GELU_K * v, v, 1.0f)), d = q * (1.0f - q);
+    // far out d is 0 and the polynomial may be infinite
+    return d == 0.0f ? q : fmaf(d * GELU_2C * v, fmaf(3.0f * GELU_K * v, v, 1.0f), q);
+  }
+  return 1.0f;
+}
 
 // ---------------------------------------------------------------------------
 // Gated scan.  A chain is one batch row and one block of GATED_CW channels.
@@ -50,5 +87,53 @@ hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st);
 template <typename T>
 hipError_t launch_gated_step(const Rows& x, const Rows& r, const Rows& i, void* y, int64_t B, int64_t D,
                              const float* gamma, const float* h, float* h_out, hipStream_t st);
+
+
+// ---------------------------------------------------------------------------
+// Linear product with epilogue: C[m][n] = sum_k A(m, k) B(k, n), where
+// A(m, k) = A[m sam + k sak] and B(k, n) = B[k sbk + n sbn] (one stride of each
+// is 1), then out = act(C + bias[n]) + res[m][n]; pre receives C + bias[n].
+// ---------------------------------------------------------------------------
+struct GemmArgs {
+  const void* A;
+  const void* B;
+  int64_t sam, sak, sbk, sbn;
+  int64_t M, N, K;
+  const float* bias;  // [N] or null
+  const void* res;    // [M][N] or null
+  float* pre;         // [M][N] or null
+  void* out;          // [M][N]
+  int act;
+  int splits;         // parts of the K axis; more than one leave float32 partial sums in `part` [splits][M][N]
+  float* part;
+};
+int64_t linear_splits(int64_t M, int64_t N, int64_t K);
+template <typename T>
+hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);
+// dpre = dy act'(pre) (out null for the sums alone) and, where part is not null, the sums of its columns over blocks of
+// rows [linear_row_blocks(R)][N], then over the blocks into db
+int64_t linear_row_blocks(int64_t R);
+template <typename T>
+hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, float* db, int64_t R,
+                          int64_t N, hipStream_t st);
+
+// ---------------------------------------------------------------------------
+// AdamW over many tensors (states: flat buffers, RES_ADAMW_BLOCK elements a scale)
+// ---------------------------------------------------------------------------
+struct AdamWArgs {
+  const void *m, *v;
+  const float *sm, *sv, *master;
+  void *m_out, *v_out;
+  float *sm_out, *sv_out, *master_out;
+  const float* grad_scale;  // [1] or null
+  float b1, b1c, b2, b2c, eps;
+  float decay;              // 1 - lr weight_decay
+  float step;               // lr / (1 - beta1^t)
+  float root;               // 1 / sqrt(1 - beta2^t)
+};
+hipError_t launch_adamw(const AdamWArgs& a, const res_adamw_tensor_t* tensors, int64_t count, bool p_bf16, bool g_bf16,
+                        int bits, hipStream_t st);
+hipError_t launch_adamw_values(const void* m, const void* v, const float* sm, const float* sv, int64_t n, float* mo,
+                               float* vo, hipStream_t st);
 
 }  // namespace res

@@ -1173,3 +1173,254 @@ class GatedScanFunction(torch.autograd.Function):
 def resonator_gated_scan(x, r, i, gamma, h0=None, lengths=None):
     """Differentiable gated scan: (y, last state); x, r, i, gamma and h0 receive gradients."""
     return GatedScanFunction.apply(x, r, i, gamma, h0, lengths)
+
+
+# ---------------------------------------------------------------------------
+# Gated recurrent layer: linear product with bias, activation and residual
+# ---------------------------------------------------------------------------
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu_tanh": 3}
+
+
+def _act_code(act):
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)} (got {act!r})")
+    return ACTIVATIONS[act]
+
+
+def _rows2(x, name, K=None):
+    """(rows, elements between rows) of a tensor [..., K] whose rows lie at one distance."""
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if x.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {x.device})")
+    _code(x)
+    if x.dim() < 1 or (K is not None and x.shape[-1] != K):
+        raise ValueError(f"{name} must be [..., {K}] (got {list(x.shape)})")
+    K = x.shape[-1]
+    R = x.numel() // K if K else 0
+    if x.is_contiguous() or R <= 1:
+        if K > 1 and R == 1 and x.stride(-1) != 1:
+            raise ValueError(f"{name}'s last dimension must be consecutive in memory")
+        return R, K
+    if K > 1 and x.stride(-1) != 1:
+        raise ValueError(f"{name}'s last dimension must be consecutive in memory")
+    dims = [(n, s) for n, s in zip(x.shape[:-1], x.stride()[:-1]) if n != 1]
+    for (n0, s0), (n1, s1) in zip(dims, dims[1:]):
+        if s0 != n1 * s1:
+            raise ValueError(f"{name}'s rows must lie at one distance in memory")
+    if dims[-1][1] < K:
+        raise ValueError(f"{name}'s rows must not overlap")
+    return R, dims[-1][1]
+
+
+def _weight(W, dtype, K):
+    _dev(W, "W")
+    if W.dim() != 2 or W.dtype != dtype or W.shape[0] != K:
+        raise ValueError(f"W must be {dtype} [{K}, N] (got {W.dtype} {list(W.shape)})")
+    return W.shape[1]
+
+
+def _like(t, name, dtype, shape):
+    if t is None:
+        return None
+    _dev(t, name)
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {list(shape)} (got {t.dtype} {list(t.shape)})")
+    return t
+
+
+def _linear_ws(ws, backward, dtype, act, R, K, N, device):
+    if ws is not None:
+        _dev(ws, "ws")
+        return ws, ws.numel() * ws.element_size()
+    n = int(_lib.lib().resonator_linear_workspace_bytes(backward, _DT[dtype], act, R, K, N))
+    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+
+
+class LinearSaved:
+    """What a forward of the linear product keeps for its backward: the float32 ``pre`` = x W + bias (None where the
+    activation is "none") and the ``bias``."""
+
+    __slots__ = ("pre", "bias")
+
+    def __init__(self, pre, bias):
+        self.pre, self.bias = pre, bias
+
+
+def resonator_linear_fwd(x, W, bias=None, act="none", residual=None, save=False, out=None, ws=None):
+    """y = act(x W + bias) + residual: x [..., K] (rows at one distance), W [K, N] of x's type, bias [N] float32,
+    residual [..., N] of x's type; act "none", "relu", "silu" or "gelu_tanh".  With ``save`` returns (y, saved),
+    a LinearSaved for resonator_linear_bwd.  ``out`` may be the residual itself."""
+    code = _act_code(act)
+    R, ldx = _rows2(x, "x")
+    K = x.shape[-1]
+    N = _weight(W, x.dtype, K)
+    shape = tuple(x.shape[:-1]) + (N,)
+    _f32(bias, "bias", (N,))
+    _like(residual, "residual", x.dtype, shape)
+    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else _given(out, "out", R * N, x.dtype)
+    pre = torch.empty(shape, dtype=torch.float32, device=x.device) if save and code else None
+    ws, n = _linear_ws(ws, 0, x.dtype, code, R, K, N, x.device)
+    check(_lib.lib().resonator_linear_fwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(bias), code, _ptr(residual), _ptr(y),
+                                          _ptr(pre), R, K, N, _ptr(ws), n, _stream(x.device)))
+    return (y, LinearSaved(pre, bias)) if save else y
+
+
+def resonator_linear_bwd(x, W, dy, pre=None, act="none", residual=None, want_dx=True, want_dw=True, want_db=False,
+                         ws=None):
+    """Gradients of sum(dy y) for y = act(x W + bias) + ...: dict with dx (plus ``residual`` where given: the gradient that
+    reaches x on another path), dW and, where wanted, db (float32).  ``pre`` is what a forward with ``save`` returned, or
+    the float32 x W + bias itself; without an activation it is not needed."""
+    code = _act_code(act)
+    R, ldx = _rows2(x, "x")
+    K = x.shape[-1]
+    N = _weight(W, x.dtype, K)
+    shape = tuple(x.shape[:-1]) + (N,)
+    if dy is None or (code and pre is None):
+        raise TypeError("dy and, with an activation, pre must be given")
+    _like(dy, "dy", x.dtype, shape)
+    if isinstance(pre, LinearSaved):
+        pre = pre.pre
+    _like(pre, "pre", torch.float32, shape)
+    _like(residual, "residual", x.dtype, x.shape)
+    dx = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device) if want_dx else None
+    dW = torch.empty_like(W) if want_dw else None
+    db = torch.empty((N,), dtype=torch.float32, device=x.device) if want_db else None
+    ws, n = _linear_ws(ws, 1, x.dtype, code, R, K, N, x.device)
+    check(_lib.lib().resonator_linear_bwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(dy), _ptr(pre), code, _ptr(residual),
+                                          _ptr(dx), _ptr(dW), _ptr(db), R, K, N, _ptr(ws), n, _stream(x.device)))
+    return {k: v for k, v in (("dx", dx), ("dW", dW), ("db", db)) if v is not None}
+
+
+class LinearFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_linear_fwd and resonator_linear_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, W, bias=None, act="none", residual=None):
+        need = any(ctx.needs_input_grad[:3])
+        y, pre = resonator_linear_fwd(x, W, bias, act=act, residual=residual, save=True) if need else (
+            resonator_linear_fwd(x, W, bias, act=act, residual=residual), None)
+        ctx.save_for_backward(x, W, None if pre is None else pre.pre, None if pre is None else pre.bias)
+        ctx.act = act
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, W, pre, bias = ctx.saved_tensors
+        pre = LinearSaved(pre, bias)
+        nx, nw, nb = ctx.needs_input_grad[:3]
+        dy = dy.contiguous()
+        g = {}
+        if nx or nw or nb:
+            g = resonator_linear_bwd(x, W, dy, pre=pre, act=ctx.act, want_dx=nx, want_dw=nw, want_db=nb)
+        return g.get("dx"), g.get("dW"), g.get("db"), None, dy if ctx.needs_input_grad[4] else None
+
+
+def resonator_linear(x, W, bias=None, act="none", residual=None):
+    """Differentiable act(x W + bias) + residual (x, W, bias and residual receive gradients)."""
+    return LinearFunction.apply(x, W, bias, act, residual)
+
+
+# ---------------------------------------------------------------------------
+# AdamW over many tensors
+# ---------------------------------------------------------------------------
+ADAMW_BLOCK = _lib.RES_ADAMW_BLOCK
+
+
+def adamw_offsets(params):
+    """Where each parameter's state begins in the flat state buffers (every tensor at a multiple of ADAMW_BLOCK
+    elements), and the buffers' length."""
+    at, off = [], 0
+    for p in params:
+        at.append(off)
+        off += -(-p.numel() // ADAMW_BLOCK) * ADAMW_BLOCK
+    return at, off
+
+
+def adamw_state(params, bits=32, master=None):
+    """A new optimizer state (zeros) for a list of GPU parameters: a dict of flat buffers laid out by adamw_offsets.
+
+    bits 32: exp_avg, exp_avg_sq float32; bits 8: int8 and uint8 codes with scale_avg, scale_sq float32, one a block.
+    ``master`` (default: for bfloat16 parameters) adds a float32 copy of the parameters, which the step then updates."""
+    if bits not in (8, 32):
+        raise ValueError("bits must be 8 or 32")
+    params = list(params)
+    if not params:
+        raise ValueError("params must not be empty")
+    dt = params[0].dtype
+    for k, p in enumerate(params):
+        _dev(p, f"params[{k}]")
+        _code(p)
+        if p.dtype != dt:
+            raise ValueError("the parameters must be of one type")
+    master = dt == torch.bfloat16 if master is None else master
+    if master and dt != torch.bfloat16:
+        raise ValueError("float32 parameters need no master copy")
+    at, n = adamw_offsets(params)
+    dev = params[0].device
+    if bits == 32:
+        st = {"exp_avg": torch.zeros(n, device=dev), "exp_avg_sq": torch.zeros(n, device=dev)}
+    else:
+        st = {"exp_avg": torch.zeros(n, dtype=torch.int8, device=dev),
+              "exp_avg_sq": torch.zeros(n, dtype=torch.uint8, device=dev),
+              "scale_avg": torch.zeros(n // ADAMW_BLOCK, device=dev), "scale_sq": torch.zeros(n // ADAMW_BLOCK, device=dev)}
+    if master:
+        st["master"] = torch.zeros(n, device=dev)
+        for p, o in zip(params, at):
+            st["master"][o:o + p.numel()] = p.detach().reshape(-1).float()
+    return st
+
+
+def _adamw_state(state, n, name):
+    """The library's struct of a state dict whose buffers hold n elements (a multiple of the block)."""
+    m, v = state["exp_avg"], state["exp_avg_sq"]
+    bits = 8 if m.dtype == torch.int8 else 32
+    want = {"exp_avg": (torch.int8, n), "exp_avg_sq": (torch.uint8, n), "scale_avg": (torch.float32, n // ADAMW_BLOCK),
+            "scale_sq": (torch.float32, n // ADAMW_BLOCK)} if bits == 8 else {
+                "exp_avg": (torch.float32, n), "exp_avg_sq": (torch.float32, n)}
+    if "master" in state:
+        want["master"] = (torch.float32, n)
+    for k, (dt, c) in want.items():
+        _dev(state[k], f"{name}[{k!r}]")
+        if state[k].dtype != dt or state[k].numel() != c:
+            raise ValueError(f"{name}[{k!r}] must be {dt} of {c} elements (got {state[k].dtype} of {state[k].numel()})")
+    ptr = lambda k: state[k].data_ptr() if k in want else None
+    return _lib.AdamWState(bits, m.data_ptr(), v.data_ptr(), ptr("scale_avg"), ptr("scale_sq"), ptr("master"))
+
+
+def resonator_adamw_step(params, grads, state, step, lr, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01,
+                         grad_scale=None, out=None):
+    """One AdamW step over all tensors (one launch for up to 64): params (float32 or bfloat16) and their gradients
+    (either type), ``state`` from adamw_state, ``step`` counting from 1.  ``grad_scale``: float32 [1] on the GPU, multiplies
+    the gradients.  Parameters and state are updated in place, unless ``out`` = (new parameters, new state) receives them."""
+    params, grads = list(params), list(grads)
+    new, new_state = (params, state) if out is None else (list(out[0]), out[1])
+    if len(grads) != len(params) or len(new) != len(params):
+        raise ValueError(f"{len(params)} parameters, {len(grads)} gradients and {len(new)} new parameters")
+    if not params:
+        return
+    at, n = adamw_offsets(params)
+    old_s, new_s = _adamw_state(state, n, "state"), _adamw_state(new_state, n, "new state")
+    table = (_lib.AdamWTensor * len(params))()
+    pd, gd = params[0].dtype, grads[0].dtype
+    for k, (p, g, o) in enumerate(zip(params, grads, new)):
+        for name, t, dt in (("params", p, pd), ("grads", g, gd), ("new parameters", o, pd)):
+            _dev(t, f"{name}[{k}]")
+            if t.dtype != dt or t.shape != p.shape:
+                raise ValueError(f"{name}[{k}] must be {dt} {list(p.shape)} (got {t.dtype} {list(t.shape)})")
+        table[k] = _lib.AdamWTensor(p.data_ptr(), g.data_ptr(), o.data_ptr(), p.numel(), at[k])
+    _f32(grad_scale, "grad_scale", (1,))
+    dev = params[0].device
+    check(_lib.lib().resonator_adamw_step(table, len(params), _code(params[0]), _code(grads[0]), ctypes.byref(old_s),
+                                          ctypes.byref(new_s), float(lr), float(betas[0]), float(betas[1]), float(eps),
+                                          float(weight_decay), int(step), _ptr(grad_scale), _stream(dev)))
+
+
+def resonator_adamw_values(state):
+    """(exp_avg, exp_avg_sq) as float32 flat buffers: what the codes of a state in 8 bits stand for."""
+    n = state["exp_avg"].numel()
+    s = _adamw_state(state, n, "state")
+    m = torch.empty(n, device=state["exp_avg"].device)
+    v = torch.empty_like(m)
+    check(_lib.lib().resonator_adamw_values(ctypes.byref(s), n, _ptr(m), _ptr(v), _stream(m.device)))
+    return m, v

@@ -64,3 +64,49 @@ def test_scan_backward_against_differences(lengths):
             lo[name][k] -= eps
             num = (loss(**hi) - loss(**lo)) / (2 * eps)
             assert abs(num - got[k]) <= 2e-8 * max(1.0, abs(num)), (name, k)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "silu", "gelu_tanh"])
+def test_linear_backward_against_differences(act):
+    r = np.random.default_rng(7)
+    p = dict(x=r.normal(size=(4, 3)), W=r.normal(size=(3, 5)), b=r.normal(size=5))
+    dy, res = r.normal(size=(4, 5)), r.normal(size=(4, 3))
+    g = O.linear_bwd(p["x"], p["W"], dy, p["b"], act)
+    assert np.array_equal(O.linear_bwd(p["x"], p["W"], dy, p["b"], act, res)["dx"], g["dx"] + res)
+    for name in p:
+        for k in np.ndindex(p[name].shape):
+            v = []
+            for e in (1e-6, -1e-6):
+                q = {n: a.copy() for n, a in p.items()}
+                q[name][k] += e
+                v.append(np.sum(dy * O.linear_fwd(q["x"], q["W"], q["b"], act)[0]))
+            assert abs((v[0] - v[1]) / 2e-6 - g["d" + name][k]) <= 1e-7 * max(1.0, abs(g["d" + name][k]))
+
+
+def test_activations_closed_forms():
+    assert O.act_value(np.array([0.0]), "gelu_tanh")[0] == 0.0 and O.act_slope(np.array([0.0]), "gelu_tanh")[0] == 0.5
+    assert abs(O.act_value(np.array([40.0]), "silu")[0] - 40.0) < 1e-14
+    assert np.array_equal(O.act_value(np.array([-2.0, 3.0]), "relu"), [0.0, 3.0])
+
+
+def test_adamw_first_step_and_decay():
+    p, g = np.array([1.0, -2.0, 0.5]), np.array([0.3, -4.0, 0.0])
+    z = np.zeros(3)
+    q, m, v = O.adamw(p, g, z, z, 1, 0.1, (0.9, 0.99), 0.0 + 1e-300, 0.5)
+    # the first step moves by lr against the gradient's sign, after the decay
+    assert np.allclose(q, p * (1 - 0.05) - 0.1 * np.sign(g), rtol=1e-13)
+    assert np.allclose(m, 0.1 * g) and np.allclose(v, 0.01 * g * g)
+
+
+def test_adamw_codes():
+    r = np.random.default_rng(5)
+    v = np.concatenate([r.normal(size=256), np.zeros(256), 1e-35 * r.normal(size=256)])
+    place, scale = O.adamw_encode(v, False)
+    back = O.adamw_decode(np.rint(place), scale, False)
+    big = np.abs(v[:256]).max()
+    # half a code of the square-root grid: |sqrt(value) - sqrt(kept)| <= sqrt(big) / 254
+    assert np.all(np.abs(np.sqrt(np.abs(v[:256])) - np.sqrt(np.abs(back[:256]))) <= np.sqrt(big) / 254 * (1 + 1e-12))
+    assert np.all(back[256:] == 0)
+    w = v[:256] ** 2
+    place, scale = O.adamw_encode(w, True)
+    assert np.all(np.rint(place)[w > 0] >= 1) and np.rint(place).max() == 255
