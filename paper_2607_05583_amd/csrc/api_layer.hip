@@ -247,11 +247,16 @@ int check_linear(int64_t R, int64_t K, int64_t N, res_dtype_t dt, int act) {
 }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-size_t split_bytes(int64_t M, int64_t N, int64_t K) {
-  const int64_t s = linear_splits(M, N, K);
-  return s > 1 ? (size_t)(s * M * N) * 4 : 0;
+// room for the parts of a split product, whichever kernel its operands' alignment allows
+size_t split_bytes(int64_t M, int64_t N, int64_t K, size_t es) {
+  size_t most = 0;
+  for (bool fast : {false, true}) {
+    const int64_t s = linear_plan(M, N, K, es, fast).splits;
+    if (s > 1) most = std::max(most, (size_t)(s * M * N) * 4);
+  }
+  return most;
 }
-size_t linear_fwd_bytes(int64_t R, int64_t K, int64_t N) { return up256(split_bytes(R, N, K)); }
+size_t linear_fwd_bytes(res_dtype_t dt, int64_t R, int64_t K, int64_t N) { return up256(split_bytes(R, N, K, elt(dt))); }
 struct LinearBwdLayout {
   size_t dpre, part, split, total;
 };
@@ -263,7 +268,7 @@ LinearBwdLayout linear_bwd_layout(res_dtype_t dt, int act, int64_t R, int64_t K,
   w.part = off;
   off += up256((size_t)(linear_row_blocks(R) * N) * 4);
   w.split = off;
-  off += up256(std::max(split_bytes(R, K, N), split_bytes(K, N, R)));
+  off += up256(std::max(split_bytes(R, K, N, elt(dt)), split_bytes(K, N, R, elt(dt))));
   w.total = off;
   return w;
 }
@@ -278,7 +283,14 @@ int check_mat(const char* name, const void* p, size_t es, bool needed) {
   return aligned(p, es) ? RES_OK : api_error(RES_ERR_MISALIGNED, "%s must be aligned to its element", name);
 }
 hipError_t gemm(res_dtype_t dt, GemmArgs& g, float* part, hipStream_t st) {
-  g.splits = (int)linear_splits(g.M, g.N, g.K);
+  // whole 16-byte pieces: rows of both operands, and rows of four outputs at a time
+  const int64_t ep = 16 / (int64_t)elt(dt), lda = g.sak == 1 ? g.sam : g.sak, ldb = g.sbk == 1 ? g.sbn : g.sbk;
+  const int64_t xa = g.sak == 1 ? g.K : g.M, xb = g.sbk == 1 ? g.K : g.N;
+  const bool fast = aligned(g.A, 16) && aligned(g.B, 16) && aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) &&
+                    aligned(g.pre, 16) && lda % ep == 0 && ldb % ep == 0 && xa % ep == 0 && xb % ep == 0 && g.N % 4 == 0;
+  const LinearPlan p = linear_plan(g.M, g.N, g.K, elt(dt), fast);
+  g.tile = p.tile;
+  g.splits = p.splits;
   g.part = part;
   return dt == RES_BF16 ? launch_gemm<bf16_t>(g, st) : launch_gemm<float>(g, st);
 }
@@ -289,7 +301,7 @@ extern "C" {
 
 size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N) {
   if (check_linear(R, K, N, dt, act)) return 0;
-  return backward ? linear_bwd_layout(dt, act, R, K, N).total : linear_fwd_bytes(R, K, N);
+  return backward ? linear_bwd_layout(dt, act, R, K, N).total : linear_fwd_bytes(dt, R, K, N);
 }
 
 int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, int act,
@@ -304,7 +316,7 @@ int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
   if ((rc = check_mat("x", x, es, true)) || (rc = check_mat("y", y, es, true)) || (rc = check_f32("pre", pre, false)) ||
       (rc = check_mat("residual", residual, es, false)))
     return rc;
-  const size_t need = linear_fwd_bytes(R, K, N);
+  const size_t need = linear_fwd_bytes(dt, R, K, N);
   if ((rc = check_ws(ws, ws_bytes, need))) return rc;
   const Span in[] = {span(x, 0, ldx, 1, R, K, es), flat(W, es * K * N), flat(bias, 4 * N), flat(residual, es * R * N)};
   const Span out[] = {flat(y, es * R * N), flat(pre, 4 * R * N), flat(need ? ws : nullptr, need)};

@@ -104,10 +104,15 @@ struct GemmArgs {
   float* pre;         // [M][N] or null
   void* out;          // [M][N]
   int act;
+  int tile;           // tile of a work-group: 64 (any operands), 128 or 256 (16-byte aligned ones)
   int splits;         // parts of the K axis; more than one leave float32 partial sums in `part` [splits][M][N]
   float* part;
 };
-int64_t linear_splits(int64_t M, int64_t N, int64_t K);
+struct LinearPlan {
+  int tile, splits;
+};
+// fast: both operands, the outputs and what the epilogue reads are 16-byte aligned with rows of whole 16-byte pieces
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast);
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);
 // dpre = dy act'(pre) (out null for the sums alone) and, where part is not null, the sums of its columns over blocks of

@@ -3,6 +3,7 @@
 //   dpre = dy act'(pre), dx = dpre W^T, dW = x^T dpre, db = sum over rows of dpre.
 // All three products are one kernel over strided operands; sums are float32 (MFMA).
 #include "layer.h"
+#include "stream.h"
 
 namespace res {
 namespace {
@@ -16,6 +17,32 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int64_t n, 
   c = act_value(c, g.act);
   if (g.res != nullptr) c += to_f32(((const T*)g.res)[at]);
   ((T*)g.out)[at] = from_f32<T>(c);
+}
+
+// Four columns at once: n, N a multiple of 4 and every pointer of 4 elements' alignment.
+template <typename T> struct __align__(4 * sizeof(T)) Quad { T v[4]; };
+template <typename T>
+__device__ __forceinline__ void finish4(const GemmArgs& g, int64_t m, int64_t n, f4 c) {
+  const int64_t at = m * g.N + n;
+  if (g.splits > 1) {
+    *reinterpret_cast<f4*>(g.part + blockIdx.y * g.M * g.N + at) = c;
+    return;
+  }
+  if (g.bias != nullptr) c += *reinterpret_cast<const f4*>(g.bias + n);
+  if (g.pre != nullptr) *reinterpret_cast<f4*>(g.pre + at) = c;
+  if (g.act != ACT_NONE) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c[r] = act_value(c[r], g.act);
+  }
+  if (g.res != nullptr) {
+    const auto q = *reinterpret_cast<const Quad<T>*>((const T*)g.res + at);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c[r] += to_f32(q.v[r]);
+  }
+  Quad<T> o;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) o.v[r] = from_f32<T>(c[r]);
+  *reinterpret_cast<Quad<T>*>((T*)g.out + at) = o;
 }
 
 // Any sizes, strides and alignments: 64 x 64 outputs of a work-group of four waves
@@ -82,6 +109,151 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(GemmArgs g) {
       }
 }
 
+
+// ---------------------------------------------------------------------------
+// Tiles of BM x BN outputs for 16-byte aligned operands.  A wave owns WM x WN of
+// them in registers; 128 bytes of the K axis at a time (KB elements) go straight to
+// LDS (16 bytes a lane, no registers), the next ones while these are multiplied.
+//
+// An operand whose K axis is consecutive in memory lies in LDS as rows of 128
+// bytes, 16-byte piece s of row r in slot s ^ (r & 7): 16 lanes reading one piece of
+// 16 rows meet different banks.  One whose other axis is consecutive (X bytes a row)
+// lies as it is in memory, one row for each k, and is transposed by the read: bf16 by
+// the transposing LDS load (a group of 16 lanes reads 4 k of 16 columns, and lane i
+// gets the 4 k of column i), float by single words.  There the 16 columns of a fragment
+// are one granule (32 or 64 bytes), and granule c of row k is in slot c ^ f(k) with an f
+// that tells apart the rows that are read at once.
+// The loads go to LDS in order, so the swizzles are applied to the source addresses.
+//
+// The product is taken as C^T (the column operand first), so that a lane's four
+// results are four columns of one row: 8-byte stores for bf16.
+// ---------------------------------------------------------------------------
+__device__ __align__(16) const uint32_t zero_piece[4] = {};  // what lies outside an operand
+
+template <typename T> struct Gemm {
+  static constexpr int ES = sizeof(T), KB = 128 / ES, EP = 16 / ES;  // K elements of a step; elements of a piece
+  typedef typename Path<T>::XOp Frag;
+  static constexpr int DEPTH = ES == 2 ? 32 : 16;  // K elements of a fragment
+};
+
+// Loads rows x0.. (X in all) and K elements k0.. (to kend) of an operand into `lds`.
+// KC: element (x, k) at p[x ld + k], else at p[k ld + x].
+template <typename T, int BX, int NW, bool KC>
+__device__ __forceinline__ void tile_to_lds(const T* p, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t kend,
+                                            char* lds, int wave, int lane) {
+  constexpr int ES = sizeof(T), EP = 16 / ES, RB = KC ? 128 : BX * ES, PR = RB / 16, RU = 1024 / RB;
+  constexpr int UNITS = BX / 8 / NW;
+  static_assert(BX % (8 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
+#pragma unroll
+  for (int u = 0; u < UNITS; ++u) {
+    const int unit = wave * UNITS + u, row = unit * RU + lane / PR, slot = lane % PR;
+    int piece;
+    if constexpr (KC)
+      piece = slot ^ (row & 7);
+    else if constexpr (ES == 2)
+      piece = slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+    else
+      piece = slot ^ (((row >> 2) & 3) << 2);
+    const int64_t x = x0 + (KC ? row : piece * EP), k = k0 + (KC ? piece * EP : row);
+    const void* src = x < X && k < kend ? (const void*)(KC ? p + x * ld + k : p + k * ld + x) : (const void*)zero_piece;
+    lds_dma16_lane(src, lds + unit * 1024);
+  }
+}
+
+// The fragment of columns (or rows) c.. of K elements DEPTH h ..
+template <typename T, int BX, bool KC>
+__device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int c, int h, int li, int lq) {
+  if constexpr (KC) {
+    const int row = c + li;
+    return *reinterpret_cast<const typename Gemm<T>::Frag*>(lds + row * 128 + (((h * 4 + lq) ^ (row & 7)) << 4));
+  } else if constexpr (sizeof(T) == 2) {
+    constexpr int RB = BX * 2;
+    typedef __attribute__((address_space(3))) s4 lds_s4;
+    const int row = h * 32 + 8 * lq + (li >> 2), f = (li >> 2) | ((lq & 1) << 2);
+    const char* p = lds + row * RB + (((c >> 4) ^ f) << 5) + (li & 3) * 8;
+    const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
+    const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * RB));
+    typedef short s8 __attribute__((ext_vector_type(8)));
+    return __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    constexpr int RB = BX * 4;
+    const char* p = lds + (h * 16 + 4 * lq) * RB + (((c >> 4) ^ lq) << 6) + li * 4;
+    f4 v;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(p + j * RB);
+    return v;
+  }
+}
+
+// Tile of a work-group: work-groups go to the eight dies in turn, so die d takes the
+// d-th eighth of the tiles; there, blocks of eight rows of tiles, column after column,
+// so that the work-groups that run together share operands in the die's cache.
+__device__ __forceinline__ void tile_of(int64_t id, int64_t tm, int64_t tn, int64_t* m, int64_t* n) {
+  const int64_t all = tm * tn, q = all / 8, r = all % 8, d = id % 8;
+  id = d * q + (d < r ? d : r) + id / 8;
+  const int64_t g = id / (8 * tn), first = g * 8, rows = tm - first < 8 ? tm - first : 8, in = id - g * 8 * tn;
+  *m = first + in % rows;
+  *n = in / rows;
+}
+
+template <typename T, int BM, int BN, int WM, int WN, bool AK, bool BK>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void gemm_tile_kernel(GemmArgs g) {
+  constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16;
+  __shared__ __align__(1024) char lds[2][(BM + BN) * 128];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lq = lane >> 4;
+  int64_t tm, tn;
+  tile_of(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, &tm, &tn);
+  const int64_t m0 = tm * BM, n0 = tn * BN;
+  const int64_t per = ((g.K + g.splits - 1) / g.splits + KB - 1) / KB * KB;
+  const int64_t k0 = blockIdx.y * per, k1 = k0 + per < g.K ? k0 + per : g.K;
+  const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
+  const T* A = (const T*)g.A;
+  const T* B = (const T*)g.B;
+  const int64_t lda = AK ? g.sam : g.sak, ldb = BK ? g.sbn : g.sbk;
+  auto load = [&](int64_t k, int buf) {
+    tile_to_lds<T, BM, NW, AK>(A, lda, m0, g.M, k, k1, lds[buf], wave, lane);
+    tile_to_lds<T, BN, NW, BK>(B, ldb, n0, g.N, k, k1, lds[buf] + BM * 128, wave, lane);
+  };
+  f4 acc[FM][FN] = {};
+  const int steps = k1 > k0 ? (int)((k1 - k0 + KB - 1) / KB) : 0;
+  if (steps > 0) load(k0, 0);
+  for (int s = 0; s < steps; ++s) {
+    wait_vm<0>();  // this wave's pieces of step s are there, and past the barrier everyone's;
+    __builtin_amdgcn_s_barrier();  // the other buffer has been read by all
+    asm volatile("" ::: "memory");
+    if (s + 1 < steps) load(k0 + (int64_t)(s + 1) * KB, (s + 1) & 1);
+    const char* la = lds[s & 1];
+    const char* lb = la + BM * 128;
+#pragma unroll
+    for (int h = 0; h < KB / Gemm<T>::DEPTH; ++h) {
+      typename Gemm<T>::Frag fb[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = fragment<T, BN, BK>(lb, wn + j * 16, h, li, lq);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const auto fa = fragment<T, BM, AK>(la, wm + i * 16, h, li, lq);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          if constexpr (sizeof(T) == 2)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa, acc[i][j], 0, 0, 0);
+          else
+            acc[i][j] = mma_f32(fb[j], fa, acc[i][j]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int64_t m = m0 + wm + i * 16 + li;
+    if (m >= g.M) continue;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int64_t n = n0 + wn + j * 16 + lq * 4;
+      if (n < g.N) finish4<T>(g, m, n, acc[i][j]);
+    }
+  }
+}
+
 // the parts of a split sum, in order, then the epilogue
 template <typename T>
 __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs g) {
@@ -120,19 +292,43 @@ __global__ __launch_bounds__(256) void col_sum_kernel(const float* part, int64_t
 
 int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 
-// Parts of the K axis, so that about 512 work-groups run where the outputs alone give
-// fewer; a part has at least 256 terms.
-int64_t linear_splits(int64_t M, int64_t N, int64_t K) {
-  const int64_t tiles = ((M + 63) / 64) * ((N + 63) / 64);
-  int64_t s = tiles > 0 ? 512 / tiles : 1;
+// Tiles of a product, and the parts its K axis is cut into where they are fewer than
+// the compute units: as many as fill them, a part having at least 256 terms.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast) {
+  LinearPlan p{};
+  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
+  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 ? 256 : 128;
+  const int64_t t = tiles(p.tile), want = fast ? 512 : 512;
+  int64_t s = t > 0 ? want / t : 1;
   if (s > K / 256) s = K / 256;
-  return s < 1 ? 1 : s > 64 ? 64 : s;
+  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  return p;
 }
+
+namespace {
+template <typename T, int BM, int BN, int WM, int WN>
+void launch_tiles(const GemmArgs& a, hipStream_t st) {
+  const dim3 grid((unsigned)(((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN)), (unsigned)a.splits);
+  constexpr int NT = 64 * (BM / WM) * (BN / WN);
+  if (a.sak == 1 && a.sbk == 1)
+    gemm_tile_kernel<T, BM, BN, WM, WN, true, true><<<grid, NT, 0, st>>>(a);
+  else if (a.sak == 1)
+    gemm_tile_kernel<T, BM, BN, WM, WN, true, false><<<grid, NT, 0, st>>>(a);
+  else
+    gemm_tile_kernel<T, BM, BN, WM, WN, false, false><<<grid, NT, 0, st>>>(a);
+}
+}  // namespace
 
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
-  const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64);
-  gemm_any_kernel<T><<<dim3((unsigned)tiles, (unsigned)a.splits), 256, 0, st>>>(a);
+  if (a.tile == 256) {
+    if constexpr (sizeof(T) == 2) launch_tiles<T, 256, 256, 128, 64>(a, st);
+  } else if (a.tile == 128) {
+    launch_tiles<T, 128, 128, 64, 64>(a, st);
+  } else {
+    const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64);
+    gemm_any_kernel<T><<<dim3((unsigned)tiles, (unsigned)a.splits), 256, 0, st>>>(a);
+  }
   if (a.splits > 1) gemm_join_kernel<T><<<dim3((unsigned)((a.M * a.N + 255) / 256)), 256, 0, st>>>(a);
   return hipGetLastError();
 }
