@@ -36,11 +36,14 @@ __device__ __forceinline__ float sigmoid_fast(float v) {
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU_TANH = 3 };
 constexpr float GELU_2C = 1.59576912160573071176f;  // 2 sqrt(2 / pi)
 constexpr float GELU_K = 0.044715f;
+__device__ __forceinline__ float gelu_sigmoid(float v) {  // sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3))
+  return __builtin_amdgcn_rcpf(1.0f + exp2_fast(v * fmaf(-LOG2E * GELU_2C * GELU_K * v, v, -LOG2E * GELU_2C)));
+}
 
 __device__ __forceinline__ float act_value(float v, int act) {
   if (act == ACT_RELU) return v > 0.0f ? v : (v != v ? v : 0.0f);
   if (act == ACT_SILU) return v * sigmoid_fast(v);
-  if (act == ACT_GELU_TANH) return v * sigmoid_fast(GELU_2C * v * fmaf(GELU_K * v, v, 1.0f));
+  if (act == ACT_GELU_TANH) return v * gelu_sigmoid(v);
   return v;
 }
 __device__ __forceinline__ float act_slope(float v, int act) {
@@ -50,7 +53,7 @@ __device__ __forceinline__ float act_slope(float v, int act) {
     return q * fmaf(v, 1.0f - q, 1.0f);
   }
   if (act == ACT_GELU_TANH) {
-    const float q = sigmoid_fast(GELU_2C * v * fmaf(GELU_K * v, v, 1.0f)), d = q * (1.0f - q);
+    const float q = gelu_sigmoid(v), d = q * (1.0f - q);
     // far out d is 0 and the polynomial may be infinite
     return d == 0.0f ? q : fmaf(d * GELU_2C * v, fmaf(3.0f * GELU_K * v, v, 1.0f), q);
   }

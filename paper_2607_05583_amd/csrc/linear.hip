@@ -19,30 +19,11 @@ __device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int64_t n, 
   ((T*)g.out)[at] = from_f32<T>(c);
 }
 
-// Four columns at once: n, N a multiple of 4 and every pointer of 4 elements' alignment.
 template <typename T> struct __align__(4 * sizeof(T)) Quad { T v[4]; };
-template <typename T>
-__device__ __forceinline__ void finish4(const GemmArgs& g, int64_t m, int64_t n, f4 c) {
-  const int64_t at = m * g.N + n;
-  if (g.splits > 1) {
-    *reinterpret_cast<f4*>(g.part + blockIdx.y * g.M * g.N + at) = c;
-    return;
-  }
-  if (g.bias != nullptr) c += *reinterpret_cast<const f4*>(g.bias + n);
-  if (g.pre != nullptr) *reinterpret_cast<f4*>(g.pre + at) = c;
-  if (g.act != ACT_NONE) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = act_value(c[r], g.act);
-  }
-  if (g.res != nullptr) {
-    const auto q = *reinterpret_cast<const Quad<T>*>((const T*)g.res + at);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] += to_f32(q.v[r]);
-  }
-  Quad<T> o;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) o.v[r] = from_f32<T>(c[r]);
-  *reinterpret_cast<Quad<T>*>((T*)g.out + at) = o;
+__device__ __forceinline__ Quad<float> round_quad(const f4& c, float) { return __builtin_bit_cast(Quad<float>, c); }
+__device__ __forceinline__ Quad<bf16_t> round_quad(const f4& c, bf16_t) {
+  typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(Quad<bf16_t>, __builtin_convertvector(c, bf4));
 }
 
 // Any sizes, strides and alignments: 64 x 64 outputs of a work-group of four waves
@@ -128,7 +109,7 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(GemmArgs g) {
 // The product is taken as C^T (the column operand first), so that a lane's four
 // results are four columns of one row: 8-byte stores for bf16.
 // ---------------------------------------------------------------------------
-__device__ __align__(16) const uint32_t zero_piece[4] = {};  // what lies outside an operand
+__device__ __align__(16) const uint32_t zero_piece[4] = {};  // what lies behind the K axis
 
 template <typename T> struct Gemm {
   static constexpr int ES = sizeof(T), KB = 128 / ES, EP = 16 / ES;  // K elements of a step; elements of a piece
@@ -136,29 +117,60 @@ template <typename T> struct Gemm {
   static constexpr int DEPTH = ES == 2 ? 32 : 16;  // K elements of a fragment
 };
 
-// Loads rows x0.. (X in all) and K elements k0.. (to kend) of an operand into `lds`.
-// KC: element (x, k) at p[x ld + k], else at p[k ld + x].
-template <typename T, int BX, int NW, bool KC>
-__device__ __forceinline__ void tile_to_lds(const T* p, int64_t ld, int64_t x0, int64_t X, int64_t k0, int64_t kend,
-                                            char* lds, int wave, int lane) {
-  constexpr int ES = sizeof(T), EP = 16 / ES, RB = KC ? 128 : BX * ES, PR = RB / 16, RU = 1024 / RB;
-  constexpr int UNITS = BX / 8 / NW;
-  static_assert(BX % (8 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
-#pragma unroll
-  for (int u = 0; u < UNITS; ++u) {
-    const int unit = wave * UNITS + u, row = unit * RU + lane / PR, slot = lane % PR;
-    int piece;
-    if constexpr (KC)
-      piece = slot ^ (row & 7);
-    else if constexpr (ES == 2)
-      piece = slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
-    else
-      piece = slot ^ (((row >> 2) & 3) << 2);
-    const int64_t x = x0 + (KC ? row : piece * EP), k = k0 + (KC ? piece * EP : row);
-    const void* src = x < X && k < kend ? (const void*)(KC ? p + x * ld + k : p + k * ld + x) : (const void*)zero_piece;
-    lds_dma16_lane(src, lds + unit * 1024);
-  }
+// a value that is the same in all lanes, in scalar registers
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return (const char*)((uint64_t)hi << 32 | lo);
 }
+
+// Loads an operand's tile: rows x0.. of X and KB elements of the K axis.  KC: element (x, k) at p[x ld + k], else at
+// p[k ld + x].  A lane's byte offsets from the tile's start do not change along K (only the scalar base does), and
+// rows past the end are the last ones again: what they give is not stored.
+template <typename T, int BX, int NW, bool KC> struct TileLoad {
+  static constexpr int ES = sizeof(T), EP = 16 / ES, RB = KC ? 128 : BX * ES, PR = RB / 16, RU = 1024 / RB;
+  static constexpr int UNITS = BX / 8 / NW;
+  static_assert(BX % (8 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
+  uint32_t off[UNITS];
+  const char* start;  // the tile's first element at k = 0
+  int64_t step;       // bytes of an element along K
+
+  __device__ static __forceinline__ int row_of(int u, int wave, int lane) { return (wave * UNITS + u) * RU + lane / PR; }
+  __device__ static __forceinline__ int piece_of(int row, int lane) {
+    const int slot = lane % PR;
+    if constexpr (KC) return slot ^ (row & 7);
+    if constexpr (ES == 2) return slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+    return slot ^ (((row >> 2) & 3) << 2);
+  }
+  __device__ __forceinline__ TileLoad(const T* p, int64_t ld, int64_t x0, int64_t X, int wave, int lane) {
+    start = (const char*)(p + x0 * (KC ? ld : 1));
+    step = (KC ? 1 : ld) * ES;
+    const int64_t left = X - x0;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
+      if constexpr (KC)
+        off[u] = (uint32_t)((row < left ? row : left - 1) * ld * ES + piece * 16);
+      else
+        off[u] = (uint32_t)(row * ld * ES + (piece * EP < left ? piece * EP : left - EP) * ES);
+    }
+  }
+  // K elements k .. k + KB - 1, those from kend on as zeros
+  __device__ __forceinline__ void operator()(int64_t k, int64_t kend, char* lds, int wave, int lane) const {
+    const char* base = uniform(start + k * step);
+    if (k + Gemm<T>::KB <= kend) {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) lds_dma16(base, off[u], lds + (wave * UNITS + u) * 1024);
+    } else {
+#pragma unroll
+      for (int u = 0; u < UNITS; ++u) {
+        const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
+        const void* src = k + (KC ? piece * EP : row) < kend ? (const void*)(base + off[u]) : (const void*)zero_piece;
+        lds_dma16_lane(src, lds + (wave * UNITS + u) * 1024);
+      }
+    }
+  }
+};
 
 // The fragment of columns (or rows) c.. of K elements DEPTH h ..
 template <typename T, int BX, bool KC>
@@ -173,7 +185,6 @@ __device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int 
     const char* p = lds + row * RB + (((c >> 4) ^ f) << 5) + (li & 3) * 8;
     const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
     const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * RB));
-    typedef short s8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   } else {
     constexpr int RB = BX * 4;
@@ -188,31 +199,90 @@ __device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int 
 // Tile of a work-group: work-groups go to the eight dies in turn, so die d takes the
 // d-th eighth of the tiles; there, blocks of eight rows of tiles, column after column,
 // so that the work-groups that run together share operands in the die's cache.
-__device__ __forceinline__ void tile_of(int64_t id, int64_t tm, int64_t tn, int64_t* m, int64_t* n) {
-  const int64_t all = tm * tn, q = all / 8, r = all % 8, d = id % 8;
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, int64_t* m, int64_t* n) {
+  const uint32_t all = tm * tn, q = all / 8, r = all % 8, d = id % 8;
   id = d * q + (d < r ? d : r) + id / 8;
-  const int64_t g = id / (8 * tn), first = g * 8, rows = tm - first < 8 ? tm - first : 8, in = id - g * 8 * tn;
-  *m = first + in % rows;
-  *n = in / rows;
+  const uint32_t g = id / (8 * tn), first = g * 8, rows = tm - first < 8 ? tm - first : 8, in = id - g * 8 * tn;
+  *m = __builtin_amdgcn_readfirstlane(first + in % rows);
+  *n = __builtin_amdgcn_readfirstlane(in / rows);
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool AK, bool BK>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void gemm_tile_kernel(GemmArgs g) {
+// A wave's outputs through its part of the LDS (rows of WN elements, 16-byte piece p of row m in slot p ^ (m & 7)), so
+// that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout gives 32-byte pieces.  Rows and
+// columns past the end are computed from the last ones' operands and not stored.
+template <typename T, int ACT, int WM, int WN>
+__device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
+                                         char* mine, int lane) {
+  constexpr int ES = sizeof(T), RB = WN * ES, PR = RB / 16, EP = 16 / ES, SW = PR < 8 ? PR - 1 : 7, FN = WN / 16;
+  const int li = lane & 15, lq = lane >> 4;
+  int64_t n[FN];
+  f4 bias[FN];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    n[j] = n0 + j * 16 + lq * 4;
+    n[j] = n[j] < g.N ? n[j] : g.N - 4;
+    bias[j] = g.bias != nullptr ? *reinterpret_cast<const f4*>(g.bias + n[j]) : f4{};
+  }
+#pragma unroll
+  for (int i = 0; i < WM / 16; ++i) {
+    int64_t m = m0 + i * 16 + li;
+    const bool in = m < g.M;
+    m = in ? m : g.M - 1;
+    f4 c[FN];
+#pragma unroll
+    for (int j = 0; j < FN; ++j) c[j] = acc[i][j] + bias[j];
+    if (g.pre != nullptr && in) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        if (n0 + j * 16 + lq * 4 < g.N) *reinterpret_cast<f4*>(g.pre + m * g.N + n[j]) = c[j];
+    }
+    if constexpr (ACT != ACT_NONE) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[j][r] = act_value(c[j][r], ACT);
+    }
+    if (g.res != nullptr) {
+      Quad<T> q[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) q[j] = *reinterpret_cast<const Quad<T>*>((const T*)g.res + m * g.N + n[j]);
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) c[j][r] += to_f32(q[j].v[r]);
+    }
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const int byte = (j * 16 + lq * 4) * ES;
+      *reinterpret_cast<Quad<T>*>(mine + (i * 16 + li) * RB + (((byte >> 4) ^ (li & SW)) << 4) + (byte & 15)) = round_quad(c[j], T());
+    }
+  }
+  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+  for (int u = 0; u < WM * PR / 64; ++u) {
+    const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
+    const int64_t m = m0 + row, col = n0 + ((slot ^ (row & SW)) * EP);
+    const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
+    if (m < g.M && col < g.N) *reinterpret_cast<u4*>((T*)g.out + m * g.N + col) = v;
+  }
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int OCC, bool AK, bool BK>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_kernel(GemmArgs g) {
   constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16;
   __shared__ __align__(1024) char lds[2][(BM + BN) * 128];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, lq = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lq = lane >> 4;
   int64_t tm, tn;
-  tile_of(blockIdx.x, (g.M + BM - 1) / BM, (g.N + BN - 1) / BN, &tm, &tn);
+  tile_of(blockIdx.x, (uint32_t)((g.M + BM - 1) / BM), (uint32_t)((g.N + BN - 1) / BN), &tm, &tn);
   const int64_t m0 = tm * BM, n0 = tn * BN;
   const int64_t per = ((g.K + g.splits - 1) / g.splits + KB - 1) / KB * KB;
   const int64_t k0 = blockIdx.y * per, k1 = k0 + per < g.K ? k0 + per : g.K;
   const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-  const T* A = (const T*)g.A;
-  const T* B = (const T*)g.B;
-  const int64_t lda = AK ? g.sam : g.sak, ldb = BK ? g.sbn : g.sbk;
+  const TileLoad<T, BM, NW, AK> load_a((const T*)g.A, AK ? g.sam : g.sak, m0, g.M, wave, lane);
+  const TileLoad<T, BN, NW, BK> load_b((const T*)g.B, BK ? g.sbn : g.sbk, n0, g.N, wave, lane);
   auto load = [&](int64_t k, int buf) {
-    tile_to_lds<T, BM, NW, AK>(A, lda, m0, g.M, k, k1, lds[buf], wave, lane);
-    tile_to_lds<T, BN, NW, BK>(B, ldb, n0, g.N, k, k1, lds[buf] + BM * 128, wave, lane);
+    load_a(k, k1, lds[buf], wave, lane);
+    load_b(k, k1, lds[buf] + BM * 128, wave, lane);
   };
   f4 acc[FM][FN] = {};
   const int steps = k1 > k0 ? (int)((k1 - k0 + KB - 1) / KB) : 0;
@@ -242,15 +312,28 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN)) void gemm_tile_kernel(G
       }
     }
   }
+  if (g.splits > 1) {
+    float* part = g.part + blockIdx.y * g.M * g.N;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) {
-    const int64_t m = m0 + wm + i * 16 + li;
-    if (m >= g.M) continue;
+    for (int i = 0; i < FM; ++i) {
+      const int64_t m = m0 + wm + i * 16 + li;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      const int64_t n = n0 + wn + j * 16 + lq * 4;
-      if (n < g.N) finish4<T>(g, m, n, acc[i][j]);
+      for (int j = 0; j < FN; ++j) {
+        const int64_t n = n0 + wn + j * 16 + lq * 4;
+        if (m < g.M && n < g.N) *reinterpret_cast<f4*>(part + m * g.N + n) = acc[i][j];
+      }
     }
+    return;
+  }
+  __builtin_amdgcn_s_barrier();  // the operands' LDS has been read by all
+  asm volatile("" ::: "memory");
+  char* mine = lds[0] + wave * (2 * (BM + BN) * 128 / NW);
+  static_assert(WM * WN * sizeof(T) <= 2 * (BM + BN) * 128 / NW, "a wave's outputs fit into its share of the LDS");
+  switch (g.act) {
+    case ACT_RELU: tile_out<T, ACT_RELU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+    case ACT_SILU: tile_out<T, ACT_SILU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+    case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+    default: tile_out<T, ACT_NONE, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
   }
 }
 
@@ -297,7 +380,7 @@ int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast) {
   LinearPlan p{};
   auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 ? 256 : 128;
+  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 && K >= 1024 ? 256 : 128;
   const int64_t t = tiles(p.tile), want = fast ? 512 : 512;
   int64_t s = t > 0 ? want / t : 1;
   if (s > K / 256) s = K / 256;
@@ -306,25 +389,25 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast) {
 }
 
 namespace {
-template <typename T, int BM, int BN, int WM, int WN>
+template <typename T, int BM, int BN, int WM, int WN, int OCC>
 void launch_tiles(const GemmArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)(((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN)), (unsigned)a.splits);
   constexpr int NT = 64 * (BM / WM) * (BN / WN);
   if (a.sak == 1 && a.sbk == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, true, true><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, true, true><<<grid, NT, 0, st>>>(a);
   else if (a.sak == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, true, false><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, true, false><<<grid, NT, 0, st>>>(a);
   else
-    gemm_tile_kernel<T, BM, BN, WM, WN, false, false><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, false, false><<<grid, NT, 0, st>>>(a);
 }
 }  // namespace
 
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
   if (a.tile == 256) {
-    if constexpr (sizeof(T) == 2) launch_tiles<T, 256, 256, 128, 64>(a, st);
+    if constexpr (sizeof(T) == 2) launch_tiles<T, 256, 256, 128, 64, 2>(a, st);
   } else if (a.tile == 128) {
-    launch_tiles<T, 128, 128, 64, 64>(a, st);
+    launch_tiles<T, 128, 128, 64, 32, 4>(a, st);
   } else {
     const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64);
     gemm_any_kernel<T><<<dim3((unsigned)tiles, (unsigned)a.splits), 256, 0, st>>>(a);
