@@ -286,7 +286,7 @@ hipError_t gemm(res_dtype_t dt, GemmArgs& g, float* part, hipStream_t st) {
   // whole 16-byte pieces: rows of both operands, and rows of four outputs at a time
   const int64_t ep = 16 / (int64_t)elt(dt), lda = g.sak == 1 ? g.sam : g.sak, ldb = g.sbk == 1 ? g.sbn : g.sbk;
   const int64_t xa = g.sak == 1 ? g.K : g.M, xb = g.sbk == 1 ? g.K : g.N;
-  const bool fast = aligned(g.A, 16) && aligned(g.B, 16) && aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) &&
+  const bool fast = g.K > 0 && aligned(g.A, 16) && aligned(g.B, 16) && aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) &&
                     aligned(g.pre, 16) && lda % ep == 0 && ldb % ep == 0 && xa % ep == 0 && xb % ep == 0 && g.N % ep == 0 &&
                     lda < (1 << 21) && ldb < (1 << 21);  // (a tile's bytes have 32-bit offsets)
   const LinearPlan p = linear_plan(g.M, g.N, g.K, elt(dt), fast);

@@ -93,12 +93,13 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(GemmArgs g) {
 
 // ---------------------------------------------------------------------------
 // Tiles of BM x BN outputs for 16-byte aligned operands.  A wave owns WM x WN of
-// them in registers; 128 bytes of the K axis at a time (KB elements) go straight to
-// LDS (16 bytes a lane, no registers), the next ones while these are multiplied.
+// them in registers; 64 bytes of the K axis at a time (KB elements, the depth of one
+// fragment) go straight to LDS (16 bytes a lane, no registers), the next ones while
+// these are multiplied.
 //
-// An operand whose K axis is consecutive in memory lies in LDS as rows of 128
-// bytes, 16-byte piece s of row r in slot s ^ (r & 7): 16 lanes reading one piece of
-// 16 rows meet different banks.  One whose other axis is consecutive (X bytes a row)
+// An operand whose K axis is consecutive in memory lies in LDS as rows of 64
+// bytes, 16-byte piece s of row r in slot s ^ (r >> 2 & 3): the lanes that read one
+// piece of eight rows meet different banks.  One whose other axis is consecutive (X bytes a row)
 // lies as it is in memory, one row for each k, and is transposed by the read: bf16 by
 // the transposing LDS load (a group of 16 lanes reads 4 k of 16 columns, and lane i
 // gets the 4 k of column i), float by single words.  There the 16 columns of a fragment
@@ -112,9 +113,8 @@ __global__ __launch_bounds__(256) void gemm_any_kernel(GemmArgs g) {
 __device__ __align__(16) const uint32_t zero_piece[4] = {};  // what lies behind the K axis
 
 template <typename T> struct Gemm {
-  static constexpr int ES = sizeof(T), KB = 128 / ES, EP = 16 / ES;  // K elements of a step; elements of a piece
+  static constexpr int ES = sizeof(T), KB = 64 / ES, EP = 16 / ES;  // K elements of a step; elements of a piece
   typedef typename Path<T>::XOp Frag;
-  static constexpr int DEPTH = ES == 2 ? 32 : 16;  // K elements of a fragment
 };
 
 // a value that is the same in all lanes, in scalar registers
@@ -128,9 +128,9 @@ __device__ __forceinline__ const char* uniform(const char* p) {
 // p[k ld + x].  A lane's byte offsets from the tile's start do not change along K (only the scalar base does), and
 // rows past the end are the last ones again: what they give is not stored.
 template <typename T, int BX, int NW, bool KC> struct TileLoad {
-  static constexpr int ES = sizeof(T), EP = 16 / ES, RB = KC ? 128 : BX * ES, PR = RB / 16, RU = 1024 / RB;
-  static constexpr int UNITS = BX / 8 / NW;
-  static_assert(BX % (8 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
+  static constexpr int ES = sizeof(T), EP = 16 / ES, RB = KC ? 64 : BX * ES, PR = RB / 16, RU = 1024 / RB;
+  static constexpr int UNITS = BX / 16 / NW;
+  static_assert(BX % (16 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
   uint32_t off[UNITS];
   const char* start;  // the tile's first element at k = 0
   int64_t step;       // bytes of an element along K
@@ -138,11 +138,11 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
   __device__ static __forceinline__ int row_of(int u, int wave, int lane) { return (wave * UNITS + u) * RU + lane / PR; }
   __device__ static __forceinline__ int piece_of(int row, int lane) {
     const int slot = lane % PR;
-    if constexpr (KC) return slot ^ (row & 7);
+    if constexpr (KC) return slot ^ ((row >> 2) & 3);
     if constexpr (ES == 2) return slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
     return slot ^ (((row >> 2) & 3) << 2);
   }
-  __device__ __forceinline__ TileLoad(const T* p, int64_t ld, int64_t x0, int64_t X, int wave, int lane) {
+  __device__ __forceinline__ void open(const T* p, int64_t ld, int64_t x0, int64_t X, int wave, int lane) {
     start = (const char*)(p + x0 * (KC ? ld : 1));
     step = (KC ? 1 : ld) * ES;
     const int64_t left = X - x0;
@@ -172,23 +172,22 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
   }
 };
 
-// The fragment of columns (or rows) c.. of K elements DEPTH h ..
+// The fragment of columns (or rows) c .. c + 15.
 template <typename T, int BX, bool KC>
-__device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int c, int h, int li, int lq) {
+__device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int c, int li, int lq) {
   if constexpr (KC) {
-    const int row = c + li;
-    return *reinterpret_cast<const typename Gemm<T>::Frag*>(lds + row * 128 + (((h * 4 + lq) ^ (row & 7)) << 4));
+    return *reinterpret_cast<const typename Gemm<T>::Frag*>(lds + (c + li) * 64 + ((lq ^ (li >> 2)) << 4));
   } else if constexpr (sizeof(T) == 2) {
     constexpr int RB = BX * 2;
     typedef __attribute__((address_space(3))) s4 lds_s4;
-    const int row = h * 32 + 8 * lq + (li >> 2), f = (li >> 2) | ((lq & 1) << 2);
+    const int row = 8 * lq + (li >> 2), f = (li >> 2) | ((lq & 1) << 2);
     const char* p = lds + row * RB + (((c >> 4) ^ f) << 5) + (li & 3) * 8;
     const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
     const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * RB));
     return __builtin_bit_cast(bf8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
   } else {
     constexpr int RB = BX * 4;
-    const char* p = lds + (h * 16 + 4 * lq) * RB + (((c >> 4) ^ lq) << 6) + li * 4;
+    const char* p = lds + 4 * lq * RB + (((c >> 4) ^ lq) << 6) + li * 4;
     f4 v;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = *reinterpret_cast<const float*>(p + j * RB);
@@ -207,9 +206,11 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, i
   *n = __builtin_amdgcn_readfirstlane(in / rows);
 }
 
-// A wave's outputs through its part of the LDS (rows of WN elements, 16-byte piece p of row m in slot p ^ (m & 7)), so
-// that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout gives 32-byte pieces.  Rows and
-// columns past the end are computed from the last ones' operands and not stored.
+// LDS of a wave's outputs on their way out: rows of one fragment
+template <typename T, int WN> constexpr int out_lds() { return 16 * WN * (int)sizeof(T); }
+
+// A wave's outputs through its own part of the LDS, 16 rows at a time (16-byte piece p of row m in slot p ^ (m & 7)), so that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout
+// gives 32-byte pieces.  Rows and columns past the end are computed from the last ones' operands and not stored.
 template <typename T, int ACT, int WM, int WN>
 __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
                                          char* mine, int lane) {
@@ -254,54 +255,90 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
       const int byte = (j * 16 + lq * 4) * ES;
-      *reinterpret_cast<Quad<T>*>(mine + (i * 16 + li) * RB + (((byte >> 4) ^ (li & SW)) << 4) + (byte & 15)) = round_quad(c[j], T());
+      *reinterpret_cast<Quad<T>*>(mine + li * RB + (((byte >> 4) ^ (li & SW)) << 4) + (byte & 15)) = round_quad(c[j], T());
     }
-  }
-  typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 #pragma unroll
-  for (int u = 0; u < WM * PR / 64; ++u) {
-    const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
-    const int64_t m = m0 + row, col = n0 + ((slot ^ (row & SW)) * EP);
-    const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
-    if (m < g.M && col < g.N) *reinterpret_cast<u4*>((T*)g.out + m * g.N + col) = v;
+    for (int u = 0; u < 16 * PR / 64; ++u) {
+      const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
+      const int64_t m = m0 + i * 16 + row, col = n0 + ((slot ^ (row & SW)) * EP);
+      const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
+      if (m < g.M && col < g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>((T*)g.out + m * g.N + col));
+    }
   }
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int OCC, bool AK, bool BK>
+// Work-groups stay: each takes every gridDim-th item (a tile and a part of the K axis), and the loads run NB - 1 steps
+// ahead of the products over the borders of the items, so that neither an item's first loads nor its stores are waited
+// for.  NB buffers of a step and the LDS of each wave's outputs.
+template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC, bool AK, bool BK>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_kernel(GemmArgs g) {
-  constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16;
-  __shared__ __align__(1024) char lds[2][(BM + BN) * 128];
+  constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16, STEP = (BM + BN) * 64;
+  __shared__ __align__(1024) char lds[NB * STEP + NW * out_lds<T, WN>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lq = lane >> 4;
-  int64_t tm, tn;
-  tile_of(blockIdx.x, (uint32_t)((g.M + BM - 1) / BM), (uint32_t)((g.N + BN - 1) / BN), &tm, &tn);
-  const int64_t m0 = tm * BM, n0 = tn * BN;
-  const int64_t per = ((g.K + g.splits - 1) / g.splits + KB - 1) / KB * KB;
-  const int64_t k0 = blockIdx.y * per, k1 = k0 + per < g.K ? k0 + per : g.K;
   const int wm = wave / (BN / WN) * WM, wn = wave % (BN / WN) * WN;
-  const TileLoad<T, BM, NW, AK> load_a((const T*)g.A, AK ? g.sam : g.sak, m0, g.M, wave, lane);
-  const TileLoad<T, BN, NW, BK> load_b((const T*)g.B, BK ? g.sbn : g.sbk, n0, g.N, wave, lane);
-  auto load = [&](int64_t k, int buf) {
-    load_a(k, k1, lds[buf], wave, lane);
-    load_b(k, k1, lds[buf] + BM * 128, wave, lane);
+  const uint32_t mt = (uint32_t)((g.M + BM - 1) / BM), nt = (uint32_t)((g.N + BN - 1) / BN), tiles = mt * nt, items = tiles * g.splits;
+  const int64_t per = ((g.K + g.splits - 1) / g.splits + KB - 1) / KB * KB;  // (no part is empty: see linear_plan)
+  typedef TileLoad<T, BM, NW, AK> LoadA;
+  typedef TileLoad<T, BN, NW, BK> LoadB;
+  constexpr int UNITS = LoadA::UNITS + LoadB::UNITS;  // loads of a step by one wave
+
+  // the next step to load: item, and where in its part of the K axis
+  LoadA load_a;
+  LoadB load_b;
+  uint32_t next = blockIdx.x;
+  int64_t nk = 0, nk1 = 0;
+  auto open = [&] {
+    int64_t tm, tn;
+    const uint32_t part = next / tiles;
+    tile_of(next - part * tiles, mt, nt, &tm, &tn);
+    nk = part * per;
+    nk1 = nk + per < g.K ? nk + per : g.K;
+    load_a.open((const T*)g.A, AK ? g.sam : g.sak, tm * BM, g.M, wave, lane);
+    load_b.open((const T*)g.B, BK ? g.sbn : g.sbk, tn * BN, g.N, wave, lane);
   };
-  f4 acc[FM][FN] = {};
-  const int steps = k1 > k0 ? (int)((k1 - k0 + KB - 1) / KB) : 0;
-  if (steps > 0) load(k0, 0);
-  for (int s = 0; s < steps; ++s) {
-    wait_vm<0>();  // this wave's pieces of step s are there, and past the barrier everyone's;
-    __builtin_amdgcn_s_barrier();  // the other buffer has been read by all
-    asm volatile("" ::: "memory");
-    if (s + 1 < steps) load(k0 + (int64_t)(s + 1) * KB, (s + 1) & 1);
-    const char* la = lds[s & 1];
-    const char* lb = la + BM * 128;
+  int ahead = 0;  // steps loaded or on their way that are not multiplied yet
+  auto prefetch = [&](int buf) {
+    if (next >= items) return;
+    load_a(nk, nk1, lds + buf * STEP, wave, lane);
+    load_b(nk, nk1, lds + buf * STEP + BM * 64, wave, lane);
+    ++ahead;
+    nk += KB;
+    if (nk >= nk1) {
+      next += gridDim.x;
+      if (next < items) open();
+    }
+  };
+  open();
 #pragma unroll
-    for (int h = 0; h < KB / Gemm<T>::DEPTH; ++h) {
+  for (int b = 0; b < NB - 1; ++b) prefetch(b);
+
+  int buf = 0;
+  bool waited = false;
+  for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+    int64_t tm, tn;
+    const uint32_t part = item / tiles;
+    tile_of(item - part * tiles, mt, nt, &tm, &tn);
+    const int64_t m0 = tm * BM, n0 = tn * BN, k0 = part * per, k1 = k0 + per < g.K ? k0 + per : g.K;
+    f4 acc[FM][FN] = {};
+    for (int64_t k = k0; k < k1; k += KB) {
+      // this wave's pieces of the step are there (loads arrive in order), and past the barrier everyone's; the buffer of
+      // the step before has been read by all
+      if (!waited) {
+        if (ahead >= NB - 1) wait_vm<(NB - 2) * UNITS>(); else wait_vm<0>();
+      }
+      waited = false;
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      prefetch(buf == 0 ? NB - 1 : buf - 1);
+      const char* la = lds + buf * STEP;
+      const char* lb = la + BM * 64;
       typename Gemm<T>::Frag fb[FN];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = fragment<T, BN, BK>(lb, wn + j * 16, h, li, lq);
+      for (int j = 0; j < FN; ++j) fb[j] = fragment<T, BN, BK>(lb, wn + j * 16, li, lq);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const auto fa = fragment<T, BM, AK>(la, wm + i * 16, h, li, lq);
+        const auto fa = fragment<T, BM, AK>(la, wm + i * 16, li, lq);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           if constexpr (sizeof(T) == 2)
@@ -310,30 +347,32 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
             acc[i][j] = mma_f32(fb[j], fa, acc[i][j]);
         }
       }
+      --ahead;
+      buf = buf == NB - 1 ? 0 : buf + 1;
     }
-  }
-  if (g.splits > 1) {
-    float* part = g.part + blockIdx.y * g.M * g.N;
+    // the next step's loads are waited for before the stores are issued, so that no step waits for the stores
+    if (ahead >= NB - 1) wait_vm<(NB - 2) * UNITS>(); else wait_vm<0>();
+    waited = true;
+    if (g.splits > 1) {
+      float* o = g.part + part * g.M * g.N;
 #pragma unroll
-    for (int i = 0; i < FM; ++i) {
-      const int64_t m = m0 + wm + i * 16 + li;
+      for (int i = 0; i < FM; ++i) {
+        const int64_t m = m0 + wm + i * 16 + li;
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const int64_t n = n0 + wn + j * 16 + lq * 4;
-        if (m < g.M && n < g.N) *reinterpret_cast<f4*>(part + m * g.N + n) = acc[i][j];
+        for (int j = 0; j < FN; ++j) {
+          const int64_t n = n0 + wn + j * 16 + lq * 4;
+          if (m < g.M && n < g.N) *reinterpret_cast<f4*>(o + m * g.N + n) = acc[i][j];
+        }
       }
+      continue;
     }
-    return;
-  }
-  __builtin_amdgcn_s_barrier();  // the operands' LDS has been read by all
-  asm volatile("" ::: "memory");
-  char* mine = lds[0] + wave * (2 * (BM + BN) * 128 / NW);
-  static_assert(WM * WN * sizeof(T) <= 2 * (BM + BN) * 128 / NW, "a wave's outputs fit into its share of the LDS");
-  switch (g.act) {
-    case ACT_RELU: tile_out<T, ACT_RELU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-    case ACT_SILU: tile_out<T, ACT_SILU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-    case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-    default: tile_out<T, ACT_NONE, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
+    char* mine = lds + NB * STEP + wave * out_lds<T, WN>();
+    switch (g.act) {
+      case ACT_RELU: tile_out<T, ACT_RELU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      case ACT_SILU: tile_out<T, ACT_SILU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      default: tile_out<T, ACT_NONE, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
+    }
   }
 }
 
@@ -380,34 +419,37 @@ int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast) {
   LinearPlan p{};
   auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 && K >= 1024 ? 256 : 128;
-  const int64_t t = tiles(p.tile), want = fast ? 512 : 512;
+  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 ? 256 : 128;
+  const int64_t t = tiles(p.tile), want = fast ? 256 : 512;
   int64_t s = t > 0 ? want / t : 1;
   if (s > K / 256) s = K / 256;
-  p.splits = (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+  s = s < 1 ? 1 : s > 64 ? 64 : s;
+  const int64_t kb = 64 / es, per = ((K + s - 1) / s + kb - 1) / kb * kb;  // whole steps, and no part without any
+  p.splits = per > 0 ? (int)((K + per - 1) / per) : 1;
   return p;
 }
 
 namespace {
-template <typename T, int BM, int BN, int WM, int WN, int OCC>
+template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC>
 void launch_tiles(const GemmArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)(((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN)), (unsigned)a.splits);
+  const int64_t items = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
+  const dim3 grid((unsigned)(items < 512 ? items : 512));  // (two work-groups on each of 256 compute units)
   constexpr int NT = 64 * (BM / WM) * (BN / WN);
   if (a.sak == 1 && a.sbk == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, true, true><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, true, true><<<grid, NT, 0, st>>>(a);
   else if (a.sak == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, true, false><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, true, false><<<grid, NT, 0, st>>>(a);
   else
-    gemm_tile_kernel<T, BM, BN, WM, WN, OCC, false, false><<<grid, NT, 0, st>>>(a);
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, false, false><<<grid, NT, 0, st>>>(a);
 }
 }  // namespace
 
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
   if (a.tile == 256) {
-    if constexpr (sizeof(T) == 2) launch_tiles<T, 256, 256, 128, 64, 2>(a, st);
+    if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, 2>(a, st);
   } else if (a.tile == 128) {
-    launch_tiles<T, 128, 128, 64, 32, 4>(a, st);
+    launch_tiles<T, 128, 128, 64, 64, 4, 2>(a, st);
   } else {
     const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64);
     gemm_any_kernel<T><<<dim3((unsigned)tiles, (unsigned)a.splits), 256, 0, st>>>(a);
