@@ -582,19 +582,23 @@ int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtyp
  *   x         R rows of K consecutive elements of dt, ldx >= K elements apart
  *   W         [K][N] of dt; bias [N] float32 or NULL
  *   residual  [R][N] of dt or NULL; y [R][N] of dt (may be the residual itself)
- *   pre       [R][N] float32 or NULL: receives pre, which the backward needs unless act is none
- *             (float32, since db sums what its rounding would be: with a bf16 pre the bias
- *             gradient is off by 2.6e-3 of its size)
+ *   pre       [R][N] float32 or NULL: receives pre for the backward, where
+ *             resonator_linear_keeps_pre(dt, act, K) says that keeping it costs less than
+ *             computing it again (float32, since db sums what its rounding would be: with a
+ *             bf16 pre the bias gradient is off by 2.6e-3 of its size)
  *   act       RES_ACT_*: none; relu; silu = v sigmoid(v);
  *             gelu_tanh = v/2 (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3)))
  * Sums, bias, activation and residual are float32, rounded once to dt.  Sums run in
  * an order that depends on the sizes alone.  K, N >= 1, R >= 0.
  *   ws        resonator_linear_workspace_bytes(0, ...) bytes (may be none), 256-byte
- *             aligned; contents need not be initialised
+ *             aligned; contents need not be initialised.  `loose` of the query: x, W or dy are
+ *             not 16-byte aligned, or K, N or ldx are not multiples of 16 bytes; such operands
+ *             are copied into the workspace first
  * Outputs must not overlap inputs or each other otherwise.
  */
 enum { RES_ACT_NONE = 0, RES_ACT_RELU = 1, RES_ACT_SILU = 2, RES_ACT_GELU_TANH = 3 };
-size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N);
+size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N, int loose);
+int resonator_linear_keeps_pre(res_dtype_t dt, int act, int64_t K);
 int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, int act,
                          const void* residual, void* y, float* pre, int64_t R, int64_t K, int64_t N, void* ws,
                          size_t ws_bytes, void* stream);
@@ -605,14 +609,15 @@ int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
  *                              the gradient that reaches x on another path)
  *   dW = x^T dpre              [K][N] of dt, or NULL
  *   db = sum over rows of dpre [N] float32, or NULL
- * (the forward's own residual has the gradient dy).  pre is the forward's (not read
- * when act is none); x may be NULL without dW, W without dx.  For bf16 the products
+ * (the forward's own residual has the gradient dy).  pre is the forward's, or NULL: it is
+ * then computed again from x, W and bias, unless act is none.  Where pre is given or not
+ * needed, bias is not read, and x may be NULL without dW, W without dx.  For bf16 the products
  * take dpre rounded to bf16; db sums it unrounded.  With R = 0, dW and db are zero.
  * ws: resonator_linear_workspace_bytes(1, ...).
  */
-int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const void* dy, const float* pre,
-                         int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K, int64_t N,
-                         void* ws, size_t ws_bytes, void* stream);
+int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, const void* dy,
+                         const float* pre, int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K,
+                         int64_t N, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * AdamW step over many tensors (one launch for up to 64 of them):

@@ -36,7 +36,7 @@ SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd"
            "resonator_fwd_status_noalloc",
            "resonator_gated_scan_workspace_bytes", "resonator_gated_scan_fwd", "resonator_gated_scan_bwd",
            "resonator_gated_scan_step",
-           "resonator_linear_workspace_bytes", "resonator_linear_fwd", "resonator_linear_bwd",
+           "resonator_linear_workspace_bytes", "resonator_linear_keeps_pre", "resonator_linear_fwd", "resonator_linear_bwd",
            "resonator_adamw_step", "resonator_adamw_values")
 
 class Rows(ctypes.Structure):
@@ -168,11 +168,13 @@ def _declare(lib):
     lib.resonator_gated_scan_step.restype = i32
     lib.resonator_gated_scan_step.argtypes = [Rows, Rows, Rows, i32, vp, i64, i64, fp, fp, fp, vp]
     lib.resonator_linear_workspace_bytes.restype = sz
-    lib.resonator_linear_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i64]
+    lib.resonator_linear_workspace_bytes.argtypes = [i32, i32, i32, i64, i64, i64, i32]
+    lib.resonator_linear_keeps_pre.restype = i32
+    lib.resonator_linear_keeps_pre.argtypes = [i32, i32, i64]
     lib.resonator_linear_fwd.restype = i32
     lib.resonator_linear_fwd.argtypes = [vp, i64, vp, i32, fp, i32, vp, vp, vp, i64, i64, i64, vp, sz, vp]
     lib.resonator_linear_bwd.restype = i32
-    lib.resonator_linear_bwd.argtypes = [vp, i64, vp, i32, vp, vp, i32, vp, vp, vp, fp, i64, i64, i64, vp, sz, vp]
+    lib.resonator_linear_bwd.argtypes = [vp, i64, vp, i32, fp, vp, fp, i32, vp, vp, vp, fp, i64, i64, i64, vp, sz, vp]
     f64 = ctypes.c_double
     lib.resonator_adamw_step.restype = i32
     lib.resonator_adamw_step.argtypes = [ctypes.POINTER(AdamWTensor), i64, i32, i32, ctypes.POINTER(AdamWState),

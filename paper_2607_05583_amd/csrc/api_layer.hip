@@ -247,30 +247,175 @@ int check_linear(int64_t R, int64_t K, int64_t N, res_dtype_t dt, int act) {
 }
 
 size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
-// room for the parts of a split product, whichever kernel its operands' alignment allows
-size_t split_bytes(int64_t M, int64_t N, int64_t K, size_t es) {
-  size_t most = 0;
-  for (bool fast : {false, true}) {
-    const int64_t s = linear_plan(M, N, K, es, fast).splits;
-    if (s > 1) most = std::max(most, (size_t)(s * M * N) * 4);
+int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Whether pre is computed again in the backward rather than kept: the product costs 2 R K N operations, keeping pre 8 R N
+// bytes written and read.  At 65536 x 256 x 1024 bf16 (R, K, N) the step took 475 us keeping it.
+bool computes_pre(res_dtype_t dt, int act, int64_t K) { return act != RES_ACT_NONE && K <= (dt == RES_BF16 ? 512 : 96); }
+
+// The workspace, a piece at a time; with a null base it only counts.
+struct Pieces {
+  char* base;
+  size_t off;
+  void* take(size_t bytes) {
+    void* p = base != nullptr ? base + off : nullptr;
+    off += up256(bytes);
+    return p;
   }
-  return most;
-}
-size_t linear_fwd_bytes(res_dtype_t dt, int64_t R, int64_t K, int64_t N) { return up256(split_bytes(R, N, K, elt(dt))); }
-struct LinearBwdLayout {
-  size_t dpre, part, split, total;
 };
-LinearBwdLayout linear_bwd_layout(res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N) {
-  LinearBwdLayout w{};
-  size_t off = 0;
-  w.dpre = off;
-  if (act != RES_ACT_NONE) off += up256((size_t)(R * N) * elt(dt));
-  w.part = off;
-  off += up256((size_t)(linear_row_blocks(R) * N) * 4);
-  w.split = off;
-  off += up256(std::max(split_bytes(R, K, N, elt(dt)), split_bytes(K, N, R, elt(dt))));
-  w.total = off;
-  return w;
+
+// An operand of a product: [rows][cols] at distance ld.  `k`: its K axis is the consecutive one.
+struct Operand {
+  const void* p;
+  int64_t ld, rows, cols;
+};
+bool whole(const Operand& o, size_t es) {
+  const int64_t ep = 16 / (int64_t)es;
+  return aligned(o.p, 16) && o.ld % ep == 0 && o.cols % ep == 0 && o.ld < (1 << 21);  // (32-bit offsets within a tile)
+}
+// The operand as the kernels take it, copied where it is not.
+hipError_t pack(Operand* o, res_dtype_t dt, bool loose, Pieces* ws, bool count, hipStream_t st) {
+  const size_t es = elt(dt);
+  if (!loose || (!count && whole(*o, es))) return hipSuccess;
+  const int64_t to = up(o->cols, 16 / (int64_t)es);
+  void* dst = ws->take((size_t)(o->rows * to) * es);
+  if (count) return hipSuccess;
+  const hipError_t e = dt == RES_BF16 ? launch_pack<bf16_t>(o->p, o->ld, o->rows, o->cols, dst, to, st)
+                                      : launch_pack<float>(o->p, o->ld, o->rows, o->cols, dst, to, st);
+  o->p = dst;
+  o->ld = to;
+  return e;
+}
+
+// C [M][N] from A and B whose K axis is consecutive (ak, bk) or not; `count` only counts the workspace.
+hipError_t gemm(res_dtype_t dt, GemmArgs& g, const Operand& A, const Operand& B, bool ak, bool bk, bool loose, Pieces ws,
+                size_t* need, hipStream_t st) {
+  const size_t es = elt(dt);
+  const int64_t ep = 16 / (int64_t)es;
+  g.ak = ak;
+  g.bk = bk;
+  g.A = A.p;
+  g.B = B.p;
+  g.lda = A.ld;
+  g.ldb = B.ld;
+  g.xa = ak ? A.rows : up(A.cols, ep);
+  g.xb = bk ? B.rows : up(B.cols, ep);
+  g.loose = g.N % ep != 0 || !(aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) && aligned(g.pre, 16) && aligned(g.dy, 16));
+  if (need != nullptr) {  // (the outputs' alignment is not known yet)
+    for (bool wide : {false, true}) {
+      const int64_t s = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, wide).splits;
+      *need = std::max(*need, ws.off + (s > 1 ? up256((size_t)(s * g.M * g.N) * 4) : 0));
+    }
+    return hipSuccess;
+  }
+  const LinearPlan p = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, !g.loose && g.dy == nullptr);
+  g.tile = p.tile;
+  g.splits = p.splits;
+  g.part = static_cast<float*>(ws.take(p.splits > 1 ? (size_t)(p.splits * g.M * g.N) * 4 : 0));
+  return dt == RES_BF16 ? launch_gemm<bf16_t>(g, st) : launch_gemm<float>(g, st);
+}
+
+struct LinearCall {
+  const void *x, *W;
+  int64_t ldx;
+  res_dtype_t dt;
+  int act;
+  int64_t R, K, N;
+  bool loose;  // operands that may have to be copied
+};
+
+// The forward's launches; `need` counts the workspace instead.
+hipError_t linear_fwd(const LinearCall& c, const float* bias, const void* residual, void* y, float* pre, Pieces ws, size_t* need,
+                      hipStream_t st) {
+  Operand x{c.x, c.ldx, c.R, c.K}, W{c.W, c.N, c.K, c.N};
+  hipError_t e = pack(&x, c.dt, c.loose, &ws, need != nullptr, st);
+  if (e == hipSuccess) e = pack(&W, c.dt, c.loose, &ws, need != nullptr, st);
+  if (e != hipSuccess) return e;
+  GemmArgs g{};
+  g.M = c.R;
+  g.N = c.N;
+  g.K = c.K;
+  g.bias = bias;
+  g.res = residual;
+  g.pre = pre;
+  g.out = y;
+  g.act = c.act;
+  return gemm(c.dt, g, x, W, true, false, c.loose, ws, need, st);
+}
+
+// The backward's launches; `need` counts the workspace instead (then pre and dx, dW, db only say what is asked for).
+hipError_t linear_bwd(const LinearCall& c, const float* bias, const void* dy, const float* pre, const void* residual, void* dx,
+                      void* dW, float* db, Pieces ws, size_t* need, hipStream_t st) {
+  const bool count = need != nullptr, again = c.act != RES_ACT_NONE && pre == nullptr && c.R > 0;
+  const size_t es = elt(c.dt);
+  Operand x{c.x, c.ldx, c.R, c.K}, W{c.W, c.N, c.K, c.N}, d{dy, c.N, c.R, c.N};
+  hipError_t e = hipSuccess;
+  if (dW != nullptr || again) e = pack(&x, c.dt, c.loose, &ws, count, st);
+  if (e == hipSuccess && (dx != nullptr || again)) e = pack(&W, c.dt, c.loose, &ws, count, st);
+  if (e != hipSuccess) return e;
+  int64_t blocks = 0;
+  float* part = nullptr;
+  if (c.act != RES_ACT_NONE || db != nullptr) {
+    blocks = again ? linear_col_blocks(c.R) : linear_row_blocks(c.R);
+    if (db != nullptr) part = static_cast<float*>(ws.take((size_t)(blocks * c.N) * 4));
+    void* out = c.act != RES_ACT_NONE ? ws.take((size_t)(c.R * c.N) * es) : nullptr;
+    if (again) {
+      GemmArgs g{};
+      g.M = c.R;
+      g.N = c.N;
+      g.K = c.K;
+      g.bias = bias;
+      g.out = out;
+      g.act = c.act;
+      g.dy = count ? &g : dy;
+      g.colpart = part;
+      e = gemm(c.dt, g, x, W, true, false, c.loose, ws, need, st);
+    } else if (!count && c.R > 0) {
+      const bool loose = c.N % 4 != 0 || !(aligned(dy, 16) && aligned(pre, 16));
+      e = c.dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, pre, c.act, out, part, c.R, c.N, loose, st)
+                           : launch_act_bwd<float>(dy, pre, c.act, out, part, c.R, c.N, loose, st);
+    }
+    if (e == hipSuccess && !count && db != nullptr) e = launch_col_sum(part, blocks, c.N, db, st);
+    if (out != nullptr || count) d.p = out;
+  }
+  if (e == hipSuccess && (dx != nullptr || dW != nullptr)) e = pack(&d, c.dt, c.loose, &ws, count, st);
+  if (e == hipSuccess && dx != nullptr && c.R > 0) {
+    GemmArgs g{};
+    g.M = c.R;
+    g.N = c.K;
+    g.K = c.N;
+    g.res = residual;
+    g.out = dx;
+    e = gemm(c.dt, g, d, W, true, true, c.loose, ws, need, st);
+  }
+  if (e == hipSuccess && dW != nullptr) {
+    GemmArgs g{};
+    g.M = c.K;
+    g.N = c.N;
+    g.K = c.R;
+    g.out = dW;
+    e = gemm(c.dt, g, x, d, false, false, c.loose, ws, need, st);
+  }
+  if (count) *need = std::max(*need, ws.off);
+  return e;
+}
+
+size_t linear_bytes(bool backward, const LinearCall& c) {
+  size_t need = 0;
+  char* any = reinterpret_cast<char*>(256);  // stands for what a call asks for; nothing is read
+  if (!backward) {
+    (void)linear_fwd(c, nullptr, nullptr, nullptr, nullptr, Pieces{nullptr, 0}, &need, nullptr);
+  } else {
+    for (const float* pre : {static_cast<const float*>(nullptr), reinterpret_cast<const float*>(any)})
+      (void)linear_bwd(c, nullptr, any, pre, nullptr, any, any, reinterpret_cast<float*>(any), Pieces{nullptr, 0}, &need, nullptr);
+  }
+  return need;
+}
+// whether some operand, as given, is not whole pieces
+bool loose_call(const LinearCall& c, const void* dy) {
+  const size_t es = elt(c.dt);
+  return !((c.x == nullptr || whole(Operand{c.x, c.ldx, c.R, c.K}, es)) && (c.W == nullptr || whole(Operand{c.W, c.N, c.K, c.N}, es)) &&
+           (dy == nullptr || whole(Operand{dy, c.N, c.R, c.N}, es)) && c.K % (16 / (int64_t)es) == 0 && c.N % (16 / (int64_t)es) == 0);
 }
 int check_ws(const void* ws, size_t have, size_t need) {
   if (need == 0) return RES_OK;
@@ -282,28 +427,17 @@ int check_mat(const char* name, const void* p, size_t es, bool needed) {
   if (p == nullptr) return needed ? api_error(RES_ERR_INVALID_ARG, "%s must be non-null", name) : RES_OK;
   return aligned(p, es) ? RES_OK : api_error(RES_ERR_MISALIGNED, "%s must be aligned to its element", name);
 }
-hipError_t gemm(res_dtype_t dt, GemmArgs& g, float* part, hipStream_t st) {
-  // whole 16-byte pieces: rows of both operands, and rows of four outputs at a time
-  const int64_t ep = 16 / (int64_t)elt(dt), lda = g.sak == 1 ? g.sam : g.sak, ldb = g.sbk == 1 ? g.sbn : g.sbk;
-  const int64_t xa = g.sak == 1 ? g.K : g.M, xb = g.sbk == 1 ? g.K : g.N;
-  const bool fast = g.K > 0 && aligned(g.A, 16) && aligned(g.B, 16) && aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) &&
-                    aligned(g.pre, 16) && lda % ep == 0 && ldb % ep == 0 && xa % ep == 0 && xb % ep == 0 && g.N % ep == 0 &&
-                    lda < (1 << 21) && ldb < (1 << 21);  // (a tile's bytes have 32-bit offsets)
-  const LinearPlan p = linear_plan(g.M, g.N, g.K, elt(dt), fast);
-  g.tile = p.tile;
-  g.splits = p.splits;
-  g.part = part;
-  return dt == RES_BF16 ? launch_gemm<bf16_t>(g, st) : launch_gemm<float>(g, st);
-}
 
 }  // namespace
 
 extern "C" {
 
-size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N) {
+size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N, int loose) {
   if (check_linear(R, K, N, dt, act)) return 0;
-  return backward ? linear_bwd_layout(dt, act, R, K, N).total : linear_fwd_bytes(dt, R, K, N);
+  return linear_bytes(backward != 0, LinearCall{nullptr, nullptr, K, dt, act, R, K, N, loose != 0});
 }
+
+int resonator_linear_keeps_pre(res_dtype_t dt, int act, int64_t K) { return act != RES_ACT_NONE && !computes_pre(dt, act, K); }
 
 int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, int act,
                          const void* residual, void* y, float* pre, int64_t R, int64_t K, int64_t N, void* ws,
@@ -317,7 +451,9 @@ int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
   if ((rc = check_mat("x", x, es, true)) || (rc = check_mat("y", y, es, true)) || (rc = check_f32("pre", pre, false)) ||
       (rc = check_mat("residual", residual, es, false)))
     return rc;
-  const size_t need = linear_fwd_bytes(dt, R, K, N);
+  LinearCall c{x, W, ldx, dt, act, R, K, N, false};
+  c.loose = loose_call(c, nullptr);
+  const size_t need = linear_bytes(false, c);
   if ((rc = check_ws(ws, ws_bytes, need))) return rc;
   const Span in[] = {span(x, 0, ldx, 1, R, K, es), flat(W, es * K * N), flat(bias, 4 * N), flat(residual, es * R * N)};
   const Span out[] = {flat(y, es * R * N), flat(pre, 4 * R * N), flat(need ? ws : nullptr, need)};
@@ -328,94 +464,47 @@ int resonator_linear_fwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
     for (int k = 0; k < o; ++k)
       if (touch(out[o], out[k])) return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap each other");
   }
-  GemmArgs g{};
-  g.A = x;
-  g.B = W;
-  g.sam = ldx;
-  g.sak = 1;
-  g.sbk = N;
-  g.sbn = 1;
-  g.M = R;
-  g.N = N;
-  g.K = K;
-  g.bias = bias;
-  g.res = residual;
-  g.pre = pre;
-  g.out = y;
-  g.act = act;
-  return launched(gemm(dt, g, static_cast<float*>(ws), (hipStream_t)stream), "linear launch");
+  return launched(linear_fwd(c, bias, residual, y, pre, Pieces{static_cast<char*>(ws), 0}, nullptr, (hipStream_t)stream), "linear launch");
 }
 
-int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const void* dy, const float* pre,
-                         int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K, int64_t N,
-                         void* ws, size_t ws_bytes, void* stream) {
+int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t dt, const float* bias, const void* dy,
+                         const float* pre, int act, const void* residual, void* dx, void* dW, float* db, int64_t R, int64_t K,
+                         int64_t N, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_linear(R, K, N, dt, act);
   if (rc) return rc;
   const size_t es = elt(dt);
   if (dx == nullptr && dW == nullptr && db == nullptr)
     return api_error(RES_ERR_INVALID_ARG, "one of dx, dW and db must be non-null");
-  if (R > 0 && ((rc = check_mat("dy", dy, es, true)) || (rc = check_f32("pre", pre, act != RES_ACT_NONE)) ||
-                (rc = check_mat("x", x, es, dW != nullptr)) || (rc = check_mat("W", W, es, dx != nullptr))))
+  const bool again = act != RES_ACT_NONE && pre == nullptr;
+  if (R > 0 && ((rc = check_mat("dy", dy, es, true)) || (rc = check_f32("pre", pre, false)) || (rc = check_f32("bias", bias, false)) ||
+                (rc = check_mat("x", x, es, dW != nullptr || again)) || (rc = check_mat("W", W, es, dx != nullptr || again))))
     return rc;
   if ((rc = check_mat("residual", residual, es, false)) || (rc = check_mat("dx", dx, es, false)) ||
       (rc = check_mat("dW", dW, es, false)) || (rc = check_f32("db", db, false)))
     return rc;
-  if (R > 0 && dW != nullptr && (ldx < K || ldx > (1LL << 40)))
+  if (R > 0 && (dW != nullptr || again) && (ldx < K || ldx > (1LL << 40)))
     return api_error(RES_ERR_INVALID_ARG, "ldx must be in [K, 2^40]");
-  const LinearBwdLayout w = linear_bwd_layout(dt, act, R, K, N);
-  if ((rc = check_ws(ws, ws_bytes, w.total))) return rc;
-  const Span in[] = {span(dW ? x : nullptr, 0, ldx, 1, R, K, es), flat(W, es * K * N), flat(dy, es * R * N),
-                     flat(pre, 4 * R * N), flat(residual, es * R * K)};
-  const Span out[] = {flat(dx, es * R * K), flat(dW, es * K * N), flat(db, 4 * N), flat(w.total ? ws : nullptr, w.total)};
+  LinearCall c{dW != nullptr || again ? x : nullptr, dx != nullptr || again ? W : nullptr, ldx, dt, act, R, K, N, false};
+  c.loose = loose_call(c, dy);
+  size_t need = 0;
+  {
+    char* any = reinterpret_cast<char*>(256);
+    (void)linear_bwd(c, nullptr, any, pre != nullptr ? reinterpret_cast<const float*>(any) : nullptr, nullptr, dx, dW, db,
+               Pieces{nullptr, 0}, &need, nullptr);
+  }
+  if ((rc = check_ws(ws, ws_bytes, need))) return rc;
+  const Span in[] = {span(c.x, 0, ldx, 1, R, K, es), flat(c.W, es * K * N), flat(dy, es * R * N), flat(pre, 4 * R * N),
+                     flat(residual, es * R * K), flat(bias, 4 * N)};
+  const Span out[] = {flat(dx, es * R * K), flat(dW, es * K * N), flat(db, 4 * N), flat(need ? ws : nullptr, need)};
   for (int o = 0; o < 4; ++o) {
-    for (int k = 0; k < 5; ++k)
+    for (int k = 0; k < 6; ++k)
       if (touch(out[o], in[k]) && !(o == 0 && k == 4 && dx == residual))
         return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap inputs (dx may be the residual itself)");
     for (int k = 0; k < o; ++k)
       if (touch(out[o], out[k])) return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap each other");
   }
-  hipStream_t st = (hipStream_t)stream;
-  char* base = static_cast<char*>(ws);
-  const void* dpre = dy;
-  hipError_t e = hipSuccess;
-  if (act != RES_ACT_NONE || db != nullptr) {
-    void* o = act != RES_ACT_NONE ? base + w.dpre : nullptr;
-    float* part = db != nullptr ? reinterpret_cast<float*>(base + w.part) : nullptr;
-    const float* p = act != RES_ACT_NONE ? pre : nullptr;
-    e = dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, p, act, o, part, db, R, N, st)
-                       : launch_act_bwd<float>(dy, p, act, o, part, db, R, N, st);
-    if (o != nullptr) dpre = o;
-  }
-  if (e == hipSuccess && dx != nullptr && R > 0) {
-    GemmArgs g{};
-    g.A = dpre;
-    g.B = W;
-    g.sam = N;
-    g.sak = 1;
-    g.sbk = 1;
-    g.sbn = N;
-    g.M = R;
-    g.N = K;
-    g.K = N;
-    g.res = residual;
-    g.out = dx;
-    e = gemm(dt, g, reinterpret_cast<float*>(base + w.split), st);
-  }
-  if (e == hipSuccess && dW != nullptr) {
-    GemmArgs g{};
-    g.A = x;
-    g.B = dpre;
-    g.sam = 1;
-    g.sak = ldx;
-    g.sbk = N;
-    g.sbn = 1;
-    g.M = K;
-    g.N = N;
-    g.K = R;
-    g.out = dW;
-    e = gemm(dt, g, reinterpret_cast<float*>(base + w.split), st);
-  }
-  return launched(e, "linear backward launch");
+  return launched(linear_bwd(c, bias, dy, pre, residual, dx, dW, db, Pieces{static_cast<char*>(ws), 0}, nullptr, (hipStream_t)stream),
+                  "linear backward launch");
 }
 
 }  // extern "C"

@@ -93,37 +93,47 @@ hipError_t launch_gated_step(const Rows& x, const Rows& r, const Rows& i, void* 
 
 
 // ---------------------------------------------------------------------------
-// Linear product with epilogue: C[m][n] = sum_k A(m, k) B(k, n), where
-// A(m, k) = A[m sam + k sak] and B(k, n) = B[k sbk + n sbn] (one stride of each
-// is 1), then out = act(C + bias[n]) + res[m][n]; pre receives C + bias[n].
+// Linear product with epilogue: C[m][n] = sum_k A(m, k) B(k, n), then out =
+// act(C + bias[n]) + res[m][n]; pre receives C + bias[n].
 // ---------------------------------------------------------------------------
+enum { TILE_THIN = 0, TILE_SQUARE = 1, TILE_WIDE = 2 };  // 64 x 128, 128 x 128, 128 x 256 (bf16) outputs of a work-group
+
 struct GemmArgs {
-  const void* A;
-  const void* B;
-  int64_t sam, sak, sbk, sbn;
+  const void* A;      // ak: A(m, k) = A[m lda + k], else A[k lda + m]
+  const void* B;      // bk: B(k, n) = B[n ldb + k], else B[k ldb + n]
+  int64_t lda, ldb;   // 16-byte aligned operands with rows of whole 16-byte pieces (behind K: zeros)
+  int64_t xa, xb;     // rows (ak, bk) or columns that the operands hold: M, N, or padded to whole pieces
+  bool ak, bk;
   int64_t M, N, K;
   const float* bias;  // [N] or null
   const void* res;    // [M][N] or null
   float* pre;         // [M][N] or null
   void* out;          // [M][N]
   int act;
-  int tile;           // tile of a work-group: 64 (any operands), 128 or 256 (16-byte aligned ones)
+  const void* dy;     // [M][N]: out = dy act'(C + bias) instead, and
+  float* colpart;     // [linear_col_blocks][N] or null: the sums of its columns over blocks of rows
+  bool loose;         // out, res, pre, bias or dy not 16-byte aligned, or N not a whole number of 16-byte pieces
+  int tile;           // TILE_*
   int splits;         // parts of the K axis; more than one leave float32 partial sums in `part` [splits][M][N]
   float* part;
 };
 struct LinearPlan {
   int tile, splits;
 };
-// fast: both operands, the outputs and what the epilogue reads are 16-byte aligned with rows of whole 16-byte pieces
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast);
+// whole: the K axis is not cut; wide: the widest tile, which takes neither `loose` nor `dy`, may be taken
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide);
+inline int64_t linear_col_blocks(int64_t M) { return (M + 63) / 64; }  // rows of colpart: one for each wave's rows
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);
-// dpre = dy act'(pre) (out null for the sums alone) and, where part is not null, the sums of its columns over blocks of
-// rows [linear_row_blocks(R)][N], then over the blocks into db
+template <typename T>
+hipError_t launch_pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t to, hipStream_t st);
+// out (or none) = dy act'(pre) (pre null: dy) and, where part is not null, the sums of its columns over blocks of rows
+// [linear_row_blocks(R)][N]
 int64_t linear_row_blocks(int64_t R);
 template <typename T>
-hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, float* db, int64_t R,
-                          int64_t N, hipStream_t st);
+hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, int64_t R, int64_t N, bool loose,
+                          hipStream_t st);
+hipError_t launch_col_sum(const float* part, int64_t blocks, int64_t N, float* db, hipStream_t st);
 
 // ---------------------------------------------------------------------------
 // AdamW over many tensors (states: flat buffers, RES_ADAMW_BLOCK elements a scale)

@@ -1,23 +1,13 @@
 // Linear product with bias, activation and residual, and its gradients:
 //   pre = x W + b, y = act(pre) + residual;
 //   dpre = dy act'(pre), dx = dpre W^T, dW = x^T dpre, db = sum over rows of dpre.
-// All three products are one kernel over strided operands; sums are float32 (MFMA).
+// All products are one tiled kernel over operands of either order; sums are float32 (MFMA).
+// dpre is made by a product too where computing pre again costs less than keeping it.
 #include "layer.h"
 #include "stream.h"
 
 namespace res {
 namespace {
-
-// What a product's element becomes: the epilogue of its row m and column n.
-template <typename T>
-__device__ __forceinline__ void finish(const GemmArgs& g, int64_t m, int64_t n, float c) {
-  const int64_t at = m * g.N + n;
-  if (g.bias != nullptr) c += g.bias[n];
-  if (g.pre != nullptr) g.pre[at] = c;
-  c = act_value(c, g.act);
-  if (g.res != nullptr) c += to_f32(((const T*)g.res)[at]);
-  ((T*)g.out)[at] = from_f32<T>(c);
-}
 
 template <typename T> struct __align__(4 * sizeof(T)) Quad { T v[4]; };
 __device__ __forceinline__ Quad<float> round_quad(const f4& c, float) { return __builtin_bit_cast(Quad<float>, c); }
@@ -25,74 +15,24 @@ __device__ __forceinline__ Quad<bf16_t> round_quad(const f4& c, bf16_t) {
   typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(Quad<bf16_t>, __builtin_convertvector(c, bf4));
 }
-
-// Any sizes, strides and alignments: 64 x 64 outputs of a work-group of four waves
-// (32 x 32 each), 32 terms of the sum at a time through LDS, both operands with the
-// terms of a row or column side by side.
+// Columns n .. n + 3 of a row of N; loose: no alignment, and columns from N on are the last one again.
 template <typename T>
-__global__ __launch_bounds__(256) void gemm_any_kernel(GemmArgs g) {
-  constexpr int BM = 64, BK = 32, PAD = 16 / sizeof(T), LD = BK + PAD;
-  __shared__ __align__(16) T sa[BM * LD], sb[BM * LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int li = lane & 15, lq = lane >> 4;
-  const int64_t tn = (g.N + BM - 1) / BM;
-  const int64_t m0 = (blockIdx.x / tn) * BM, n0 = (blockIdx.x % tn) * BM;
-  const int64_t per = ((g.K + g.splits - 1) / g.splits + BK - 1) / BK * BK;
-  const int64_t k0 = blockIdx.y * per, k1 = k0 + per < g.K ? k0 + per : g.K;
-  f4 acc[2][2] = {};
-  for (int64_t k = k0; k < k1; k += BK) {
+__device__ __forceinline__ f4 load_quad(const T* row, int64_t n, int64_t N, bool loose) {
+  f4 c;
+  if (!loose) {
+    const auto q = *reinterpret_cast<const Quad<T>*>(row + n);
 #pragma unroll
-    for (int e = 0; e < BM * BK / 256; ++e) {
-      const int id = e * 256 + tid;
-      const int am = g.sak == 1 ? id / BK : id % BM, ak = g.sak == 1 ? id % BK : id / BM;
-      const int bn = g.sbk == 1 ? id / BK : id % BM, bk = g.sbk == 1 ? id % BK : id / BM;
-      sa[am * LD + ak] = m0 + am < g.M && k + ak < k1 ? ((const T*)g.A)[(m0 + am) * g.sam + (k + ak) * g.sak] : T(0);
-      sb[bn * LD + bk] = n0 + bn < g.N && k + bk < k1 ? ((const T*)g.B)[(k + bk) * g.sbk + (n0 + bn) * g.sbn] : T(0);
-    }
-    __syncthreads();
-    const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32;
-    if constexpr (sizeof(T) == 2) {
+    for (int r = 0; r < 4; ++r) c[r] = to_f32(q.v[r]);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const bf8 a = *reinterpret_cast<const bf8*>(&sa[(wm + i * 16 + li) * LD + lq * 8]);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf8 b = *reinterpret_cast<const bf8*>(&sb[(wn + j * 16 + li) * LD + lq * 8]);
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, acc[i][j], 0, 0, 0);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int h = 0; h < BK; h += 16)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const f4 a = *reinterpret_cast<const f4*>(&sa[(wm + i * 16 + li) * LD + h + lq * 4]);
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[i][j] = mma_f32(a, *reinterpret_cast<const f4*>(&sb[(wn + j * 16 + li) * LD + h + lq * 4]), acc[i][j]);
-        }
-    }
-    __syncthreads();
+    for (int r = 0; r < 4; ++r) c[r] = to_f32(row[n + r < N ? n + r : N - 1]);
   }
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int64_t m = m0 + (wave >> 1) * 32 + i * 16 + lq * 4 + r, n = n0 + (wave & 1) * 32 + j * 16 + li;
-        if (m < g.M && n < g.N) {
-          if (g.splits > 1)
-            g.part[(blockIdx.y * g.M + m) * g.N + n] = acc[i][j][r];
-          else
-            finish<T>(g, m, n, acc[i][j][r]);
-        }
-      }
+  return c;
 }
 
-
 // ---------------------------------------------------------------------------
-// Tiles of BM x BN outputs for 16-byte aligned operands.  A wave owns WM x WN of
+// Tiles of BM x BN outputs; operands are 16-byte aligned with rows of whole 16-byte
+// pieces (others are copied into such a form first).  A wave owns WM x WN of
 // them in registers; 64 bytes of the K axis at a time (KB elements, the depth of one
 // fragment) go straight to LDS (16 bytes a lane, no registers), the next ones while
 // these are multiplied.
@@ -132,19 +72,20 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
   static constexpr int UNITS = BX / 16 / NW;
   static_assert(BX % (16 * NW) == 0 && RB <= 1024, "whole units of a kilobyte for each wave");
   uint32_t off[UNITS];
-  const char* start;  // the tile's first element at k = 0
-  int64_t step;       // bytes of an element along K
+  const char* base;  // the next step's first element (the same in all lanes)
+  int64_t step;      // bytes of a step
 
   __device__ static __forceinline__ int row_of(int u, int wave, int lane) { return (wave * UNITS + u) * RU + lane / PR; }
   __device__ static __forceinline__ int piece_of(int row, int lane) {
     const int slot = lane % PR;
     if constexpr (KC) return slot ^ ((row >> 2) & 3);
-    if constexpr (ES == 2) return slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+    if constexpr (ES == 2 && RB >= 256) return slot ^ (((row & 3) | ((row >> 1) & 4)) << 1);
+    if constexpr (ES == 2) return slot ^ ((((row >> 1) & 1) | ((row >> 2) & 2)) << 1);  // (four granules a row)
     return slot ^ (((row >> 2) & 3) << 2);
   }
-  __device__ __forceinline__ void open(const T* p, int64_t ld, int64_t x0, int64_t X, int wave, int lane) {
-    start = (const char*)(p + x0 * (KC ? ld : 1));
-    step = (KC ? 1 : ld) * ES;
+  __device__ __forceinline__ void open(const T* p, int64_t ld, int64_t x0, int64_t X, int64_t k0, int wave, int lane) {
+    base = uniform((const char*)(p + x0 * (KC ? ld : 1) + k0 * (KC ? 1 : ld)));
+    step = (KC ? 1 : ld) * ES * Gemm<T>::KB;
     const int64_t left = X - x0;
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
@@ -155,19 +96,19 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
         off[u] = (uint32_t)(row * ld * ES + (piece * EP < left ? piece * EP : left - EP) * ES);
     }
   }
-  // K elements k .. k + KB - 1, those from kend on as zeros
-  __device__ __forceinline__ void operator()(int64_t k, int64_t kend, char* lds, int wave, int lane) const {
-    const char* base = uniform(start + k * step);
-    if (k + Gemm<T>::KB <= kend) {
+  // the next step's elements
+  __device__ __forceinline__ void load(char* lds, int wave) {
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u) lds_dma16(base, off[u], lds + (wave * UNITS + u) * 1024);
-    } else {
+    for (int u = 0; u < UNITS; ++u) lds_dma16(base, off[u], lds + (wave * UNITS + u) * 1024);
+    base = uniform(base + step);
+  }
+  // the same where only `left` elements of the K axis are left: zeros behind them
+  __device__ __forceinline__ void load_last(int left, char* lds, int wave, int lane) {
 #pragma unroll
-      for (int u = 0; u < UNITS; ++u) {
-        const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
-        const void* src = k + (KC ? piece * EP : row) < kend ? (const void*)(base + off[u]) : (const void*)zero_piece;
-        lds_dma16_lane(src, lds + (wave * UNITS + u) * 1024);
-      }
+    for (int u = 0; u < UNITS; ++u) {
+      const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
+      const void* src = (KC ? piece * EP : row) < left ? (const void*)(base + off[u]) : (const void*)zero_piece;
+      lds_dma16_lane(src, lds + (wave * UNITS + u) * 1024);
     }
   }
 };
@@ -180,7 +121,7 @@ __device__ __forceinline__ typename Gemm<T>::Frag fragment(const char* lds, int 
   } else if constexpr (sizeof(T) == 2) {
     constexpr int RB = BX * 2;
     typedef __attribute__((address_space(3))) s4 lds_s4;
-    const int row = 8 * lq + (li >> 2), f = (li >> 2) | ((lq & 1) << 2);
+    const int row = 8 * lq + (li >> 2), f = RB >= 256 ? (li >> 2) | ((lq & 1) << 2) : (li >> 3) | ((lq & 1) << 1);
     const char* p = lds + row * RB + (((c >> 4) ^ f) << 5) + (li & 3) * 8;
     const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)p);
     const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(p + 4 * RB));
@@ -209,20 +150,25 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, i
 // LDS of a wave's outputs on their way out: rows of one fragment
 template <typename T, int WN> constexpr int out_lds() { return 16 * WN * (int)sizeof(T); }
 
-// A wave's outputs through its own part of the LDS, 16 rows at a time (16-byte piece p of row m in slot p ^ (m & 7)), so that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout
-// gives 32-byte pieces.  Rows and columns past the end are computed from the last ones' operands and not stored.
-template <typename T, int ACT, int WM, int WN>
+// A wave's outputs through its own part of the LDS, 16 rows at a time (16-byte piece p of row m in slot p ^ (m & 7)), so
+// that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout gives 32-byte pieces.  The
+// stores are non-temporal (131072 x 256 x 1024 bf16: 139 to 123 us).  Rows and columns past the end are computed from the
+// last ones' operands and not stored.
+// ANY: takes outputs of any alignment (g.loose).  SLOPE: the results are pre, and what is stored is dy act'(pre); its columns' sums go to g.colpart.
+template <typename T, int ACT, bool SLOPE, bool ANY, int WM, int WN>
 __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
                                          char* mine, int lane) {
   constexpr int ES = sizeof(T), RB = WN * ES, PR = RB / 16, EP = 16 / ES, SW = PR < 8 ? PR - 1 : 7, FN = WN / 16;
   const int li = lane & 15, lq = lane >> 4;
-  int64_t n[FN];
-  f4 bias[FN];
+  const bool loose = ANY && g.loose;
+  int n[FN];
+  f4 bias[FN], sum[FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
-    n[j] = n0 + j * 16 + lq * 4;
-    n[j] = n[j] < g.N ? n[j] : g.N - 4;
-    bias[j] = g.bias != nullptr ? *reinterpret_cast<const f4*>(g.bias + n[j]) : f4{};
+    n[j] = (int)n0 + j * 16 + lq * 4;
+    n[j] = n[j] < (int)g.N ? n[j] : ((int)g.N - 1) & ~3;
+    bias[j] = g.bias != nullptr ? load_quad(g.bias, n[j], g.N, loose) : f4{};
+    sum[j] = f4{};
   }
 #pragma unroll
   for (int i = 0; i < WM / 16; ++i) {
@@ -232,25 +178,44 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
     f4 c[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) c[j] = acc[i][j] + bias[j];
-    if (g.pre != nullptr && in) {
+    if constexpr (SLOPE) {
+      f4 d[FN];
 #pragma unroll
-      for (int j = 0; j < FN; ++j)
-        if (n0 + j * 16 + lq * 4 < g.N) *reinterpret_cast<f4*>(g.pre + m * g.N + n[j]) = c[j];
-    }
-    if constexpr (ACT != ACT_NONE) {
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) c[j][r] = act_value(c[j][r], ACT);
-    }
-    if (g.res != nullptr) {
-      Quad<T> q[FN];
-#pragma unroll
-      for (int j = 0; j < FN; ++j) q[j] = *reinterpret_cast<const Quad<T>*>((const T*)g.res + m * g.N + n[j]);
+      for (int j = 0; j < FN; ++j) d[j] = load_quad((const T*)g.dy + m * g.N, n[j], g.N, loose);
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) c[j][r] += to_f32(q[j].v[r]);
+        for (int r = 0; r < 4; ++r) {
+          c[j][r] = d[j][r] * act_slope(c[j][r], ACT);
+          sum[j][r] += in ? c[j][r] : 0.0f;
+        }
+    } else {
+      if (g.pre != nullptr && in) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          if (n0 + j * 16 + lq * 4 < g.N) {
+            if (!loose) {
+              *reinterpret_cast<f4*>(g.pre + m * g.N + n[j]) = c[j];
+            } else {
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (n[j] + r < g.N) g.pre[m * g.N + n[j] + r] = c[j][r];
+            }
+          }
+      }
+      if constexpr (ACT != ACT_NONE) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) c[j][r] = act_value(c[j][r], ACT);
+      }
+      if (g.res != nullptr) {
+        f4 q[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) q[j] = load_quad((const T*)g.res + m * g.N, n[j], g.N, loose);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) c[j] += q[j];
+      }
     }
 #pragma unroll
     for (int j = 0; j < FN; ++j) {
@@ -258,12 +223,36 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
       *reinterpret_cast<Quad<T>*>(mine + li * RB + (((byte >> 4) ^ (li & SW)) << 4) + (byte & 15)) = round_quad(c[j], T());
     }
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    if (!loose) {
 #pragma unroll
-    for (int u = 0; u < 16 * PR / 64; ++u) {
-      const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
-      const int64_t m = m0 + i * 16 + row, col = n0 + ((slot ^ (row & SW)) * EP);
-      const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
-      if (m < g.M && col < g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>((T*)g.out + m * g.N + col));
+      for (int u = 0; u < 16 * PR / 64; ++u) {
+        const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
+        const int64_t mo = m0 + i * 16 + row, col = n0 + ((slot ^ (row & SW)) * EP);
+        const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
+        if (mo < g.M && col < g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>((T*)g.out + mo * g.N + col));
+      }
+    } else {
+      for (int e = lane; e < 16 * WN; e += 64) {
+        const int row = e / WN, byte = e % WN * ES;
+        const int64_t mo = m0 + i * 16 + row, col = n0 + e % WN;
+        const T v = *reinterpret_cast<const T*>(mine + row * RB + (((byte >> 4) ^ (row & SW)) << 4) + (byte & 15));
+        if (mo < g.M && col < g.N) ((T*)g.out)[mo * g.N + col] = v;
+      }
+    }
+  }
+  if constexpr (SLOPE) {
+    if (g.colpart != nullptr && m0 < g.M) {
+      float* part = g.colpart + m0 / WM * g.N;
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v = sum[j][r];
+#pragma unroll
+          for (int k = 1; k < 16; k <<= 1) v += __shfl_xor(v, k, 64);
+          const int64_t col = n0 + j * 16 + lq * 4 + r;
+          if (li == 0 && col < g.N) part[col] = v;
+        }
     }
   }
 }
@@ -271,7 +260,7 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 // Work-groups stay: each takes every gridDim-th item (a tile and a part of the K axis), and the loads run NB - 1 steps
 // ahead of the products over the borders of the items, so that neither an item's first loads nor its stores are waited
 // for.  NB buffers of a step and the LDS of each wave's outputs.
-template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC, bool AK, bool BK>
+template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC, bool ANY, bool AK, bool BK, bool SLOPE>
 __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_kernel(GemmArgs g) {
   constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16, STEP = (BM + BN) * 64;
   __shared__ __align__(1024) char lds[NB * STEP + NW * out_lds<T, WN>()];
@@ -283,45 +272,54 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
   typedef TileLoad<T, BN, NW, BK> LoadB;
   constexpr int UNITS = LoadA::UNITS + LoadB::UNITS;  // loads of a step by one wave
 
-  // the next step to load: item, and where in its part of the K axis
+  // Steps of an item's part of the K axis, and the elements of its last one.
+  auto steps_of = [&](uint32_t part, int* last) {
+    const int64_t k0 = part * per, n = k0 + per < g.K ? per : g.K - k0;
+    const int steps = (int)((n + KB - 1) / KB);
+    *last = __builtin_amdgcn_readfirstlane((int)(n - (int64_t)(steps - 1) * KB));
+    return __builtin_amdgcn_readfirstlane(steps);
+  };
+
+  // the loads: the item they are at, and the steps left of it
   LoadA load_a;
   LoadB load_b;
   uint32_t next = blockIdx.x;
-  int64_t nk = 0, nk1 = 0;
-  auto open = [&] {
-    int64_t tm, tn;
-    const uint32_t part = next / tiles;
-    tile_of(next - part * tiles, mt, nt, &tm, &tn);
-    nk = part * per;
-    nk1 = nk + per < g.K ? nk + per : g.K;
-    load_a.open((const T*)g.A, AK ? g.sam : g.sak, tm * BM, g.M, wave, lane);
-    load_b.open((const T*)g.B, BK ? g.sbn : g.sbk, tn * BN, g.N, wave, lane);
-  };
+  int left = 0, last = 0;
   int ahead = 0;  // steps loaded or on their way that are not multiplied yet
-  auto prefetch = [&](int buf) {
-    if (next >= items) return;
-    load_a(nk, nk1, lds + buf * STEP, wave, lane);
-    load_b(nk, nk1, lds + buf * STEP + BM * 64, wave, lane);
-    ++ahead;
-    nk += KB;
-    if (nk >= nk1) {
+  auto prefetch = [&](int at) {
+    if (left == 0) {
+      if (next >= items) return;
+      int64_t tm, tn;
+      const uint32_t part = next / tiles;
+      tile_of(next - part * tiles, mt, nt, &tm, &tn);
+      left = steps_of(part, &last);
+      load_a.open((const T*)g.A, g.lda, tm * BM, g.xa, part * per, wave, lane);
+      load_b.open((const T*)g.B, g.ldb, tn * BN, g.xb, part * per, wave, lane);
       next += gridDim.x;
-      if (next < items) open();
+    }
+    --left;
+    ++ahead;
+    if (left > 0 || last == KB) {
+      load_a.load(lds + at, wave);
+      load_b.load(lds + at + BM * 64, wave);
+    } else {
+      load_a.load_last(last, lds + at, wave, lane);
+      load_b.load_last(last, lds + at + BM * 64, wave, lane);
     }
   };
-  open();
 #pragma unroll
-  for (int b = 0; b < NB - 1; ++b) prefetch(b);
+  for (int b = 0; b < NB - 1; ++b) prefetch(b * STEP);
 
-  int buf = 0;
+  int at = 0, to = (NB - 1) * STEP;  // buffers of the step that is multiplied and of the one that is loaded meanwhile
   bool waited = false;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     int64_t tm, tn;
     const uint32_t part = item / tiles;
     tile_of(item - part * tiles, mt, nt, &tm, &tn);
-    const int64_t m0 = tm * BM, n0 = tn * BN, k0 = part * per, k1 = k0 + per < g.K ? k0 + per : g.K;
+    const int64_t m0 = tm * BM, n0 = tn * BN;
     f4 acc[FM][FN] = {};
-    for (int64_t k = k0; k < k1; k += KB) {
+    int unused;
+    for (int s = steps_of(part, &unused); s > 0; --s) {
       // this wave's pieces of the step are there (loads arrive in order), and past the barrier everyone's; the buffer of
       // the step before has been read by all
       if (!waited) {
@@ -330,25 +328,30 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
       waited = false;
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
-      prefetch(buf == 0 ? NB - 1 : buf - 1);
-      const char* la = lds + buf * STEP;
+      const char* la = lds + at;
       const char* lb = la + BM * 64;
-      typename Gemm<T>::Frag fb[FN];
+      // all fragments first, so that the products run through (left to itself the compiler reads them two at a time
+      // and waits for each pair)
+      typename Gemm<T>::Frag fb[FN], fa[FM];
 #pragma unroll
       for (int j = 0; j < FN; ++j) fb[j] = fragment<T, BN, BK>(lb, wn + j * 16, li, lq);
 #pragma unroll
+      for (int i = 0; i < FM; ++i) fa[i] = fragment<T, BM, AK>(la, wm + i * 16, li, lq);
+      prefetch(to);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const auto fa = fragment<T, BM, AK>(la, wm + i * 16, li, lq);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           if constexpr (sizeof(T) == 2)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa, acc[i][j], 0, 0, 0);
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
           else
-            acc[i][j] = mma_f32(fb[j], fa, acc[i][j]);
+            acc[i][j] = mma_f32(fb[j], fa[i], acc[i][j]);
         }
       }
       --ahead;
-      buf = buf == NB - 1 ? 0 : buf + 1;
+      to = at;
+      at = at == (NB - 1) * STEP ? 0 : at + STEP;
     }
     // the next step's loads are waited for before the stores are issued, so that no step waits for the stores
     if (ahead >= NB - 1) wait_vm<(NB - 2) * UNITS>(); else wait_vm<0>();
@@ -361,117 +364,228 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
           const int64_t n = n0 + wn + j * 16 + lq * 4;
-          if (m < g.M && n < g.N) *reinterpret_cast<f4*>(o + m * g.N + n) = acc[i][j];
+          if (m >= g.M) continue;
+          if (g.N % 4 == 0) {
+            if (n < g.N) *reinterpret_cast<f4*>(o + m * g.N + n) = acc[i][j];
+          } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (n + r < g.N) o[m * g.N + n + r] = acc[i][j][r];
+          }
         }
       }
       continue;
     }
     char* mine = lds + NB * STEP + wave * out_lds<T, WN>();
     switch (g.act) {
-      case ACT_RELU: tile_out<T, ACT_RELU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      case ACT_SILU: tile_out<T, ACT_SILU, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      default: tile_out<T, ACT_NONE, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
+      case ACT_RELU: tile_out<T, ACT_RELU, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      case ACT_SILU: tile_out<T, ACT_SILU, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
+      default: tile_out<T, ACT_NONE, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
     }
   }
 }
 
-// the parts of a split sum, in order, then the epilogue
-template <typename T>
+// The parts of a split sum (none: zeros), in order, then the epilogue.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs g) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, n = g.M * g.N;
-  if (id >= n) return;
-  float c = 0.0f;
-  for (int s = 0; s < g.splits; ++s) c += g.part[s * n + id];
-  finish<T>(g, id / g.N, id % g.N, c);
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * V, all = g.M * g.N;
+  if (at >= all) return;
+  const int64_t n = at % g.N;
+  float c[V] = {};
+  for (int s = 0; s < g.splits; ++s) {
+    if constexpr (V == 4) {
+      const f4 p = *reinterpret_cast<const f4*>(g.part + s * all + at);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) c[r] += p[r];
+    } else {
+      c[0] += g.part[s * all + at];
+    }
+  }
+#pragma unroll
+  for (int r = 0; r < V; ++r) {
+    if (g.bias != nullptr) c[r] += g.bias[n + r];
+    if (g.pre != nullptr) g.pre[at + r] = c[r];
+    c[r] = act_value(c[r], g.act);
+    if (g.res != nullptr) c[r] += to_f32(((const T*)g.res)[at + r]);
+    ((T*)g.out)[at + r] = from_f32<T>(c[r]);
+  }
 }
 
-// dpre and the sums of its columns: a work-group takes ACT_ROWS rows of 256 columns
-constexpr int ACT_ROWS = 128;
+// An operand [rows][cols] with any start and ld as rows of `to` elements (whole 16-byte pieces), zeros behind cols.
 template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(const T* src, int64_t ld, int64_t rows, int64_t cols, T* dst, int64_t to) {
+  constexpr int EP = 16 / sizeof(T);
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = to / EP;
+  if (id >= rows * per) return;
+  const int64_t row = id / per, c = (id - row * per) * EP;
+  struct __align__(16) Piece { T v[EP]; } o;
+#pragma unroll
+  for (int e = 0; e < EP; ++e) o.v[e] = c + e < cols ? src[row * ld + c + e] : T(0);
+  *reinterpret_cast<Piece*>(dst + row * to + c) = o;
+}
+
+// dpre from a kept pre, and the sums of its columns over ACT_ROWS rows: a work-group takes 256 columns (four a lane, or
+// one where V is 1), its four waves every fourth row.
+constexpr int ACT_ROWS = 64;
+template <typename T, int V>
 __global__ __launch_bounds__(256) void act_bwd_kernel(const T* dy, const float* pre, int act, T* out, float* part, int64_t R,
                                                       int64_t N) {
-  const int64_t cols = (N + 255) / 256, block = blockIdx.x / cols;
-  const int64_t n = (blockIdx.x % cols) * 256 + threadIdx.x, r0 = block * ACT_ROWS;
-  if (n >= N) return;
-  float sum = 0.0f;
-  for (int64_t r = r0; r < R && r < r0 + ACT_ROWS; ++r) {
-    const float d = to_f32(dy[r * N + n]) * (pre != nullptr ? act_slope(pre[r * N + n], act) : 1.0f);
-    if (out != nullptr) out[r * N + n] = from_f32<T>(d);
-    sum += d;
+  __shared__ float sums[4][64 * V];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t cols = (N + 64 * V - 1) / (64 * V), block = blockIdx.x / cols;
+  const int64_t n = (blockIdx.x % cols) * (64 * V) + lane * V, r0 = block * ACT_ROWS;
+  float sum[V] = {};
+  if (n < N) {
+#pragma unroll 4
+    for (int k = 0; k < ACT_ROWS / 4; ++k) {
+      const int64_t r = r0 + k * 4 + wave, at = r * N + n;
+      if (r >= R) break;
+      float d[V], p[V];
+      if constexpr (V == 4) {
+        const f4 q = load_quad(dy + r * N, n, N, false);
+        const f4 z = pre != nullptr ? *reinterpret_cast<const f4*>(pre + at) : f4{};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] = q[e], p[e] = z[e];
+      } else {
+        d[0] = to_f32(dy[at]);
+        p[0] = pre != nullptr ? pre[at] : 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if (pre != nullptr) d[e] *= act_slope(p[e], act);
+        sum[e] += d[e];
+      }
+      if (out != nullptr) {
+        if constexpr (V == 4)
+          *reinterpret_cast<Quad<T>*>(out + at) = round_quad(f4{d[0], d[1], d[2], d[3]}, T());
+        else
+          out[at] = from_f32<T>(d[0]);
+      }
+    }
   }
-  if (part != nullptr) part[block * N + n] = sum;
+#pragma unroll
+  for (int e = 0; e < V; ++e) sums[wave][lane * V + e] = sum[e];
+  __syncthreads();
+  if (part != nullptr && wave == 0 && n < N)
+#pragma unroll
+    for (int e = 0; e < V; ++e)
+      part[block * N + n + e] = (sums[0][lane * V + e] + sums[1][lane * V + e]) + (sums[2][lane * V + e] + sums[3][lane * V + e]);
 }
-__global__ __launch_bounds__(256) void col_sum_kernel(const float* part, int64_t blocks, int64_t N, float* db) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
+
+// db = sums of the columns of part [blocks][N]: 16 columns of a work-group, its 64 rows of threads every 64th block, then
+// their sums in order, in float64.
+__global__ __launch_bounds__(1024) void col_sum_kernel(const float* part, int64_t blocks, int64_t N, float* db) {
+  __shared__ double sums[64][16];
+  const int c = threadIdx.x & 15, g = threadIdx.x >> 4;
+  const int64_t n = (int64_t)blockIdx.x * 16 + c;
   double s = 0.0;
-  for (int64_t b = 0; b < blocks; ++b) s += part[b * N + n];
-  db[n] = (float)s;
+  if (n < N)
+    for (int64_t b = g; b < blocks; b += 64) s += part[b * N + n];
+  sums[g][c] = s;
+  __syncthreads();
+  if (g == 0 && n < N) {
+    for (int k = 1; k < 64; ++k) s += sums[k][c];
+    db[n] = (float)s;
+  }
+}
+
+template <typename T, int BM, int BN, int WM, int WN, int NB, bool WIDE>
+void launch_tiles(const GemmArgs& a, hipStream_t st) {
+  const int64_t items = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
+  const dim3 grid((unsigned)(items < 512 ? items : 512));  // (two work-groups on each of 256 compute units)
+  constexpr int NT = 64 * (BM / WM) * (BN / WN);
+  if constexpr (!WIDE) {
+    if (a.dy != nullptr) {
+      gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, true, true, false, true><<<grid, NT, 0, st>>>(a);
+      return;
+    }
+  }
+  if (a.ak && a.bk)
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, true, true, false><<<grid, NT, 0, st>>>(a);
+  else if (a.ak)
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, true, false, false><<<grid, NT, 0, st>>>(a);
+  else
+    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, false, false, false><<<grid, NT, 0, st>>>(a);
 }
 
 }  // namespace
 
 int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 
-// Tiles of a product, and the parts its K axis is cut into where they are fewer than
-// the compute units: as many as fill them, a part having at least 256 terms.
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool fast) {
+// Tiles of a product, and the parts its K axis is cut into where the tiles are fewer than the compute units: as many as
+// fill them, a part having at least 256 terms.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide) {
   LinearPlan p{};
-  auto tiles = [&](int b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  p.tile = !fast ? 64 : es == 2 && tiles(256) >= 256 ? 256 : 128;
-  const int64_t t = tiles(p.tile), want = fast ? 256 : 512;
-  int64_t s = t > 0 ? want / t : 1;
-  if (s > K / 256) s = K / 256;
-  s = s < 1 ? 1 : s > 64 ? 64 : s;
+  auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
+  int64_t most = whole ? 1 : K / 256;
+  most = most < 1 ? 1 : most > 64 ? 64 : most;
+  int64_t t;
+  if (M <= 64) {
+    p.tile = TILE_THIN;
+    t = tiles(64, 128);
+  } else if (es == 2 && wide && tiles(128, 256) * most >= 256) {
+    p.tile = TILE_WIDE;
+    t = tiles(128, 256);
+  } else {
+    p.tile = TILE_SQUARE;
+    t = tiles(128, 128);
+  }
+  int64_t s = t > 0 ? 256 / t : 1;
+  s = s < 1 ? 1 : s > most ? most : s;
   const int64_t kb = 64 / es, per = ((K + s - 1) / s + kb - 1) / kb * kb;  // whole steps, and no part without any
-  p.splits = per > 0 ? (int)((K + per - 1) / per) : 1;
+  p.splits = K > 0 ? (int)((K + per - 1) / per) : 0;
   return p;
 }
 
-namespace {
-template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC>
-void launch_tiles(const GemmArgs& a, hipStream_t st) {
-  const int64_t items = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
-  const dim3 grid((unsigned)(items < 512 ? items : 512));  // (two work-groups on each of 256 compute units)
-  constexpr int NT = 64 * (BM / WM) * (BN / WN);
-  if (a.sak == 1 && a.sbk == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, true, true><<<grid, NT, 0, st>>>(a);
-  else if (a.sak == 1)
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, true, false><<<grid, NT, 0, st>>>(a);
-  else
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, OCC, false, false><<<grid, NT, 0, st>>>(a);
-}
-}  // namespace
-
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
-  if (a.tile == 256) {
-    if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, 2>(a, st);
-  } else if (a.tile == 128) {
-    launch_tiles<T, 128, 128, 64, 64, 4, 2>(a, st);
-  } else {
-    const int64_t tiles = ((a.M + 63) / 64) * ((a.N + 63) / 64);
-    gemm_any_kernel<T><<<dim3((unsigned)tiles, (unsigned)a.splits), 256, 0, st>>>(a);
+  if (a.splits > 0) {
+    if (a.tile == TILE_WIDE) {
+      if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, true>(a, st);
+    } else if (a.tile == TILE_SQUARE) {
+      launch_tiles<T, 128, 128, 64, 64, 4, false>(a, st);
+    } else {
+      launch_tiles<T, 64, 128, 64, 32, 6, false>(a, st);
+    }
   }
-  if (a.splits > 1) gemm_join_kernel<T><<<dim3((unsigned)((a.M * a.N + 255) / 256)), 256, 0, st>>>(a);
+  if (a.splits != 1) {
+    const int64_t n = a.M * a.N;
+    if (!a.loose && a.N % 4 == 0)
+      gemm_join_kernel<T, 4><<<dim3((unsigned)((n / 4 + 255) / 256)), 256, 0, st>>>(a);
+    else
+      gemm_join_kernel<T, 1><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>(a);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, float* db, int64_t R,
-                          int64_t N, hipStream_t st) {
-  const int64_t blocks = linear_row_blocks(R);
-  if (blocks > 0)
-    act_bwd_kernel<T><<<dim3((unsigned)((N + 255) / 256 * blocks)), 256, 0, st>>>(
-        (const T*)dy, pre, act, (T*)out, part, R, N);
-  if (db != nullptr) col_sum_kernel<<<dim3((unsigned)((N + 255) / 256)), 256, 0, st>>>(part, blocks, N, db);
+hipError_t launch_pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t to, hipStream_t st) {
+  const int64_t n = rows * to / (16 / (int64_t)sizeof(T));
+  pack_kernel<T><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>((const T*)src, ld, rows, cols, (T*)dst, to);
   return hipGetLastError();
 }
 
-#define RES_LINEAR(T)                                                                                        \
-  template hipError_t launch_gemm<T>(const GemmArgs&, hipStream_t);                                          \
-  template hipError_t launch_act_bwd<T>(const void*, const float*, int, void*, float*, float*, int64_t, int64_t, hipStream_t);
+template <typename T>
+hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, int64_t R, int64_t N, bool loose,
+                          hipStream_t st) {
+  const int64_t blocks = linear_row_blocks(R);
+  if (!loose && N % 4 == 0)
+    act_bwd_kernel<T, 4><<<dim3((unsigned)((N + 255) / 256 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, part, R, N);
+  else
+    act_bwd_kernel<T, 1><<<dim3((unsigned)((N + 63) / 64 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, part, R, N);
+  return hipGetLastError();
+}
+
+hipError_t launch_col_sum(const float* part, int64_t blocks, int64_t N, float* db, hipStream_t st) {
+  col_sum_kernel<<<dim3((unsigned)((N + 15) / 16)), 1024, 0, st>>>(part, blocks, N, db);
+  return hipGetLastError();
+}
+
+#define RES_LINEAR(T)                                                                                                 \
+  template hipError_t launch_gemm<T>(const GemmArgs&, hipStream_t);                                                   \
+  template hipError_t launch_pack<T>(const void*, int64_t, int64_t, int64_t, void*, int64_t, hipStream_t);            \
+  template hipError_t launch_act_bwd<T>(const void*, const float*, int, void*, float*, int64_t, int64_t, bool, hipStream_t);
 RES_LINEAR(float)
 RES_LINEAR(bf16_t)
 

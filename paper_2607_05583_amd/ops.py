@@ -1229,17 +1229,22 @@ def _like(t, name, dtype, shape):
     return t
 
 
-def _linear_ws(ws, backward, dtype, act, R, K, N, device):
+def _linear_ws(ws, backward, act, x, ldx, W, dy=None):
+    """The caller's workspace or a new one of the size that this call needs."""
     if ws is not None:
         _dev(ws, "ws")
         return ws, ws.numel() * ws.element_size()
-    n = int(_lib.lib().resonator_linear_workspace_bytes(backward, _DT[dtype], act, R, K, N))
-    return (torch.empty(n, dtype=torch.uint8, device=device) if n else None), n
+    K, N = W.shape
+    ep = 16 // x.element_size()
+    loose = bool(K % ep or N % ep or ldx % ep or x.data_ptr() % 16 or W.data_ptr() % 16
+                 or (dy is not None and dy.data_ptr() % 16))
+    n = int(_lib.lib().resonator_linear_workspace_bytes(backward, _code(x), act, x.numel() // K, K, N, loose))
+    return (torch.empty(n, dtype=torch.uint8, device=x.device) if n else None), n
 
 
 class LinearSaved:
-    """What a forward of the linear product keeps for its backward: the float32 ``pre`` = x W + bias (None where the
-    activation is "none") and the ``bias``."""
+    """What a forward of the linear product keeps for its backward: the float32 ``pre`` = x W + bias, or None where the
+    backward computes it again (that costs less for a short K axis), and the ``bias`` for it."""
 
     __slots__ = ("pre", "bias")
 
@@ -1259,8 +1264,9 @@ def resonator_linear_fwd(x, W, bias=None, act="none", residual=None, save=False,
     _f32(bias, "bias", (N,))
     _like(residual, "residual", x.dtype, shape)
     y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else _given(out, "out", R * N, x.dtype)
-    pre = torch.empty(shape, dtype=torch.float32, device=x.device) if save and code else None
-    ws, n = _linear_ws(ws, 0, x.dtype, code, R, K, N, x.device)
+    keep = save and _lib.lib().resonator_linear_keeps_pre(_code(x), code, K)
+    pre = torch.empty(shape, dtype=torch.float32, device=x.device) if keep else None
+    ws, n = _linear_ws(ws, 0, code, x, ldx, W)
     check(_lib.lib().resonator_linear_fwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(bias), code, _ptr(residual), _ptr(y),
                                           _ptr(pre), R, K, N, _ptr(ws), n, _stream(x.device)))
     return (y, LinearSaved(pre, bias)) if save else y
@@ -1279,15 +1285,16 @@ def resonator_linear_bwd(x, W, dy, pre=None, act="none", residual=None, want_dx=
     if dy is None or (code and pre is None):
         raise TypeError("dy and, with an activation, pre must be given")
     _like(dy, "dy", x.dtype, shape)
+    bias = None
     if isinstance(pre, LinearSaved):
-        pre = pre.pre
+        pre, bias = pre.pre, _f32(pre.bias, "bias", (N,))
     _like(pre, "pre", torch.float32, shape)
     _like(residual, "residual", x.dtype, x.shape)
     dx = torch.empty(tuple(x.shape), dtype=x.dtype, device=x.device) if want_dx else None
     dW = torch.empty_like(W) if want_dw else None
     db = torch.empty((N,), dtype=torch.float32, device=x.device) if want_db else None
-    ws, n = _linear_ws(ws, 1, x.dtype, code, R, K, N, x.device)
-    check(_lib.lib().resonator_linear_bwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(dy), _ptr(pre), code, _ptr(residual),
+    ws, n = _linear_ws(ws, 1, code, x, ldx, W, dy)
+    check(_lib.lib().resonator_linear_bwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(bias), _ptr(dy), _ptr(pre), code, _ptr(residual),
                                           _ptr(dx), _ptr(dW), _ptr(db), R, K, N, _ptr(ws), n, _stream(x.device)))
     return {k: v for k, v in (("dx", dx), ("dW", dW), ("db", db)) if v is not None}
 

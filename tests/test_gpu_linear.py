@@ -48,10 +48,14 @@ def check(q, act, fn, say_it):
     yr, pr = O.linear_fwd(h["x"], h["W"], h["b"], fn, h["res"])
     gr = O.linear_bwd(h["x"], h["W"], h["dy"], h["b"], fn, h["into"])
     assert rel_err(host(y), yr) <= TOL[act]
-    if pre is not None:
-        assert rel_err(host(pre), pr) <= 1e-4
+    assert pre is None or rel_err(host(pre), pr) <= 1e-4
+    if fn != "none":  # the other of the two ways: pre kept, or computed again
+        if pre is None:
+            pre = torch.from_numpy(pr.astype(np.float32)).cuda()
         again = ops.resonator_linear_bwd(q["x"], q["W"], q["dy"], pre=pre, act=fn, residual=q["into"], want_db=True)
-        assert all(torch.equal(g[k], again[k]) for k in g)
+        for k in ("dx", "dW"):
+            assert rel_err(host(again[k]), gr[k]) <= TOL[act], k
+        assert rel_err(host(again["db"]), gr["db"]) <= 1e-4
     for k in ("dx", "dW"):
         assert rel_err(host(g[k]), gr[k]) <= TOL[act], k
     assert rel_err(host(g["db"]), gr["db"]) <= 1e-4
