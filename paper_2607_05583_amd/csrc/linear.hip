@@ -10,6 +10,13 @@ namespace res {
 namespace {
 
 template <typename T> struct __align__(4 * sizeof(T)) Quad { T v[4]; };
+template <typename T>
+__device__ __forceinline__ f4 wide(const Quad<T>& q) {
+  f4 c;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) c[r] = to_f32(q.v[r]);
+  return c;
+}
 __device__ __forceinline__ Quad<float> round_quad(const f4& c, float) { return __builtin_bit_cast(Quad<float>, c); }
 __device__ __forceinline__ Quad<bf16_t> round_quad(const f4& c, bf16_t) {
   typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
@@ -17,17 +24,12 @@ __device__ __forceinline__ Quad<bf16_t> round_quad(const f4& c, bf16_t) {
 }
 // Columns n .. n + 3 of a row of N; loose: no alignment, and columns from N on are the last one again.
 template <typename T>
-__device__ __forceinline__ f4 load_quad(const T* row, int64_t n, int64_t N, bool loose) {
-  f4 c;
-  if (!loose) {
-    const auto q = *reinterpret_cast<const Quad<T>*>(row + n);
+__device__ __forceinline__ Quad<T> load_quad(const T* row, int n, int64_t N, bool loose) {
+  if (!loose) return *reinterpret_cast<const Quad<T>*>(row + n);
+  Quad<T> q;
 #pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = to_f32(q.v[r]);
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) c[r] = to_f32(row[n + r < N ? n + r : N - 1]);
-  }
-  return c;
+  for (int r = 0; r < 4; ++r) q.v[r] = row[n + r < N ? n + r : N - 1];
+  return q;
 }
 
 // ---------------------------------------------------------------------------
@@ -159,47 +161,64 @@ template <typename T, int ACT, bool SLOPE, bool ANY, int WM, int WN>
 __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
                                          char* mine, int lane) {
   constexpr int ES = sizeof(T), RB = WN * ES, PR = RB / 16, EP = 16 / ES, SW = PR < 8 ? PR - 1 : 7, FN = WN / 16;
+  constexpr int RS = 64 / PR;  // rows of a store
   const int li = lane & 15, lq = lane >> 4;
   const bool loose = ANY && g.loose;
+  const int rows = (int)(g.M - m0 < WM ? (g.M > m0 ? g.M - m0 : 0) : WM);  // of this wave's that there are
   int n[FN];
   f4 bias[FN], sum[FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j) {
     n[j] = (int)n0 + j * 16 + lq * 4;
     n[j] = n[j] < (int)g.N ? n[j] : ((int)g.N - 1) & ~3;
-    bias[j] = g.bias != nullptr ? load_quad(g.bias, n[j], g.N, loose) : f4{};
+    bias[j] = g.bias != nullptr ? wide(load_quad(g.bias, n[j], g.N, loose)) : f4{};
     sum[j] = f4{};
   }
+  // what is read beside the results (dy or the residual), some fragments of rows ahead of the stores, which the compiler
+  // does not move loads across
+  const T* side = (const T*)(SLOPE ? g.dy : g.res);
+  constexpr int AHEAD = WM / 16 > 4 ? 2 : 4;
+  Quad<T> q[AHEAD][FN];
+  // stores: this lane's row of a fragment's first RS, and on from there
+  T* to = (T*)g.out + (m0 + lane / PR) * g.N + n0;
+  const int64_t next = RS * g.N;
 #pragma unroll
   for (int i = 0; i < WM / 16; ++i) {
-    int64_t m = m0 + i * 16 + li;
-    const bool in = m < g.M;
-    m = in ? m : g.M - 1;
+    const int row = i * 16 + li;
+    if (i % AHEAD == 0 && side != nullptr) {
+#pragma unroll
+      for (int k = 0; k < AHEAD; ++k) {
+        const int64_t m = m0 + row + k * 16;
+        const T* from = side + (m < g.M ? m : g.M - 1) * g.N;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) q[k][j] = load_quad(from, n[j], g.N, loose);
+      }
+    }
     f4 c[FN];
 #pragma unroll
     for (int j = 0; j < FN; ++j) c[j] = acc[i][j] + bias[j];
     if constexpr (SLOPE) {
-      f4 d[FN];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) d[j] = load_quad((const T*)g.dy + m * g.N, n[j], g.N, loose);
-#pragma unroll
-      for (int j = 0; j < FN; ++j)
+      for (int j = 0; j < FN; ++j) {
+        const f4 d = wide(q[i % AHEAD][j]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          c[j][r] = d[j][r] * act_slope(c[j][r], ACT);
-          sum[j][r] += in ? c[j][r] : 0.0f;
+          c[j][r] = d[r] * act_slope(c[j][r], ACT);
+          sum[j][r] += row < rows ? c[j][r] : 0.0f;
         }
+      }
     } else {
-      if (g.pre != nullptr && in) {
+      if (g.pre != nullptr && row < rows) {
+        float* pre = g.pre + (m0 + row) * g.N;
 #pragma unroll
         for (int j = 0; j < FN; ++j)
-          if (n0 + j * 16 + lq * 4 < g.N) {
+          if ((int)n0 + j * 16 + lq * 4 < (int)g.N) {
             if (!loose) {
-              *reinterpret_cast<f4*>(g.pre + m * g.N + n[j]) = c[j];
+              *reinterpret_cast<f4*>(pre + n[j]) = c[j];
             } else {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
-                if (n[j] + r < g.N) g.pre[m * g.N + n[j] + r] = c[j][r];
+                if (n[j] + r < (int)g.N) pre[n[j] + r] = c[j][r];
             }
           }
       }
@@ -209,12 +228,9 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 #pragma unroll
           for (int r = 0; r < 4; ++r) c[j][r] = act_value(c[j][r], ACT);
       }
-      if (g.res != nullptr) {
-        f4 q[FN];
+      if (side != nullptr) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) q[j] = load_quad((const T*)g.res + m * g.N, n[j], g.N, loose);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) c[j] += q[j];
+        for (int j = 0; j < FN; ++j) c[j] += wide(q[i % AHEAD][j]);
       }
     }
 #pragma unroll
@@ -225,17 +241,17 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
     if (!loose) {
 #pragma unroll
-      for (int u = 0; u < 16 * PR / 64; ++u) {
-        const int row = u * (64 / PR) + lane / PR, slot = lane % PR;
-        const int64_t mo = m0 + i * 16 + row, col = n0 + ((slot ^ (row & SW)) * EP);
-        const u4 v = *reinterpret_cast<const u4*>(mine + row * RB + slot * 16);
-        if (mo < g.M && col < g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>((T*)g.out + mo * g.N + col));
+      for (int u = 0; u < 16 / RS; ++u) {
+        const int r = u * RS + lane / PR, slot = lane % PR, col = (slot ^ (r & SW)) * EP;
+        const u4 v = *reinterpret_cast<const u4*>(mine + r * RB + slot * 16);
+        if (i * 16 + r < rows && (int)n0 + col < (int)g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>(to + col));
+        to += next;
       }
     } else {
       for (int e = lane; e < 16 * WN; e += 64) {
-        const int row = e / WN, byte = e % WN * ES;
-        const int64_t mo = m0 + i * 16 + row, col = n0 + e % WN;
-        const T v = *reinterpret_cast<const T*>(mine + row * RB + (((byte >> 4) ^ (row & SW)) << 4) + (byte & 15));
+        const int r = e / WN, byte = e % WN * ES;
+        const int64_t mo = m0 + i * 16 + r, col = n0 + e % WN;
+        const T v = *reinterpret_cast<const T*>(mine + r * RB + (((byte >> 4) ^ (r & SW)) << 4) + (byte & 15));
         if (mo < g.M && col < g.N) ((T*)g.out)[mo * g.N + col] = v;
       }
     }
@@ -443,7 +459,7 @@ __global__ __launch_bounds__(256) void act_bwd_kernel(const T* dy, const float* 
       if (r >= R) break;
       float d[V], p[V];
       if constexpr (V == 4) {
-        const f4 q = load_quad(dy + r * N, n, N, false);
+        const f4 q = wide(load_quad(dy + r * N, (int)n, N, false));
         const f4 z = pre != nullptr ? *reinterpret_cast<const f4*>(pre + at) : f4{};
 #pragma unroll
         for (int e = 0; e < 4; ++e) d[e] = q[e], p[e] = z[e];
