@@ -64,7 +64,9 @@ int check_scan(int64_t B, int64_t L, int64_t D, res_dtype_t dt) {
     return api_error(RES_ERR_INVALID_ARG, "B and D must be >= 1 and L >= 0 (got B=%lld L=%lld D=%lld)", (long long)B,
                      (long long)L, (long long)D);
   const int64_t NB = (D + GATED_CW - 1) / GATED_CW;
-  if (D > (1 << 24) || L >= (1LL << 31) - 65536 || B > (1LL << 31) || B * NB >= (1LL << 31))
+  // (tiles of a call and tickets are 32-bit counts)
+  if (D > (1 << 24) || L >= (1LL << 31) - 65536 || B > (1LL << 31) || B * NB >= (1LL << 30) ||
+      B * NB * (L / GATED_BWD_TILE + 1) >= (1LL << 31))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld D=%lld)", (long long)B,
                      (long long)L, (long long)D);
   return RES_OK;
@@ -86,7 +88,9 @@ extern "C" {
 size_t resonator_gated_scan_workspace_bytes(res_dtype_t dt, int64_t B, int64_t L, int64_t D) {
   if (check_scan(B, L, D, dt)) return 0;
   const int64_t NB = (D + GATED_CW - 1) / GATED_CW;
-  return 256 + (size_t)B * NB * GATED_CW * 8;
+  // the forward's or the backward's published words, and behind the backward's its partial sums
+  const int64_t f = gated_tiles(L, GATED_FWD_TILE), b = gated_tiles(L, GATED_BWD_TILE);
+  return 256 + (size_t)(B * NB) * (size_t)std::max(f * GATED_TILE_WORDS, b * (GATED_TILE_WORDS + GATED_CW)) * 8;
 }
 
 int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype_t dt, void* y, int64_t B, int64_t L,
@@ -136,6 +140,8 @@ int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype
   a.lengths = lengths;
   a.h_out = h_out;
   a.carry = carry;
+  a.hdr = static_cast<uint32_t*>(ws);
+  a.words = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + 256);
   return launched(dt == RES_BF16 ? launch_gated_fwd<bf16_t>(a, (hipStream_t)stream) : launch_gated_fwd<float>(a, (hipStream_t)stream),
                   "gated scan launch");
 }
@@ -196,7 +202,9 @@ int resonator_gated_scan_bwd(res_rows_t x, res_rows_t r, res_rows_t i, res_rows_
   a.carry = const_cast<float*>(carry);
   a.dh_out = dh_out;
   a.dh0 = dh0;
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + 256);
+  a.hdr = static_cast<uint32_t*>(ws);
+  a.words = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + 256);
+  a.part = a.words + B * a.NB * gated_tiles(L, GATED_BWD_TILE) * GATED_TILE_WORDS;
   return launched(dt == RES_BF16 ? launch_gated_bwd<bf16_t>(a, dgamma, (hipStream_t)stream)
                                  : launch_gated_bwd<float>(a, dgamma, (hipStream_t)stream),
                   "gated scan backward launch");

@@ -7,10 +7,21 @@
 // Where s = 0 (beta = 0) the derivative of beta is taken as zero.
 //
 // Both directions are scans of affine maps: steps t0..t1 take h to A h + H with A the
-// product of their a, and the adjoint c_t = a_t g_t to A c + C with the same A.  A
-// thread owns S consecutive steps of VEC channels in registers, composes their map,
-// and gets the state before its first step from the maps of the threads before it
-// (LDS); then it runs its steps again from that state.
+// product of their a, and the adjoint c_t = a_t g_t to A c + C with the same A.
+//
+// A work-group takes a tile of a chain (one batch row, 64 channels: 128-byte rows of
+// bf16) and holds it in registers: a thread has S consecutive steps of VEC channels and
+// composes their map; the maps of the threads before it come from a scan over the wave
+// and over the waves' totals (LDS).  Inputs are read once and outputs written once.
+//
+// The state before a tile comes from the tiles before it in one pass: a tile publishes
+// its map as soon as it has it, and its end state as soon as it has that; a tile looks
+// back over at most WINDOW tiles for the nearest end state and applies the maps from
+// there on, one after the other.  That is the same sequence of operations wherever the
+// search ends, so results do not depend on timing.  Tiles are taken in order from a
+// ticket counter by work-groups that stay, so the tiles that one waits for are always at
+// work.  A published value is a 64-bit word with the call's number beside it: a word is
+// its own flag, and nothing has to be cleared between calls.
 #include "layer.h"
 
 namespace res {
@@ -29,20 +40,22 @@ __device__ __forceinline__ float one_minus_a2(float s, float a) {
   return t < 0.3f ? t * p : fmaf(-a, a, 1.0f);
 }
 
-// a and 1 / beta (0 where beta is 0) and beta of a step
+// beta = sqrt(1 - a^2) and 1 / beta, both 0 where the square is no float32 to speak of
+struct DriveGate {
+  float beta, rbeta;
+};
+__device__ __forceinline__ DriveGate drive_gate(float s, float a) {
+  const float e = one_minus_a2(s, a);
+  const bool some = !(e <= 1e-36f);  // NaN stays NaN
+  const float r = some ? __builtin_amdgcn_rsqf(e) : 0.0f;
+  return DriveGate{e * r, r};
+}
 struct Gate {
-  float s, sr, a, beta, rbeta;
+  float a, beta;
 };
 __device__ __forceinline__ Gate gate(float r, float gamma) {
-  Gate g;
-  g.sr = sigmoid_fast(r);
-  g.s = gamma * g.sr;
-  g.a = exp2_fast(-LOG2E * g.s);
-  const float e = one_minus_a2(g.s, g.a);
-  const bool some = !(e <= 1e-36f);  // NaN stays NaN
-  g.rbeta = some ? __builtin_amdgcn_rsqf(e) : 0.0f;
-  g.beta = e * g.rbeta;
-  return g;
+  const float s = gamma * sigmoid_fast(r), a = exp2_fast(-LOG2E * s);
+  return Gate{a, drive_gate(s, a).beta};
 }
 
 template <typename T, int VEC> struct __align__(sizeof(T) * VEC) Vec { T v[VEC]; };
@@ -78,44 +91,183 @@ __device__ __forceinline__ int row_len(const int* lengths, int64_t b, int64_t L)
   return n < 0 ? 0 : n < (int)L ? n : (int)L;
 }
 
-// One work-group a chain, tile after tile.
-template <typename T, int VEC, int S, int NT, bool VIO>
-__global__ __launch_bounds__(NT) void gated_fwd_kernel(GatedArgs A) {
-  constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG;
-  __shared__ float2 agg[TG][GATED_CW];
-  __shared__ float enter[GATED_CW];
-  const int lane = threadIdx.x % CGL, tg = threadIdx.x / CGL;
-  const int64_t b = blockIdx.x / A.NB;
-  const int cl = lane * VEC, c = (int)(blockIdx.x % A.NB) * GATED_CW + cl;
-  const int len = row_len(A.lengths, b, A.L);
-  const int64_t NC = (A.L + GATED_CARRY - 1) / GATED_CARRY;
-  float gam[VEC];
+// ---------------------------------------------------------------------------
+// Tiles in order, and the look-back
+// ---------------------------------------------------------------------------
+constexpr int WINDOW = 8;       // tiles looked back over at a time
+constexpr int NONE = -2, END = -1;  // kinds of a published map, in the place of its A (which is never negative)
+
+__device__ __forceinline__ uint64_t word(float v, uint32_t tag) { return (uint64_t)tag << 32 | __float_as_uint(v); }
+__device__ __forceinline__ uint64_t load_word(const uint64_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void store_word(uint64_t* p, float v, uint32_t tag) {
+  __hip_atomic_store(p, word(v, tag), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+struct LookShared {
+  float2 map[WINDOW][GATED_CW];
+  float enter[GATED_CW];
+  int ticket, found;
+};
+
+// The value that enters tile `o` of a chain (in the order that they are taken; `words`: the chain's) into sh.enter, for
+// the 64 channels; `init`: what enters tile 0.  Called by the whole work-group.
+__device__ __forceinline__ void look_back(const uint64_t* words, int64_t o, uint32_t tag, float init, uint32_t* status,
+                                          LookShared& sh) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int EACH = 1;
+  for (int tries = 0;; ++tries) {
+    if (wave < WINDOW / EACH) {
+      uint64_t a[EACH], h[EACH], e[EACH];
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
-  if (tg == 0)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) enter[cl + v] = A.h0 != nullptr && c + v < A.D ? A.h0[b * A.D + c + v] : 0.0f;
-  for (int64_t tile = 0; tile * TILE < A.L; ++tile) {
-    const int64_t t0 = tile * TILE + tg * S;
-    float a[S][VEC], u[S][VEC];
-#pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int64_t t = t0 + s;
-      if (t < len) {
-        const auto xv = load_row<T, VEC, VIO>((const T*)A.x.p + b * A.x.sb + t * A.x.st, c, A.D);
-        const auto rv = load_row<T, VEC, VIO>((const T*)A.r.p + b * A.r.sb + t * A.r.st, c, A.D);
-        const auto iv = load_row<T, VEC, VIO>((const T*)A.i.p + b * A.i.sb + t * A.i.st, c, A.D);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          const Gate g = gate(to_f32(rv.v[v]), gam[v]);
-          a[s][v] = g.a;
-          u[s][v] = g.beta * sigmoid_fast(to_f32(iv.v[v])) * to_f32(xv.v[v]);
+      for (int j = 0; j < EACH; ++j) {
+        const int g = wave * EACH + j;
+        if (g < o) {
+          const uint64_t* w = words + (o - 1 - g) * GATED_TILE_WORDS + lane;
+          e[j] = load_word(w + 128);
+          a[j] = load_word(w);
+          h[j] = load_word(w + 64);
         }
-      } else {
+      }
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) a[s][v] = 1.0f, u[s][v] = 0.0f;
+      for (int j = 0; j < EACH; ++j) {
+        const int g = wave * EACH + j;
+        float2 m = make_float2(NONE, 0.0f);
+        if (g == o) {
+          m = make_float2(END, init);
+        } else if (g < o) {
+          if ((uint32_t)(e[j] >> 32) == tag)
+            m = make_float2(END, __uint_as_float((uint32_t)e[j]));
+          else if ((uint32_t)(a[j] >> 32) == tag && (uint32_t)(h[j] >> 32) == tag)
+            m = make_float2(__uint_as_float((uint32_t)a[j]), __uint_as_float((uint32_t)h[j]));
+        }
+        sh.map[g][lane] = m;
       }
     }
+    __syncthreads();
+    if (wave == 0) {
+      float v = 0.0f;
+      bool have = false;
+#pragma unroll
+      for (int g = WINDOW - 1; g >= 0; --g) {
+        const float2 m = sh.map[g][lane];
+        if (m.x == END) {
+          v = m.y;
+          have = true;
+        } else if (m.x == NONE) {
+          have = false;
+        } else {
+          v = fmaf(m.x, v, m.y);
+        }
+      }
+      if (tries > (1 << 20)) {  // (seconds: a work-group before it is gone; the result says so)
+        if (lane == 0) *status = 1;
+        v = __uint_as_float(0x7fc00000u);
+        have = true;
+      }
+      sh.enter[lane] = v;
+      if (lane == 0) sh.found = 0;
+      if (__all(have) && lane == 0) sh.found = 1;
+    }
+    __syncthreads();
+    if (sh.found) return;
+    __builtin_amdgcn_s_sleep(2);
+  }
+}
+
+// The next tile of this work-group (whole work-group).
+__device__ __forceinline__ uint32_t take_ticket(uint32_t* hdr, LookShared& sh) {
+  if (threadIdx.x == 0) sh.ticket = (int)atomicAdd(hdr + 2, 1u);
+  __syncthreads();
+  const uint32_t t = (uint32_t)sh.ticket;
+  __syncthreads();
+  return t;
+}
+// The last work-group to end makes the counters ready for the next call.
+__device__ __forceinline__ void leave(uint32_t* hdr, uint32_t tag) {
+  if (threadIdx.x == 0 && atomicAdd(hdr + 3, 1u) == gridDim.x - 1) {
+    hdr[2] = 0;
+    hdr[3] = 0;
+    hdr[1] = tag;
+  }
+}
+
+// Maps of the threads of a wave that have the same channels (lane groups of CGL, in time order).
+template <int CGL>
+__device__ __forceinline__ void scan_up(float& A, float& H) {  // inclusive: all up to and with this one
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = CGL; d < 64; d <<= 1) {
+    const float pa = __shfl_up(A, d, 64), ph = __shfl_up(H, d, 64);
+    if (lane >= d) {
+      H = fmaf(A, ph, H);
+      A *= pa;
+    }
+  }
+}
+template <int CGL>
+__device__ __forceinline__ void scan_down(float& A, float& C) {  // inclusive: this one and all after it
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = CGL; d < 64; d <<= 1) {
+    const float pa = __shfl_down(A, d, 64), pc = __shfl_down(C, d, 64);
+    if (lane + d < 64) {
+      C = fmaf(A, pc, C);
+      A *= pa;
+    }
+  }
+}
+
+template <typename T, int VEC, int S, int NT, bool VIO, bool LOOK>
+__global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
+  constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG, NW = NT / 64, WG = 64 / CGL;
+  __shared__ float2 total[NW][GATED_CW];
+  __shared__ LookShared sh;
+  const int wl = threadIdx.x & 63, wave = threadIdx.x >> 6, lane = wl % CGL, tg = threadIdx.x / CGL, cl = lane * VEC;
+  const int64_t tiles = gated_tiles(A.L, TILE), chains = A.B * A.NB, NC = (A.L + GATED_CARRY - 1) / GATED_CARRY;
+  const uint32_t tag = LOOK ? A.hdr[1] + 1 : 0;
+  for (int64_t turn = 0;; ++turn) {
+    int64_t o = 0, chain = blockIdx.x;
+    if constexpr (LOOK) {
+      const uint32_t t = take_ticket(A.hdr, sh);
+      if (t >= tiles * chains) break;
+      o = t / (uint32_t)chains;
+      chain = t % (uint32_t)chains;
+    } else if (turn > 0) {
+      break;
+    }
+    const int64_t b = chain / A.NB;
+    const int cb = (int)(chain % A.NB) * GATED_CW, c = cb + cl;
+    const int len = row_len(A.lengths, b, A.L);
+    const int64_t t0 = o * TILE + tg * S;
+    float a[S][VEC], u[S][VEC];
+    {
+      float gam[VEC];
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
+      const T* px = (const T*)A.x.p + b * A.x.sb + t0 * A.x.st;
+      const T* pr = (const T*)A.r.p + b * A.r.sb + t0 * A.r.st;
+      const T* pi = (const T*)A.i.p + b * A.i.sb + t0 * A.i.st;
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        if (t0 + s < len) {
+          const auto xv = load_row<T, VEC, VIO>(px + s * A.x.st, c, A.D);
+          const auto rv = load_row<T, VEC, VIO>(pr + s * A.r.st, c, A.D);
+          const auto iv = load_row<T, VEC, VIO>(pi + s * A.i.st, c, A.D);
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) {
+            const Gate g = gate(to_f32(rv.v[v]), gam[v]);
+            a[s][v] = g.a;
+            u[s][v] = g.beta * sigmoid_fast(to_f32(iv.v[v])) * to_f32(xv.v[v]);
+          }
+        } else {
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) a[s][v] = 1.0f, u[s][v] = 0.0f;
+        }
+      }
+    }
+    float ea[VEC], eh[VEC];  // the map of this wave's steps before this thread's
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float pa = 1.0f, ph = 0.0f;
@@ -124,178 +276,275 @@ __global__ __launch_bounds__(NT) void gated_fwd_kernel(GatedArgs A) {
         pa *= a[s][v];
         ph = fmaf(a[s][v], ph, u[s][v]);
       }
-      agg[tg][cl + v] = make_float2(pa, ph);
+      scan_up<CGL>(pa, ph);
+      if (wl >= 64 - CGL) total[wave][cl + v] = make_float2(pa, ph);
+      ea[v] = 1.0f;
+      eh[v] = 0.0f;
+      if constexpr (WG > 1) {
+        const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
+        if (wl >= CGL) ea[v] = xa, eh[v] = xh;
+      }
     }
     __syncthreads();
+    float ta = 1.0f, th = 0.0f;  // the tile's map (wave 0: a channel a lane)
+    uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
+    const int cw = cb + wl;
+    const float init = A.h0 != nullptr && cw < A.D ? A.h0[b * A.D + cw] : 0.0f;
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float2 m = total[w][wl];
+        th = fmaf(m.x, th, m.y);
+        ta *= m.x;
+      }
+      if (LOOK && o + 1 < tiles) {
+        uint64_t* w = words + o * GATED_TILE_WORDS + wl;
+        store_word(w, ta, tag);
+        store_word(w + 64, th, tag);
+      }
+    }
+    if constexpr (LOOK) {
+      look_back(words, o, tag, init, A.hdr, sh);
+    } else {
+      if (wave == 0) sh.enter[wl] = init;
+      __syncthreads();
+    }
+    if (wave == 0) {
+      const float end = fmaf(ta, sh.enter[wl], th);
+      if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
+      if (A.h_out != nullptr && o + 1 == tiles && cw < A.D) A.h_out[b * A.D + cw] = end;
+    }
     float h[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) h[v] = enter[cl + v];
-    for (int g = 0; g < tg; ++g)
+    for (int v = 0; v < VEC; ++v) h[v] = sh.enter[cl + v];
+    for (int w = 0; w < wave; ++w)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float2 m = agg[g][cl + v];
+        const float2 m = total[w][cl + v];
         h[v] = fmaf(m.x, h[v], m.y);
       }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) h[v] = fmaf(ea[v], h[v], eh[v]);
     if (A.carry != nullptr && t0 % GATED_CARRY == 0 && t0 < A.L) {
 #pragma unroll
       for (int v = 0; v < VEC; ++v)
         if (c + v < A.D) A.carry[(b * NC + t0 / GATED_CARRY) * A.D + c + v] = h[v];
     }
+    if (A.y != nullptr) {
+      T* py = (T*)A.y + (b * A.L + t0) * A.D;
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      Vec<T, VEC> o;
+      for (int s = 0; s < S; ++s) {
+        Vec<T, VEC> ov;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        h[v] = fmaf(a[s][v], h[v], u[s][v]);
-        o.v[v] = from_f32<T>(t0 + s < len ? h[v] : 0.0f);
+        for (int v = 0; v < VEC; ++v) {
+          h[v] = fmaf(a[s][v], h[v], u[s][v]);
+          ov.v[v] = from_f32<T>(t0 + s < len ? h[v] : 0.0f);
+        }
+        if (t0 + s < A.L) store_row<T, VEC, VIO>(py + (int64_t)s * A.D, c, A.D, ov);
       }
-      if (A.y != nullptr && t0 + s < A.L) store_row<T, VEC, VIO>((T*)A.y + (b * A.L + t0 + s) * A.D, c, A.D, o);
     }
-    __syncthreads();
-    if (tg == TG - 1)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) enter[cl + v] = h[v];
-    __syncthreads();
+    if constexpr (LOOK) __syncthreads();  // total and sh are free for the next tile
   }
-  if (A.h_out != nullptr && tg == 0)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      if (c + v < A.D) A.h_out[b * A.D + c + v] = enter[cl + v];
+  if constexpr (LOOK) leave(A.hdr, tag);
 }
 
-// One work-group a chain, from the last tile to the first.  A tile starts at a
-// kept state, so only the adjoint is carried from tile to tile.
-template <typename T, int VEC, int S, int NT, bool VIO>
-__global__ __launch_bounds__(NT) void gated_bwd_kernel(GatedArgs A) {
-  constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG;
+// Tiles from the last to the first; one starts at a kept state, so only the adjoint is looked back for.
+template <typename T, int VEC, int S, int NT, bool VIO, bool LOOK>
+__global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(GatedArgs A) {
+  constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG, NW = NT / 64, WG = 64 / CGL;
   static_assert(TILE % GATED_CARRY == 0, "a tile starts at a kept state");
-  __shared__ float4 agg[TG][GATED_CW];  // A, H, C
-  __shared__ float enter[GATED_CW];
-  __shared__ double gsum[TG][GATED_CW];
-  const int lane = threadIdx.x % CGL, tg = threadIdx.x / CGL;
-  const int64_t b = blockIdx.x / A.NB;
-  const int cl = lane * VEC, c = (int)(blockIdx.x % A.NB) * GATED_CW + cl;
-  const int len = row_len(A.lengths, b, A.L);
-  const int64_t NC = (A.L + GATED_CARRY - 1) / GATED_CARRY, tiles = (A.L + TILE - 1) / TILE;
-  float gam[VEC];
-  double sum[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) {
-    gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
-    sum[v] = 0.0;
-  }
-  if (tg == 0)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) enter[cl + v] = A.dh_out != nullptr && c + v < A.D ? A.dh_out[b * A.D + c + v] : 0.0f;
-  for (int64_t tile = tiles - 1; tile >= 0; --tile) {
+  __shared__ float total[3][NW][GATED_CW];  // A, H, C of a wave's steps
+  __shared__ float sums[NW][GATED_CW];
+  __shared__ LookShared sh;
+  const int wl = threadIdx.x & 63, wave = threadIdx.x >> 6, lane = wl % CGL, tg = threadIdx.x / CGL, cl = lane * VEC;
+  const int64_t tiles = gated_tiles(A.L, TILE), chains = A.B * A.NB, NC = (A.L + GATED_CARRY - 1) / GATED_CARRY;
+  const uint32_t tag = LOOK ? A.hdr[1] + 1 : 0;
+  for (int64_t turn = 0;; ++turn) {
+    int64_t o = 0, chain = blockIdx.x;
+    if constexpr (LOOK) {
+      const uint32_t t = take_ticket(A.hdr, sh);
+      if (t >= tiles * chains) break;
+      o = t / (uint32_t)chains;
+      chain = t % (uint32_t)chains;
+    } else if (turn > 0) {
+      break;
+    }
+    const int64_t tile = tiles - 1 - o, b = chain / A.NB;
+    const int cb = (int)(chain % A.NB) * GATED_CW, c = cb + cl;
+    const int len = row_len(A.lengths, b, A.L);
     const int64_t t0 = tile * TILE + tg * S;
-    float x[S][VEC], q[S][VEC], d[S][VEC], hp[S][VEC];
-    Gate gt[S][VEC];
+    float gam[VEC];
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const int64_t t = t0 + s;
-      if (t < len) {
-        const auto xv = load_row<T, VEC, VIO>((const T*)A.x.p + b * A.x.sb + t * A.x.st, c, A.D);
-        const auto rv = load_row<T, VEC, VIO>((const T*)A.r.p + b * A.r.sb + t * A.r.st, c, A.D);
-        const auto iv = load_row<T, VEC, VIO>((const T*)A.i.p + b * A.i.sb + t * A.i.st, c, A.D);
-        const auto dv = load_row<T, VEC, VIO>((const T*)A.dy.p + b * A.dy.sb + t * A.dy.st, c, A.D);
+    for (int v = 0; v < VEC; ++v) gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
+    Vec<T, VEC> x[S], d[S];
+    float a[S][VEC], sr[S][VEC], q[S][VEC];
+    {
+      const T* px = (const T*)A.x.p + b * A.x.sb + t0 * A.x.st;
+      const T* pr = (const T*)A.r.p + b * A.r.sb + t0 * A.r.st;
+      const T* pi = (const T*)A.i.p + b * A.i.sb + t0 * A.i.st;
+      const T* pd = (const T*)A.dy.p + b * A.dy.sb + t0 * A.dy.st;
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          gt[s][v] = gate(to_f32(rv.v[v]), gam[v]);
-          x[s][v] = to_f32(xv.v[v]);
-          q[s][v] = sigmoid_fast(to_f32(iv.v[v]));
-          d[s][v] = to_f32(dv.v[v]);
-        }
-      } else {
+      for (int s = 0; s < S; ++s) {
+        if (t0 + s < len) {
+          x[s] = load_row<T, VEC, VIO>(px + s * A.x.st, c, A.D);
+          d[s] = load_row<T, VEC, VIO>(pd + s * A.dy.st, c, A.D);
+          const auto rv = load_row<T, VEC, VIO>(pr + s * A.r.st, c, A.D);
+          const auto iv = load_row<T, VEC, VIO>(pi + s * A.i.st, c, A.D);
 #pragma unroll
-        for (int v = 0; v < VEC; ++v) {
-          gt[s][v] = Gate{0.0f, 0.0f, 1.0f, 0.0f, 0.0f};
-          x[s][v] = q[s][v] = d[s][v] = 0.0f;
+          for (int v = 0; v < VEC; ++v) {
+            sr[s][v] = sigmoid_fast(to_f32(rv.v[v]));
+            q[s][v] = sigmoid_fast(to_f32(iv.v[v]));
+            a[s][v] = exp2_fast(-LOG2E * (gam[v] * sr[s][v]));
+          }
+        } else {  // s = 0: a = 1 and nothing is added
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) x[s].v[v] = d[s].v[v] = T(0), a[s][v] = 1.0f, sr[s][v] = q[s][v] = 0.0f;
         }
       }
     }
+    float hp[S][VEC];           // beta q x, then the state before the step
+    float ea[VEC], eh[VEC];     // maps of this wave's steps before this thread's
+    float fa[VEC], fc[VEC];     // and, for the adjoint, after them
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float pa = 1.0f, ph = 0.0f, pc = 0.0f;
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        const Gate& g = gt[s][v];
-        pa *= g.a;
-        ph = fmaf(g.a, ph, g.beta * q[s][v] * x[s][v]);
+        hp[s][v] = drive_gate(gam[v] * sr[s][v], a[s][v]).beta * q[s][v] * to_f32(x[s].v[v]);
+        pa *= a[s][v];
+        ph = fmaf(a[s][v], ph, hp[s][v]);
       }
 #pragma unroll
-      for (int s = S - 1; s >= 0; --s) pc = gt[s][v].a * (d[s][v] + pc);
-      agg[tg][cl + v] = make_float4(pa, ph, pc, 0.0f);
+      for (int s = S - 1; s >= 0; --s) pc = a[s][v] * (to_f32(d[s].v[v]) + pc);
+      float da = pa, dc = pc;
+      scan_up<CGL>(pa, ph);
+      scan_down<CGL>(da, dc);
+      if (wl >= 64 - CGL) {
+        total[0][wave][cl + v] = pa;
+        total[1][wave][cl + v] = ph;
+      }
+      if (wl < CGL) total[2][wave][cl + v] = dc;
+      ea[v] = fa[v] = 1.0f;
+      eh[v] = fc[v] = 0.0f;
+      if constexpr (WG > 1) {
+        const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
+        const float ya = __shfl_down(da, CGL, 64), yc = __shfl_down(dc, CGL, 64);
+        if (wl >= CGL) ea[v] = xa, eh[v] = xh;
+        if (wl < 64 - CGL) fa[v] = ya, fc[v] = yc;
+      }
     }
     __syncthreads();
-    float h[VEC], cc[VEC];
+    float ta = 1.0f, tc = 0.0f;
+    uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
+    const int cw = cb + wl;
+    const float init = A.dh_out != nullptr && cw < A.D ? A.dh_out[b * A.D + cw] : 0.0f;
+    if (wave == 0) {
+#pragma unroll
+      for (int w = NW - 1; w >= 0; --w) {
+        const float m = total[0][w][wl];
+        tc = fmaf(m, tc, total[2][w][wl]);
+        ta *= m;
+      }
+      if (LOOK && o + 1 < tiles) {
+        uint64_t* w = words + o * GATED_TILE_WORDS + wl;
+        store_word(w, ta, tag);
+        store_word(w + 64, tc, tag);
+      }
+    }
+    if constexpr (LOOK) {
+      look_back(words, o, tag, init, A.hdr, sh);
+    } else {
+      if (wave == 0) sh.enter[wl] = init;
+      __syncthreads();
+    }
+    if (wave == 0) {
+      const float end = fmaf(ta, sh.enter[wl], tc);
+      if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
+      if (A.dh0 != nullptr && o + 1 == tiles && cw < A.D) A.dh0[b * A.D + cw] = end;
+    }
+    float h[VEC], cc[VEC], sum[VEC];
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      h[v] = c + v < A.D ? A.carry[(b * NC + tile * (TILE / GATED_CARRY)) * A.D + c + v] : 0.0f;
-      cc[v] = enter[cl + v];
+      h[v] = c + v < A.D && A.L > 0 ? A.carry[(b * NC + tile * (TILE / GATED_CARRY)) * A.D + c + v] : 0.0f;
+      cc[v] = sh.enter[cl + v];
+      sum[v] = 0.0f;
     }
-    for (int g = 0; g < tg; ++g)
+    for (int w = 0; w < wave; ++w)
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) h[v] = fmaf(agg[g][cl + v].x, h[v], agg[g][cl + v].y);
-    for (int g = TG - 1; g > tg; --g)
+      for (int v = 0; v < VEC; ++v) h[v] = fmaf(total[0][w][cl + v], h[v], total[1][w][cl + v]);
+    for (int w = NW - 1; w > wave; --w)
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) cc[v] = fmaf(agg[g][cl + v].x, cc[v], agg[g][cl + v].z);
+      for (int v = 0; v < VEC; ++v) cc[v] = fmaf(total[0][w][cl + v], cc[v], total[2][w][cl + v]);
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+    for (int v = 0; v < VEC; ++v) {
+      h[v] = fmaf(ea[v], h[v], eh[v]);
+      cc[v] = fmaf(fa[v], cc[v], fc[v]);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        hp[s][v] = h[v];
-        h[v] = fmaf(gt[s][v].a, h[v], gt[s][v].beta * q[s][v] * x[s][v]);
+      for (int s = 0; s < S; ++s) {
+        const float before = h[v];
+        h[v] = fmaf(a[s][v], h[v], hp[s][v]);
+        hp[s][v] = before;
       }
+    }
+    T* ox = (T*)A.dx.p + b * A.dx.sb + t0 * A.dx.st;
+    T* orr = (T*)A.dr.p + b * A.dr.sb + t0 * A.dr.st;
+    T* oi = (T*)A.di.p + b * A.di.sb + t0 * A.di.st;
 #pragma unroll
     for (int s = S - 1; s >= 0; --s) {
-      Vec<T, VEC> ox, orr, oi;
+      Vec<T, VEC> vx, vr, vi;
       const bool in = t0 + s < len;
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const Gate& k = gt[s][v];
-        const float g = d[s][v] + cc[v];
-        cc[v] = k.a * g;
-        const float gb = g * k.beta * q[s][v];
-        const float w = g * fmaf(k.a * k.a * k.rbeta * q[s][v], x[s][v], -k.a * hp[s][v]);
-        ox.v[v] = from_f32<T>(in ? gb : 0.0f);
-        oi.v[v] = from_f32<T>(in ? gb * (1.0f - q[s][v]) * x[s][v] : 0.0f);
-        orr.v[v] = from_f32<T>(in ? w * k.s * (1.0f - k.sr) : 0.0f);
-        sum[v] += in ? w * k.sr : 0.0f;
+        const float sv = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
+        const DriveGate k = drive_gate(sv, av);
+        const float g = to_f32(d[s].v[v]) + cc[v];
+        cc[v] = av * g;
+        const float gb = g * k.beta * qv;
+        const float w = g * fmaf(av * av * k.rbeta * qv, xv, -av * hp[s][v]);
+        vx.v[v] = from_f32<T>(in ? gb : 0.0f);
+        vi.v[v] = from_f32<T>(in ? gb * (1.0f - qv) * xv : 0.0f);
+        vr.v[v] = from_f32<T>(in ? w * sv * (1.0f - sr[s][v]) : 0.0f);
+        sum[v] += in ? w * sr[s][v] : 0.0f;
       }
       if (t0 + s < A.L) {
-        const int64_t t = t0 + s;
-        store_row<T, VEC, VIO>((T*)A.dx.p + b * A.dx.sb + t * A.dx.st, c, A.D, ox);
-        store_row<T, VEC, VIO>((T*)A.dr.p + b * A.dr.sb + t * A.dr.st, c, A.D, orr);
-        store_row<T, VEC, VIO>((T*)A.di.p + b * A.di.sb + t * A.di.st, c, A.D, oi);
+        store_row<T, VEC, VIO>(ox + s * A.dx.st, c, A.D, vx);
+        store_row<T, VEC, VIO>(orr + s * A.dr.st, c, A.D, vr);
+        store_row<T, VEC, VIO>(oi + s * A.di.st, c, A.D, vi);
       }
     }
-    __syncthreads();
-    if (tg == 0)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) enter[cl + v] = cc[v];
-    __syncthreads();
-  }
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) gsum[tg][cl + v] = sum[v];
-  __syncthreads();
-  if (tg == 0)
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      if (A.dh0 != nullptr && c + v < A.D) A.dh0[b * A.D + c + v] = enter[cl + v];
-      double s = 0.0;
-      for (int g = 0; g < TG; ++g) s += gsum[g][cl + v];
-      A.part[b * ((int64_t)A.NB * GATED_CW) + c + v] = (float)s;
+#pragma unroll
+      for (int k = CGL; k < 64; k <<= 1) sum[v] += __shfl_xor(sum[v], k, 64);
+      if (wl < CGL) sums[wave][cl + v] = sum[v];
     }
+    __syncthreads();
+    if (wave == 0) {
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) t += sums[w][wl];
+      // (a word like the others, so that what a later call finds here is never taken for one of its own)
+      A.part[(b * tiles + tile) * ((int64_t)A.NB * GATED_CW) + cw] = word(t, tag);
+    }
+    if constexpr (LOOK) __syncthreads();
+  }
+  if constexpr (LOOK) leave(A.hdr, tag);
 }
 
-// dgamma[c] = sum of the rows of part [n][Dp], in order, in float64
-__global__ __launch_bounds__(256) void gated_reduce_kernel(const float* part, int64_t n, int Dp, int D, float* dgamma) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= D) return;
+// dgamma[c] = sum of the rows of part [n][Dp]: 16 channels of a work-group, its 64 rows of threads every 64th row, then
+// their sums in order, in float64
+__global__ __launch_bounds__(1024) void gated_reduce_kernel(const uint64_t* part, int64_t n, int Dp, int D, float* dgamma) {
+  __shared__ double sums[64][16];
+  const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
   double s = 0.0;
-  for (int64_t k = 0; k < n; ++k) s += part[k * Dp + c];
-  dgamma[c] = (float)s;
+  if (c < D)
+    for (int64_t k = g; k < n; k += 64) s += __uint_as_float((uint32_t)part[k * Dp + c]);
+  sums[g][l] = s;
+  __syncthreads();
+  if (g == 0 && c < D) {
+    for (int k = 1; k < 64; ++k) s += sums[k][l];
+    dgamma[c] = (float)s;
+  }
 }
 
 template <typename T>
@@ -311,28 +560,54 @@ __global__ __launch_bounds__(256) void gated_step_kernel(Rows x, Rows r, Rows i,
   y[k] = from_f32<T>(v);
 }
 
+// Work-groups of a call whose chains have several tiles: two on each of 256 compute units.
+unsigned gated_groups(int64_t B, int64_t L, int64_t NB, int64_t tile) {
+  const int64_t n = B * NB * gated_tiles(L, tile);
+  return (unsigned)(n < 512 ? n : 512);
+}
+
+// A chain of one tile needs no look-back, no tickets and no words: the smallest tile that holds it.
+template <typename T, int VEC, int S, bool VIO>
+void gated_fwd(const GatedArgs& a, hipStream_t st) {
+  constexpr int STEPS = S * VEC;  // of a wave
+  const dim3 chains((unsigned)(a.B * a.NB));
+  if (a.L <= STEPS)
+    gated_fwd_kernel<T, VEC, S, 64, VIO, false><<<chains, 64, 0, st>>>(a);
+  else if (a.L <= 4 * STEPS)
+    gated_fwd_kernel<T, VEC, S, 256, VIO, false><<<chains, 256, 0, st>>>(a);
+  else if (a.L <= 8 * STEPS)
+    gated_fwd_kernel<T, VEC, S, 512, VIO, false><<<chains, 512, 0, st>>>(a);
+  else
+    gated_fwd_kernel<T, VEC, S, 512, VIO, true><<<dim3(gated_groups(a.B, a.L, a.NB, 8 * STEPS)), 512, 0, st>>>(a);
+}
+template <typename T, int VEC, int S, bool VIO>
+void gated_bwd(const GatedArgs& a, hipStream_t st) {
+  constexpr int STEPS = S * VEC;
+  if (a.L <= 8 * STEPS)
+    gated_bwd_kernel<T, VEC, S, 512, VIO, false><<<dim3((unsigned)(a.B * a.NB)), 512, 0, st>>>(a);
+  else
+    gated_bwd_kernel<T, VEC, S, 512, VIO, true><<<dim3(gated_groups(a.B, a.L, a.NB, 8 * STEPS)), 512, 0, st>>>(a);
+}
+
 }  // namespace
 
 template <typename T>
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t st) {
-  constexpr int VEC = 4, S = 8, NT = 256;
-  const dim3 grid((unsigned)(a.B * a.NB));
   if (a.vec)
-    gated_fwd_kernel<T, VEC, S, NT, true><<<grid, NT, 0, st>>>(a);
+    gated_fwd<T, 4, 8, true>(a, st);
   else
-    gated_fwd_kernel<T, VEC, S, NT, false><<<grid, NT, 0, st>>>(a);
+    gated_fwd<T, 1, 32, false>(a, st);  // a channel a lane: rows of any alignment read in one piece
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st) {
-  constexpr int VEC = 4, S = 8, NT = 256;
-  const dim3 grid((unsigned)(a.B * a.NB));
   if (a.vec)
-    gated_bwd_kernel<T, VEC, S, NT, true><<<grid, NT, 0, st>>>(a);
+    gated_bwd<T, 4, 4, true>(a, st);
   else
-    gated_bwd_kernel<T, VEC, S, NT, false><<<grid, NT, 0, st>>>(a);
-  gated_reduce_kernel<<<dim3((unsigned)((a.D + 255) / 256)), 256, 0, st>>>(a.part, a.B, a.NB * GATED_CW, a.D, dgamma);
+    gated_bwd<T, 1, 16, false>(a, st);
+  const int64_t rows = a.B * gated_tiles(a.L, GATED_BWD_TILE);
+  gated_reduce_kernel<<<dim3((unsigned)((a.D + 15) / 16)), 1024, 0, st>>>(a.part, rows, a.NB * GATED_CW, a.D, dgamma);
   return hipGetLastError();
 }
 

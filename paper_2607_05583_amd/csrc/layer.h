@@ -65,6 +65,11 @@ __device__ __forceinline__ float act_slope(float v, int act) {
 // ---------------------------------------------------------------------------
 constexpr int GATED_CW = 64;      // channels of a chain: 128-byte rows of bf16
 constexpr int GATED_CARRY = 128;  // steps between the states that a forward keeps for its backward
+constexpr int GATED_FWD_TILE = 256, GATED_BWD_TILE = 128;  // steps of a tile (of 512 threads)
+constexpr int GATED_TILE_WORDS = 3 * GATED_CW;             // words that a tile publishes
+
+// tiles of a chain: one where there is no step, which hands the state through
+__host__ __device__ inline int64_t gated_tiles(int64_t L, int64_t tile) { return L > 0 ? (L + tile - 1) / tile : 1; }
 
 struct GatedArgs {
   Rows x, r, i, dy;
@@ -80,7 +85,9 @@ struct GatedArgs {
   float* carry;         // [B][ceil(L / GATED_CARRY)][D]: the state before each such step (forward: written where not null)
   const float* dh_out;  // [B][D] or null
   float* dh0;           // [B][D] or null
-  float* part;          // [B][NB * GATED_CW] partial sums of dgamma
+  uint32_t* hdr;        // [0] status (a wait gave up), [1] number of calls so far, [2] next ticket, [3] work-groups done
+  uint64_t* words;      // published maps and end values: [chain][tile][A, H or C, end][GATED_CW]
+  uint64_t* part;       // backward: partial sums of dgamma [B][tiles][NB * GATED_CW]
 };
 
 template <typename T>
