@@ -536,7 +536,8 @@ typedef struct {
  *   y        [B][L][D] of dt, or NULL
  *   gamma    [D]; h0 [B][D] or NULL (zero); h_out [B][D] or NULL (may be h0 itself)
  *   lengths  [B] int32 or NULL: row b has its first lengths[b] steps (clamped to
- *            0..L); behind them nothing is read, y is 0 and the state stays
+ *            0..L); what x, r and i hold behind them does not matter, y is 0 there and the
+ *            state stays
  *   carry    [B][ceil(L / RES_GATED_CARRY)][D] or NULL: receives the state before
  *            every RES_GATED_CARRY-th step, which the backward starts from
  *   ws       resonator_gated_scan_workspace_bytes(dt, B, L, D) bytes, 256-byte aligned

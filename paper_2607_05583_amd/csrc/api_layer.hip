@@ -53,8 +53,9 @@ bool rows_apart(int64_t sb, int64_t st, int64_t B, int64_t L, int64_t D) {
 int check_rows(const char* name, const void* p, int64_t sb, int64_t st, size_t es) {
   if (p == nullptr) return api_error(RES_ERR_INVALID_ARG, "%s must be non-null", name);
   if (!aligned(p, es)) return api_error(RES_ERR_MISALIGNED, "%s must be aligned to its element", name);
-  if (sb < 0 || st < 0 || sb > (1LL << 40) || st > (1LL << 40))
-    return api_error(RES_ERR_INVALID_ARG, "%s: strides must be in [0, 2^40] elements", name);
+  // (a tile's bytes have 32-bit offsets)
+  if (sb < 0 || st < 0 || sb > (1LL << 40) || st > (1LL << 21))
+    return api_error(RES_ERR_UNSUPPORTED, "%s: strides must be in [0, 2^40] (rows) and [0, 2^21] (steps) elements", name);
   return RES_OK;
 }
 
@@ -65,7 +66,7 @@ int check_scan(int64_t B, int64_t L, int64_t D, res_dtype_t dt) {
                      (long long)L, (long long)D);
   const int64_t NB = (D + GATED_CW - 1) / GATED_CW;
   // (tiles of a call and tickets are 32-bit counts)
-  if (D > (1 << 24) || L >= (1LL << 31) - 65536 || B > (1LL << 31) || B * NB >= (1LL << 30) ||
+  if (D > (1 << 21) || L >= (1LL << 31) - 65536 || B > (1LL << 31) || B * NB >= (1LL << 30) ||
       B * NB * (L / GATED_BWD_TILE + 1) >= (1LL << 31))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld D=%lld)", (long long)B,
                      (long long)L, (long long)D);

@@ -19,8 +19,8 @@
 // back over at most WINDOW tiles for the nearest end state and applies the maps from
 // there on, one after the other.  That is the same sequence of operations wherever the
 // search ends, so results do not depend on timing.  Tiles are taken in order from a
-// ticket counter by work-groups that stay, so the tiles that one waits for are always at
-// work.  A published value is a 64-bit word with the call's number beside it: a word is
+// ticket counter, so the tiles that one waits for are always at work (one work-group a
+// tile: a loop over tiles took 60 registers more).  A published value is a 64-bit word with the call's number beside it: a word is
 // its own flag, and nothing has to be cleared between calls.
 #include "layer.h"
 
@@ -60,29 +60,29 @@ __device__ __forceinline__ Gate gate(float r, float gamma) {
 
 template <typename T, int VEC> struct __align__(sizeof(T) * VEC) Vec { T v[VEC]; };
 
-// VEC channels from channel c of a row; channels from D on are zero
-template <typename T, int VEC, bool VIO>
-__device__ __forceinline__ Vec<T, VEC> load_row(const T* p, int c, int D) {
-  Vec<T, VEC> o;
-  if constexpr (VIO) {
-    if (c < D) return *reinterpret_cast<const Vec<T, VEC>*>(p + c);
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) o.v[v] = T(0);
-  } else {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) o.v[v] = c + v < D ? p[c + v] : T(0);
-  }
-  return o;
+// A thread's rows of a tile: the tile's first element (the same for all threads) and this thread's bytes from there.
+struct Walk {
+  const char* base;
+  int64_t st;    // bytes of a step
+  uint32_t off;  // this thread's first step, its channel
+};
+template <typename T>
+__device__ __forceinline__ Walk walk(const void* p, int64_t sb, int64_t st, int64_t b, int64_t t0, int mine, int c) {
+  return Walk{(const char*)((const T*)p + b * sb + t0 * st), st * (int64_t)sizeof(T), (uint32_t)((mine * st + c) * (int64_t)sizeof(T))};
 }
-template <typename T, int VEC, bool VIO>
-__device__ __forceinline__ void store_row(T* p, int c, int D, const Vec<T, VEC>& o) {
-  if constexpr (VIO) {
-    if (c < D) *reinterpret_cast<Vec<T, VEC>*>(p + c) = o;
-  } else {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v)
-      if (c + v < D) p[c + v] = o.v[v];
-  }
+// step s of this thread's, or (clamped) the step `most` of the tile where that comes first
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> load_row(const Walk& w, int s) {
+  return *reinterpret_cast<const Vec<T, VEC>*>(w.base + s * w.st + w.off);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ Vec<T, VEC> load_row_clamped(const Walk& w, int s, int mine, int most) {
+  const int back = mine + s > most ? mine + s - most : 0;  // steps past it
+  return *reinterpret_cast<const Vec<T, VEC>*>(w.base + s * w.st + w.off - back * w.st);
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void store_row(const Walk& w, int s, const Vec<T, VEC>& o) {
+  *reinterpret_cast<Vec<T, VEC>*>(const_cast<char*>(w.base) + s * w.st + w.off) = o;
 }
 
 __device__ __forceinline__ int row_len(const int* lengths, int64_t b, int64_t L) {
@@ -171,16 +171,16 @@ __device__ __forceinline__ void look_back(const uint64_t* words, int64_t o, uint
       if (__all(have) && lane == 0) sh.found = 1;
     }
     __syncthreads();
-    if (sh.found) return;
+    if (__builtin_amdgcn_readfirstlane(sh.found)) return;
     __builtin_amdgcn_s_sleep(2);
   }
 }
 
-// The next tile of this work-group (whole work-group).
+// This work-group's tile (whole work-group).
 __device__ __forceinline__ uint32_t take_ticket(uint32_t* hdr, LookShared& sh) {
   if (threadIdx.x == 0) sh.ticket = (int)atomicAdd(hdr + 2, 1u);
   __syncthreads();
-  const uint32_t t = (uint32_t)sh.ticket;
+  const uint32_t t = (uint32_t)__builtin_amdgcn_readfirstlane(sh.ticket);
   __syncthreads();
   return t;
 }
@@ -219,7 +219,7 @@ __device__ __forceinline__ void scan_down(float& A, float& C) {  // inclusive: t
   }
 }
 
-template <typename T, int VEC, int S, int NT, bool VIO, bool LOOK>
+template <typename T, int VEC, int S, int NT, bool LOOK>
 __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
   constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG, NW = NT / 64, WG = 64 / CGL;
   __shared__ float2 total[NW][GATED_CW];
@@ -227,129 +227,144 @@ __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
   const int wl = threadIdx.x & 63, wave = threadIdx.x >> 6, lane = wl % CGL, tg = threadIdx.x / CGL, cl = lane * VEC;
   const int64_t tiles = gated_tiles(A.L, TILE), chains = A.B * A.NB, NC = (A.L + GATED_CARRY - 1) / GATED_CARRY;
   const uint32_t tag = LOOK ? A.hdr[1] + 1 : 0;
-  for (int64_t turn = 0;; ++turn) {
-    int64_t o = 0, chain = blockIdx.x;
-    if constexpr (LOOK) {
-      const uint32_t t = take_ticket(A.hdr, sh);
-      if (t >= tiles * chains) break;
-      o = t / (uint32_t)chains;
-      chain = t % (uint32_t)chains;
-    } else if (turn > 0) {
-      break;
-    }
-    const int64_t b = chain / A.NB;
-    const int cb = (int)(chain % A.NB) * GATED_CW, c = cb + cl;
-    const int len = row_len(A.lengths, b, A.L);
-    const int64_t t0 = o * TILE + tg * S;
-    float a[S][VEC], u[S][VEC];
-    {
-      float gam[VEC];
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
-      const T* px = (const T*)A.x.p + b * A.x.sb + t0 * A.x.st;
-      const T* pr = (const T*)A.r.p + b * A.r.sb + t0 * A.r.st;
-      const T* pi = (const T*)A.i.p + b * A.i.sb + t0 * A.i.st;
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        if (t0 + s < len) {
-          const auto xv = load_row<T, VEC, VIO>(px + s * A.x.st, c, A.D);
-          const auto rv = load_row<T, VEC, VIO>(pr + s * A.r.st, c, A.D);
-          const auto iv = load_row<T, VEC, VIO>(pi + s * A.i.st, c, A.D);
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            const Gate g = gate(to_f32(rv.v[v]), gam[v]);
-            a[s][v] = g.a;
-            u[s][v] = g.beta * sigmoid_fast(to_f32(iv.v[v])) * to_f32(xv.v[v]);
-          }
-        } else {
-#pragma unroll
-          for (int v = 0; v < VEC; ++v) a[s][v] = 1.0f, u[s][v] = 0.0f;
-        }
-      }
-    }
-    float ea[VEC], eh[VEC];  // the map of this wave's steps before this thread's
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      float pa = 1.0f, ph = 0.0f;
+  int64_t o = 0, chain = blockIdx.x;
+  if constexpr (LOOK) {
+    const uint32_t t = take_ticket(A.hdr, sh);
+    o = t / (uint32_t)chains;
+    chain = t - (uint32_t)o * (uint32_t)chains;
+  }
+  const int64_t b = (uint32_t)chain / (uint32_t)A.NB;
+  const int cb = (int)(chain - b * A.NB) * GATED_CW, c = cb + cl, cs = c < A.D ? c : 0;
+  const int len = row_len(A.lengths, b, A.L);
+  // steps of the tile: this thread's first, those before the row's end, those before the tensor's
+  const int64_t tt = o * TILE;
+  const int mine = tg * S, valid = (int)((len < tt ? 0 : len - tt) < TILE ? (len < tt ? 0 : len - tt) : TILE),
+            there = (int)(A.L - tt < TILE ? A.L - tt : TILE);
+  float a[S][VEC], u[S][VEC];
+  {
+    // All loads first and without branches: steps behind the row's end load its last one again, channels behind the
+    // last one the first, and what they give is not used.
+    Vec<T, VEC> x[S], r[S], i[S];
+    const Walk wx = walk<T>(A.x.p, A.x.sb, A.x.st, b, tt, mine, cs), wr = walk<T>(A.r.p, A.r.sb, A.r.st, b, tt, mine, cs),
+               wi = walk<T>(A.i.p, A.i.sb, A.i.st, b, tt, mine, cs);
+    if (valid == TILE) {
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        pa *= a[s][v];
-        ph = fmaf(a[s][v], ph, u[s][v]);
+        r[s] = load_row<T, VEC>(wr, s);
+        i[s] = load_row<T, VEC>(wi, s);
+        x[s] = load_row<T, VEC>(wx, s);
       }
-      scan_up<CGL>(pa, ph);
-      if (wl >= 64 - CGL) total[wave][cl + v] = make_float2(pa, ph);
-      ea[v] = 1.0f;
-      eh[v] = 0.0f;
-      if constexpr (WG > 1) {
-        const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
-        if (wl >= CGL) ea[v] = xa, eh[v] = xh;
-      }
-    }
-    __syncthreads();
-    float ta = 1.0f, th = 0.0f;  // the tile's map (wave 0: a channel a lane)
-    uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
-    const int cw = cb + wl;
-    const float init = A.h0 != nullptr && cw < A.D ? A.h0[b * A.D + cw] : 0.0f;
-    if (wave == 0) {
+    } else if (there > 0) {
+      const int most = valid > 0 ? valid - 1 : 0;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float2 m = total[w][wl];
-        th = fmaf(m.x, th, m.y);
-        ta *= m.x;
-      }
-      if (LOOK && o + 1 < tiles) {
-        uint64_t* w = words + o * GATED_TILE_WORDS + wl;
-        store_word(w, ta, tag);
-        store_word(w + 64, th, tag);
+      for (int s = 0; s < S; ++s) {
+        r[s] = load_row_clamped<T, VEC>(wr, s, mine, most);
+        i[s] = load_row_clamped<T, VEC>(wi, s, mine, most);
+        x[s] = load_row_clamped<T, VEC>(wx, s, mine, most);
       }
     }
-    if constexpr (LOOK) {
-      look_back(words, o, tag, init, A.hdr, sh);
-    } else {
-      if (wave == 0) sh.enter[wl] = init;
-      __syncthreads();
-    }
-    if (wave == 0) {
-      const float end = fmaf(ta, sh.enter[wl], th);
-      if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
-      if (A.h_out != nullptr && o + 1 == tiles && cw < A.D) A.h_out[b * A.D + cw] = end;
-    }
-    float h[VEC];
+    float gam[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) h[v] = sh.enter[cl + v];
-    for (int w = 0; w < wave; ++w)
+    for (int v = 0; v < VEC; ++v) gam[v] = A.gamma[cs + v];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const float2 m = total[w][cl + v];
-        h[v] = fmaf(m.x, h[v], m.y);
+        const Gate g = gate(to_f32(r[s].v[v]), gam[v]);
+        a[s][v] = g.a;
+        u[s][v] = g.beta * sigmoid_fast(to_f32(i[s].v[v])) * to_f32(x[s].v[v]);
       }
+    if (valid < TILE) {  // behind the end the state is kept
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) h[v] = fmaf(ea[v], h[v], eh[v]);
-    if (A.carry != nullptr && t0 % GATED_CARRY == 0 && t0 < A.L) {
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (c + v < A.D) A.carry[(b * NC + t0 / GATED_CARRY) * A.D + c + v] = h[v];
-    }
-    if (A.y != nullptr) {
-      T* py = (T*)A.y + (b * A.L + t0) * A.D;
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        Vec<T, VEC> ov;
+      for (int s = 0; s < S; ++s)
 #pragma unroll
         for (int v = 0; v < VEC; ++v) {
-          h[v] = fmaf(a[s][v], h[v], u[s][v]);
-          ov.v[v] = from_f32<T>(t0 + s < len ? h[v] : 0.0f);
+          a[s][v] = mine + s < valid ? a[s][v] : 1.0f;
+          u[s][v] = mine + s < valid ? u[s][v] : 0.0f;
         }
-        if (t0 + s < A.L) store_row<T, VEC, VIO>(py + (int64_t)s * A.D, c, A.D, ov);
-      }
     }
-    if constexpr (LOOK) __syncthreads();  // total and sh are free for the next tile
+  }
+  float ea[VEC], eh[VEC];  // the map of this wave's steps before this thread's
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    float pa = 1.0f, ph = 0.0f;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      pa *= a[s][v];
+      ph = fmaf(a[s][v], ph, u[s][v]);
+    }
+    scan_up<CGL>(pa, ph);
+    if (wl >= 64 - CGL) total[wave][cl + v] = make_float2(pa, ph);
+    ea[v] = 1.0f;
+    eh[v] = 0.0f;
+    if constexpr (WG > 1) {
+      const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
+      if (wl >= CGL) ea[v] = xa, eh[v] = xh;
+    }
+  }
+  __syncthreads();
+  float ta = 1.0f, th = 0.0f;  // the tile's map (wave 0: a channel a lane)
+  uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
+  const int cw = cb + wl;
+  const float init = A.h0 != nullptr && cw < A.D ? A.h0[b * A.D + cw] : 0.0f;
+  if (wave == 0) {
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float2 m = total[w][wl];
+      th = fmaf(m.x, th, m.y);
+      ta *= m.x;
+    }
+    if (LOOK && o + 1 < tiles) {
+      uint64_t* w = words + o * GATED_TILE_WORDS + wl;
+      store_word(w, ta, tag);
+      store_word(w + 64, th, tag);
+    }
+  }
+  if constexpr (LOOK) {
+    look_back(words, o, tag, init, A.hdr, sh);
+  } else {
+    if (wave == 0) sh.enter[wl] = init;
+    __syncthreads();
+  }
+  if (wave == 0) {
+    const float end = fmaf(ta, sh.enter[wl], th);
+    if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
+    if (A.h_out != nullptr && o + 1 == tiles && cw < A.D) A.h_out[b * A.D + cw] = end;
+  }
+  float h[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = sh.enter[cl + v];
+  for (int w = 0; w < wave; ++w)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      const float2 m = total[w][cl + v];
+      h[v] = fmaf(m.x, h[v], m.y);
+    }
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) h[v] = fmaf(ea[v], h[v], eh[v]);
+  if (A.carry != nullptr && mine % GATED_CARRY == 0 && mine < there && c < A.D) {
+    float* to = A.carry + (b * NC + (tt + mine) / GATED_CARRY) * A.D + c;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) to[v] = h[v];
+  }
+  if (A.y != nullptr && c < A.D) {
+    const Walk wy = walk<T>(A.y, A.L * A.D, A.D, b, tt, mine, c);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      Vec<T, VEC> ov;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        h[v] = fmaf(a[s][v], h[v], u[s][v]);
+        ov.v[v] = from_f32<T>(mine + s < valid ? h[v] : 0.0f);
+      }
+      if (mine + s < there) store_row<T, VEC>(wy, s, ov);
+    }
   }
   if constexpr (LOOK) leave(A.hdr, tag);
 }
 
 // Tiles from the last to the first; one starts at a kept state, so only the adjoint is looked back for.
-template <typename T, int VEC, int S, int NT, bool VIO, bool LOOK>
+template <typename T, int VEC, int S, int NT, bool LOOK>
 __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(GatedArgs A) {
   constexpr int CGL = GATED_CW / VEC, TG = NT / CGL, TILE = S * TG, NW = NT / 64, WG = 64 / CGL;
   static_assert(TILE % GATED_CARRY == 0, "a tile starts at a kept state");
@@ -359,174 +374,204 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
   const int wl = threadIdx.x & 63, wave = threadIdx.x >> 6, lane = wl % CGL, tg = threadIdx.x / CGL, cl = lane * VEC;
   const int64_t tiles = gated_tiles(A.L, TILE), chains = A.B * A.NB, NC = (A.L + GATED_CARRY - 1) / GATED_CARRY;
   const uint32_t tag = LOOK ? A.hdr[1] + 1 : 0;
-  for (int64_t turn = 0;; ++turn) {
-    int64_t o = 0, chain = blockIdx.x;
-    if constexpr (LOOK) {
-      const uint32_t t = take_ticket(A.hdr, sh);
-      if (t >= tiles * chains) break;
-      o = t / (uint32_t)chains;
-      chain = t % (uint32_t)chains;
-    } else if (turn > 0) {
-      break;
-    }
-    const int64_t tile = tiles - 1 - o, b = chain / A.NB;
-    const int cb = (int)(chain % A.NB) * GATED_CW, c = cb + cl;
-    const int len = row_len(A.lengths, b, A.L);
-    const int64_t t0 = tile * TILE + tg * S;
-    float gam[VEC];
+  int64_t o = 0, chain = blockIdx.x;
+  if constexpr (LOOK) {
+    const uint32_t t = take_ticket(A.hdr, sh);
+    o = t / (uint32_t)chains;
+    chain = t - (uint32_t)o * (uint32_t)chains;
+  }
+  const int64_t tile = tiles - 1 - o, b = (uint32_t)chain / (uint32_t)A.NB;
+  const int cb = (int)(chain - b * A.NB) * GATED_CW, c = cb + cl, cs = c < A.D ? c : 0;
+  const int len = row_len(A.lengths, b, A.L);
+  const int64_t tt = tile * TILE;
+  const int mine = tg * S, valid = (int)((len < tt ? 0 : len - tt) < TILE ? (len < tt ? 0 : len - tt) : TILE),
+            there = (int)(A.L - tt < TILE ? A.L - tt : TILE);
+  float gam[VEC];
+  Vec<T, VEC> x[S], d[S];
+  float a[S][VEC], sr[S][VEC], q[S][VEC];
+  float h[VEC];  // the state before the tile
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) gam[v] = c + v < A.D ? A.gamma[c + v] : 0.0f;
-    Vec<T, VEC> x[S], d[S];
-    float a[S][VEC], sr[S][VEC], q[S][VEC];
-    {
-      const T* px = (const T*)A.x.p + b * A.x.sb + t0 * A.x.st;
-      const T* pr = (const T*)A.r.p + b * A.r.sb + t0 * A.r.st;
-      const T* pi = (const T*)A.i.p + b * A.i.sb + t0 * A.i.st;
-      const T* pd = (const T*)A.dy.p + b * A.dy.sb + t0 * A.dy.st;
+  for (int v = 0; v < VEC; ++v) h[v] = 0.0f;
+  {
+    Vec<T, VEC> r[S], i[S];
+    const Walk wx = walk<T>(A.x.p, A.x.sb, A.x.st, b, tt, mine, cs), wr = walk<T>(A.r.p, A.r.sb, A.r.st, b, tt, mine, cs),
+               wi = walk<T>(A.i.p, A.i.sb, A.i.st, b, tt, mine, cs), wd = walk<T>(A.dy.p, A.dy.sb, A.dy.st, b, tt, mine, cs);
+    if (valid == TILE) {
 #pragma unroll
       for (int s = 0; s < S; ++s) {
-        if (t0 + s < len) {
-          x[s] = load_row<T, VEC, VIO>(px + s * A.x.st, c, A.D);
-          d[s] = load_row<T, VEC, VIO>(pd + s * A.dy.st, c, A.D);
-          const auto rv = load_row<T, VEC, VIO>(pr + s * A.r.st, c, A.D);
-          const auto iv = load_row<T, VEC, VIO>(pi + s * A.i.st, c, A.D);
+        r[s] = load_row<T, VEC>(wr, s);
+        i[s] = load_row<T, VEC>(wi, s);
+        x[s] = load_row<T, VEC>(wx, s);
+        d[s] = load_row<T, VEC>(wd, s);
+      }
+    } else if (there > 0) {
+      const int most = valid > 0 ? valid - 1 : 0;
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            sr[s][v] = sigmoid_fast(to_f32(rv.v[v]));
-            q[s][v] = sigmoid_fast(to_f32(iv.v[v]));
-            a[s][v] = exp2_fast(-LOG2E * (gam[v] * sr[s][v]));
-          }
-        } else {  // s = 0: a = 1 and nothing is added
+      for (int s = 0; s < S; ++s) {
+        r[s] = load_row_clamped<T, VEC>(wr, s, mine, most);
+        i[s] = load_row_clamped<T, VEC>(wi, s, mine, most);
+        x[s] = load_row_clamped<T, VEC>(wx, s, mine, most);
+        d[s] = load_row_clamped<T, VEC>(wd, s, mine, most);
+      }
+    }
+    if (there > 0) {
+      const float* from = A.carry + (b * NC + tile * (TILE / GATED_CARRY)) * A.D + cs;
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) x[s].v[v] = d[s].v[v] = T(0), a[s][v] = 1.0f, sr[s][v] = q[s][v] = 0.0f;
+      for (int v = 0; v < VEC; ++v) h[v] = from[v];
+    }
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) gam[v] = A.gamma[cs + v];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        sr[s][v] = sigmoid_fast(to_f32(r[s].v[v]));
+        q[s][v] = sigmoid_fast(to_f32(i[s].v[v]));
+        a[s][v] = exp2_fast(-LOG2E * (gam[v] * sr[s][v]));
+      }
+    if (valid < TILE) {  // behind the end s = 0: a = 1 and nothing is added
+#pragma unroll
+      for (int s = 0; s < S; ++s) {
+        const bool in = mine + s < valid;
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) {
+          a[s][v] = in ? a[s][v] : 1.0f;
+          sr[s][v] = in ? sr[s][v] : 0.0f;
+          q[s][v] = in ? q[s][v] : 0.0f;
+          x[s].v[v] = in ? x[s].v[v] : T(0);
+          d[s].v[v] = in ? d[s].v[v] : T(0);
         }
       }
     }
-    float hp[S][VEC];           // beta q x, then the state before the step
-    float ea[VEC], eh[VEC];     // maps of this wave's steps before this thread's
-    float fa[VEC], fc[VEC];     // and, for the adjoint, after them
+  }
+  float hp[S][VEC];        // beta q x, then the state before the step
+  float ea[VEC], eh[VEC];  // maps of this wave's steps before this thread's
+  float fa[VEC], fc[VEC];  // and, for the adjoint, after them
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      float pa = 1.0f, ph = 0.0f, pc = 0.0f;
+  for (int v = 0; v < VEC; ++v) {
+    float pa = 1.0f, ph = 0.0f, pc = 0.0f;
 #pragma unroll
-      for (int s = 0; s < S; ++s) {
-        hp[s][v] = drive_gate(gam[v] * sr[s][v], a[s][v]).beta * q[s][v] * to_f32(x[s].v[v]);
-        pa *= a[s][v];
-        ph = fmaf(a[s][v], ph, hp[s][v]);
-      }
-#pragma unroll
-      for (int s = S - 1; s >= 0; --s) pc = a[s][v] * (to_f32(d[s].v[v]) + pc);
-      float da = pa, dc = pc;
-      scan_up<CGL>(pa, ph);
-      scan_down<CGL>(da, dc);
-      if (wl >= 64 - CGL) {
-        total[0][wave][cl + v] = pa;
-        total[1][wave][cl + v] = ph;
-      }
-      if (wl < CGL) total[2][wave][cl + v] = dc;
-      ea[v] = fa[v] = 1.0f;
-      eh[v] = fc[v] = 0.0f;
-      if constexpr (WG > 1) {
-        const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
-        const float ya = __shfl_down(da, CGL, 64), yc = __shfl_down(dc, CGL, 64);
-        if (wl >= CGL) ea[v] = xa, eh[v] = xh;
-        if (wl < 64 - CGL) fa[v] = ya, fc[v] = yc;
-      }
+    for (int s = 0; s < S; ++s) {
+      hp[s][v] = drive_gate(gam[v] * sr[s][v], a[s][v]).beta * q[s][v] * to_f32(x[s].v[v]);
+      pa *= a[s][v];
+      ph = fmaf(a[s][v], ph, hp[s][v]);
     }
+#pragma unroll
+    for (int s = S - 1; s >= 0; --s) pc = a[s][v] * (to_f32(d[s].v[v]) + pc);
+    float da = pa, dc = pc;
+    scan_up<CGL>(pa, ph);
+    scan_down<CGL>(da, dc);
+    if (wl >= 64 - CGL) {
+      total[0][wave][cl + v] = pa;
+      total[1][wave][cl + v] = ph;
+    }
+    if (wl < CGL) total[2][wave][cl + v] = dc;
+    ea[v] = fa[v] = 1.0f;
+    eh[v] = fc[v] = 0.0f;
+    if constexpr (WG > 1) {
+      const float xa = __shfl_up(pa, CGL, 64), xh = __shfl_up(ph, CGL, 64);
+      const float ya = __shfl_down(da, CGL, 64), yc = __shfl_down(dc, CGL, 64);
+      if (wl >= CGL) ea[v] = xa, eh[v] = xh;
+      if (wl < 64 - CGL) fa[v] = ya, fc[v] = yc;
+    }
+  }
+  __syncthreads();
+  float ta = 1.0f, tc = 0.0f;
+  uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
+  const int cw = cb + wl;
+  const float init = A.dh_out != nullptr && cw < A.D ? A.dh_out[b * A.D + cw] : 0.0f;
+  if (wave == 0) {
+#pragma unroll
+    for (int w = NW - 1; w >= 0; --w) {
+      const float m = total[0][w][wl];
+      tc = fmaf(m, tc, total[2][w][wl]);
+      ta *= m;
+    }
+    if (LOOK && o + 1 < tiles) {
+      uint64_t* w = words + o * GATED_TILE_WORDS + wl;
+      store_word(w, ta, tag);
+      store_word(w + 64, tc, tag);
+    }
+  }
+  // the states before the steps (nothing of this waits for other tiles)
+  for (int w = 0; w < wave; ++w)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) h[v] = fmaf(total[0][w][cl + v], h[v], total[1][w][cl + v]);
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) {
+    h[v] = fmaf(ea[v], h[v], eh[v]);
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const float before = h[v];
+      h[v] = fmaf(a[s][v], h[v], hp[s][v]);
+      hp[s][v] = before;
+    }
+  }
+  if constexpr (LOOK) {
+    look_back(words, o, tag, init, A.hdr, sh);
+  } else {
+    if (wave == 0) sh.enter[wl] = init;
     __syncthreads();
-    float ta = 1.0f, tc = 0.0f;
-    uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
-    const int cw = cb + wl;
-    const float init = A.dh_out != nullptr && cw < A.D ? A.dh_out[b * A.D + cw] : 0.0f;
-    if (wave == 0) {
+  }
+  if (wave == 0) {
+    const float end = fmaf(ta, sh.enter[wl], tc);
+    if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
+    if (A.dh0 != nullptr && o + 1 == tiles && cw < A.D) A.dh0[b * A.D + cw] = end;
+  }
+  float cc[VEC], sum[VEC];
 #pragma unroll
-      for (int w = NW - 1; w >= 0; --w) {
-        const float m = total[0][w][wl];
-        tc = fmaf(m, tc, total[2][w][wl]);
-        ta *= m;
-      }
-      if (LOOK && o + 1 < tiles) {
-        uint64_t* w = words + o * GATED_TILE_WORDS + wl;
-        store_word(w, ta, tag);
-        store_word(w + 64, tc, tag);
-      }
-    }
-    if constexpr (LOOK) {
-      look_back(words, o, tag, init, A.hdr, sh);
-    } else {
-      if (wave == 0) sh.enter[wl] = init;
-      __syncthreads();
-    }
-    if (wave == 0) {
-      const float end = fmaf(ta, sh.enter[wl], tc);
-      if (LOOK && o + 1 < tiles) store_word(words + o * GATED_TILE_WORDS + 128 + wl, end, tag);
-      if (A.dh0 != nullptr && o + 1 == tiles && cw < A.D) A.dh0[b * A.D + cw] = end;
-    }
-    float h[VEC], cc[VEC], sum[VEC];
+  for (int v = 0; v < VEC; ++v) {
+    cc[v] = sh.enter[cl + v];
+    sum[v] = 0.0f;
+  }
+  for (int w = NW - 1; w > wave; --w)
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
-      h[v] = c + v < A.D && A.L > 0 ? A.carry[(b * NC + tile * (TILE / GATED_CARRY)) * A.D + c + v] : 0.0f;
-      cc[v] = sh.enter[cl + v];
-      sum[v] = 0.0f;
-    }
-    for (int w = 0; w < wave; ++w)
+    for (int v = 0; v < VEC; ++v) cc[v] = fmaf(total[0][w][cl + v], cc[v], total[2][w][cl + v]);
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) h[v] = fmaf(total[0][w][cl + v], h[v], total[1][w][cl + v]);
-    for (int w = NW - 1; w > wave; --w)
+  for (int v = 0; v < VEC; ++v) {
+    cc[v] = fmaf(fa[v], cc[v], fc[v]);
+    // beta is computed again below: kept from above it would cost a third of the registers
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) cc[v] = fmaf(total[0][w][cl + v], cc[v], total[2][w][cl + v]);
+    for (int s = 0; s < S; ++s) asm volatile("" : "+v"(sr[s][v]), "+v"(a[s][v]));
+  }
+  const Walk ox = walk<T>(A.dx.p, A.dx.sb, A.dx.st, b, tt, mine, cs), orr = walk<T>(A.dr.p, A.dr.sb, A.dr.st, b, tt, mine, cs),
+             oi = walk<T>(A.di.p, A.di.sb, A.di.st, b, tt, mine, cs);
+#pragma unroll
+  for (int s = S - 1; s >= 0; --s) {
+    Vec<T, VEC> vx, vr, vi;
+    const bool in = mine + s < valid;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      h[v] = fmaf(ea[v], h[v], eh[v]);
-      cc[v] = fmaf(fa[v], cc[v], fc[v]);
-#pragma unroll
-      for (int s = 0; s < S; ++s) {
-        const float before = h[v];
-        h[v] = fmaf(a[s][v], h[v], hp[s][v]);
-        hp[s][v] = before;
-      }
+      const float sv = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
+      const DriveGate k = drive_gate(sv, av);
+      const float g = to_f32(d[s].v[v]) + cc[v];
+      cc[v] = av * g;
+      const float gb = g * k.beta * qv;
+      const float w = g * fmaf(av * av * k.rbeta * qv, xv, -av * hp[s][v]);
+      vx.v[v] = from_f32<T>(in ? gb : 0.0f);
+      vi.v[v] = from_f32<T>(in ? gb * (1.0f - qv) * xv : 0.0f);
+      vr.v[v] = from_f32<T>(in ? w * sv * (1.0f - sr[s][v]) : 0.0f);
+      sum[v] += in ? w * sr[s][v] : 0.0f;
     }
-    T* ox = (T*)A.dx.p + b * A.dx.sb + t0 * A.dx.st;
-    T* orr = (T*)A.dr.p + b * A.dr.sb + t0 * A.dr.st;
-    T* oi = (T*)A.di.p + b * A.di.sb + t0 * A.di.st;
-#pragma unroll
-    for (int s = S - 1; s >= 0; --s) {
-      Vec<T, VEC> vx, vr, vi;
-      const bool in = t0 + s < len;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        const float sv = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
-        const DriveGate k = drive_gate(sv, av);
-        const float g = to_f32(d[s].v[v]) + cc[v];
-        cc[v] = av * g;
-        const float gb = g * k.beta * qv;
-        const float w = g * fmaf(av * av * k.rbeta * qv, xv, -av * hp[s][v]);
-        vx.v[v] = from_f32<T>(in ? gb : 0.0f);
-        vi.v[v] = from_f32<T>(in ? gb * (1.0f - qv) * xv : 0.0f);
-        vr.v[v] = from_f32<T>(in ? w * sv * (1.0f - sr[s][v]) : 0.0f);
-        sum[v] += in ? w * sr[s][v] : 0.0f;
-      }
-      if (t0 + s < A.L) {
-        store_row<T, VEC, VIO>(ox + s * A.dx.st, c, A.D, vx);
-        store_row<T, VEC, VIO>(orr + s * A.dr.st, c, A.D, vr);
-        store_row<T, VEC, VIO>(oi + s * A.di.st, c, A.D, vi);
-      }
+    if (mine + s < there && c < A.D) {
+      store_row<T, VEC>(ox, s, vx);
+      store_row<T, VEC>(orr, s, vr);
+      store_row<T, VEC>(oi, s, vi);
     }
+  }
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) {
+  for (int v = 0; v < VEC; ++v) {
 #pragma unroll
-      for (int k = CGL; k < 64; k <<= 1) sum[v] += __shfl_xor(sum[v], k, 64);
-      if (wl < CGL) sums[wave][cl + v] = sum[v];
-    }
-    __syncthreads();
-    if (wave == 0) {
-      float t = 0.0f;
+    for (int k = CGL; k < 64; k <<= 1) sum[v] += __shfl_xor(sum[v], k, 64);
+    if (wl < CGL) sums[wave][cl + v] = sum[v];
+  }
+  __syncthreads();
+  if (wave == 0) {
+    float t = 0.0f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) t += sums[w][wl];
-      // (a word like the others, so that what a later call finds here is never taken for one of its own)
-      A.part[(b * tiles + tile) * ((int64_t)A.NB * GATED_CW) + cw] = word(t, tag);
-    }
-    if constexpr (LOOK) __syncthreads();
+    for (int w = 0; w < NW; ++w) t += sums[w][wl];
+    // (a word like the others, so that what a later call finds here is never taken for one of its own)
+    A.part[(b * tiles + tile) * ((int64_t)A.NB * GATED_CW) + cw] = word(t, tag);
   }
   if constexpr (LOOK) leave(A.hdr, tag);
 }
@@ -560,33 +605,27 @@ __global__ __launch_bounds__(256) void gated_step_kernel(Rows x, Rows r, Rows i,
   y[k] = from_f32<T>(v);
 }
 
-// Work-groups of a call whose chains have several tiles: two on each of 256 compute units.
-unsigned gated_groups(int64_t B, int64_t L, int64_t NB, int64_t tile) {
-  const int64_t n = B * NB * gated_tiles(L, tile);
-  return (unsigned)(n < 512 ? n : 512);
-}
-
 // A chain of one tile needs no look-back, no tickets and no words: the smallest tile that holds it.
-template <typename T, int VEC, int S, bool VIO>
+template <typename T, int VEC, int S>
 void gated_fwd(const GatedArgs& a, hipStream_t st) {
   constexpr int STEPS = S * VEC;  // of a wave
   const dim3 chains((unsigned)(a.B * a.NB));
   if (a.L <= STEPS)
-    gated_fwd_kernel<T, VEC, S, 64, VIO, false><<<chains, 64, 0, st>>>(a);
+    gated_fwd_kernel<T, VEC, S, 64, false><<<chains, 64, 0, st>>>(a);
   else if (a.L <= 4 * STEPS)
-    gated_fwd_kernel<T, VEC, S, 256, VIO, false><<<chains, 256, 0, st>>>(a);
+    gated_fwd_kernel<T, VEC, S, 256, false><<<chains, 256, 0, st>>>(a);
   else if (a.L <= 8 * STEPS)
-    gated_fwd_kernel<T, VEC, S, 512, VIO, false><<<chains, 512, 0, st>>>(a);
+    gated_fwd_kernel<T, VEC, S, 512, false><<<chains, 512, 0, st>>>(a);
   else
-    gated_fwd_kernel<T, VEC, S, 512, VIO, true><<<dim3(gated_groups(a.B, a.L, a.NB, 8 * STEPS)), 512, 0, st>>>(a);
+    gated_fwd_kernel<T, VEC, S, 512, true><<<dim3((unsigned)(a.B * a.NB * gated_tiles(a.L, 8 * STEPS))), 512, 0, st>>>(a);
 }
-template <typename T, int VEC, int S, bool VIO>
+template <typename T, int VEC, int S>
 void gated_bwd(const GatedArgs& a, hipStream_t st) {
   constexpr int STEPS = S * VEC;
   if (a.L <= 8 * STEPS)
-    gated_bwd_kernel<T, VEC, S, 512, VIO, false><<<dim3((unsigned)(a.B * a.NB)), 512, 0, st>>>(a);
+    gated_bwd_kernel<T, VEC, S, 512, false><<<dim3((unsigned)(a.B * a.NB)), 512, 0, st>>>(a);
   else
-    gated_bwd_kernel<T, VEC, S, 512, VIO, true><<<dim3(gated_groups(a.B, a.L, a.NB, 8 * STEPS)), 512, 0, st>>>(a);
+    gated_bwd_kernel<T, VEC, S, 512, true><<<dim3((unsigned)(a.B * a.NB * gated_tiles(a.L, 8 * STEPS))), 512, 0, st>>>(a);
 }
 
 }  // namespace
@@ -594,18 +633,18 @@ void gated_bwd(const GatedArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t st) {
   if (a.vec)
-    gated_fwd<T, 4, 8, true>(a, st);
+    gated_fwd<T, 4, 8>(a, st);
   else
-    gated_fwd<T, 1, 32, false>(a, st);  // a channel a lane: rows of any alignment read in one piece
+    gated_fwd<T, 1, 32>(a, st);  // a channel a lane: rows of any alignment read in one piece
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st) {
   if (a.vec)
-    gated_bwd<T, 4, 4, true>(a, st);
+    gated_bwd<T, 4, 4>(a, st);
   else
-    gated_bwd<T, 1, 16, false>(a, st);
+    gated_bwd<T, 1, 16>(a, st);
   const int64_t rows = a.B * gated_tiles(a.L, GATED_BWD_TILE);
   gated_reduce_kernel<<<dim3((unsigned)((a.D + 15) / 16)), 1024, 0, st>>>(a.part, rows, a.NB * GATED_CW, a.D, dgamma);
   return hipGetLastError();

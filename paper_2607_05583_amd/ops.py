@@ -1072,7 +1072,7 @@ def resonator_gated_scan_fwd(x, r, i, gamma, h0=None, lengths=None, return_state
     x, r, i: [B, L, D] of one type, the last dimension consecutive (columns of a
     fused projection are taken as they are); gamma [D], h0 [B, D] float32;
     ``lengths`` [B] int32: row b has its first lengths[b] steps (y is 0 behind
-    them and nothing there is read).  Returns y; with ``return_state`` also the
+    them, and what x, r, i hold there does not matter).  Returns y; with ``return_state`` also the
     last state [B, D] float32 (written to ``h_out`` where given, which may be h0
     itself); with ``save`` also the states that resonator_gated_scan_bwd starts
     from.  ``ws``: a gated_scan_workspace, else one is made for the call."""
