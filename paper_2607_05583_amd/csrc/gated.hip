@@ -27,36 +27,18 @@
 namespace res {
 namespace {
 
-// 1 - exp(-2 s), without the cancellation of 1 - a a for small s: the series of
-// 1 - exp(-t) up to t^7 below t = 0.3 (relative error 6e-9 there).
-__device__ __forceinline__ float one_minus_a2(float s, float a) {
-  const float t = 2.0f * s;
-  float p = fmaf(t, -1.0f / 7.0f, 1.0f);
-  p = fmaf(t * (-1.0f / 6.0f), p, 1.0f);
-  p = fmaf(t * (-1.0f / 5.0f), p, 1.0f);
-  p = fmaf(t * (-1.0f / 4.0f), p, 1.0f);
-  p = fmaf(t * (-1.0f / 3.0f), p, 1.0f);
-  p = fmaf(t * (-1.0f / 2.0f), p, 1.0f);
-  return t < 0.3f ? t * p : fmaf(-a, a, 1.0f);
+// The gate's exponent is kept as z = s log2(e), so that a = 2^-z.
+// 1 - a^2 = 1 - 4^-z without the cancellation for small z: the series up to z^5 below z = 0.108 (2 s = 0.15; relative
+// error 1e-7 there, and 4e-7 above).
+__device__ __forceinline__ float one_minus_a2(float z, float a) {
+  constexpr double L = 2.0 * 0.69314718055994530942;  // ln 4
+  float p = fmaf(z, (float)(L * L * L * L * L / 120), (float)(-L * L * L * L / 24));
+  p = fmaf(z, p, (float)(L * L * L / 6));
+  p = fmaf(z, p, (float)(-L * L / 2));
+  p = fmaf(z, p, (float)L);
+  return z < 0.108f ? z * p : fmaf(-a, a, 1.0f);
 }
-
-// beta = sqrt(1 - a^2) and 1 / beta, both 0 where the square is no float32 to speak of
-struct DriveGate {
-  float beta, rbeta;
-};
-__device__ __forceinline__ DriveGate drive_gate(float s, float a) {
-  const float e = one_minus_a2(s, a);
-  const bool some = !(e <= 1e-36f);  // NaN stays NaN
-  const float r = some ? __builtin_amdgcn_rsqf(e) : 0.0f;
-  return DriveGate{e * r, r};
-}
-struct Gate {
-  float a, beta;
-};
-__device__ __forceinline__ Gate gate(float r, float gamma) {
-  const float s = gamma * sigmoid_fast(r), a = exp2_fast(-LOG2E * s);
-  return Gate{a, drive_gate(s, a).beta};
-}
+__device__ __forceinline__ float beta_of(float z, float a) { return __builtin_amdgcn_sqrtf(one_minus_a2(z, a)); }
 
 template <typename T, int VEC> struct __align__(sizeof(T) * VEC) Vec { T v[VEC]; };
 
@@ -265,14 +247,14 @@ __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
     }
     float gam[VEC];
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) gam[v] = A.gamma[cs + v];
+    for (int v = 0; v < VEC; ++v) gam[v] = LOG2E * A.gamma[cs + v];
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
-        const Gate g = gate(to_f32(r[s].v[v]), gam[v]);
-        a[s][v] = g.a;
-        u[s][v] = g.beta * sigmoid_fast(to_f32(i[s].v[v])) * to_f32(x[s].v[v]);
+        const float z = gam[v] * sigmoid_fast(to_f32(r[s].v[v]));
+        a[s][v] = exp2_fast(-z);
+        u[s][v] = beta_of(z, a[s][v]) * sigmoid_fast(to_f32(i[s].v[v])) * to_f32(x[s].v[v]);
       }
     if (valid < TILE) {  // behind the end the state is kept
 #pragma unroll
@@ -350,14 +332,21 @@ __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
   if (A.y != nullptr && c < A.D) {
     const Walk wy = walk<T>(A.y, A.L * A.D, A.D, b, tt, mine, c);
 #pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) h[v] = a[s][v] = fmaf(a[s][v], h[v], u[s][v]);
+    if (valid < TILE) {
+#pragma unroll
+      for (int s = 0; s < S; ++s)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) a[s][v] = mine + s < valid ? a[s][v] : 0.0f;
+    }
+#pragma unroll
     for (int s = 0; s < S; ++s) {
       Vec<T, VEC> ov;
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        h[v] = fmaf(a[s][v], h[v], u[s][v]);
-        ov.v[v] = from_f32<T>(mine + s < valid ? h[v] : 0.0f);
-      }
-      if (mine + s < there) store_row<T, VEC>(wy, s, ov);
+      for (int v = 0; v < VEC; ++v) ov.v[v] = from_f32<T>(a[s][v]);
+      if (there == TILE || mine + s < there) store_row<T, VEC>(wy, s, ov);
     }
   }
   if constexpr (LOOK) leave(A.hdr, tag);
@@ -420,14 +409,14 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
       for (int v = 0; v < VEC; ++v) h[v] = from[v];
     }
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) gam[v] = A.gamma[cs + v];
+    for (int v = 0; v < VEC; ++v) gam[v] = LOG2E * A.gamma[cs + v];
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         sr[s][v] = sigmoid_fast(to_f32(r[s].v[v]));
         q[s][v] = sigmoid_fast(to_f32(i[s].v[v]));
-        a[s][v] = exp2_fast(-LOG2E * (gam[v] * sr[s][v]));
+        a[s][v] = exp2_fast(-gam[v] * sr[s][v]);
       }
     if (valid < TILE) {  // behind the end s = 0: a = 1 and nothing is added
 #pragma unroll
@@ -452,7 +441,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
     float pa = 1.0f, ph = 0.0f, pc = 0.0f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      hp[s][v] = drive_gate(gam[v] * sr[s][v], a[s][v]).beta * q[s][v] * to_f32(x[s].v[v]);
+      hp[s][v] = beta_of(gam[v] * sr[s][v], a[s][v]) * q[s][v] * to_f32(x[s].v[v]);
       pa *= a[s][v];
       ph = fmaf(a[s][v], ph, hp[s][v]);
     }
@@ -534,26 +523,32 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
 #pragma unroll
     for (int s = 0; s < S; ++s) asm volatile("" : "+v"(sr[s][v]), "+v"(a[s][v]));
   }
+  float dgam[VEC];  // gamma itself: dr = w s (1 - sr)
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) dgam[v] = A.gamma[cs + v];
   const Walk ox = walk<T>(A.dx.p, A.dx.sb, A.dx.st, b, tt, mine, cs), orr = walk<T>(A.dr.p, A.dr.sb, A.dr.st, b, tt, mine, cs),
              oi = walk<T>(A.di.p, A.di.sb, A.di.st, b, tt, mine, cs);
 #pragma unroll
   for (int s = S - 1; s >= 0; --s) {
     Vec<T, VEC> vx, vr, vi;
-    const bool in = mine + s < valid;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const float sv = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
-      const DriveGate k = drive_gate(sv, av);
-      const float g = to_f32(d[s].v[v]) + cc[v];
-      cc[v] = av * g;
-      const float gb = g * k.beta * qv;
-      const float w = g * fmaf(av * av * k.rbeta * qv, xv, -av * hp[s][v]);
-      vx.v[v] = from_f32<T>(in ? gb : 0.0f);
-      vi.v[v] = from_f32<T>(in ? gb * (1.0f - qv) * xv : 0.0f);
-      vr.v[v] = from_f32<T>(in ? w * sv * (1.0f - sr[s][v]) : 0.0f);
-      sum[v] += in ? w * sr[s][v] : 0.0f;
+      const float z = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
+      const float e = one_minus_a2(z, av), rb = e <= 1e-36f ? 0.0f : __builtin_amdgcn_rsqf(e);  // 1 / beta
+      const float g = to_f32(d[s].v[v]) + cc[v], ag = av * g, gb = g * (e * rb) * qv;
+      cc[v] = ag;
+      const float w = ag * fmaf(av * rb * qv, xv, -hp[s][v]);
+      vx.v[v] = from_f32<T>(gb);
+      vi.v[v] = from_f32<T>(gb * xv * (1.0f - qv));
+      const float ws = w * sr[s][v];
+      sum[v] += ws;
+      vr.v[v] = from_f32<T>(ws * (1.0f - sr[s][v]) * dgam[v]);
     }
-    if (mine + s < there && c < A.D) {
+    if (valid < TILE && mine + s >= valid) {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) vx.v[v] = vr.v[v] = vi.v[v] = T(0);
+    }
+    if (c < A.D && (there == TILE || mine + s < there)) {
       store_row<T, VEC>(ox, s, vx);
       store_row<T, VEC>(orr, s, vr);
       store_row<T, VEC>(oi, s, vi);
@@ -598,9 +593,9 @@ __global__ __launch_bounds__(256) void gated_step_kernel(Rows x, Rows r, Rows i,
   const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (k >= B * D) return;
   const int64_t b = k / D, c = k - b * D;
-  const Gate g = gate(to_f32(((const T*)r.p)[b * r.sb + c]), gamma[c]);
-  const float u = g.beta * sigmoid_fast(to_f32(((const T*)i.p)[b * i.sb + c])) * to_f32(((const T*)x.p)[b * x.sb + c]);
-  const float v = fmaf(g.a, h[k], u);
+  const float z = LOG2E * gamma[c] * sigmoid_fast(to_f32(((const T*)r.p)[b * r.sb + c])), a = exp2_fast(-z);
+  const float u = beta_of(z, a) * sigmoid_fast(to_f32(((const T*)i.p)[b * i.sb + c])) * to_f32(((const T*)x.p)[b * x.sb + c]);
+  const float v = fmaf(a, h[k], u);
   h_out[k] = v;
   y[k] = from_f32<T>(v);
 }
