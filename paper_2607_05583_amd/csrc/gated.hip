@@ -42,6 +42,26 @@ __device__ __forceinline__ float beta_of(float z, float a) { return __builtin_am
 
 template <typename T, int VEC> struct __align__(sizeof(T) * VEC) Vec { T v[VEC]; };
 
+// Makes the compiler take the values for new ones.
+template <typename T, int VEC, int S>
+__device__ __forceinline__ void opaque(Vec<T, VEC> (&x)[S]) {
+  typedef uint32_t u __attribute__((ext_vector_type(VEC * sizeof(T) > 4 ? VEC * sizeof(T) / 4 : 2)));
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    if constexpr (VEC * sizeof(T) == 2) {
+      asm volatile("" : "+v"(x[s].v[0]));
+    } else if constexpr (VEC * sizeof(T) == 4) {
+      uint32_t w = __builtin_bit_cast(uint32_t, x[s]);
+      asm volatile("" : "+v"(w));
+      x[s] = __builtin_bit_cast(Vec<T, VEC>, w);
+    } else {
+      u w = __builtin_bit_cast(u, x[s]);
+      asm volatile("" : "+v"(w));
+      x[s] = __builtin_bit_cast(Vec<T, VEC>, w);
+    }
+  }
+}
+
 // A thread's rows of a tile: the tile's first element (the same for all threads) and this thread's bytes from there.
 struct Walk {
   const char* base;
@@ -64,7 +84,8 @@ __device__ __forceinline__ Vec<T, VEC> load_row_clamped(const Walk& w, int s, in
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void store_row(const Walk& w, int s, const Vec<T, VEC>& o) {
-  *reinterpret_cast<Vec<T, VEC>*>(const_cast<char*>(w.base) + s * w.st + w.off) = o;
+  typedef uint16_t u1 __attribute__((ext_vector_type(VEC * sizeof(T) / 2)));
+  __builtin_nontemporal_store(__builtin_bit_cast(u1, o), reinterpret_cast<u1*>(const_cast<char*>(w.base) + s * w.st + w.off));
 }
 
 __device__ __forceinline__ int row_len(const int* lengths, int64_t b, int64_t L) {
@@ -376,13 +397,13 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
   const int mine = tg * S, valid = (int)((len < tt ? 0 : len - tt) < TILE ? (len < tt ? 0 : len - tt) : TILE),
             there = (int)(A.L - tt < TILE ? A.L - tt : TILE);
   float gam[VEC];
-  Vec<T, VEC> x[S], d[S];
-  float a[S][VEC], sr[S][VEC], q[S][VEC];
+  Vec<T, VEC> x[S], d[S], i[S];
+  float a[S][VEC], sr[S][VEC];
   float h[VEC];  // the state before the tile
 #pragma unroll
   for (int v = 0; v < VEC; ++v) h[v] = 0.0f;
   {
-    Vec<T, VEC> r[S], i[S];
+    Vec<T, VEC> r[S];
     const Walk wx = walk<T>(A.x.p, A.x.sb, A.x.st, b, tt, mine, cs), wr = walk<T>(A.r.p, A.r.sb, A.r.st, b, tt, mine, cs),
                wi = walk<T>(A.i.p, A.i.sb, A.i.st, b, tt, mine, cs), wd = walk<T>(A.dy.p, A.dy.sb, A.dy.st, b, tt, mine, cs);
     if (valid == TILE) {
@@ -415,7 +436,6 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
 #pragma unroll
       for (int v = 0; v < VEC; ++v) {
         sr[s][v] = sigmoid_fast(to_f32(r[s].v[v]));
-        q[s][v] = sigmoid_fast(to_f32(i[s].v[v]));
         a[s][v] = exp2_fast(-gam[v] * sr[s][v]);
       }
     if (valid < TILE) {  // behind the end s = 0: a = 1 and nothing is added
@@ -426,7 +446,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
         for (int v = 0; v < VEC; ++v) {
           a[s][v] = in ? a[s][v] : 1.0f;
           sr[s][v] = in ? sr[s][v] : 0.0f;
-          q[s][v] = in ? q[s][v] : 0.0f;
+          i[s].v[v] = in ? i[s].v[v] : T(0);
           x[s].v[v] = in ? x[s].v[v] : T(0);
           d[s].v[v] = in ? d[s].v[v] : T(0);
         }
@@ -441,7 +461,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
     float pa = 1.0f, ph = 0.0f, pc = 0.0f;
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      hp[s][v] = beta_of(gam[v] * sr[s][v], a[s][v]) * q[s][v] * to_f32(x[s].v[v]);
+      hp[s][v] = beta_of(gam[v] * sr[s][v], a[s][v]) * sigmoid_fast(to_f32(i[s].v[v])) * to_f32(x[s].v[v]);
       pa *= a[s][v];
       ph = fmaf(a[s][v], ph, hp[s][v]);
     }
@@ -519,10 +539,11 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
 #pragma unroll
   for (int v = 0; v < VEC; ++v) {
     cc[v] = fmaf(fa[v], cc[v], fc[v]);
-    // beta is computed again below: kept from above it would cost a third of the registers
+    // a, beta and sigmoid(i) are computed again below: kept from above they would take half of the registers
 #pragma unroll
-    for (int s = 0; s < S; ++s) asm volatile("" : "+v"(sr[s][v]), "+v"(a[s][v]));
+    for (int s = 0; s < S; ++s) asm volatile("" : "+v"(sr[s][v]));
   }
+  opaque(i);
   float dgam[VEC];  // gamma itself: dr = w s (1 - sr)
 #pragma unroll
   for (int v = 0; v < VEC; ++v) dgam[v] = A.gamma[cs + v];
@@ -533,7 +554,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
     Vec<T, VEC> vx, vr, vi;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      const float z = gam[v] * sr[s][v], av = a[s][v], xv = to_f32(x[s].v[v]), qv = q[s][v];
+      const float z = gam[v] * sr[s][v], av = exp2_fast(-z), xv = to_f32(x[s].v[v]), qv = sigmoid_fast(to_f32(i[s].v[v]));
       const float e = one_minus_a2(z, av), rb = e <= 1e-36f ? 0.0f : __builtin_amdgcn_rsqf(e);  // 1 / beta
       const float g = to_f32(d[s].v[v]) + cc[v], ag = av * g, gb = g * (e * rb) * qv;
       cc[v] = ag;
@@ -637,7 +658,7 @@ hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t st) {
 template <typename T>
 hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st) {
   if (a.vec)
-    gated_bwd<T, 4, 4>(a, st);
+    gated_bwd<T, sizeof(T) == 2 ? 2 : 4, sizeof(T) == 2 ? 8 : 4>(a, st);
   else
     gated_bwd<T, 1, 16>(a, st);
   const int64_t rows = a.B * gated_tiles(a.L, GATED_BWD_TILE);
