@@ -21,6 +21,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "../../include/resonator.h"
 
 namespace {
@@ -547,6 +549,318 @@ PyObject* epilogue_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// The gated recurrent layer
+// ---------------------------------------------------------------------------
+// A plain GPU tensor whose last dimension is consecutive (other strides as they are).
+const Tensor* rows(PyObject* o) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || !t.has_storage() || t.key_set().has_any(kWrapped) ||
+      t.dim() < 1 || (t.size(-1) > 1 && t.stride(-1) != 1))
+    return nullptr;
+  return &t;
+}
+res_rows_t as_rows(const Tensor& t) { return res_rows_t{t.data_ptr(), t.stride(0), t.dim() == 3 ? t.stride(1) : 0}; }
+res_rows_out_t as_rows_out(const Tensor& t) { return res_rows_out_t{t.data_ptr(), t.stride(0), t.stride(1)}; }
+
+// An optional tensor of a type and shape: false if it is something else.
+bool maybe(PyObject* o, at::ScalarType dt, at::IntArrayRef s, const Tensor** t) {
+  *t = nullptr;
+  if (o == Py_None) return true;
+  *t = plain(o);
+  return *t && (*t)->scalar_type() == dt && (*t)->sizes() == s;
+}
+const float* fp0(const Tensor* t) { return t ? fp(*t) : nullptr; }
+
+struct Gated {
+  const Tensor *x, *r, *i, *gamma;
+  int64_t B, L, D;
+  res_dtype_t dt;
+};
+// (x, r, i, gamma)
+bool gated(PyObject* const* a, int dims, Gated* g) {
+  g->x = rows(a[0]);
+  g->r = rows(a[1]);
+  g->i = rows(a[2]);
+  g->gamma = plain(a[3]);
+  if (!g->x || !g->r || !g->i || !g->gamma || g->x->dim() != dims || code(*g->x) < 0) return false;
+  for (const Tensor* t : {g->r, g->i})
+    if (t->sizes() != g->x->sizes() || t->scalar_type() != g->x->scalar_type()) return false;
+  g->B = g->x->size(0);
+  g->L = dims == 3 ? g->x->size(1) : 1;
+  g->D = g->x->size(-1);
+  g->dt = (res_dtype_t)code(*g->x);
+  return f32(*g->gamma) && shape(*g->gamma, {g->D});
+}
+// The caller's workspace or a new zero-filled one.
+bool gated_ws(PyObject* o, const Gated& g, Tensor* ws) {
+  if (o != Py_None) {
+    const Tensor* w = plain(o);
+    if (!w) return false;
+    *ws = *w;
+    return true;
+  }
+  const size_t nb = resonator_gated_scan_workspace_bytes(g.dt, g.B, g.L, g.D);
+  if (nb == 0) return false;
+  *ws = at::zeros({(int64_t)nb}, at::TensorOptions().device(g.x->device()).dtype(at::kByte));
+  return true;
+}
+size_t bytes(const Tensor& t) { return (size_t)(t.numel() * t.element_size()); }
+
+// (x, r, i, gamma, h0, lengths, return_state, save, out, ws, h_out) -> y, or a tuple of y, the state and the carry
+PyObject* gated_scan_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Gated g;
+  const Tensor *h0, *len, *out, *ho;
+  bool want, save;
+  if (n != 11 || !gated(a, 3, &g) || !truth(a[6], &want) || !truth(a[7], &save) || !maybe(a[4], at::kFloat, {g.B, g.D}, &h0) ||
+      !maybe(a[5], at::kInt, {g.B}, &len) || !maybe(a[8], g.x->scalar_type(), g.x->sizes(), &out) ||
+      !maybe(a[10], at::kFloat, {g.B, g.D}, &ho))
+    return none();
+  Tensor ws;
+  if (!gated_ws(a[9], g, &ws)) return none();
+  const Tensor y = out ? *out : empty({g.B, g.L, g.D}, *g.x, g.x->scalar_type());
+  Tensor h, carry;
+  if (ho) h = *ho;
+  else if (want) h = empty({g.B, g.D}, *g.x, at::kFloat);
+  if (save) carry = empty({g.B, (g.L + RES_GATED_CARRY - 1) / RES_GATED_CARRY, g.D}, *g.x, at::kFloat);
+  const OnDevice on(*g.x);
+  const int rc = call([&] {
+    return resonator_gated_scan_fwd(as_rows(*g.x), as_rows(*g.r), as_rows(*g.i), g.dt, y.data_ptr(), g.B, g.L, g.D, fp(*g.gamma),
+                                    fp0(h0), len ? static_cast<const int32_t*>(len->data_ptr()) : nullptr,
+                                    h.defined() ? fpm(h) : nullptr, save ? fpm(carry) : nullptr, ws.data_ptr(), bytes(ws), on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  if (want) return save ? pack({y, h, carry}) : pack({y, h});
+  return save ? pack({y, carry}) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, r, i, gamma, dy, lengths, dh_out, carry, want_dh0, out, ws) -> (dx, dr, di, dgamma, dh0 or None)
+PyObject* gated_scan_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Gated g;
+  const Tensor *len, *dh, *carry;
+  bool want;
+  if (n != 11 || !gated(a, 3, &g) || !truth(a[8], &want)) return none();
+  const Tensor* dy = rows(a[4]);
+  if (!dy || dy->sizes() != g.x->sizes() || dy->scalar_type() != g.x->scalar_type() || a[7] == Py_None ||
+      !maybe(a[5], at::kInt, {g.B}, &len) || !maybe(a[6], at::kFloat, {g.B, g.D}, &dh) ||
+      !maybe(a[7], at::kFloat, {g.B, (g.L + RES_GATED_CARRY - 1) / RES_GATED_CARRY, g.D}, &carry))
+    return none();
+  Tensor o[3], ws, dh0;
+  if (a[9] != Py_None) {
+    if (!PyTuple_CheckExact(a[9]) && !PyList_CheckExact(a[9])) return none();
+    if (PySequence_Fast_GET_SIZE(a[9]) != 3) return none();
+    for (int k = 0; k < 3; ++k) {
+      const Tensor* t = rows(PySequence_Fast_GET_ITEM(a[9], k));
+      if (!t || t->sizes() != g.x->sizes() || t->scalar_type() != g.x->scalar_type()) return none();
+      o[k] = *t;
+    }
+  }
+  if (!gated_ws(a[10], g, &ws)) return none();
+  if (!o[0].defined())
+    for (Tensor& t : o) t = empty({g.B, g.L, g.D}, *g.x, g.x->scalar_type());
+  const Tensor dgamma = empty({g.D}, *g.x, at::kFloat);
+  if (want) dh0 = empty({g.B, g.D}, *g.x, at::kFloat);
+  const OnDevice on(*g.x);
+  const int rc = call([&] {
+    return resonator_gated_scan_bwd(as_rows(*g.x), as_rows(*g.r), as_rows(*g.i), as_rows(*dy), g.dt, as_rows_out(o[0]),
+                                    as_rows_out(o[1]), as_rows_out(o[2]), g.B, g.L, g.D, fp(*g.gamma), fp(*carry),
+                                    len ? static_cast<const int32_t*>(len->data_ptr()) : nullptr, fp0(dh), fpm(dgamma),
+                                    want ? fpm(dh0) : nullptr, ws.data_ptr(), bytes(ws), on.stream);
+  });
+  return rc ? PyLong_FromLong(rc) : pack({o[0], o[1], o[2], dgamma, dh0});
+  END_HANDLE_TH_ERRORS
+}
+
+// (x_t, r_t, i_t, gamma, h, h_out, out) -> y_t
+PyObject* gated_scan_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Gated g;
+  const Tensor *h, *ho, *out;
+  if (n != 7 || !gated(a, 2, &g) || a[4] == Py_None || !maybe(a[4], at::kFloat, {g.B, g.D}, &h) ||
+      !maybe(a[5], at::kFloat, {g.B, g.D}, &ho) || !maybe(a[6], g.x->scalar_type(), g.x->sizes(), &out))
+    return none();
+  const Tensor y = out ? *out : empty({g.B, g.D}, *g.x, g.x->scalar_type());
+  const OnDevice on(*g.x);
+  const int rc = call([&] {
+    return resonator_gated_scan_step(as_rows(*g.x), as_rows(*g.r), as_rows(*g.i), g.dt, y.data_ptr(), g.B, g.D, fp(*g.gamma), fp(*h),
+                                     fpm(ho ? *ho : *h), on.stream);
+  });
+  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+struct Linear {
+  const Tensor *x, *W;
+  int64_t R, K, N, ldx;
+  res_dtype_t dt;
+  bool loose;
+};
+// x [..., K] with rows at one distance, W [K, N]
+bool linear(PyObject* ox, PyObject* oW, Linear* l) {
+  l->x = rows(ox);
+  l->W = plain(oW);
+  if (!l->x || !l->W || code(*l->x) < 0 || l->W->dim() != 2 || l->W->scalar_type() != l->x->scalar_type()) return false;
+  const Tensor& x = *l->x;
+  l->K = x.size(-1);
+  if (l->K < 1 || l->W->size(0) != l->K) return false;
+  l->N = l->W->size(1);
+  l->R = x.numel() / l->K;
+  l->ldx = l->K;
+  if (l->R > 1 && !x.is_contiguous()) {
+    int64_t want = -1;  // distance that the dimension before must have
+    for (int64_t d = x.dim() - 2; d >= 0; --d) {
+      if (x.size(d) == 1) continue;
+      if (want < 0) l->ldx = x.stride(d);
+      else if (x.stride(d) != want) return false;
+      want = x.stride(d) * x.size(d);
+    }
+    if (l->ldx < l->K) return false;
+  }
+  l->dt = (res_dtype_t)code(x);
+  const int64_t ep = 16 / x.element_size();
+  l->loose = l->K % ep || l->N % ep || l->ldx % ep || (uintptr_t)x.data_ptr() % 16 || (uintptr_t)l->W->data_ptr() % 16;
+  return true;
+}
+bool linear_ws(PyObject* o, int backward, int act, const Linear& l, bool loose, Tensor* ws) {
+  if (o != Py_None) {
+    const Tensor* w = plain(o);
+    if (!w) return false;
+    *ws = *w;
+    return true;
+  }
+  const size_t nb = resonator_linear_workspace_bytes(backward, l.dt, act, l.R, l.K, l.N, loose);
+  if (nb > 0) *ws = empty({(int64_t)nb}, *l.x, at::kByte);
+  return true;
+}
+
+// (x, W, bias, act code, residual, save, out, ws) -> (y, pre or None)
+PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Linear l;
+  int64_t act;
+  bool save;
+  const Tensor *bias, *res, *out;
+  if (n != 8 || !linear(a[0], a[1], &l) || !integer(a[3], &act) || !truth(a[5], &save)) return none();
+  auto s = l.x->sizes().vec();
+  s.back() = l.N;
+  if (!maybe(a[2], at::kFloat, {l.N}, &bias) || !maybe(a[4], l.x->scalar_type(), s, &res) || !maybe(a[6], l.x->scalar_type(), s, &out))
+    return none();
+  Tensor ws, pre;
+  if (!linear_ws(a[7], 0, (int)act, l, l.loose, &ws)) return none();
+  const Tensor y = out ? *out : empty(s, *l.x, l.x->scalar_type());
+  if (save && resonator_linear_keeps_pre(l.dt, (int)act, l.K)) pre = empty(s, *l.x, at::kFloat);
+  const OnDevice on(*l.x);
+  const int rc = call([&] {
+    return resonator_linear_fwd(l.x->data_ptr(), l.ldx, l.W->data_ptr(), l.dt, fp0(bias), (int)act, res ? res->data_ptr() : nullptr,
+                                y.data_ptr(), pre.defined() ? fpm(pre) : nullptr, l.R, l.K, l.N,
+                                ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? bytes(ws) : 0, on.stream);
+  });
+  return rc ? PyLong_FromLong(rc) : pack({y, pre});
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, W, dy, pre, bias, act code, residual, want_dx, want_dw, want_db, ws) -> (dx, dW, db), None where not wanted
+PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Linear l;
+  int64_t act;
+  bool wx, ww, wb;
+  const Tensor *dy, *pre, *bias, *res;
+  if (n != 11 || !linear(a[0], a[1], &l) || !integer(a[5], &act) || !truth(a[7], &wx) || !truth(a[8], &ww) || !truth(a[9], &wb))
+    return none();
+  auto s = l.x->sizes().vec();
+  s.back() = l.N;
+  if (a[2] == Py_None || !maybe(a[2], l.x->scalar_type(), s, &dy) || !maybe(a[3], at::kFloat, s, &pre) ||
+      !maybe(a[4], at::kFloat, {l.N}, &bias) || !maybe(a[6], l.x->scalar_type(), l.x->sizes(), &res))
+    return none();
+  Tensor ws, dx, dW, db;
+  if (!linear_ws(a[10], 1, (int)act, l, l.loose || (uintptr_t)dy->data_ptr() % 16, &ws)) return none();
+  if (wx) dx = empty(l.x->sizes(), *l.x, l.x->scalar_type());
+  if (ww) dW = empty({l.K, l.N}, *l.x, l.x->scalar_type());
+  if (wb) db = empty({l.N}, *l.x, at::kFloat);
+  const OnDevice on(*l.x);
+  const int rc = call([&] {
+    return resonator_linear_bwd(l.x->data_ptr(), l.ldx, l.W->data_ptr(), l.dt, fp0(bias), dy->data_ptr(), fp0(pre), (int)act,
+                                res ? res->data_ptr() : nullptr, wx ? dx.data_ptr() : nullptr, ww ? dW.data_ptr() : nullptr,
+                                wb ? fpm(db) : nullptr, l.R, l.K, l.N, ws.defined() ? ws.data_ptr() : nullptr,
+                                ws.defined() ? bytes(ws) : 0, on.stream);
+  });
+  return rc ? PyLong_FromLong(rc) : pack({dx, dW, db});
+  END_HANDLE_TH_ERRORS
+}
+
+// A state dict's buffers for n elements.
+bool adamw_state(PyObject* d, int64_t n, res_adamw_state_t* s) {
+  if (!PyDict_CheckExact(d)) return false;
+  const Tensor* t[5] = {};
+  static const char* const names[5] = {"exp_avg", "exp_avg_sq", "scale_avg", "scale_sq", "master"};
+  for (int k = 0; k < 5; ++k) {
+    PyObject* o = PyDict_GetItemString(d, names[k]);
+    if (o && !(t[k] = plain(o))) return false;
+  }
+  if (!t[0] || !t[1]) return false;
+  const bool eight = t[0]->scalar_type() == at::kChar;
+  if (t[0]->numel() != n || t[1]->numel() != n || t[1]->scalar_type() != (eight ? at::kByte : at::kFloat) || (!eight && !f32(*t[0])))
+    return false;
+  if (eight)
+    for (int k = 2; k < 4; ++k)
+      if (!t[k] || !f32(*t[k]) || t[k]->numel() != n / RES_ADAMW_BLOCK) return false;
+  if (t[4] && (!f32(*t[4]) || t[4]->numel() != n)) return false;
+  *s = res_adamw_state_t{eight ? 8 : 32, t[0]->data_ptr(), t[1]->data_ptr(), eight ? fpm(*t[2]) : nullptr,
+                         eight ? fpm(*t[3]) : nullptr, t[4] ? fpm(*t[4]) : nullptr};
+  return true;
+}
+
+// (params, grads, new params, state, new state, step, lr, beta1, beta2, eps, weight_decay, grad_scale): lists; True when done
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 12) return none();
+  for (int k = 0; k < 3; ++k)
+    if (!PyList_CheckExact(a[k])) return none();
+  const Py_ssize_t count = PyList_GET_SIZE(a[0]);
+  if (count == 0 || PyList_GET_SIZE(a[1]) != count || PyList_GET_SIZE(a[2]) != count) return none();
+  int64_t step;
+  double h[5];
+  const Tensor* scale;
+  if (!integer(a[5], &step) || !maybe(a[11], at::kFloat, {1}, &scale)) return none();
+  for (int k = 0; k < 5; ++k) {
+    if (!PyFloat_CheckExact(a[6 + k])) return none();
+    h[k] = PyFloat_AS_DOUBLE(a[6 + k]);
+  }
+  std::vector<res_adamw_tensor_t> t((size_t)count);
+  const Tensor *p0 = nullptr, *g0 = nullptr;
+  int64_t at = 0;
+  for (Py_ssize_t k = 0; k < count; ++k) {
+    const Tensor *p = plain(PyList_GET_ITEM(a[0], k)), *g = plain(PyList_GET_ITEM(a[1], k)), *o = plain(PyList_GET_ITEM(a[2], k));
+    if (!p || !g || !o) return none();
+    if (k == 0) {
+      p0 = p;
+      g0 = g;
+      if (code(*p) < 0 || code(*g) < 0) return none();
+    }
+    if (p->scalar_type() != p0->scalar_type() || o->scalar_type() != p0->scalar_type() || g->scalar_type() != g0->scalar_type() ||
+        g->sizes() != p->sizes() || o->sizes() != p->sizes() || p->device() != p0->device() || g->device() != p0->device())
+      return none();
+    const int64_t c = p->numel();
+    t[(size_t)k] = res_adamw_tensor_t{p->data_ptr(), g->data_ptr(), o->data_ptr(), c, at};
+    at += (c + RES_ADAMW_BLOCK - 1) / RES_ADAMW_BLOCK * RES_ADAMW_BLOCK;
+  }
+  res_adamw_state_t s, so;
+  if (!adamw_state(a[3], at, &s) || !adamw_state(a[4], at, &so)) return none();
+  const OnDevice on(*p0);
+  const int rc = call([&] {
+    return resonator_adamw_step(t.data(), count, (res_dtype_t)code(*p0), (res_dtype_t)code(*g0), &s, &so, h[0], h[1], h[2], h[3], h[4],
+                                step, fp0(scale), on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  Py_RETURN_TRUE;
+  END_HANDLE_TH_ERRORS
+}
+
 #define RES_FN(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RES_FN("mix_fwd", mix_fwd),
                          RES_FN("mix_bwd", mix_bwd),
@@ -562,6 +876,12 @@ PyMethodDef methods[] = {RES_FN("mix_fwd", mix_fwd),
                          RES_FN("epilogue_fwd", epilogue_fwd),
                          RES_FN("epilogue_proj_fwd", epilogue_proj_fwd),
                          RES_FN("epilogue_bwd", epilogue_bwd),
+                         RES_FN("gated_scan_fwd", gated_scan_fwd),
+                         RES_FN("gated_scan_bwd", gated_scan_bwd),
+                         RES_FN("gated_scan_step", gated_scan_step),
+                         RES_FN("linear_fwd", linear_fwd),
+                         RES_FN("linear_bwd", linear_bwd),
+                         RES_FN("adamw_step", adamw_step),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the hot entry points.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

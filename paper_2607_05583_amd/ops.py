@@ -1076,6 +1076,9 @@ def resonator_gated_scan_fwd(x, r, i, gamma, h0=None, lengths=None, return_state
     last state [B, D] float32 (written to ``h_out`` where given, which may be h0
     itself); with ``save`` also the states that resonator_gated_scan_bwd starts
     from.  ``ws``: a gated_scan_workspace, else one is made for the call."""
+    done = (_NATIVE or _native()).gated_scan_fwd(x, r, i, gamma, h0, lengths, return_state, save, out, ws, h_out)
+    if done is not None:
+        return _done(done)
     rows = _gated_inputs(x, r, i, gamma, 3)
     B, L, D = x.shape
     _f32(h0, "h0", (B, D))
@@ -1105,6 +1108,12 @@ def resonator_gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh_out=N
     ``carry``: the states of a forward with ``save`` on the same inputs, else
     they are computed again from ``h0``.  ``out`` = (dx, dr, di) receives the
     gradients (they may be columns of one tensor)."""
+    done = (_NATIVE or _native()).gated_scan_bwd(x, r, i, gamma, dy, lengths, dh_out, carry, want_dh0, out, ws)
+    if done is not None:
+        g = dict(zip(("dx", "dr", "di", "dgamma", "dh0"), _done(done)))
+        if not want_dh0:
+            del g["dh0"]
+        return g
     rows = _gated_inputs(x, r, i, gamma, 3)
     B, L, D = x.shape
     rows.append(_rows(dy, "dy", x.dtype, x.shape))
@@ -1139,6 +1148,9 @@ def resonator_gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh_out=N
 def resonator_gated_scan_step(x_t, r_t, i_t, gamma, h, h_out=None, out=None):
     """One step of the gated scan: x_t, r_t, i_t [B, D], state h [B, D] float32, advanced in place unless ``h_out``
     receives the new one; returns y_t [B, D]."""
+    done = (_NATIVE or _native()).gated_scan_step(x_t, r_t, i_t, gamma, h, h_out, out)
+    if done is not None:
+        return _done(done)
     rows = _gated_inputs(x_t, r_t, i_t, gamma, 2)
     B, D = x_t.shape
     if h is None:
@@ -1257,6 +1269,10 @@ def resonator_linear_fwd(x, W, bias=None, act="none", residual=None, save=False,
     residual [..., N] of x's type; act "none", "relu", "silu" or "gelu_tanh".  With ``save`` returns (y, saved),
     a LinearSaved for resonator_linear_bwd.  ``out`` may be the residual itself."""
     code = _act_code(act)
+    done = (_NATIVE or _native()).linear_fwd(x, W, bias, code, residual, save, out, ws)
+    if done is not None:
+        y, pre = _done(done)
+        return (y, LinearSaved(pre, bias)) if save else y
     R, ldx = _rows2(x, "x")
     K = x.shape[-1]
     N = _weight(W, x.dtype, K)
@@ -1278,15 +1294,20 @@ def resonator_linear_bwd(x, W, dy, pre=None, act="none", residual=None, want_dx=
     reaches x on another path), dW and, where wanted, db (float32).  ``pre`` is what a forward with ``save`` returned, or
     the float32 x W + bias itself; without an activation it is not needed."""
     code = _act_code(act)
+    if dy is None or (code and pre is None):
+        raise TypeError("dy and, with an activation, pre must be given")
+    saved = isinstance(pre, LinearSaved)
+    done = (_NATIVE or _native()).linear_bwd(x, W, dy, pre.pre if saved else pre, pre.bias if saved else None, code, residual,
+                                             want_dx, want_dw, want_db, ws)
+    if done is not None:
+        return {k: v for k, v in zip(("dx", "dW", "db"), _done(done)) if v is not None}
     R, ldx = _rows2(x, "x")
     K = x.shape[-1]
     N = _weight(W, x.dtype, K)
     shape = tuple(x.shape[:-1]) + (N,)
-    if dy is None or (code and pre is None):
-        raise TypeError("dy and, with an activation, pre must be given")
     _like(dy, "dy", x.dtype, shape)
     bias = None
-    if isinstance(pre, LinearSaved):
+    if saved:
         pre, bias = pre.pre, _f32(pre.bias, "bias", (N,))
     _like(pre, "pre", torch.float32, shape)
     _like(residual, "residual", x.dtype, x.shape)
@@ -1405,6 +1426,11 @@ def resonator_adamw_step(params, grads, state, step, lr, betas=(0.9, 0.999), eps
     if len(grads) != len(params) or len(new) != len(params):
         raise ValueError(f"{len(params)} parameters, {len(grads)} gradients and {len(new)} new parameters")
     if not params:
+        return
+    done = (_NATIVE or _native()).adamw_step(params, grads, new, state, new_state, step, float(lr), float(betas[0]),
+                                             float(betas[1]), float(eps), float(weight_decay), grad_scale)
+    if done is not None:
+        _done(done)
         return
     at, n = adamw_offsets(params)
     old_s, new_s = _adamw_state(state, n, "state"), _adamw_state(new_state, n, "new state")
