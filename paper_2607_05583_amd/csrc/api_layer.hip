@@ -317,7 +317,7 @@ hipError_t gemm(res_dtype_t dt, GemmArgs& g, const Operand& A, const Operand& B,
     }
     return hipSuccess;
   }
-  const LinearPlan p = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, !g.loose && g.dy == nullptr);
+  const LinearPlan p = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, !g.loose);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = static_cast<float*>(ws.take(p.splits > 1 ? (size_t)(p.splits * g.M * g.N) * 4 : 0));
@@ -365,7 +365,8 @@ hipError_t linear_bwd(const LinearCall& c, const float* bias, const void* dy, co
   int64_t blocks = 0;
   float* part = nullptr;
   if (c.act != RES_ACT_NONE || db != nullptr) {
-    blocks = again ? linear_col_blocks(c.R) : linear_row_blocks(c.R);
+    // (room for the most rows of sums: which tile is taken depends on the alignments too)
+    blocks = again ? linear_col_blocks(TILE_SMALL, c.R) : linear_row_blocks(c.R);
     if (db != nullptr) part = static_cast<float*>(ws.take((size_t)(blocks * c.N) * 4));
     void* out = c.act != RES_ACT_NONE ? ws.take((size_t)(c.R * c.N) * es) : nullptr;
     if (again) {
@@ -379,6 +380,7 @@ hipError_t linear_bwd(const LinearCall& c, const float* bias, const void* dy, co
       g.dy = count ? &g : dy;
       g.colpart = part;
       e = gemm(c.dt, g, x, W, true, false, c.loose, ws, need, st);
+      blocks = linear_col_blocks(g.tile, c.R);
     } else if (!count && c.R > 0) {
       const bool loose = c.N % 4 != 0 || !(aligned(dy, 16) && aligned(pre, 16));
       e = c.dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, pre, c.act, out, part, c.R, c.N, loose, st)

@@ -66,6 +66,13 @@ __device__ __forceinline__ const char* uniform(const char* p) {
   return (const char*)((uint64_t)hi << 32 | lo);
 }
 
+// The lane again, as a value that the compiler does not know: what is computed from it stays where it is used.  (Hoisted out
+// of the loop over items, the addresses of its rarer parts took 60 registers.)
+__device__ __forceinline__ int lane_here(int lane) {
+  asm volatile("" : "+v"(lane));
+  return lane;
+}
+
 // Loads an operand's tile: rows x0.. of X and KB elements of the K axis.  KC: element (x, k) at p[x ld + k], else at
 // p[k ld + x].  A lane's byte offsets from the tile's start do not change along K (only the scalar base does), and
 // rows past the end are the last ones again: what they give is not stored.
@@ -89,6 +96,7 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
     base = uniform((const char*)(p + x0 * (KC ? ld : 1) + k0 * (KC ? 1 : ld)));
     step = (KC ? 1 : ld) * ES * Gemm<T>::KB;
     const int64_t left = X - x0;
+    lane = lane_here(lane);
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
@@ -106,6 +114,7 @@ template <typename T, int BX, int NW, bool KC> struct TileLoad {
   }
   // the same where only `left` elements of the K axis are left: zeros behind them
   __device__ __forceinline__ void load_last(int left, char* lds, int wave, int lane) {
+    lane = lane_here(lane);
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
       const int row = row_of(u, wave, lane), piece = piece_of(row, lane);
@@ -152,16 +161,47 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, i
 // LDS of a wave's outputs on their way out: rows of one fragment
 template <typename T, int WN> constexpr int out_lds() { return 16 * WN * (int)sizeof(T); }
 
+// What an item reads beside its operands (the residual, or dy) comes through the buffers too, behind its last step: SR
+// rows of each wave's outputs at a time, every wave its own.  Reading it where it is needed exposed a memory latency and
+// took 32-byte pieces.
+template <typename T, int WM, int WN> struct SideLoad {
+  static constexpr int ES = sizeof(T), EP = 16 / ES, RB = WN * ES, PR = RB / 16, SR = 64 / ES, STEPS = WM / SR, SW = PR < 8 ? PR - 1 : 7;
+  static constexpr int BYTES = SR * RB, UNITS = BYTES / 1024, RU = 1024 / RB;
+  static_assert(WM % SR == 0 && BYTES % 1024 == 0, "whole units");
+  // rows m0 + SR s .. of the wave's, columns n0 ..; those past the end are the last ones again
+  __device__ static __forceinline__ void load(const T* side, int64_t m0, int64_t n0, int64_t M, int64_t N, int s, char* lds, int lane) {
+    const char* base = uniform((const char*)side);
+    lane = lane_here(lane);
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int r = u * RU + lane / PR;
+      int64_t m = m0 + s * SR + r, n = n0 + (((lane % PR) ^ (r & SW)) * EP);
+      m = m < M ? m : M - 1;
+      n = n < N ? n : N - EP;
+      lds_dma16_lane(base + (m * N + n) * ES, lds + u * 1024);
+    }
+  }
+  // columns 16 j + 4 lq .. of row r of a step
+  __device__ static __forceinline__ Quad<T> read(const char* lds, int r, int j, int lq) {
+    const int byte = (j * 16 + lq * 4) * ES;
+    return *reinterpret_cast<const Quad<T>*>(lds + r * RB + (((byte >> 4) ^ (r & SW)) << 4) + (byte & 15));
+  }
+};
+
 // A wave's outputs through its own part of the LDS, 16 rows at a time (16-byte piece p of row m in slot p ^ (m & 7)), so
 // that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout gives 32-byte pieces.  The
 // stores are non-temporal (131072 x 256 x 1024 bf16: 139 to 123 us).  Rows and columns past the end are computed from the
 // last ones' operands and not stored.
-// ANY: takes outputs of any alignment (g.loose).  SLOPE: the results are pre, and what is stored is dy act'(pre); its columns' sums go to g.colpart.
-template <typename T, int ACT, bool SLOPE, bool ANY, int WM, int WN>
+// ANY: takes outputs of any alignment (g.loose).  SLOPE: the results are pre, and what is stored is dy act'(pre); its
+// columns' sums go to g.colpart.  stage(s): this wave's step s of the side input in the LDS, null where it is not there.
+template <typename T, int ACT, bool SLOPE, bool ANY, int WM, int WN, typename Stage>
 __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
-                                         char* mine, int lane) {
+                                         char* mine, int lane, Stage&& stage) {
   constexpr int ES = sizeof(T), RB = WN * ES, PR = RB / 16, EP = 16 / ES, SW = PR < 8 ? PR - 1 : 7, FN = WN / 16;
   constexpr int RS = 64 / PR;  // rows of a store
+  typedef SideLoad<T, WM, WN> Side;
+  constexpr int SF = Side::SR / 16;  // fragments of rows in a side step
+  lane = lane_here(lane);
   const int li = lane & 15, lq = lane >> 4;
   const bool loose = ANY && g.loose;
   const int rows = (int)(g.M - m0 < WM ? (g.M > m0 ? g.M - m0 : 0) : WM);  // of this wave's that there are
@@ -174,24 +214,24 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
     bias[j] = g.bias != nullptr ? wide(load_quad(g.bias, n[j], g.N, loose)) : f4{};
     sum[j] = f4{};
   }
-  // what is read beside the results (dy or the residual), some fragments of rows ahead of the stores, which the compiler
-  // does not move loads across
   const T* side = (const T*)(SLOPE ? g.dy : g.res);
-  constexpr int AHEAD = WM / 16 > 4 ? 2 : 4;
-  Quad<T> q[AHEAD][FN];
+  const char* staged = nullptr;
   // stores: this lane's row of a fragment's first RS, and on from there
   T* to = (T*)g.out + (m0 + lane / PR) * g.N + n0;
   const int64_t next = RS * g.N;
 #pragma unroll
   for (int i = 0; i < WM / 16; ++i) {
     const int row = i * 16 + li;
-    if (i % AHEAD == 0 && side != nullptr) {
+    f4 q[FN];
+    if (side != nullptr) {
+      if (i % SF == 0) staged = stage(i / SF);
+      if (!loose) {
 #pragma unroll
-      for (int k = 0; k < AHEAD; ++k) {
-        const int64_t m = m0 + row + k * 16;
-        const T* from = side + (m < g.M ? m : g.M - 1) * g.N;
+        for (int j = 0; j < FN; ++j) q[j] = wide(Side::read(staged, i % SF * 16 + li, j, lq));
+      } else {
+        const T* from = side + (m0 + row < g.M ? m0 + row : g.M - 1) * g.N;
 #pragma unroll
-        for (int j = 0; j < FN; ++j) q[k][j] = load_quad(from, n[j], g.N, loose);
+        for (int j = 0; j < FN; ++j) q[j] = wide(load_quad(from, n[j], g.N, true));
       }
     }
     f4 c[FN];
@@ -199,14 +239,12 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
     for (int j = 0; j < FN; ++j) c[j] = acc[i][j] + bias[j];
     if constexpr (SLOPE) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) {
-        const f4 d = wide(q[i % AHEAD][j]);
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          c[j][r] = d[r] * act_slope(c[j][r], ACT);
+          c[j][r] = q[j][r] * act_slope(c[j][r], ACT);
           sum[j][r] += row < rows ? c[j][r] : 0.0f;
         }
-      }
     } else {
       if (g.pre != nullptr && row < rows) {
         float* pre = g.pre + (m0 + row) * g.N;
@@ -230,7 +268,7 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
       }
       if (side != nullptr) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) c[j] += wide(q[i % AHEAD][j]);
+        for (int j = 0; j < FN; ++j) c[j] += q[j];
       }
     }
 #pragma unroll
@@ -276,8 +314,8 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 // Work-groups stay: each takes every gridDim-th item (a tile and a part of the K axis), and the loads run NB - 1 steps
 // ahead of the products over the borders of the items, so that neither an item's first loads nor its stores are waited
 // for.  NB buffers of a step and the LDS of each wave's outputs.
-template <typename T, int BM, int BN, int WM, int WN, int NB, int OCC, bool ANY, bool AK, bool BK, bool SLOPE>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_kernel(GemmArgs g) {
+template <typename T, int BM, int BN, int WM, int WN, int NB, bool ANY, bool AK, bool BK, int ACT, bool SLOPE>
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void gemm_tile_kernel(GemmArgs g) {
   constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16, STEP = (BM + BN) * 64;
   __shared__ __align__(1024) char lds[NB * STEP + NW * out_lds<T, WN>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lq = lane >> 4;
@@ -286,7 +324,12 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
   const int64_t per = ((g.K + g.splits - 1) / g.splits + KB - 1) / KB * KB;  // (no part is empty: see linear_plan)
   typedef TileLoad<T, BM, NW, AK> LoadA;
   typedef TileLoad<T, BN, NW, BK> LoadB;
+  typedef SideLoad<T, WM, WN> Side;
+  static_assert(NW * Side::BYTES <= STEP, "a side step fits into a buffer");
   constexpr int UNITS = LoadA::UNITS + LoadB::UNITS;  // loads of a step by one wave
+  constexpr int FEWER = Side::UNITS < UNITS ? Side::UNITS : UNITS;
+  const T* side = (const T*)(SLOPE ? g.dy : g.res);
+  const bool staged = side != nullptr && g.splits == 1 && !(ANY && g.loose);
 
   // Steps of an item's part of the K axis, and the elements of its last one.
   auto steps_of = [&](uint32_t part, int* last) {
@@ -296,14 +339,15 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
     return __builtin_amdgcn_readfirstlane(steps);
   };
 
-  // the loads: the item they are at, and the steps left of it
+  // the loads: the item they are at, and the steps left of it (the side input's are counted below zero)
   LoadA load_a;
   LoadB load_b;
   uint32_t next = blockIdx.x;
-  int left = 0, last = 0;
-  int ahead = 0;  // steps loaded or on their way that are not multiplied yet
+  int64_t pm = 0, pn = 0;
+  int left = 0, last = 0, beside = 0;
+  int ahead = 0;  // steps loaded or on their way that are not used yet
   auto prefetch = [&](int at) {
-    if (left == 0) {
+    if (left == 0 && beside == 0) {
       if (next >= items) return;
       int64_t tm, tn;
       const uint32_t part = next / tiles;
@@ -311,22 +355,42 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
       left = steps_of(part, &last);
       load_a.open((const T*)g.A, g.lda, tm * BM, g.xa, part * per, wave, lane);
       load_b.open((const T*)g.B, g.ldb, tn * BN, g.xb, part * per, wave, lane);
+      pm = tm * BM + wm;
+      pn = tn * BN + wn;
+      if (staged) beside = Side::STEPS;
       next += gridDim.x;
     }
-    --left;
     ++ahead;
-    if (left > 0 || last == KB) {
-      load_a.load(lds + at, wave);
-      load_b.load(lds + at + BM * 64, wave);
+    if (left > 0) {
+      --left;
+      if (left > 0 || last == KB) {
+        load_a.load(lds + at, wave);
+        load_b.load(lds + at + BM * 64, wave);
+      } else {
+        load_a.load_last(last, lds + at, wave, lane);
+        load_b.load_last(last, lds + at + BM * 64, wave, lane);
+      }
     } else {
-      load_a.load_last(last, lds + at, wave, lane);
-      load_b.load_last(last, lds + at + BM * 64, wave, lane);
+      Side::load(side, pm, pn, g.M, g.N, Side::STEPS - beside, lds + at + wave * Side::BYTES, lane);
+      --beside;
     }
+  };
+  // Of the steps on their way all but NB - 2 have come: a wave's loads come in order, and none of the steps behind the one
+  // that is waited for has fewer than UNITS (or, with side steps among them, FEWER).
+  auto arrived = [&] {
+    if (ahead < NB - 1) wait_vm<0>();
+    else if (staged) wait_vm<(NB - 2) * FEWER>();
+    else wait_vm<(NB - 2) * UNITS>();
   };
 #pragma unroll
   for (int b = 0; b < NB - 1; ++b) prefetch(b * STEP);
 
-  int at = 0, to = (NB - 1) * STEP;  // buffers of the step that is multiplied and of the one that is loaded meanwhile
+  int at = 0, to = (NB - 1) * STEP;  // buffers of the step that is used and of the one that is loaded meanwhile
+  auto advance = [&] {
+    --ahead;
+    to = at;
+    at = at == (NB - 1) * STEP ? 0 : at + STEP;
+  };
   bool waited = false;
   for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
     int64_t tm, tn;
@@ -336,11 +400,9 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
     f4 acc[FM][FN] = {};
     int unused;
     for (int s = steps_of(part, &unused); s > 0; --s) {
-      // this wave's pieces of the step are there (loads arrive in order), and past the barrier everyone's; the buffer of
-      // the step before has been read by all
-      if (!waited) {
-        if (ahead >= NB - 1) wait_vm<(NB - 2) * UNITS>(); else wait_vm<0>();
-      }
+      // this wave's pieces of the step are there, and past the barrier everyone's; the buffer of the step before has been
+      // read by all
+      if (!waited) arrived();
       waited = false;
       __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
@@ -365,21 +427,19 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
             acc[i][j] = mma_f32(fb[j], fa[i], acc[i][j]);
         }
       }
-      --ahead;
-      to = at;
-      at = at == (NB - 1) * STEP ? 0 : at + STEP;
+      advance();
     }
-    // the next step's loads are waited for before the stores are issued, so that no step waits for the stores
-    if (ahead >= NB - 1) wait_vm<(NB - 2) * UNITS>(); else wait_vm<0>();
-    waited = true;
     if (g.splits > 1) {
+      arrived();  // as below
+      waited = true;
       float* o = g.part + part * g.M * g.N;
+      const int l = lane_here(lane);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const int64_t m = m0 + wm + i * 16 + li;
+        const int64_t m = m0 + wm + i * 16 + (l & 15);
 #pragma unroll
         for (int j = 0; j < FN; ++j) {
-          const int64_t n = n0 + wn + j * 16 + lq * 4;
+          const int64_t n = n0 + wn + j * 16 + (l >> 4) * 4;
           if (m >= g.M) continue;
           if (g.N % 4 == 0) {
             if (n < g.N) *reinterpret_cast<f4*>(o + m * g.N + n) = acc[i][j];
@@ -392,13 +452,21 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), OCC) void gemm_tile_ker
       }
       continue;
     }
-    char* mine = lds + NB * STEP + wave * out_lds<T, WN>();
-    switch (g.act) {
-      case ACT_RELU: tile_out<T, ACT_RELU, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      case ACT_SILU: tile_out<T, ACT_SILU, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      case ACT_GELU_TANH: tile_out<T, ACT_GELU_TANH, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane); break;
-      default: tile_out<T, ACT_NONE, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, mine, lane);
+    if (!staged) {
+      // the next step's loads are waited for before the stores are issued, so that no step waits for the stores
+      arrived();
+      waited = true;
     }
+    tile_out<T, ACT, SLOPE, ANY, WM, WN>(g, m0 + wm, n0 + wn, acc, lds + NB * STEP + wave * out_lds<T, WN>(), lane, [&](int) -> const char* {
+      if (!staged) return nullptr;
+      arrived();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      prefetch(to);
+      const char* here = lds + at + wave * Side::BYTES;
+      advance();
+      return here;
+    });
   }
 }
 
@@ -506,63 +574,81 @@ __global__ __launch_bounds__(1024) void col_sum_kernel(const float* part, int64_
   }
 }
 
-template <typename T, int BM, int BN, int WM, int WN, int NB, bool WIDE>
+template <typename T, int BM, int BN, int WM, int WN, int NB, bool ANY>
 void launch_tiles(const GemmArgs& a, hipStream_t st) {
   const int64_t items = ((a.M + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
   const dim3 grid((unsigned)(items < 512 ? items : 512));  // (two work-groups on each of 256 compute units)
   constexpr int NT = 64 * (BM / WM) * (BN / WN);
-  if constexpr (!WIDE) {
-    if (a.dy != nullptr) {
-      gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, true, true, false, true><<<grid, NT, 0, st>>>(a);
-      return;
+#define RES_TILES(AK, BK, ACT, SLOPE) gemm_tile_kernel<T, BM, BN, WM, WN, NB, ANY, AK, BK, ACT, SLOPE><<<grid, NT, 0, st>>>(a)
+  const int act = a.splits > 1 ? ACT_NONE : a.act;  // (a split product's is applied where its parts are joined)
+  if (!a.ak)
+    RES_TILES(false, false, ACT_NONE, false);
+  else if (a.bk)
+    RES_TILES(true, true, ACT_NONE, false);
+  else if (a.dy != nullptr) {
+    if constexpr (ANY) {  // (the widest tile would keep its sums of columns in memory)
+      if (act == ACT_RELU) RES_TILES(true, false, ACT_RELU, true);
+      else if (act == ACT_SILU) RES_TILES(true, false, ACT_SILU, true);
+      else RES_TILES(true, false, ACT_GELU_TANH, true);
     }
-  }
-  if (a.ak && a.bk)
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, true, true, false><<<grid, NT, 0, st>>>(a);
-  else if (a.ak)
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, true, false, false><<<grid, NT, 0, st>>>(a);
+  } else if (act == ACT_RELU)
+    RES_TILES(true, false, ACT_RELU, false);
+  else if (act == ACT_SILU)
+    RES_TILES(true, false, ACT_SILU, false);
+  else if (act == ACT_GELU_TANH)
+    RES_TILES(true, false, ACT_GELU_TANH, false);
   else
-    gemm_tile_kernel<T, BM, BN, WM, WN, NB, 2, !WIDE, false, false, false><<<grid, NT, 0, st>>>(a);
+    RES_TILES(true, false, ACT_NONE, false);
+#undef RES_TILES
 }
 
 }  // namespace
 
 int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 
-// Tiles of a product, and the parts its K axis is cut into where the tiles are fewer than the compute units: as many as
-// fill them, a part having at least 256 terms.
+// Tiles of a product, and the parts its K axis is cut into where the tiles are fewer than the work-groups that the card
+// runs: as many as fill it, a part having at least 256 terms (128 with the small tile).
+// The widest tile reads least (24 KB for 512 matrix cycles of a unit's SIMD; 128 x 128 needs 16 KB for 256, as much as a
+// unit gets from the cache), but takes many outputs: the others are for products that would leave units idle.
 LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide) {
   LinearPlan p{};
   auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
-  int64_t most = whole ? 1 : K / 256;
-  most = most < 1 ? 1 : most > 64 ? 64 : most;
-  int64_t t;
-  if (M <= 64) {
-    p.tile = TILE_THIN;
-    t = tiles(64, 128);
-  } else if (es == 2 && wide && tiles(128, 256) * most >= 256) {
+  auto parts = [&](int64_t least) { return whole || K < 2 * least ? 1 : K / least < 64 ? K / least : 64; };
+  int64_t t, want, most = parts(256);
+  if (es == 2 && wide && !whole && M > 64 && tiles(128, 256) * most >= 256) {
     p.tile = TILE_WIDE;
     t = tiles(128, 256);
-  } else {
+    want = 256;
+  } else if (M > 64 && tiles(128, 128) * most >= 256) {
     p.tile = TILE_SQUARE;
     t = tiles(128, 128);
+    want = 256;
+  } else {
+    p.tile = TILE_SMALL;
+    t = tiles(64, 64);
+    want = 512;
+    most = parts(128);
   }
-  int64_t s = t > 0 ? 256 / t : 1;
+  int64_t s = t > 0 ? want / t : 1;
   s = s < 1 ? 1 : s > most ? most : s;
   const int64_t kb = 64 / es, per = ((K + s - 1) / s + kb - 1) / kb * kb;  // whole steps, and no part without any
   p.splits = K > 0 ? (int)((K + per - 1) / per) : 0;
   return p;
+}
+int64_t linear_col_blocks(int tile, int64_t M) {
+  const int64_t w = tile == TILE_WIDE ? 128 : tile == TILE_SQUARE ? 64 : 32;
+  return (M + w - 1) / w;
 }
 
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
   if (a.splits > 0) {
     if (a.tile == TILE_WIDE) {
-      if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, true>(a, st);
+      if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, false>(a, st);
     } else if (a.tile == TILE_SQUARE) {
-      launch_tiles<T, 128, 128, 64, 64, 4, false>(a, st);
+      launch_tiles<T, 128, 128, 64, 64, 4, true>(a, st);
     } else {
-      launch_tiles<T, 64, 128, 64, 32, 6, false>(a, st);
+      launch_tiles<T, 64, 64, 32, 32, 6, true>(a, st);
     }
   }
   if (a.splits != 1) {
