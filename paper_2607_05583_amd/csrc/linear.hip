@@ -315,7 +315,7 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 // ahead of the products over the borders of the items, so that neither an item's first loads nor its stores are waited
 // for.  NB buffers of a step and the LDS of each wave's outputs.
 template <typename T, int BM, int BN, int WM, int WN, int NB, bool ANY, bool AK, bool BK, int ACT, bool SLOPE>
-__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), 2) void gemm_tile_kernel(GemmArgs g) {
+__global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) / 2) void gemm_tile_kernel(GemmArgs g) {
   constexpr int NW = (BM / WM) * (BN / WN), KB = Gemm<T>::KB, FM = WM / 16, FN = WN / 16, STEP = (BM + BN) * 64;
   __shared__ __align__(1024) char lds[NB * STEP + NW * out_lds<T, WN>()];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lq = lane >> 4;
@@ -646,7 +646,7 @@ hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
     if (a.tile == TILE_WIDE) {
       if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, false>(a, st);
     } else if (a.tile == TILE_SQUARE) {
-      launch_tiles<T, 128, 128, 64, 64, 4, true>(a, st);
+      launch_tiles<T, 128, 128, 64, 32, 4, true>(a, st);
     } else {
       launch_tiles<T, 64, 64, 32, 32, 6, true>(a, st);
     }
