@@ -6,15 +6,18 @@
 // 0..255 (a power law spends the codes on small sizes; a v that is not zero never gets
 // code 0, since the step divides by its root).  The step itself uses the unrounded m and v.
 //
-// A wave takes blocks of 256 elements, four a lane, so that a block's largest value is
-// one reduction over the wave.
+// A wave takes one block of 256 elements, four consecutive ones a lane, so that a block's largest value is one reduction
+// over the wave and every access 4 to 16 bytes a lane.  Memory bounds it: bfloat16 with float32 copies and states moves
+// 28 bytes an element, 201 M of them in 994 us (5.7 TB/s); float32 with float32 states 28 bytes, 4.7 M in 23 us (out of
+// the last cache); float32 with states of 8 bits 16 bytes, 80 M in 257 us (5.0 TB/s; 300 vector instructions a wave).
+// Two blocks a wave and element 64 j + lane took 1026, 36 and 345 us.
 #include "layer.h"
 
 namespace res {
 namespace {
 
 constexpr int TABLE = 64;      // tensors of one launch (their table is a kernel argument)
-constexpr int CHUNK_BLOCKS = 8;  // blocks of a work-group: two a wave
+constexpr int CHUNK_BLOCKS = 4;  // blocks of a work-group: two a wave
 constexpr int64_t CHUNK_ELEMS = (int64_t)CHUNK_BLOCKS * RES_ADAMW_BLOCK;
 constexpr float TINY = 1e-30f;  // a smaller scale counts as zero (its reciprocal would leave float32)
 
@@ -29,12 +32,17 @@ struct Table {
 };
 
 // The largest |value| of a wave's lanes; NaN is larger than infinity.
-__device__ __forceinline__ float wave_absmax(float a, float b, float c, float d) {
+__device__ __forceinline__ float wave_absmax(const float (&f)[4]) {
   auto bits = [](float v) { return __float_as_uint(v) & 0x7fffffffu; };
-  uint32_t x = max(max(bits(a), bits(b)), max(bits(c), bits(d)));
+  uint32_t x = max(max(bits(f[0]), bits(f[1])), max(bits(f[2]), bits(f[3])));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xb1, 0xf, 0xf, false));   // lane ^ 1
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4e, 0xf, 0xf, false));   // lane ^ 2
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x141, 0xf, 0xf, false));  // 7 - lane of eight
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x140, 0xf, 0xf, false));  // 15 - lane of sixteen
+  uint32_t y = 0;
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) x = max(x, (uint32_t)__shfl_xor((int)x, k, 64));
-  return __uint_as_float(x);
+  for (int k = 0; k < 64; k += 16) y = max(y, (uint32_t)__builtin_amdgcn_readlane((int)x, k));
+  return __uint_as_float(y);
 }
 
 __device__ __forceinline__ float value_m(int c, float s) {
@@ -48,22 +56,133 @@ __device__ __forceinline__ float value_v(int c, float s) {
   return (f2 * f2) * s;
 }
 
-// Codes are decided by correctly rounded operations (square roots, the reciprocal, no
-// contraction), so that they do not depend on how a kernel is compiled.
-__device__ __forceinline__ int code_m(float m, float inv) {
+// Codes are decided by correctly rounded operations (square roots, the reciprocal, no contraction), so that they do not
+// depend on how a kernel is compiled.  The unit's own square root is within one unit in the last place; the two ways differ
+// by less than 2^-13 before the rounding to 0..255.  Where that leaves no doubt to which whole number is rounded (all but
+// one of two thousand), the correctly rounded ones, of four times the instructions, are not computed: 80 M elements 290 to 257 us.
+__device__ __forceinline__ bool doubtful(float f) { return !(fabsf(fabsf(f - rintf(f)) - 0.5f) > 0x1p-12f); }
+__device__ __forceinline__ void codes(float m, float v, float im, float iv, int* cm, int* cv) {
 #pragma clang fp contract(off)
-  const int c = (int)rintf(sqrtf(fabsf(m) * inv) * 127.0f);
-  return m < 0.0f ? -c : c;
+  const float xm = fabsf(m) * im, xv = v * iv;
+  float fm = __builtin_amdgcn_sqrtf(xm) * 127.0f, fv = __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(xv)) * 255.0f;
+  if (__builtin_amdgcn_ballot_w64(doubtful(fm) || doubtful(fv)) != 0) {  // (a wave's branch: else both would be computed)
+    fm = sqrtf(xm) * 127.0f;
+    fv = sqrtf(sqrtf(xv)) * 255.0f;
+  }
+  *cm = (int)rintf(fm);
+  *cv = (int)rintf(fv);
+  if (m < 0.0f) *cm = -*cm;
+  if (v > 0.0f && iv > 0.0f && *cv < 1) *cv = 1;
 }
-__device__ __forceinline__ int code_v(float v, float inv) {
+
+// A lane's four elements, one behind the other at the alignment of one: all of them (WHOLE), or the first `left`.
+template <typename T> using Vec = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+template <bool WHOLE, typename T>
+__device__ __forceinline__ Vec<T> load_four(const T* from, int left) {
+  Vec<T> r = {};
+  if constexpr (WHOLE) {
+    r = *reinterpret_cast<const Vec<T>*>(from);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) r[j] = from[j];
+  }
+  return r;
+}
+// (Stored past the caches, since what follows a step reads more than they hold: 54 tensors of together 4.7 M float32: 31 to 22 us.)
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void store_four(T* to, Vec<T> v, int left) {
+  if constexpr (WHOLE) {
+    __builtin_nontemporal_store(v, reinterpret_cast<Vec<T>*>(to));
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < left) to[j] = v[j];
+  }
+}
+
+// One block: p, g and o are at this lane's elements, s is their place in the states.
+template <bool WHOLE, typename TP, typename TG, int BITS, bool MASTER>
+__device__ __forceinline__ void adamw_block(const AdamWArgs& a, float gs, const TP* p, const TG* g, TP* o, int64_t s, int left, int lane) {
+  const int64_t sb = s / RES_ADAMW_BLOCK;
+  const Vec<TG> gv = load_four<WHOLE>(g, left);
+  float m[4], v[4], w[4];
+  if constexpr (BITS == 8) {
+    const Vec<int8_t> cm = load_four<WHOLE>((const int8_t*)a.m + s, left);
+    const Vec<uint8_t> cv = load_four<WHOLE>((const uint8_t*)a.v + s, left);
+    const float sm = a.sm[sb], sv = a.sv[sb];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = value_m(cm[j], sm);
+      v[j] = value_v(cv[j], sv);
+    }
+  } else {
+    const Vec<float> mv = load_four<WHOLE>((const float*)a.m + s, left), vv = load_four<WHOLE>((const float*)a.v + s, left);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      m[j] = mv[j];
+      v[j] = vv[j];
+    }
+  }
+  if constexpr (MASTER) {
+    const Vec<float> wv = load_four<WHOLE>(a.master + s, left);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = wv[j];
+  } else {
+    const Vec<TP> wv = load_four<WHOLE>(p, left);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = to_f32((TP)wv[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
 #pragma clang fp contract(off)
-  const int c = (int)rintf(sqrtf(sqrtf(v * inv)) * 255.0f);
-  return v > 0.0f && inv > 0.0f && c < 1 ? 1 : c;
+    const float gr = to_f32((TG)gv[j]) * gs;
+    m[j] = m[j] * a.b1 + gr * a.b1c;
+    v[j] = v[j] * a.b2 + (gr * gr) * a.b2c;
+    if (!WHOLE && j >= left) m[j] = v[j] = 0.0f;
+  }
+  float im = 0.0f, iv = 0.0f;
+  if constexpr (BITS == 8) {
+    const float sm = wave_absmax(m), sv = wave_absmax(v);
+    im = sm >= TINY ? 1.0f / sm : 0.0f;
+    iv = sv >= TINY ? 1.0f / sv : 0.0f;
+    if (lane == 0) {
+      a.sm_out[sb] = sm;
+      a.sv_out[sb] = sv;
+    }
+  }
+  Vec<TP> po;
+  Vec<float> q;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float den = fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps);
+    // (a reciprocal within one unit in the last place: 2^-23 of the step, which is small beside the parameter)
+    q[j] = fmaf(w[j], a.decay, -(a.step * m[j]) * __builtin_amdgcn_rcpf(den));
+    po[j] = from_f32<TP>(q[j]);
+  }
+  store_four<WHOLE>(o, po, left);
+  if constexpr (MASTER) store_four<WHOLE>(a.master_out + s, q, left);
+  if constexpr (BITS == 8) {
+    Vec<int8_t> cm;
+    Vec<uint8_t> cv;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      int c, d;
+      codes(m[j], v[j], im, iv, &c, &d);
+      cm[j] = (int8_t)c;
+      cv[j] = (uint8_t)d;
+    }
+    store_four<WHOLE>((int8_t*)a.m_out + s, cm, left);
+    store_four<WHOLE>((uint8_t*)a.v_out + s, cv, left);
+  } else {
+    store_four<WHOLE>((float*)a.m_out + s, Vec<float>{m[0], m[1], m[2], m[3]}, left);
+    store_four<WHOLE>((float*)a.v_out + s, Vec<float>{v[0], v[1], v[2], v[3]}, left);
+  }
 }
 
 template <typename TP, typename TG, int BITS, bool MASTER>
 __global__ __launch_bounds__(256) void adamw_kernel(AdamWArgs a, Table tab) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   int k = 0;
   for (int hi = tab.count - 1; k < hi;) {  // the tensor of this chunk
     const int mid = (k + hi) >> 1;
@@ -74,58 +193,11 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWArgs a, Table tab) {
   const TG* g = (const TG*)tab.g[k];
   TP* o = (TP*)tab.o[k];
   const float gs = a.grad_scale != nullptr ? a.grad_scale[0] : 1.0f;
-  for (int blk = wave; blk < CHUNK_BLOCKS; blk += 4) {
-    const int64_t e0 = chunk * CHUNK_ELEMS + blk * RES_ADAMW_BLOCK, s0 = tab.state[k] + e0;
-    if (e0 >= n) break;
-    const int64_t sb = s0 / RES_ADAMW_BLOCK;
-    float m[4], v[4], w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t e = e0 + j * 64 + lane, s = s0 + j * 64 + lane;
-      m[j] = v[j] = w[j] = 0.0f;
-      if (e < n) {
-#pragma clang fp contract(off)
-        const float gr = to_f32(g[e]) * gs;
-        float mo, vo;
-        if constexpr (BITS == 8) {
-          mo = value_m(((const int8_t*)a.m)[s], a.sm[sb]);
-          vo = value_v(((const uint8_t*)a.v)[s], a.sv[sb]);
-        } else {
-          mo = ((const float*)a.m)[s];
-          vo = ((const float*)a.v)[s];
-        }
-        m[j] = mo * a.b1 + gr * a.b1c;
-        v[j] = vo * a.b2 + (gr * gr) * a.b2c;
-        w[j] = MASTER ? a.master[s] : to_f32(p[e]);
-      }
-    }
-    float im = 0.0f, iv = 0.0f;
-    if constexpr (BITS == 8) {
-      const float sm = wave_absmax(m[0], m[1], m[2], m[3]), sv = wave_absmax(v[0], v[1], v[2], v[3]);
-      im = sm >= TINY ? 1.0f / sm : 0.0f;
-      iv = sv >= TINY ? 1.0f / sv : 0.0f;
-      if (lane == 0) {
-        a.sm_out[sb] = sm;
-        a.sv_out[sb] = sv;
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t e = e0 + j * 64 + lane, s = s0 + j * 64 + lane;
-      if (e >= n) continue;
-      const float den = fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps);
-      const float q = fmaf(w[j], a.decay, -(a.step * m[j]) / den);
-      if constexpr (MASTER) a.master_out[s] = q;
-      o[e] = from_f32<TP>(q);
-      if constexpr (BITS == 8) {
-        ((int8_t*)a.m_out)[s] = (int8_t)code_m(m[j], im);
-        ((uint8_t*)a.v_out)[s] = (uint8_t)code_v(v[j], iv);
-      } else {
-        ((float*)a.m_out)[s] = m[j];
-        ((float*)a.v_out)[s] = v[j];
-      }
-    }
-  }
+  const int64_t e0 = chunk * CHUNK_ELEMS + wave * RES_ADAMW_BLOCK, e = e0 + lane * 4, s = tab.state[k] + e;
+  if (e0 + RES_ADAMW_BLOCK <= n)
+    adamw_block<true, TP, TG, BITS, MASTER>(a, gs, p + e, g + e, o + e, s, 4, lane);
+  else if (e0 < n)
+    adamw_block<false, TP, TG, BITS, MASTER>(a, gs, p + e, g + e, o + e, s, (int)(e < n ? (n - e < 4 ? n - e : 4) : 0), lane);
 }
 
 __global__ __launch_bounds__(256) void adamw_values_kernel(const int8_t* m, const uint8_t* v, const float* sm,
