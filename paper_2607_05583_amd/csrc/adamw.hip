@@ -17,7 +17,7 @@ namespace res {
 namespace {
 
 constexpr int TABLE = 64;      // tensors of one launch (their table is a kernel argument)
-constexpr int CHUNK_BLOCKS = 4;  // blocks of a work-group: two a wave
+constexpr int CHUNK_BLOCKS = 4;  // blocks of a work-group: one a wave (two: 1032 for 994 us with float32 copies)
 constexpr int64_t CHUNK_ELEMS = (int64_t)CHUNK_BLOCKS * RES_ADAMW_BLOCK;
 constexpr float TINY = 1e-30f;  // a smaller scale counts as zero (its reciprocal would leave float32)
 

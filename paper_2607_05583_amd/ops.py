@@ -10,6 +10,7 @@ parameters gamma, omega, amp, phase float32 [D, M]; states float32 [B, D, M, 2].
 from __future__ import annotations
 
 import ctypes
+from typing import NamedTuple
 
 import torch
 
@@ -1457,3 +1458,98 @@ def resonator_adamw_values(state):
     v = torch.empty_like(m)
     check(_lib.lib().resonator_adamw_values(ctypes.byref(s), n, _ptr(m), _ptr(v), _stream(m.device)))
     return m, v
+
+
+# ---------------------------------------------------------------------------
+# Gated recurrent layer: projection, gated scan, output projection, MLP
+# ---------------------------------------------------------------------------
+class GatedLayerParams(NamedTuple):
+    """One layer's tensors: Wp [d, 3 d] (the scan's input and its two gates' logits side by side), Wo [d, d], W1 [d, f],
+    W2 [f, d] of the activations' type; bp [3 d], gamma [d], bo [d], b1 [f], b2 [d] float32."""
+
+    Wp: torch.Tensor
+    bp: torch.Tensor
+    gamma: torch.Tensor
+    Wo: torch.Tensor
+    bo: torch.Tensor
+    W1: torch.Tensor
+    b1: torch.Tensor
+    W2: torch.Tensor
+    b2: torch.Tensor
+
+
+def resonator_gated_layer_fwd(x, p, h0=None, lengths=None, act="gelu_tanh", return_state=False, save=False, ws=None):
+    """A gated recurrent layer: y = gated scan of the columns of x Wp + bp, z = x + y Wo + bo,
+    out = z + act(z W1 + b1) W2 + b2.  x [B, L, d]; ``p`` a GatedLayerParams; ``h0``, ``lengths`` and ``ws`` (a
+    gated_scan_workspace) as in resonator_gated_scan_fwd.  Returns out; with ``return_state`` also the state after the
+    last step, from which resonator_gated_layer_step goes on; with ``save`` also the dict for resonator_gated_layer_bwd.
+    Four products and a scan: the biases, the activation and the residuals are part of the products."""
+    u = resonator_linear_fwd(x, p.Wp, p.bp)
+    keep = resonator_gated_scan_fwd(*u.split(x.shape[-1], dim=-1), p.gamma, h0=h0, lengths=lengths, return_state=True,
+                                    save=save, ws=ws)
+    y, h = keep[:2]
+    z = resonator_linear_fwd(y, p.Wo, p.bo, residual=x)
+    m, pre = resonator_linear_fwd(z, p.W1, p.b1, act=act, save=True) if save else (
+        resonator_linear_fwd(z, p.W1, p.b1, act=act), None)
+    out = resonator_linear_fwd(m, p.W2, p.b2, residual=z)
+    r = (out,) + ((h,) if return_state else ()) + (
+        (dict(u=u, y=y, carry=keep[2], z=z, m=m, pre=pre),) if save else ())
+    return r if len(r) > 1 else out
+
+
+def resonator_gated_layer_bwd(x, p, dout, saved, lengths=None, dh=None, act="gelu_tanh", want_dh0=False, ws=None):
+    """Gradients of sum(dout out) + sum(dh h): dict with dx, ``dp`` (a GatedLayerParams: weights of the activations' type,
+    the rest float32) and, where wanted, dh0.  ``saved`` is what the forward with ``save`` returned."""
+    u, d = saved["u"], x.shape[-1]
+    g2 = resonator_linear_bwd(saved["m"], p.W2, dout, want_db=True)
+    g1 = resonator_linear_bwd(saved["z"], p.W1, g2["dx"], pre=saved["pre"], act=act, residual=dout, want_db=True)
+    go = resonator_linear_bwd(saved["y"], p.Wo, g1["dx"], want_db=True)
+    du = torch.empty_like(u)
+    gs = resonator_gated_scan_bwd(*u.split(d, dim=-1), p.gamma, go["dx"], lengths=lengths, dh_out=dh, carry=saved["carry"],
+                                  want_dh0=want_dh0, out=du.split(d, dim=-1), ws=ws)
+    gp = resonator_linear_bwd(x, p.Wp, du, residual=g1["dx"], want_db=True)
+    r = {"dx": gp["dx"], "dp": GatedLayerParams(gp["dW"], gp["db"], gs["dgamma"], go["dW"], go["db"], g1["dW"], g1["db"],
+                                                g2["dW"], g2["db"])}
+    if want_dh0:
+        r["dh0"] = gs["dh0"]
+    return r
+
+
+def resonator_gated_layer_step(x_t, p, h, act="gelu_tanh", h_out=None):
+    """The layer for one token of every sequence: x_t [B, d], state h [B, d] float32, advanced in place unless ``h_out``
+    receives the new one; returns [B, d].  Five launches; a caller may capture them into a graph."""
+    u = resonator_linear_fwd(x_t, p.Wp, p.bp)
+    y = resonator_gated_scan_step(*u.split(x_t.shape[-1], dim=-1), p.gamma, h, h_out=h_out)
+    z = resonator_linear_fwd(y, p.Wo, p.bo, residual=x_t)
+    m = resonator_linear_fwd(z, p.W1, p.b1, act=act)
+    return resonator_linear_fwd(m, p.W2, p.b2, residual=z)
+
+
+class GatedLayerFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_gated_layer_fwd (the output and the last state) and resonator_gated_layer_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, h0, lengths, act, *p):
+        p = GatedLayerParams(*p)
+        out, h, saved = resonator_gated_layer_fwd(x, p, h0=h0, lengths=lengths, act=act, return_state=True, save=True)
+        pre = saved.pop("pre")
+        ctx.names, ctx.act = tuple(saved), act
+        ctx.save_for_backward(x, lengths, pre.pre, *p, *saved.values())
+        ctx.set_materialize_grads(False)
+        return out, h
+
+    @staticmethod
+    def backward(ctx, dout, dh):
+        x, lengths, pre, *rest = ctx.saved_tensors
+        n = len(GatedLayerParams._fields)
+        p, saved = GatedLayerParams(*rest[:n]), dict(zip(ctx.names, rest[n:]))
+        saved["pre"] = LinearSaved(pre, p.b1)
+        dout = torch.zeros_like(x) if dout is None else dout.contiguous()
+        g = resonator_gated_layer_bwd(x, p, dout, saved, lengths=lengths, dh=None if dh is None else dh.contiguous(),
+                                      act=ctx.act, want_dh0=ctx.needs_input_grad[1])
+        return g["dx"], g.get("dh0"), None, None, *g["dp"]
+
+
+def resonator_gated_layer(x, p, h0=None, lengths=None, act="gelu_tanh"):
+    """Differentiable gated recurrent layer: (out, last state); x, h0 and p's tensors receive gradients."""
+    return GatedLayerFunction.apply(x, h0, lengths, act, *p)
