@@ -103,7 +103,8 @@ hipError_t launch_gated_step(const Rows& x, const Rows& r, const Rows& i, void* 
 // Linear product with epilogue: C[m][n] = sum_k A(m, k) B(k, n), then out =
 // act(C + bias[n]) + res[m][n]; pre receives C + bias[n].
 // ---------------------------------------------------------------------------
-enum { TILE_SMALL = 0, TILE_SQUARE = 1, TILE_WIDE = 2 };  // 64 x 64, 128 x 128, 128 x 256 (bf16) outputs of a work-group
+// 64 x 64, 128 x 128, 128 x 256 (bf16) outputs of a work-group; 64 x 64 with the K axis spread over its waves
+enum { TILE_SMALL = 0, TILE_SQUARE = 1, TILE_WIDE = 2, TILE_DEEP = 3 };
 
 struct GemmArgs {
   const void* A;      // ak: A(m, k) = A[m lda + k], else A[k lda + m]
@@ -127,8 +128,8 @@ struct GemmArgs {
 struct LinearPlan {
   int tile, splits;
 };
-// whole: the K axis is not cut and dy is taken; wide: the widest tile, which takes neither dy nor `loose`, may be taken
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide);
+// ak: A's K axis is consecutive; whole: the K axis is not cut and dy is taken; wide: the widest tile, which takes neither dy nor `loose`, may be taken
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool ak, bool whole, bool wide);
 int64_t linear_col_blocks(int tile, int64_t M);  // rows of colpart: one for each wave's rows
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);

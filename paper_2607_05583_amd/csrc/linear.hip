@@ -470,6 +470,102 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) /
   }
 }
 
+// Few outputs: a work-group has one 64 x 64 tile, and each of its eight waves all of the tile for an eighth of the K axis,
+// loaded and multiplied without a barrier; then the eight sums are added in order through the LDS and the epilogue follows.
+// One launch instead of a split product's two and its partial sums in memory: 64 x 1024 x 4096 (R x K x N) bf16 8.4 us in a
+// graph, where the 8 MB of the weights are 1.8 us of memory and the rest is the latency of a launch and of two to four
+// loads one behind the other.
+template <typename T, bool BK>
+__global__ __launch_bounds__(512, 2) void gemm_deep_kernel(GemmArgs g) {
+  constexpr int NW = 8, NB = 2, KB = Gemm<T>::KB, STEP = 128 * 64;
+  __shared__ __align__(1024) char lds[NW * NB * STEP];
+  static_assert(NB * STEP == 64 * 64 * 4, "a wave's buffers hold its sums");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, lq = lane >> 4;
+  const uint32_t nt = (uint32_t)((g.N + 63) / 64);
+  const int64_t m0 = (int64_t)(blockIdx.x / nt) * 64, n0 = (int64_t)(blockIdx.x % nt) * 64;
+  char* mine = lds + wave * (NB * STEP);
+  typedef TileLoad<T, 64, 1, true> LoadA;
+  typedef TileLoad<T, 64, 1, BK> LoadB;
+  const int steps = (int)((g.K + KB - 1) / KB), last = (int)(g.K - (int64_t)(steps - 1) * KB);
+  const int begin = wave * steps / NW, end = (wave + 1) * steps / NW;
+  LoadA load_a;
+  LoadB load_b;
+  load_a.open((const T*)g.A, g.lda, m0, g.xa, (int64_t)begin * KB, 0, lane);
+  load_b.open((const T*)g.B, g.ldb, n0, g.xb, (int64_t)begin * KB, 0, lane);
+  int next = begin;
+  auto prefetch = [&] {
+    if (next >= end) return;
+    char* to = mine + (next - begin) % NB * STEP;
+    if (next + 1 < steps || last == KB) {
+      load_a.load(to, 0);
+      load_b.load(to + 64 * 64, 0);
+    } else {
+      load_a.load_last(last, to, 0, lane);
+      load_b.load_last(last, to + 64 * 64, 0, lane);
+    }
+    ++next;
+  };
+#pragma unroll
+  for (int b = 0; b < NB; ++b) prefetch();
+  f4 acc[4][4] = {};
+  for (int s = begin; s < end; ++s) {
+    if (next - s < NB) wait_vm<0>();
+    else wait_vm<(NB - 1) * (LoadA::UNITS + LoadB::UNITS)>();
+    asm volatile("" ::: "memory");
+    const char* la = mine + (s - begin) % NB * STEP;
+    const char* lb = la + 64 * 64;
+    typename Gemm<T>::Frag fa[4], fb[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) fb[j] = fragment<T, 64, BK>(lb, j * 16, li, lq);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) fa[i] = fragment<T, 64, true>(la, i * 16, li, lq);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read, before the buffer is loaded again
+    prefetch();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+        else
+          acc[i][j] = mma_f32(fb[j], fa[i], acc[i][j]);
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<f4*>(mine + ((i * 4 + j) * 64 + lane) * 16) = acc[i][j];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int at = k * 512 + threadIdx.x, l = at & 63, f = at >> 6;
+    f4 c = *reinterpret_cast<const f4*>(lds + at * 16);
+#pragma unroll
+    for (int w = 1; w < NW; ++w) c += *reinterpret_cast<const f4*>(lds + w * (NB * STEP) + at * 16);
+    const int64_t m = m0 + f / 4 * 16 + (l & 15);
+    const int n = (int)n0 + f % 4 * 16 + (l >> 4) * 4;
+    if (m >= g.M || n >= (int)g.N) continue;
+    if (g.bias != nullptr) c += wide(load_quad(g.bias, n, g.N, g.loose));
+    const int there = g.loose && g.N - n < 4 ? (int)(g.N - n) : 4;
+    if (g.pre != nullptr)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (r < there) g.pre[m * g.N + n + r] = c[r];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c[r] = act_value(c[r], g.act);
+    if (g.res != nullptr) c += wide(load_quad((const T*)g.res + m * g.N, n, g.N, g.loose));
+    const Quad<T> q = round_quad(c, T());
+    T* o = (T*)g.out + m * g.N + n;
+    if (!g.loose) {
+      *reinterpret_cast<Quad<T>*>(o) = q;
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (r < there) o[r] = q.v[r];
+    }
+  }
+}
+
 // The parts of a split sum (none: zeros), in order, then the epilogue.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void gemm_join_kernel(GemmArgs g) {
@@ -610,7 +706,11 @@ int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 // runs: as many as fill it, a part having at least 256 terms (128 with the small tile).
 // The widest tile reads least (24 KB for 512 matrix cycles of a unit's SIMD; 128 x 128 needs 16 KB for 256, as much as a
 // unit gets from the cache), but takes many outputs: the others are for products that would leave units idle.
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide) {
+// A small product whose K axis would be cut is summed in one work-group a tile instead where the axis is short: bf16 64 x
+// 256 x 1024 5.1 for 7.5 us, 64 x 1024 x 4096 8.4 for 14.1, 64 x 2048 x 2048 12.5 for 15.8, but 64 x 4096 x 1024 20.4 for
+// 19.2; float32, whose products take eight times the matrix cycles, 64 x 256 x 1024 9.1 for 9.8, but 16 x 512 x 2048 12.4
+// for 10.6.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool ak, bool whole, bool wide) {
   LinearPlan p{};
   auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   auto parts = [&](int64_t least) { return whole || K < 2 * least ? 1 : K / least < 64 ? K / least : 64; };
@@ -633,6 +733,10 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, b
   s = s < 1 ? 1 : s > most ? most : s;
   const int64_t kb = 64 / es, per = ((K + s - 1) / s + kb - 1) / kb * kb;  // whole steps, and no part without any
   p.splits = K > 0 ? (int)((K + per - 1) / per) : 0;
+  if (p.tile == TILE_SMALL && ak && p.splits > 1 && K * (int64_t)es <= (es == 2 ? 4096 : 1024)) {
+    p.tile = TILE_DEEP;
+    p.splits = 1;
+  }
   return p;
 }
 int64_t linear_col_blocks(int tile, int64_t M) {
@@ -645,6 +749,10 @@ hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
   if (a.splits > 0) {
     if (a.tile == TILE_WIDE) {
       if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, false>(a, st);
+    } else if (a.tile == TILE_DEEP) {
+      const dim3 grid((unsigned)(((a.M + 63) / 64) * ((a.N + 63) / 64)));
+      if (a.bk) gemm_deep_kernel<T, true><<<grid, 512, 0, st>>>(a);
+      else gemm_deep_kernel<T, false><<<grid, 512, 0, st>>>(a);
     } else if (a.tile == TILE_SQUARE) {
       launch_tiles<T, 128, 128, 64, 32, 4, true>(a, st);
     } else {
