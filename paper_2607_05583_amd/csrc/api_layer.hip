@@ -259,8 +259,10 @@ size_t up256(size_t v) { return (v + 255) & ~(size_t)255; }
 int64_t up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 // Whether pre is computed again in the backward rather than kept: the product costs 2 R K N operations, keeping pre 8 R N
-// bytes written and read.  At 65536 x 256 x 1024 bf16 (R, K, N) the step took 475 us keeping it.
-bool computes_pre(res_dtype_t dt, int act, int64_t K) { return act != RES_ACT_NONE && K <= (dt == RES_BF16 ? 512 : 96); }
+// bytes written and read.  A training step (R x K x N, bf16, gelu) computing it and keeping it: 65536 x 256 x 1024 340 and
+// 361 us, 2048 x 256 x 1024 43 and 49, 32768 x 512 x 2048 430 and 428 (and 268 MB less), 32768 x 768 x 2048 569 and 523.
+// A float32 product costs eight times as much: 16384 x 64 x 1024 159 and 155, 16384 x 256 x 1024 338 and 282.
+bool computes_pre(res_dtype_t dt, int act, int64_t K) { return act != RES_ACT_NONE && dt == RES_BF16 && K <= 512; }
 
 // The workspace, a piece at a time; with a null base it only counts.
 struct Pieces {
