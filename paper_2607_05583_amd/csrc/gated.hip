@@ -106,7 +106,9 @@ __device__ __forceinline__ int row_len(const int* lengths, int64_t b, int64_t L)
 // ---------------------------------------------------------------------------
 // Tiles in order, and the look-back
 // ---------------------------------------------------------------------------
-constexpr int WINDOW = 8;       // tiles looked back over at a time
+// Tiles looked back over at a time.  More carry a state over long chains in fewer looks, fewer poll less: forward and backward
+// of 1 x 32768 x 64 bf16 95 us with 8, 133 with 4; of 8 x 8192 x 256 123 with 8, 122 with 4, 139 with 16.
+constexpr int WINDOW = 8;
 constexpr int NONE = -2, END = -1;  // kinds of a published map, in the place of its A (which is never negative)
 
 __device__ __forceinline__ uint64_t word(float v, uint32_t tag) { return (uint64_t)tag << 32 | __float_as_uint(v); }

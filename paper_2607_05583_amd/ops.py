@@ -1054,7 +1054,8 @@ def _gated_lengths(lengths, B):
 
 
 def gated_scan_workspace(act_dtype, B, L, D, device):
-    """A zero-filled workspace of the gated scan for sizes up to (B, L, D), reusable across its calls on one stream."""
+    """A zero-filled workspace of the gated scan for sizes up to (B, L, D), reusable across its calls on one stream;
+    resonator_fwd_status reads whether a wait in one of them gave up."""
     n = _lib.lib().resonator_gated_scan_workspace_bytes(_DT[act_dtype], B, L, D)
     return torch.zeros(max(int(n), 256), dtype=torch.uint8, device=device)
 
