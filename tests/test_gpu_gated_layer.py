@@ -197,3 +197,14 @@ def test_model_learns(dtype, bits):
     assert losses[0] > 2.5 and max(losses[-10:]) < 0.5, (losses[0], losses[-10:])
     t = E.sequences(16, 64, 32, 4, torch.Generator().manual_seed(2))
     assert (E.generate(m, t[:, :32], 32) == t[:, 32:]).float().mean().item() > 0.8
+
+
+def test_workspace_status():
+    """Calls that share a workspace leave its status word at zero."""
+    q = problem("bf16", 2, 900, 64, 128, 1)
+    say("status")
+    ws = ops.gated_scan_workspace(torch.bfloat16, 2, 900, 64, "cuda")
+    for _ in range(3):
+        out, saved = ops.resonator_gated_layer_fwd(q["x"], q["p"], save=True, ws=ws)
+        ops.resonator_gated_layer_bwd(q["x"], q["p"], q["dout"], saved, ws=ws)
+    assert ops.resonator_fwd_status(ws) == 0 and torch.isfinite(out).all()
