@@ -366,11 +366,13 @@ hipError_t linear_bwd(const LinearCall& c, const float* bias, const void* dy, co
   if (e != hipSuccess) return e;
   int64_t blocks = 0;
   float* part = nullptr;
+  bool ready = false;
   if (c.act != RES_ACT_NONE || db != nullptr) {
     // (room for the most rows of sums: which tile is taken depends on the alignments too)
     blocks = again ? linear_col_blocks(TILE_SMALL, c.R) : linear_row_blocks(c.R);
     if (db != nullptr) part = static_cast<float*>(ws.take((size_t)(blocks * c.N) * 4));
-    void* out = c.act != RES_ACT_NONE ? ws.take((size_t)(c.R * c.N) * es) : nullptr;
+    const int64_t to = up(c.N, 16 / (int64_t)es);
+    void* out = c.act != RES_ACT_NONE ? ws.take((size_t)(c.R * to) * es) : nullptr;
     if (again) {
       GemmArgs g{};
       g.M = c.R;
@@ -385,13 +387,17 @@ hipError_t linear_bwd(const LinearCall& c, const float* bias, const void* dy, co
       blocks = linear_col_blocks(g.tile, c.R);
     } else if (!count && c.R > 0) {
       const bool loose = c.N % 4 != 0 || !(aligned(dy, 16) && aligned(pre, 16));
-      e = c.dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, pre, c.act, out, part, c.R, c.N, loose, st)
-                           : launch_act_bwd<float>(dy, pre, c.act, out, part, c.R, c.N, loose, st);
+      e = c.dt == RES_BF16 ? launch_act_bwd<bf16_t>(dy, pre, c.act, out, to, part, c.R, c.N, loose, st)
+                           : launch_act_bwd<float>(dy, pre, c.act, out, to, part, c.R, c.N, loose, st);
     }
     if (e == hipSuccess && !count && db != nullptr) e = launch_col_sum(part, blocks, c.N, db, st);
     if (out != nullptr || count) d.p = out;
+    if (out != nullptr || (count && c.act != RES_ACT_NONE)) {
+      if (!again) d.ld = d.cols = to;  // (with zeros from column N on)
+      ready = !again;
+    }
   }
-  if (e == hipSuccess && (dx != nullptr || dW != nullptr)) e = pack(&d, c.dt, c.loose, &ws, count, st);
+  if (e == hipSuccess && !ready && (dx != nullptr || dW != nullptr)) e = pack(&d, c.dt, c.loose, &ws, count, st);
   if (e == hipSuccess && dx != nullptr && c.R > 0) {
     GemmArgs g{};
     g.M = c.R;

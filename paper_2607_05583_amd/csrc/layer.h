@@ -135,12 +135,12 @@ template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);
 template <typename T>
 hipError_t launch_pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t to, hipStream_t st);
-// out (or none) = dy act'(pre) (pre null: dy) and, where part is not null, the sums of its columns over blocks of rows
-// [linear_row_blocks(R)][N]
+// out [R][to] (or none) = dy act'(pre) (pre null: dy), zero from column N on, and, where part is not null, the sums of its
+// columns over blocks of rows [linear_row_blocks(R)][N]
 int64_t linear_row_blocks(int64_t R);
 template <typename T>
-hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, int64_t R, int64_t N, bool loose,
-                          hipStream_t st);
+hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, int64_t to, float* part, int64_t R, int64_t N,
+                          bool loose, hipStream_t st);
 hipError_t launch_col_sum(const float* part, int64_t blocks, int64_t N, float* db, hipStream_t st);
 
 // ---------------------------------------------------------------------------

@@ -606,41 +606,45 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* src, int64_t ld, int
 }
 
 // dpre from a kept pre, and the sums of its columns over ACT_ROWS rows: a work-group takes 256 columns (four a lane, or
-// one where V is 1), its four waves every fourth row.
+// one where V is 1), its four waves every fourth row.  The rows of out are `to` elements apart, with zeros from column N on,
+// so that it is an operand as it is (2331 x 777 float32: 14 us and a copy of 4 to 8 us).
 constexpr int ACT_ROWS = 64;
 template <typename T, int V>
-__global__ __launch_bounds__(256) void act_bwd_kernel(const T* dy, const float* pre, int act, T* out, float* part, int64_t R,
-                                                      int64_t N) {
+__global__ __launch_bounds__(256) void act_bwd_kernel(const T* dy, const float* pre, int act, T* out, int64_t to, float* part,
+                                                      int64_t R, int64_t N) {
+  constexpr int AT = 8 / V > 2 ? 8 : 4;  // rows loaded at a time
   __shared__ float sums[4][64 * V];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t cols = (N + 64 * V - 1) / (64 * V), block = blockIdx.x / cols;
-  const int64_t n = (blockIdx.x % cols) * (64 * V) + lane * V, r0 = block * ACT_ROWS;
+  const int64_t cols = (to + 64 * V - 1) / (64 * V), block = blockIdx.x / cols;
+  const int64_t n = (blockIdx.x % cols) * (64 * V) + lane * V, r0 = block * ACT_ROWS + wave;
   float sum[V] = {};
-  if (n < N) {
-#pragma unroll 4
-    for (int k = 0; k < ACT_ROWS / 4; ++k) {
-      const int64_t r = r0 + k * 4 + wave, at = r * N + n;
-      if (r >= R) break;
-      float d[V], p[V];
-      if constexpr (V == 4) {
-        const f4 q = wide(load_quad(dy + r * N, (int)n, N, false));
-        const f4 z = pre != nullptr ? *reinterpret_cast<const f4*>(pre + at) : f4{};
+  for (int k = 0; k < ACT_ROWS / 4 && n < to; k += AT) {
+    f4 d[AT], p[AT];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) d[e] = q[e], p[e] = z[e];
+    for (int i = 0; i < AT; ++i) {  // (rows and columns past the end: the last ones again, not used)
+      const int64_t r = r0 + (k + i) * 4, row = (r < R ? r : R - 1) * N, c = n < N ? n : N - V;
+      if constexpr (V == 4) {
+        d[i] = wide(load_quad(dy + row, (int)c, N, false));
+        if (pre != nullptr) p[i] = *reinterpret_cast<const f4*>(pre + row + c);
       } else {
-        d[0] = to_f32(dy[at]);
-        p[0] = pre != nullptr ? pre[at] : 0.0f;
+        d[i][0] = to_f32(dy[row + c]);
+        if (pre != nullptr) p[i][0] = pre[row + c];
       }
+    }
+#pragma unroll
+    for (int i = 0; i < AT; ++i) {
+      const int64_t r = r0 + (k + i) * 4;
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        if (pre != nullptr) d[e] *= act_slope(p[e], act);
-        sum[e] += d[e];
+        if (pre != nullptr) d[i][e] *= act_slope(p[i][e], act);
+        d[i][e] = r < R && n < N ? d[i][e] : 0.0f;
+        sum[e] += d[i][e];
       }
-      if (out != nullptr) {
+      if (out != nullptr && r < R) {
         if constexpr (V == 4)
-          *reinterpret_cast<Quad<T>*>(out + at) = round_quad(f4{d[0], d[1], d[2], d[3]}, T());
+          *reinterpret_cast<Quad<T>*>(out + r * to + n) = round_quad(d[i], T());
         else
-          out[at] = from_f32<T>(d[0]);
+          out[r * to + n] = from_f32<T>(d[i][0]);
       }
     }
   }
@@ -777,13 +781,13 @@ hipError_t launch_pack(const void* src, int64_t ld, int64_t rows, int64_t cols, 
 }
 
 template <typename T>
-hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, float* part, int64_t R, int64_t N, bool loose,
-                          hipStream_t st) {
+hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, int64_t to, float* part, int64_t R, int64_t N,
+                          bool loose, hipStream_t st) {
   const int64_t blocks = linear_row_blocks(R);
   if (!loose && N % 4 == 0)
-    act_bwd_kernel<T, 4><<<dim3((unsigned)((N + 255) / 256 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, part, R, N);
+    act_bwd_kernel<T, 4><<<dim3((unsigned)((to + 255) / 256 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, to, part, R, N);
   else
-    act_bwd_kernel<T, 1><<<dim3((unsigned)((N + 63) / 64 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, part, R, N);
+    act_bwd_kernel<T, 1><<<dim3((unsigned)((to + 63) / 64 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, to, part, R, N);
   return hipGetLastError();
 }
 
@@ -795,7 +799,7 @@ hipError_t launch_col_sum(const float* part, int64_t blocks, int64_t N, float* d
 #define RES_LINEAR(T)                                                                                                 \
   template hipError_t launch_gemm<T>(const GemmArgs&, hipStream_t);                                                   \
   template hipError_t launch_pack<T>(const void*, int64_t, int64_t, int64_t, void*, int64_t, hipStream_t);            \
-  template hipError_t launch_act_bwd<T>(const void*, const float*, int, void*, float*, int64_t, int64_t, bool, hipStream_t);
+  template hipError_t launch_act_bwd<T>(const void*, const float*, int, void*, int64_t, float*, int64_t, int64_t, bool, hipStream_t);
 RES_LINEAR(float)
 RES_LINEAR(bf16_t)
 
