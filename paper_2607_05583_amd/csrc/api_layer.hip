@@ -314,12 +314,12 @@ hipError_t gemm(res_dtype_t dt, GemmArgs& g, const Operand& A, const Operand& B,
   g.loose = g.N % ep != 0 || !(aligned(g.out, 16) && aligned(g.res, 16) && aligned(g.bias, 16) && aligned(g.pre, 16) && aligned(g.dy, 16));
   if (need != nullptr) {  // (the outputs' alignment is not known yet)
     for (bool wide : {false, true}) {
-      const int64_t s = linear_plan(g.M, g.N, g.K, es, ak, g.dy != nullptr, wide).splits;
+      const int64_t s = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, wide).splits;
       *need = std::max(*need, ws.off + (s > 1 ? up256((size_t)(s * g.M * g.N) * 4) : 0));
     }
     return hipSuccess;
   }
-  const LinearPlan p = linear_plan(g.M, g.N, g.K, es, ak, g.dy != nullptr, !g.loose);
+  const LinearPlan p = linear_plan(g.M, g.N, g.K, es, g.dy != nullptr, !g.loose);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = static_cast<float*>(ws.take(p.splits > 1 ? (size_t)(p.splits * g.M * g.N) * 4 : 0));

@@ -128,8 +128,8 @@ struct GemmArgs {
 struct LinearPlan {
   int tile, splits;
 };
-// ak: A's K axis is consecutive; whole: the K axis is not cut and dy is taken; wide: the widest tile, which takes neither dy nor `loose`, may be taken
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool ak, bool whole, bool wide);
+// whole: the K axis is not cut and dy is taken; wide: the widest tile, which takes neither dy nor `loose`, may be taken
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide);
 int64_t linear_col_blocks(int tile, int64_t M);  // rows of colpart: one for each wave's rows
 template <typename T>
 hipError_t launch_gemm(const GemmArgs& a, hipStream_t st);

@@ -480,7 +480,7 @@ __global__ __launch_bounds__(64 * (BM / WM) * (BN / WN), (BM / WM) * (BN / WN) /
 // One launch instead of a split product's two and its partial sums in memory: 64 x 1024 x 4096 (R x K x N) bf16 8.4 us in a
 // graph, where the 8 MB of the weights are 1.8 us of memory and the rest is the latency of a launch and of two to four
 // loads one behind the other.
-template <typename T, bool BK>
+template <typename T, bool AK, bool BK>
 __global__ __launch_bounds__(512, 2) void gemm_deep_kernel(GemmArgs g) {
   constexpr int NW = 8, NB = 2, KB = Gemm<T>::KB, STEP = 128 * 64;
   __shared__ __align__(1024) char lds[NW * NB * STEP];
@@ -489,7 +489,7 @@ __global__ __launch_bounds__(512, 2) void gemm_deep_kernel(GemmArgs g) {
   const uint32_t nt = (uint32_t)((g.N + 63) / 64);
   const int64_t m0 = (int64_t)(blockIdx.x / nt) * 64, n0 = (int64_t)(blockIdx.x % nt) * 64;
   char* mine = lds + wave * (NB * STEP);
-  typedef TileLoad<T, 64, 1, true> LoadA;
+  typedef TileLoad<T, 64, 1, AK> LoadA;
   typedef TileLoad<T, 64, 1, BK> LoadB;
   const int steps = (int)((g.K + KB - 1) / KB), last = (int)(g.K - (int64_t)(steps - 1) * KB);
   const int begin = wave * steps / NW, end = (wave + 1) * steps / NW;
@@ -523,7 +523,7 @@ __global__ __launch_bounds__(512, 2) void gemm_deep_kernel(GemmArgs g) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) fb[j] = fragment<T, 64, BK>(lb, j * 16, li, lq);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) fa[i] = fragment<T, 64, true>(la, i * 16, li, lq);
+    for (int i = 0; i < 4; ++i) fa[i] = fragment<T, 64, AK>(la, i * 16, li, lq);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // read, before the buffer is loaded again
     prefetch();
 #pragma unroll
@@ -722,11 +722,11 @@ int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 // runs: as many as fill it, a part having at least 256 terms (128 with the small tile).
 // The widest tile reads least (24 KB for 512 matrix cycles of a unit's SIMD; 128 x 128 needs 16 KB for 256, as much as a
 // unit gets from the cache), but takes many outputs: the others are for products that would leave units idle.
-// A small product whose K axis would be cut is summed in one work-group a tile instead where the axis is short: bf16 64 x
-// 256 x 1024 5.1 for 7.5 us, 64 x 1024 x 4096 8.4 for 14.1, 64 x 2048 x 2048 12.5 for 15.8, but 64 x 4096 x 1024 20.4 for
-// 19.2; float32, whose products take eight times the matrix cycles, 64 x 256 x 1024 9.1 for 9.8, but 16 x 512 x 2048 12.4
-// for 10.6.
-LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool ak, bool whole, bool wide) {
+// A small product whose K axis would be cut is summed in one work-group a tile instead where the axis is short: bf16 (M x K x
+// N) 64 x 256 x 1024 5.1 for 7.5 us, 64 x 1024 x 4096 8.4 for 14.1, 64 x 2048 x 2048 12.5 for 15.8, the weight gradient 256 x
+// 2048 x 1024 8.4 for 12.9, but 64 x 4096 x 1024 20.4 for 19.2; float32, whose products take eight times the matrix cycles,
+// 64 x 256 x 1024 9.1 for 9.8, but 16 x 512 x 2048 12.4 for 10.6.
+LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, bool wide) {
   LinearPlan p{};
   auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   auto parts = [&](int64_t least) { return whole || K < 2 * least ? 1 : K / least < 64 ? K / least : 64; };
@@ -749,7 +749,7 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool ak, bool
   s = s < 1 ? 1 : s > most ? most : s;
   const int64_t kb = 64 / es, per = ((K + s - 1) / s + kb - 1) / kb * kb;  // whole steps, and no part without any
   p.splits = K > 0 ? (int)((K + per - 1) / per) : 0;
-  if (p.tile == TILE_SMALL && ak && p.splits > 1 && K * (int64_t)es <= (es == 2 ? 4096 : 1024)) {
+  if (p.tile == TILE_SMALL && p.splits > 1 && K * (int64_t)es <= (es == 2 ? 4096 : 1024)) {
     p.tile = TILE_DEEP;
     p.splits = 1;
   }
@@ -767,8 +767,9 @@ hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
       if constexpr (sizeof(T) == 2) launch_tiles<T, 128, 256, 128, 64, 3, false>(a, st);
     } else if (a.tile == TILE_DEEP) {
       const dim3 grid((unsigned)(((a.M + 63) / 64) * ((a.N + 63) / 64)));
-      if (a.bk) gemm_deep_kernel<T, true><<<grid, 512, 0, st>>>(a);
-      else gemm_deep_kernel<T, false><<<grid, 512, 0, st>>>(a);
+      if (!a.ak) gemm_deep_kernel<T, false, false><<<grid, 512, 0, st>>>(a);
+      else if (a.bk) gemm_deep_kernel<T, true, true><<<grid, 512, 0, st>>>(a);
+      else gemm_deep_kernel<T, true, false><<<grid, 512, 0, st>>>(a);
     } else if (a.tile == TILE_SQUARE) {
       launch_tiles<T, 128, 128, 64, 32, 4, true>(a, st);
     } else {
