@@ -22,10 +22,13 @@ __device__ __forceinline__ Quad<bf16_t> round_quad(const f4& c, bf16_t) {
   typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(Quad<bf16_t>, __builtin_convertvector(c, bf4));
 }
+// N elements at the alignment of one: the unit takes vector accesses at any address.
+template <typename T, int N> using Any = T __attribute__((ext_vector_type(N), aligned(sizeof(T))));
 // Columns n .. n + 3 of a row of N; loose: no alignment, and columns from N on are the last one again.
 template <typename T>
 __device__ __forceinline__ Quad<T> load_quad(const T* row, int n, int64_t N, bool loose) {
   if (!loose) return *reinterpret_cast<const Quad<T>*>(row + n);
+  if (n + 4 <= N) return __builtin_bit_cast(Quad<T>, *reinterpret_cast<const Any<T, 4>*>(row + n));
   Quad<T> q;
 #pragma unroll
   for (int r = 0; r < 4; ++r) q.v[r] = row[n + r < N ? n + r : N - 1];
@@ -192,7 +195,8 @@ template <typename T, int WM, int WN> struct SideLoad {
 // that they are stored as whole rows of 128 (bf16) or 256 bytes: the results' own layout gives 32-byte pieces.  The
 // stores are non-temporal (131072 x 256 x 1024 bf16: 139 to 123 us).  Rows and columns past the end are computed from the
 // last ones' operands and not stored.
-// ANY: takes outputs of any alignment (g.loose).  SLOPE: the results are pre, and what is stored is dy act'(pre); its
+// ANY: takes outputs of any alignment (g.loose): whole pieces all the same, the last of a row by elements (11573 x 32 x 1964
+// bf16, gelu, with gradients: 201 to 147 us).  SLOPE: the results are pre, and what is stored is dy act'(pre); its
 // columns' sums go to g.colpart.  stage(s): this wave's step s of the side input in the LDS, null where it is not there.
 template <typename T, int ACT, bool SLOPE, bool ANY, int WM, int WN, typename Stage>
 __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t n0, const f4 (&acc)[WM / 16][WN / 16],
@@ -251,8 +255,8 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
 #pragma unroll
         for (int j = 0; j < FN; ++j)
           if ((int)n0 + j * 16 + lq * 4 < (int)g.N) {
-            if (!loose) {
-              *reinterpret_cast<f4*>(pre + n[j]) = c[j];
+            if (!loose || n[j] + 4 <= (int)g.N) {
+              *reinterpret_cast<Any<float, 4>*>(pre + n[j]) = c[j];
             } else {
 #pragma unroll
               for (int r = 0; r < 4; ++r)
@@ -277,21 +281,25 @@ __device__ __forceinline__ void tile_out(const GemmArgs& g, int64_t m0, int64_t 
       *reinterpret_cast<Quad<T>*>(mine + li * RB + (((byte >> 4) ^ (li & SW)) << 4) + (byte & 15)) = round_quad(c[j], T());
     }
     typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    if (!loose) {
+    typedef uint32_t u4_any __attribute__((ext_vector_type(4), aligned(2)));
 #pragma unroll
-      for (int u = 0; u < 16 / RS; ++u) {
-        const int r = u * RS + lane / PR, slot = lane % PR, col = (slot ^ (r & SW)) * EP;
-        const u4 v = *reinterpret_cast<const u4*>(mine + r * RB + slot * 16);
-        if (i * 16 + r < rows && (int)n0 + col < (int)g.N) __builtin_nontemporal_store(v, reinterpret_cast<u4*>(to + col));
-        to += next;
+    for (int u = 0; u < 16 / RS; ++u) {
+      const int r = u * RS + lane / PR, slot = lane % PR, col = (slot ^ (r & SW)) * EP;
+      const u4 v = *reinterpret_cast<const u4*>(mine + r * RB + slot * 16);
+      const int there = (int)(g.N - n0) - col;  // columns of the piece that there are, or more
+      if (i * 16 + r < rows && there > 0) {
+        if (!loose) {
+          __builtin_nontemporal_store(v, reinterpret_cast<u4*>(to + col));
+        } else if (there >= EP) {
+          __builtin_nontemporal_store((u4_any)v, reinterpret_cast<u4_any*>(to + col));
+        } else {
+          const Any<T, EP> e = __builtin_bit_cast(Any<T, EP>, v);
+#pragma unroll
+          for (int k = 0; k < EP - 1; ++k)
+            if (k < there) to[col + k] = e[k];
+        }
       }
-    } else {
-      for (int e = lane; e < 16 * WN; e += 64) {
-        const int r = e / WN, byte = e % WN * ES;
-        const int64_t mo = m0 + i * 16 + r, col = n0 + e % WN;
-        const T v = *reinterpret_cast<const T*>(mine + r * RB + (((byte >> 4) ^ (r & SW)) << 4) + (byte & 15));
-        if (mo < g.M && col < g.N) ((T*)g.out)[mo * g.N + col] = v;
-      }
+      to += next;
     }
   }
   if constexpr (SLOPE) {
@@ -611,10 +619,15 @@ __global__ __launch_bounds__(256) void pack_kernel(const T* src, int64_t ld, int
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = to / EP;
   if (id >= rows * per) return;
   const int64_t row = id / per, c = (id - row * per) * EP;
-  struct __align__(16) Piece { T v[EP]; } o;
+  const T* from = src + row * ld + c;
+  T __attribute__((ext_vector_type(EP))) o;
+  if (c + EP <= cols) {
+    o = *reinterpret_cast<const Any<T, EP>*>(from);
+  } else {
 #pragma unroll
-  for (int e = 0; e < EP; ++e) o.v[e] = c + e < cols ? src[row * ld + c + e] : T(0);
-  *reinterpret_cast<Piece*>(dst + row * to + c) = o;
+    for (int e = 0; e < EP; ++e) o[e] = c + e < cols ? from[e] : T(0);
+  }
+  *reinterpret_cast<decltype(o)*>(dst + row * to + c) = o;
 }
 
 // dpre from a kept pre, and the sums of its columns over ACT_ROWS rows: a work-group takes 256 columns (four a lane, or
@@ -722,6 +735,9 @@ int64_t linear_row_blocks(int64_t R) { return (R + ACT_ROWS - 1) / ACT_ROWS; }
 // runs: as many as fill it, a part having at least 256 terms (128 with the small tile).
 // The widest tile reads least (24 KB for 512 matrix cycles of a unit's SIMD; 128 x 128 needs 16 KB for 256, as much as a
 // unit gets from the cache), but takes many outputs: the others are for products that would leave units idle.
+// Nor is one taken whose edges hold more than a third of outputs that there are not, against the next smaller one's (a
+// training step of 25024 x 1792 x 55 float32 234 us with the small tile, 333 with 128 x 128; 30000 x 512 x 128 bf16 74 with
+// 128 x 128, 83 with 128 x 256).
 // A small product whose K axis would be cut is summed in one work-group a tile instead where the axis is short: bf16 (M x K x
 // N) 64 x 256 x 1024 5.1 for 7.5 us, 64 x 1024 x 4096 8.4 for 14.1, 64 x 2048 x 2048 12.5 for 15.8, the weight gradient 256 x
 // 2048 x 1024 8.4 for 12.9, but 64 x 4096 x 1024 20.4 for 19.2; float32, whose products take eight times the matrix cycles,
@@ -731,11 +747,11 @@ LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, size_t es, bool whole, b
   auto tiles = [&](int64_t bm, int64_t bn) { return ((M + bm - 1) / bm) * ((N + bn - 1) / bn); };
   auto parts = [&](int64_t least) { return whole || K < 2 * least ? 1 : K / least < 64 ? K / least : 64; };
   int64_t t, want, most = parts(256);
-  if (es == 2 && wide && !whole && M > 64 && tiles(128, 256) * most >= 256) {
+  if (es == 2 && wide && !whole && M > 64 && tiles(128, 256) * most >= 256 && 3 * tiles(128, 256) <= 2 * tiles(128, 128)) {
     p.tile = TILE_WIDE;
     t = tiles(128, 256);
     want = 256;
-  } else if (M > 64 && tiles(128, 128) * most >= 256) {
+  } else if (M > 64 && tiles(128, 128) * most >= 256 && 3 * tiles(128, 128) <= tiles(64, 64)) {
     p.tile = TILE_SQUARE;
     t = tiles(128, 128);
     want = 256;
