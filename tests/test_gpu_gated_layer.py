@@ -208,3 +208,15 @@ def test_workspace_status():
         out, saved = ops.resonator_gated_layer_fwd(q["x"], q["p"], save=True, ws=ws)
         ops.resonator_gated_layer_bwd(q["x"], q["p"], q["dout"], saved, ws=ws)
     assert ops.resonator_fwd_status(ws) == 0 and torch.isfinite(out).all()
+
+
+def test_sequences_without_tokens():
+    """L = 0: the state passes through, and so does its gradient; the parameters' gradients are zero."""
+    q = problem("f32", 2, 1, 16, 32, 2)
+    x = q["x"][:, :0].contiguous()
+    say("no tokens")
+    out, h, saved = ops.resonator_gated_layer_fwd(x, q["p"], h0=q["h0"], return_state=True, save=True)
+    g = ops.resonator_gated_layer_bwd(x, q["p"], torch.empty_like(x), saved, dh=q["dh"], want_dh0=True)
+    assert out.shape == g["dx"].shape == x.shape
+    assert torch.equal(h, q["h0"]) and torch.equal(g["dh0"], q["dh"])
+    assert not any(v.any() for v in g["dp"])
