@@ -125,18 +125,17 @@ struct LookShared {
   int ticket, found;
 };
 
-// The value that enters tile `o` of a chain (in the order that they are taken; `words`: the chain's) into sh.enter, for
-// the 64 channels; `init`: what enters tile 0.  Called by the whole work-group.
-__device__ __forceinline__ void look_back(const uint64_t* words, int64_t o, uint32_t tag, float init, uint32_t* status,
-                                          LookShared& sh) {
+// The value that enters tile `o` > 0 of a chain (in the order that they are taken; `words`: the chain's) into sh.enter, for
+// the 64 channels.  Called by the whole work-group.
+// What enters tile 0 is read by tile 0 alone and reaches the others in its end value: the chain's last tile stores its own
+// end, which may go where the initial state came from (h_out = h0), and every tile waits for tile 0's end before it has one.
+__device__ __forceinline__ void look_back(const uint64_t* words, int64_t o, uint32_t tag, uint32_t* status, LookShared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = wave;  // this wave's tile, counted back
   for (int tries = 0;; ++tries) {
     if (g < WINDOW) {
       float2 m = make_float2(NONE, 0.0f);
-      if (g == o) {
-        m = make_float2(END, init);
-      } else if (g < o) {
+      if (g < o) {
         const uint64_t* w = words + (o - 1 - g) * GATED_TILE_WORDS + lane;
         const uint64_t e = load_word(w + 128), a = load_word(w), h = load_word(w + 64);
         if ((uint32_t)(e >> 32) == tag)
@@ -307,7 +306,7 @@ __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
   float ta = 1.0f, th = 0.0f;  // the tile's map (wave 0: a channel a lane)
   uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
   const int cw = cb + wl;
-  const float init = A.h0 != nullptr && cw < A.D ? A.h0[b * A.D + cw] : 0.0f;
+  const float init = o == 0 && wave == 0 && A.h0 != nullptr && cw < A.D ? A.h0[b * A.D + cw] : 0.0f;
   if (wave == 0) {
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
@@ -321,8 +320,8 @@ __global__ __launch_bounds__(NT, 4) void gated_fwd_kernel(GatedArgs A) {
       store_word(w + 64, th, tag);
     }
   }
-  if constexpr (LOOK) {
-    look_back(words, o, tag, init, A.hdr, sh);
+  if (LOOK && o > 0) {
+    look_back(words, o, tag, A.hdr, sh);
   } else {
     if (wave == 0) sh.enter[wl] = init;
     __syncthreads();
@@ -486,7 +485,7 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
   float ta = 1.0f, tc = 0.0f;
   uint64_t* words = A.words + (size_t)chain * tiles * GATED_TILE_WORDS;
   const int cw = cb + wl;
-  const float init = A.dh_out != nullptr && cw < A.D ? A.dh_out[b * A.D + cw] : 0.0f;
+  const float init = o == 0 && wave == 0 && A.dh_out != nullptr && cw < A.D ? A.dh_out[b * A.D + cw] : 0.0f;
   if (wave == 0) {
 #pragma unroll
     for (int w = NW - 1; w >= 0; --w) {
@@ -514,8 +513,8 @@ __global__ __launch_bounds__(NT, sizeof(T) == 2 ? 4 : 2) void gated_bwd_kernel(G
       hp[s][v] = before;
     }
   }
-  if constexpr (LOOK) {
-    look_back(words, o, tag, init, A.hdr, sh);
+  if (LOOK && o > 0) {
+    look_back(words, o, tag, A.hdr, sh);
   } else {
     if (wave == 0) sh.enter[wl] = init;
     __syncthreads();
