@@ -287,7 +287,7 @@ bool whole(const Operand& o, size_t es) {
 // The operand as the kernels take it, copied where it is not.
 hipError_t pack(Operand* o, res_dtype_t dt, bool loose, Pieces* ws, bool count, hipStream_t st) {
   const size_t es = elt(dt);
-  if (!loose || (!count && whole(*o, es))) return hipSuccess;
+  if (!loose || (!count && (o->rows == 0 || whole(*o, es)))) return hipSuccess;  // (no rows: nothing reads it)
   const int64_t to = up(o->cols, 16 / (int64_t)es);
   void* dst = ws->take((size_t)(o->rows * to) * es);
   if (count) return hipSuccess;
