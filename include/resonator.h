@@ -595,10 +595,11 @@ int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtyp
  * an order that depends on the sizes alone.  K, N >= 1, R >= 0.
  *   ws        resonator_linear_workspace_bytes(0, ...) bytes (may be none), 256-byte
  *             aligned; contents need not be initialised.  `loose` of the query: x, W or dy are
- *             not 16-byte aligned, or K, N or ldx are not multiples of 16 bytes; such operands
- *             are copied into the workspace first
+ *             not 16-byte aligned, K, N or ldx are not multiples of 16 bytes, or ldx is
+ *             RES_LINEAR_FAR or more; such operands are copied into the workspace first
  * Outputs must not overlap inputs or each other otherwise.
  */
+#define RES_LINEAR_FAR (1LL << 21)
 enum { RES_ACT_NONE = 0, RES_ACT_RELU = 1, RES_ACT_SILU = 2, RES_ACT_GELU_TANH = 3 };
 size_t resonator_linear_workspace_bytes(int backward, res_dtype_t dt, int act, int64_t R, int64_t K, int64_t N, int loose);
 int resonator_linear_keeps_pre(res_dtype_t dt, int act, int64_t K);

@@ -18,6 +18,7 @@ RES_OP_FWD, RES_OP_BWD, RES_OP_STATE_INIT = 0, 1, 2
 RES_M_MAX = 16
 RES_GATED_CARRY = 128
 RES_ADAMW_BLOCK = 256
+RES_LINEAR_FAR = 1 << 21
 
 SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd",
            "resonator_mix_bwd", "resonator_state_init", "resonator_decode_step",

@@ -282,7 +282,7 @@ struct Operand {
 };
 bool whole(const Operand& o, size_t es) {
   const int64_t ep = 16 / (int64_t)es;
-  return aligned(o.p, 16) && o.ld % ep == 0 && o.cols % ep == 0 && o.ld < (1 << 21);  // (32-bit offsets within a tile)
+  return aligned(o.p, 16) && o.ld % ep == 0 && o.cols % ep == 0 && o.ld < RES_LINEAR_FAR;  // (32-bit offsets within a tile)
 }
 // The operand as the kernels take it, copied where it is not.
 hipError_t pack(Operand* o, res_dtype_t dt, bool loose, Pieces* ws, bool count, hipStream_t st) {

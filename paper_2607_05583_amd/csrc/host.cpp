@@ -722,7 +722,7 @@ bool linear(PyObject* ox, PyObject* oW, Linear* l) {
   }
   l->dt = (res_dtype_t)code(x);
   const int64_t ep = 16 / x.element_size();
-  l->loose = l->K % ep || l->N % ep || l->ldx % ep || (uintptr_t)x.data_ptr() % 16 || (uintptr_t)l->W->data_ptr() % 16;
+  l->loose = l->K % ep || l->N % ep || l->ldx % ep || l->ldx >= RES_LINEAR_FAR || (uintptr_t)x.data_ptr() % 16 || (uintptr_t)l->W->data_ptr() % 16;
   return true;
 }
 bool linear_ws(PyObject* o, int backward, int act, const Linear& l, bool loose, Tensor* ws) {

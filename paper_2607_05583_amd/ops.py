@@ -1250,7 +1250,7 @@ def _linear_ws(ws, backward, act, x, ldx, W, dy=None):
         return ws, ws.numel() * ws.element_size()
     K, N = W.shape
     ep = 16 // x.element_size()
-    loose = bool(K % ep or N % ep or ldx % ep or x.data_ptr() % 16 or W.data_ptr() % 16
+    loose = bool(K % ep or N % ep or ldx % ep or ldx >= _lib.RES_LINEAR_FAR or x.data_ptr() % 16 or W.data_ptr() % 16
                  or (dy is not None and dy.data_ptr() % 16))
     n = int(_lib.lib().resonator_linear_workspace_bytes(backward, _code(x), act, x.numel() // K, K, N, loose))
     return (torch.empty(n, dtype=torch.uint8, device=x.device) if n else None), n
