@@ -1211,7 +1211,9 @@ def _rows2(x, name, K=None):
     if x.dim() < 1 or (K is not None and x.shape[-1] != K):
         raise ValueError(f"{name} must be [..., {K}] (got {list(x.shape)})")
     K = x.shape[-1]
-    R = x.numel() // K if K else 0
+    if K < 1:
+        raise ValueError(f"{name}'s rows must have at least one element")
+    R = x.numel() // K
     if x.is_contiguous() or R <= 1:
         if K > 1 and R == 1 and x.stride(-1) != 1:
             raise ValueError(f"{name}'s last dimension must be consecutive in memory")

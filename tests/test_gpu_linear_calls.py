@@ -1,5 +1,5 @@
 """Calls of the linear product that are plain for a user and rare for the library: no rows at all with sizes that are not whole
-16-byte pieces, and rows far apart in memory."""
+16-byte pieces, rows far apart in memory, and an empty sum."""
 import numpy as np
 import pytest
 import torch
@@ -72,3 +72,12 @@ def test_last_tokens_of_long_rows():
     say("last tokens")
     assert x[:, -1].stride(0) == 1 << 21
     assert torch.equal(ops.resonator_linear_fwd(x[:, -1], W), ops.resonator_linear_fwd(x[:, -1].contiguous(), W))
+
+
+def test_empty_sum_is_refused(path):
+    x, W = torch.empty(4, 0, device="cuda"), torch.empty(0, 8, device="cuda")
+    say(f"empty sum {path}")
+    with pytest.raises(ValueError):
+        ops.resonator_linear_fwd(x, W)
+    with pytest.raises(ValueError):
+        ops.resonator_linear_bwd(x, W, torch.empty(4, 8, device="cuda"))
