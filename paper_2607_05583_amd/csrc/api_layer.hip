@@ -65,7 +65,7 @@ int check_scan(int64_t B, int64_t L, int64_t D, res_dtype_t dt) {
     return api_error(RES_ERR_INVALID_ARG, "B and D must be >= 1 and L >= 0 (got B=%lld L=%lld D=%lld)", (long long)B,
                      (long long)L, (long long)D);
   const int64_t NB = (D + GATED_CW - 1) / GATED_CW;
-  // (tiles of a call and tickets are 32-bit counts)
+  // (tiles of a call are 32-bit counts)
   if (D > (1 << 21) || L >= (1LL << 31) - 65536 || B > (1LL << 31) || B * NB >= (1LL << 30) ||
       B * NB * (L / GATED_BWD_TILE + 1) >= (1LL << 31))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld D=%lld)", (long long)B,
@@ -75,6 +75,12 @@ int check_scan(int64_t B, int64_t L, int64_t D, res_dtype_t dt) {
 int check_f32(const char* name, const float* p, bool needed) {
   if (p == nullptr) return needed ? api_error(RES_ERR_INVALID_ARG, "%s must be non-null", name) : RES_OK;
   return aligned(p, 4) ? RES_OK : api_error(RES_ERR_MISALIGNED, "%s must be 4-byte aligned", name);
+}
+
+// A launch takes whole batch rows.
+int check_launch(int64_t L, int64_t D, int tile) {
+  if ((D + GATED_CW - 1) / GATED_CW * gated_tiles(L, tile) <= LAUNCH_THREADS / GATED_THREADS) return RES_OK;
+  return api_error(RES_ERR_UNSUPPORTED, "a row beyond one launch (L=%lld D=%lld)", (long long)L, (long long)D);
 }
 
 constexpr int GATED_VEC = 4;
@@ -98,7 +104,7 @@ int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype
                              int64_t D, const float* gamma, const float* h0, const int32_t* lengths, float* h_out,
                              float* carry, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_scan(B, L, D, dt);
-  if (rc) return rc;
+  if (rc || (rc = check_launch(L, D, GATED_FWD_TILE))) return rc;
   const size_t es = elt(dt);
   if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, es)) || (rc = check_rows("r", r.p, r.sb, r.st, es)) ||
                 (rc = check_rows("i", i.p, i.sb, i.st, es))))
@@ -152,7 +158,7 @@ int resonator_gated_scan_bwd(res_rows_t x, res_rows_t r, res_rows_t i, res_rows_
                              const float* gamma, const float* carry, const int32_t* lengths, const float* dh_out,
                              float* dgamma, float* dh0, void* ws, size_t ws_bytes, void* stream) {
   int rc = check_scan(B, L, D, dt);
-  if (rc) return rc;
+  if (rc || (rc = check_launch(L, D, GATED_BWD_TILE))) return rc;
   const size_t es = elt(dt);
   if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, es)) || (rc = check_rows("r", r.p, r.sb, r.st, es)) ||
                 (rc = check_rows("i", i.p, i.sb, i.st, es)) || (rc = check_rows("dy", dy.p, dy.sb, dy.st, es)) ||

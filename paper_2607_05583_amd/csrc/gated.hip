@@ -643,23 +643,52 @@ void gated_bwd(const GatedArgs& a, hipStream_t st) {
     gated_bwd_kernel<T, VEC, S, 512, true><<<dim3((unsigned)(a.B * a.NB * gated_tiles(a.L, 8 * STEPS))), 512, 0, st>>>(a);
 }
 
+// The batch rows from b on, n of them.
+template <typename T>
+GatedArgs batch_rows(GatedArgs a, int64_t b, int64_t n) {
+  const int64_t NC = (a.L + GATED_CARRY - 1) / GATED_CARRY;
+  auto on = [](auto*& p, int64_t k) { if (p != nullptr) p += k; };
+  for (Rows* v : {&a.x, &a.r, &a.i, &a.dy}) v->p = v->p != nullptr ? (const T*)v->p + b * v->sb : nullptr;
+  for (RowsOut* v : {&a.dx, &a.dr, &a.di}) v->p = v->p != nullptr ? (T*)v->p + b * v->sb : nullptr;
+  a.y = a.y != nullptr ? (T*)a.y + b * a.L * a.D : nullptr;
+  on(a.h0, b * a.D);
+  on(a.lengths, b);
+  on(a.h_out, b * a.D);
+  on(a.carry, b * NC * a.D);
+  on(a.dh_out, b * a.D);
+  on(a.dh0, b * a.D);
+  on(a.part, b * gated_tiles(a.L, GATED_BWD_TILE) * a.NB * GATED_CW);
+  a.B = n;
+  return a;
+}
+// Calls f with as many batch rows at a time as one launch takes.
+template <typename T, typename F>
+void in_launches(const GatedArgs& a, int tile, F&& f) {
+  const int64_t most = LAUNCH_THREADS / GATED_THREADS / (a.NB * gated_tiles(a.L, tile));
+  for (int64_t b = 0; b < a.B; b += most) f(batch_rows<T>(a, b, a.B - b < most ? a.B - b : most));
+}
+
 }  // namespace
 
 template <typename T>
-hipError_t launch_gated_fwd(const GatedArgs& a, hipStream_t st) {
-  if (a.vec)
-    gated_fwd<T, 4, 8>(a, st);
-  else
-    gated_fwd<T, 1, 32>(a, st);  // a channel a lane: rows of any alignment read in one piece
+hipError_t launch_gated_fwd(const GatedArgs& all, hipStream_t st) {
+  in_launches<T>(all, GATED_FWD_TILE, [&](const GatedArgs& a) {
+    if (a.vec)
+      gated_fwd<T, 4, 8>(a, st);
+    else
+      gated_fwd<T, 1, 32>(a, st);  // a channel a lane: rows of any alignment read in one piece
+  });
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st) {
-  if (a.vec)
-    gated_bwd<T, sizeof(T) == 2 ? 2 : 4, sizeof(T) == 2 ? 8 : 4>(a, st);
-  else
-    gated_bwd<T, 1, 16>(a, st);
+  in_launches<T>(a, GATED_BWD_TILE, [&](const GatedArgs& a) {
+    if (a.vec)
+      gated_bwd<T, sizeof(T) == 2 ? 2 : 4, sizeof(T) == 2 ? 8 : 4>(a, st);
+    else
+      gated_bwd<T, 1, 16>(a, st);
+  });
   const int64_t rows = a.B * gated_tiles(a.L, GATED_BWD_TILE);
   gated_reduce_kernel<<<dim3((unsigned)((a.D + 15) / 16)), 1024, 0, st>>>(a.part, rows, a.NB * GATED_CW, a.D, dgamma);
   return hipGetLastError();
@@ -668,7 +697,13 @@ hipError_t launch_gated_bwd(const GatedArgs& a, float* dgamma, hipStream_t st) {
 template <typename T>
 hipError_t launch_gated_step(const Rows& x, const Rows& r, const Rows& i, void* y, int64_t B, int64_t D,
                              const float* gamma, const float* h, float* h_out, hipStream_t st) {
-  gated_step_kernel<T><<<dim3((unsigned)((B * D + 255) / 256)), 256, 0, st>>>(x, r, i, (T*)y, B, D, gamma, h, h_out);
+  const int64_t most = (LAUNCH_THREADS - 255) / D;  // rows of a launch
+  for (int64_t b = 0; b < B; b += most) {
+    const int64_t n = B - b < most ? B - b : most;
+    auto rows = [&](const Rows& v) { return Rows{(const T*)v.p + b * v.sb, v.sb, v.st}; };
+    gated_step_kernel<T><<<dim3((unsigned)((n * D + 255) / 256)), 256, 0, st>>>(rows(x), rows(r), rows(i), (T*)y + b * D, n, D, gamma,
+                                                                                h + b * D, h_out + b * D);
+  }
   return hipGetLastError();
 }
 

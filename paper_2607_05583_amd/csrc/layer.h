@@ -21,6 +21,9 @@ struct RowsOut {
   int64_t sb, st;
 };
 
+// Threads of one launch: more are not refused, their last work-groups are left out without an error.
+constexpr int64_t LAUNCH_THREADS = (1LL << 32) - 1;
+
 // ---------------------------------------------------------------------------
 // Device mathematics shared by the operators
 // ---------------------------------------------------------------------------
@@ -67,6 +70,8 @@ constexpr int GATED_CW = 64;      // channels of a chain: 128-byte rows of bf16
 constexpr int GATED_CARRY = 128;  // steps between the states that a forward keeps for its backward
 constexpr int GATED_FWD_TILE = 256, GATED_BWD_TILE = 128;  // steps of a tile (of 512 threads)
 constexpr int GATED_TILE_WORDS = 3 * GATED_CW;             // words that a tile publishes
+
+constexpr int GATED_THREADS = 512;  // of a work-group, at most
 
 // tiles of a chain: one where there is no step, which hands the state through
 __host__ __device__ inline int64_t gated_tiles(int64_t L, int64_t tile) { return L > 0 ? (L + tile - 1) / tile : 1; }

@@ -1,0 +1,83 @@
+"""More work than one launch takes (2^32 threads): the scan's tiles and the token step's elements.  Each is compared, bit for
+bit, with small calls on the same rows, or on those around the place where a launch ends.
+
+The memory that a case needs is what the operator's own buffers take; a card that has not got it free skips the case.
+"""
+import gc
+
+import pytest
+import torch
+
+from gpu_util import say
+
+pytestmark = pytest.mark.gpu
+
+ops = None
+
+
+def setup_module(module):
+    global ops
+    from paper_2607_05583_amd import ops as _ops
+    ops = _ops
+
+
+@pytest.fixture
+def room():
+    """room(gigabytes): skips where the card has not got them free; what a case used is handed back after it."""
+    def ask(gb):
+        gc.collect()
+        torch.cuda.empty_cache()
+        free = torch.cuda.mem_get_info()[0] / 2 ** 30
+        if free < gb:
+            pytest.skip(f"{gb} GiB are needed, {free:.0f} are free")
+    yield ask
+    gc.collect()
+    torch.cuda.empty_cache()
+
+
+def normal(*shape, seed, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda", dtype=dtype)
+
+
+@pytest.mark.parametrize("B,L", [((1 << 23) + 5, 1), ((1 << 22) + 3, 300)])
+def test_scan_of_many_tiles(room, B, L):
+    """2^23 chains of one step (one work-group of 512 threads each in the backward), 2^22 of two and three tiles."""
+    room(70)
+    say(f"scan of many tiles {B} {L}")
+    x, r, i, dy = (normal(B, L, 1, seed=k) for k in range(4))
+    gamma, h0, dh = torch.full((1,), 0.5, device="cuda"), normal(B, 1, seed=5, dtype=torch.float32), normal(B, 1, seed=6, dtype=torch.float32)
+    lengths = torch.randint(0, L + 1, (B,), device="cuda", dtype=torch.int32)
+    y, h, carry = ops.resonator_gated_scan_fwd(x, r, i, gamma, h0=h0, lengths=lengths, return_state=True, save=True)
+    g = ops.resonator_gated_scan_bwd(x, r, i, gamma, dy, lengths=lengths, dh_out=dh, carry=carry, want_dh0=True)
+    dgamma, off = 0.0, 0.0
+    parts = 4
+    cut = [B * k // parts for k in range(parts + 1)]
+    for lo, hi in zip(cut, cut[1:]):  # (every row: each quarter is one launch)
+        s = slice(lo, hi)
+        a = [v[s] for v in (x, r, i)]
+        y2, h2, c2 = ops.resonator_gated_scan_fwd(*a, gamma, h0=h0[s], lengths=lengths[s], return_state=True, save=True)
+        assert torch.equal(y[s], y2) and torch.equal(h[s], h2) and torch.equal(carry[s], c2)
+        g2 = ops.resonator_gated_scan_bwd(*a, gamma, dy[s], lengths=lengths[s], dh_out=dh[s], carry=c2, want_dh0=True)
+        for k in ("dx", "dr", "di", "dh0"):
+            assert torch.equal(g[k][s], g2[k]), k
+        dgamma += g2["dgamma"].double()
+        # (the same float32 sums of tiles added in float64: what is left is each result's rounding, 2^-24 of its size)
+        off += 2.0 ** -24 * g2["dgamma"].abs().item()
+    assert (g["dgamma"].double() - dgamma).abs().item() <= off + 2.0 ** -24 * dgamma.abs().item()
+
+
+def test_token_step_of_many_elements(room):
+    B, D = (1 << 21) + 3, 2048
+    room(90)
+    say(f"token step of many elements {B} {D}")
+    x, r, i = (normal(B, D, seed=k) for k in range(3))
+    gamma, h = torch.linspace(0.1, 1.0, D, device="cuda"), normal(B, D, seed=3, dtype=torch.float32)
+    for s in (slice(0, 7), slice((1 << 21) - 5, B)):
+        old = h[s].clone()
+        want = ops.resonator_gated_scan_step(x[s], r[s], i[s], gamma, old)
+        if s.start == 0:
+            first = want, old
+    y = ops.resonator_gated_scan_step(x, r, i, gamma, h)
+    assert torch.equal(y[:7], first[0]) and torch.equal(h[:7], first[1])
+    assert torch.equal(y[s], want) and torch.equal(h[s], old)
