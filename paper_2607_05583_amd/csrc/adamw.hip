@@ -19,6 +19,7 @@ namespace {
 constexpr int TABLE = 64;      // tensors of one launch (their table is a kernel argument)
 constexpr int CHUNK_BLOCKS = 4;  // blocks of a work-group: one a wave (two: 1032 for 994 us with float32 copies)
 constexpr int64_t CHUNK_ELEMS = (int64_t)CHUNK_BLOCKS * RES_ADAMW_BLOCK;
+constexpr int64_t LAUNCH_CHUNKS = LAUNCH_THREADS / 256;
 constexpr float TINY = 1e-30f;  // a smaller scale counts as zero (its reciprocal would leave float32)
 
 struct Table {
@@ -226,7 +227,7 @@ hipError_t launch_tables(const AdamWArgs& a, const res_adamw_tensor_t* t, int64_
   for (int64_t k = 0; k < count; ++k) {
     // a tensor of more chunks than a launch counts is taken in pieces
     for (int64_t at = 0; at < t[k].n;) {
-      const int64_t most = ((1LL << 30) - (int64_t)chunks) * CHUNK_ELEMS;
+      const int64_t most = (LAUNCH_CHUNKS - (int64_t)chunks) * CHUNK_ELEMS;
       const int64_t n = t[k].n - at < most ? t[k].n - at : most;
       const int c = tab.count++;
       tab.p[c] = (const TP*)t[k].p + at;
@@ -237,7 +238,7 @@ hipError_t launch_tables(const AdamWArgs& a, const res_adamw_tensor_t* t, int64_
       chunks += (n + CHUNK_ELEMS - 1) / CHUNK_ELEMS;
       tab.end[c] = (uint32_t)chunks;
       at += n;
-      if (tab.count == TABLE || chunks >= (1ULL << 30)) flush();
+      if (tab.count == TABLE || chunks >= (uint64_t)LAUNCH_CHUNKS) flush();
     }
   }
   flush();
@@ -264,7 +265,7 @@ hipError_t launch_adamw(const AdamWArgs& a, const res_adamw_tensor_t* tensors, i
 
 hipError_t launch_adamw_values(const void* m, const void* v, const float* sm, const float* sv, int64_t n, float* mo,
                                float* vo, hipStream_t st) {
-  const int64_t per = 1LL << 40;  // (n / 1024 work-groups)
+  const int64_t per = LAUNCH_CHUNKS * 1024;  // elements of a launch, four a thread
   for (int64_t at = 0; at < n; at += per) {
     const int64_t c = n - at < per ? n - at : per;
     adamw_values_kernel<<<dim3((unsigned)((c + 1023) / 1024)), 256, 0, st>>>(

@@ -1,5 +1,6 @@
-"""More work than one launch takes (2^32 threads): the scan's tiles and the token step's elements.  Each is compared, bit for
-bit, with small calls on the same rows, or on those around the place where a launch ends.
+"""More work than one launch takes (2^32 threads): the scan's tiles, the token step's elements, AdamW's chunks and the values of
+its codes.  Each is compared, bit for bit, with small calls on the same rows or elements, or on those around the place where a
+launch ends.
 
 The memory that a case needs is what the operator's own buffers take; a card that has not got it free skips the case.
 """
@@ -81,3 +82,27 @@ def test_token_step_of_many_elements(room):
     y = ops.resonator_gated_scan_step(x, r, i, gamma, h)
     assert torch.equal(y[:7], first[0]) and torch.equal(h[:7], first[1])
     assert torch.equal(y[s], want) and torch.equal(h[s], old)
+
+
+def test_adamw_of_many_elements(room):
+    """2^34 elements are 2^24 chunks: around that place, the step and the values of its codes are a small tensor's."""
+    n = (1 << 34) + 256 * 7 + 11
+    room(185)
+    say(f"adamw of many elements {n}")
+    p, g = torch.zeros(n, dtype=torch.bfloat16, device="cuda"), torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    at = (1 << 34) - 4096  # (a chunk's start, with the place where a launch ends behind it)
+    p[at:], g[at:] = normal(n - at, seed=1), normal(n - at, seed=2)
+    ps, gs = p[at:].clone(), g[at:].clone()
+    st, ss = ops.adamw_state([p], bits=8, master=False), ops.adamw_state([ps], bits=8, master=False)
+    ops.resonator_adamw_step([p], [g], st, step=1, lr=0.1)
+    ops.resonator_adamw_step([ps], [gs], ss, step=1, lr=0.1)
+    assert torch.equal(p[at:], ps) and not p[:1 << 20].any()
+    for k in ("exp_avg", "exp_avg_sq"):
+        assert torch.equal(st[k][at:], ss[k]), k
+    for k in ("scale_avg", "scale_sq"):
+        assert torch.equal(st[k][at // 256:], ss[k]), k
+    del p, g
+    torch.cuda.empty_cache()
+    m, v = ops.resonator_adamw_values(st)
+    m2, v2 = ops.resonator_adamw_values(ss)
+    assert torch.equal(m[at:], m2) and torch.equal(v[at:], v2)
