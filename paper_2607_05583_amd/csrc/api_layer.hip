@@ -254,7 +254,7 @@ int check_linear(int64_t R, int64_t K, int64_t N, res_dtype_t dt, int act) {
   if (R < 0 || K < 1 || N < 1)
     return api_error(RES_ERR_INVALID_ARG, "K and N must be >= 1 and R >= 0 (got R=%lld K=%lld N=%lld)", (long long)R,
                      (long long)K, (long long)N);
-  // (work-groups of a launch, by tiles of 64 x 64 or 256 elements: below 2^31)
+  // (tiles of 64 x 64 are 32-bit counts)
   if (R > (1LL << 31) || K > (1 << 20) || N > (1 << 20) || R * std::max(K, N) > (1LL << 38))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (R=%lld K=%lld N=%lld)", (long long)R,
                      (long long)K, (long long)N);

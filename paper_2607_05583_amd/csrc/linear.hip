@@ -793,30 +793,49 @@ hipError_t launch_gemm(const GemmArgs& a, hipStream_t st) {
     }
   }
   if (a.splits != 1) {
-    const int64_t n = a.M * a.N;
-    if (!a.loose && a.N % 4 == 0)
-      gemm_join_kernel<T, 4><<<dim3((unsigned)((n / 4 + 255) / 256)), 256, 0, st>>>(a);
-    else
-      gemm_join_kernel<T, 1><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>(a);
+    // (a cut sum has fewer than 2^24 outputs; the zeros of an empty one may be more than a launch takes)
+    const int64_t most = (LAUNCH_THREADS - 255) / a.N;
+    for (int64_t m = 0; m < a.M; m += most) {
+      GemmArgs b = a;
+      b.M = a.M - m < most ? a.M - m : most;
+      b.out = (T*)a.out + m * a.N;
+      const int64_t n = b.M * a.N;
+      if (!a.loose && a.N % 4 == 0)
+        gemm_join_kernel<T, 4><<<dim3((unsigned)((n / 4 + 255) / 256)), 256, 0, st>>>(b);
+      else
+        gemm_join_kernel<T, 1><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>(b);
+    }
   }
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_pack(const void* src, int64_t ld, int64_t rows, int64_t cols, void* dst, int64_t to, hipStream_t st) {
-  const int64_t n = rows * to / (16 / (int64_t)sizeof(T));
-  pack_kernel<T><<<dim3((unsigned)((n + 255) / 256)), 256, 0, st>>>((const T*)src, ld, rows, cols, (T*)dst, to);
+  const int64_t per = to / (16 / (int64_t)sizeof(T)), most = (LAUNCH_THREADS - 255) / per;  // threads of a row, rows of a launch
+  for (int64_t r = 0; r < rows; r += most) {
+    const int64_t n = rows - r < most ? rows - r : most;
+    pack_kernel<T><<<dim3((unsigned)((n * per + 255) / 256)), 256, 0, st>>>((const T*)src + r * ld, ld, n, cols, (T*)dst + r * to, to);
+  }
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_act_bwd(const void* dy, const float* pre, int act, void* out, int64_t to, float* part, int64_t R, int64_t N,
                           bool loose, hipStream_t st) {
-  const int64_t blocks = linear_row_blocks(R);
-  if (!loose && N % 4 == 0)
-    act_bwd_kernel<T, 4><<<dim3((unsigned)((to + 255) / 256 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, to, part, R, N);
-  else
-    act_bwd_kernel<T, 1><<<dim3((unsigned)((to + 63) / 64 * blocks)), 256, 0, st>>>((const T*)dy, pre, act, (T*)out, to, part, R, N);
+  const bool four = !loose && N % 4 == 0;
+  const int64_t cols = four ? (to + 255) / 256 : (to + 63) / 64, most = LAUNCH_THREADS / 256 / cols * ACT_ROWS;  // rows of a launch
+  for (int64_t r = 0; r < R; r += most) {
+    const int64_t n = R - r < most ? R - r : most;
+    const dim3 grid((unsigned)(cols * linear_row_blocks(n)));
+    const T* d = (const T*)dy + r * N;
+    const float* p = pre != nullptr ? pre + r * N : nullptr;
+    T* o = out != nullptr ? (T*)out + r * to : nullptr;
+    float* s = part != nullptr ? part + r / ACT_ROWS * N : nullptr;
+    if (four)
+      act_bwd_kernel<T, 4><<<grid, 256, 0, st>>>(d, p, act, o, to, s, n, N);
+    else
+      act_bwd_kernel<T, 1><<<grid, 256, 0, st>>>(d, p, act, o, to, s, n, N);
+  }
   return hipGetLastError();
 }
 

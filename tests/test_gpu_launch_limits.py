@@ -1,6 +1,6 @@
 """More work than one launch takes (2^32 threads): the scan's tiles, the token step's elements, AdamW's chunks and the values of
-its codes.  Each is compared, bit for bit, with small calls on the same rows or elements, or on those around the place where a
-launch ends.
+its codes, the linear product's copies of operands and the sums of dy.  Each is compared with small calls on the same rows or
+elements, or on those around the place where a launch ends, or with its definition.
 
 The memory that a case needs is what the operator's own buffers take; a card that has not got it free skips the case.
 """
@@ -106,3 +106,51 @@ def test_adamw_of_many_elements(room):
     m, v = ops.resonator_adamw_values(st)
     m2, v2 = ops.resonator_adamw_values(ss)
     assert torch.equal(m[at:], m2) and torch.equal(v[at:], v2)
+
+
+def test_linear_copy_of_many_elements(room):
+    """An operand of 2^35 elements whose rows are not whole pieces is copied in more than one launch."""
+    R, K, N = (1 << 15) + 9, (1 << 20) - 3, 8
+    room(140)
+    say(f"linear copy of many elements {R} {K}")
+    x = torch.zeros(R, K, dtype=torch.bfloat16, device="cuda")
+    rows = [0, 1, (1 << 15) - 1, 1 << 15, R - 1]
+    for k, row in enumerate(rows):
+        x[row] = normal(K, seed=k)
+    W = normal(K, N, seed=9)
+    y = ops.resonator_linear_fwd(x, W)
+    xs = x[rows].double()
+    want = xs @ W.double()
+    # (2^-8 of the result for its rounding; K random terms in float32 add 2^-24 sqrt(K) / 2.4 of its size, 2.5e-5)
+    assert (y[rows].double() - want).abs().max() <= 2.0 ** -8 * want.abs().max()
+    rest = torch.ones(R, dtype=torch.bool, device="cuda")
+    rest[rows] = False
+    assert not y[rest].any()
+
+
+def test_linear_column_sums_of_many_elements(room):
+    """db of more rows than a launch takes (a work-group for 64 rows); whole numbers, whose sums are exact."""
+    R, N = (1 << 30) + 64 * 3 + 5, 9
+    room(90)
+    say(f"linear column sums of many elements {R} {N}")
+    dy = torch.zeros(R, N, dtype=torch.bfloat16, device="cuda")
+    at = (1 << 30) - 64  # (where a launch ends)
+    dy[at - 100:at + 100] = torch.randint(-3, 4, (200, N), device="cuda").bfloat16()
+    dy[R - 70:] = 1.0
+    want = dy[at - 100:at + 100].double().sum(0) + 70
+    x, W = torch.zeros(R, 1, dtype=torch.bfloat16, device="cuda"), torch.zeros(1, N, dtype=torch.bfloat16, device="cuda")
+    g = ops.resonator_linear_bwd(x, W, dy, want_dx=False, want_dw=False, want_db=True)
+    assert torch.equal(g["db"].double(), want)
+
+
+def test_linear_zeros_of_many_elements(room):
+    """The weight gradient of no rows: 2^32 and some zeros, one a thread."""
+    K, N = (1 << 20) - 1, 4100
+    room(40)
+    say(f"linear zeros of many elements {K} {N}")
+    W = torch.empty(K, N, dtype=torch.bfloat16, device="cuda")
+    x, dy = torch.empty(0, K, dtype=torch.bfloat16, device="cuda"), torch.empty(0, N, dtype=torch.bfloat16, device="cuda")
+    junk = torch.full((K, N), 3.0, dtype=torch.bfloat16, device="cuda")
+    del junk  # (what the allocator hands out again)
+    g = ops.resonator_linear_bwd(x, W, dy, want_dx=False)
+    assert not g["dW"].any()
