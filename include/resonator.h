@@ -640,6 +640,8 @@ int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
  *               the step reads and writes them, and p_out receives their rounding
  *   grad_scale  [1] float32 on the device, or NULL for 1 (a clipping factor, a loss scale)
  * lr, eps, weight_decay >= 0, betas in [0, 1), step >= 1 counts from one; all are host values.
+ * With eps = 0 an element whose v is 0 has no finite step, and that is also where g'^2 leaves
+ * float32 (|g'| below about 2^-72).
  * m, v and master must be 16-byte aligned, and a buffer written must not overlap one
  * read except as the same buffer.  A gradient that is not finite makes its block's state
  * (8 bits) or its element's (32) not finite.

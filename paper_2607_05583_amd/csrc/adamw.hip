@@ -76,6 +76,13 @@ __device__ __forceinline__ void codes(float m, float v, float im, float iv, int*
   if (v > 0.0f && iv > 0.0f && *cv < 1) *cv = 1;
 }
 
+// The root of a second moment.  The unit's takes what is below 2^-126 for zero, by which a step with eps = 0 is divided.
+__device__ __forceinline__ float root_of(float v) {
+  const bool small = v < 0x1p-96f;
+  const float r = __builtin_amdgcn_sqrtf(small ? v * 0x1p64f : v);
+  return small ? r * 0x1p-32f : r;
+}
+
 // A lane's four elements, one behind the other at the alignment of one: all of them (WHOLE), or the first `left`.
 template <typename T> using Vec = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
 template <bool WHOLE, typename T>
@@ -156,7 +163,7 @@ __device__ __forceinline__ void adamw_block(const AdamWArgs& a, float gs, const 
   Vec<float> q;
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const float den = fmaf(__builtin_amdgcn_sqrtf(v[j]), a.root, a.eps);
+    const float den = fmaf(root_of(v[j]), a.root, a.eps);
     // (a reciprocal within one unit in the last place: 2^-23 of the step, which is small beside the parameter)
     q[j] = fmaf(w[j], a.decay, -(a.step * m[j]) * __builtin_amdgcn_rcpf(den));
     po[j] = from_f32<TP>(q[j]);
