@@ -642,9 +642,10 @@ int resonator_linear_bwd(const void* x, int64_t ldx, const void* W, res_dtype_t 
  * lr, eps, weight_decay >= 0, betas in [0, 1), step >= 1 counts from one; all are host values.
  * With eps = 0 an element whose v is 0 has no finite step, and that is also where g'^2 leaves
  * float32 (|g'| below about 2^-72).
- * m, v and master must be 16-byte aligned, and a buffer written must not overlap one
- * read except as the same buffer.  A gradient that is not finite makes its block's state
- * (8 bits) or its element's (32) not finite.
+ * m, v and master must be 16-byte aligned, and what is written must not overlap anything else
+ * that is read or written (a new value may be in its old one's place; a tensor must not be given
+ * twice, and the tensors' places in the states must not meet).  A gradient that is not finite
+ * makes its block's state (8 bits) or its element's (32) not finite.
  */
 #define RES_ADAMW_BLOCK 256
 typedef struct {
