@@ -13,6 +13,7 @@ import ctypes
 from typing import NamedTuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import _lib
 from ._lib import RES_BF16, RES_F32, RES_OP_BWD, RES_OP_FWD, RES_OP_STATE_INIT, check
@@ -852,6 +853,7 @@ class ResonatorParamMapFunction(torch.autograd.Function):
         return resonator_params_map(theta_gamma.contiguous(), theta_omega.contiguous(), alpha_min)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dgamma, domega):
         tg, tw = ctx.saved_tensors
         dtg, dtw = resonator_params_map_bwd(tg.contiguous(), tw.contiguous(), dgamma.contiguous(),
@@ -869,6 +871,7 @@ class ResonatorMixFunction(torch.autograd.Function):
                                  amp.contiguous(), phase.contiguous())
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, gamma, omega, amp, phase = ctx.saved_tensors
         g = resonator_mix_bwd(x.contiguous(), dy.contiguous().to(x.dtype), gamma, omega, amp, phase)
@@ -1176,6 +1179,7 @@ class GatedScanFunction(torch.autograd.Function):
         return y, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy, dh):
         x, r, i, gamma, carry, lengths = ctx.saved_tensors
         dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None else dy.contiguous()
@@ -1337,6 +1341,7 @@ class LinearFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, W, pre, bias = ctx.saved_tensors
         pre = LinearSaved(pre, bias)
@@ -1542,6 +1547,7 @@ class GatedLayerFunction(torch.autograd.Function):
         return out, h
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout, dh):
         x, lengths, pre, *rest = ctx.saved_tensors
         n = len(GatedLayerParams._fields)
