@@ -606,6 +606,11 @@ bool gated_ws(PyObject* o, const Gated& g, Tensor* ws) {
   *ws = at::zeros({(int64_t)nb}, at::TensorOptions().device(g.x->device()).dtype(at::kByte));
   return true;
 }
+// Tells autograd that a caller's tensors (null: none) hold new values, so that a graph that kept the old ones says so.
+void written(std::initializer_list<const Tensor*> ts) {
+  for (const Tensor* t : ts)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
 size_t bytes(const Tensor& t) { return (size_t)(t.numel() * t.element_size()); }
 
 // (x, r, i, gamma, h0, lengths, return_state, save, out, ws, h_out) -> y, or a tuple of y, the state and the carry
@@ -632,6 +637,7 @@ PyObject* gated_scan_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                     h.defined() ? fpm(h) : nullptr, save ? fpm(carry) : nullptr, ws.data_ptr(), bytes(ws), on.stream);
   });
   if (rc) return PyLong_FromLong(rc);
+  written({out, ho});
   if (want) return save ? pack({y, h, carry}) : pack({y, h});
   return save ? pack({y, carry}) : THPVariable_Wrap(y);
   END_HANDLE_TH_ERRORS
@@ -671,7 +677,9 @@ PyObject* gated_scan_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                     len ? static_cast<const int32_t*>(len->data_ptr()) : nullptr, fp0(dh), fpm(dgamma),
                                     want ? fpm(dh0) : nullptr, ws.data_ptr(), bytes(ws), on.stream);
   });
-  return rc ? PyLong_FromLong(rc) : pack({o[0], o[1], o[2], dgamma, dh0});
+  if (rc) return PyLong_FromLong(rc);
+  if (a[9] != Py_None) written({&o[0], &o[1], &o[2]});
+  return pack({o[0], o[1], o[2], dgamma, dh0});
   END_HANDLE_TH_ERRORS
 }
 
@@ -689,7 +697,9 @@ PyObject* gated_scan_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return resonator_gated_scan_step(as_rows(*g.x), as_rows(*g.r), as_rows(*g.i), g.dt, y.data_ptr(), g.B, g.D, fp(*g.gamma), fp(*h),
                                      fpm(ho ? *ho : *h), on.stream);
   });
-  return rc ? PyLong_FromLong(rc) : THPVariable_Wrap(y);
+  if (rc) return PyLong_FromLong(rc);
+  written({ho ? ho : h, out});
+  return THPVariable_Wrap(y);
   END_HANDLE_TH_ERRORS
 }
 
@@ -759,7 +769,9 @@ PyObject* linear_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                 y.data_ptr(), pre.defined() ? fpm(pre) : nullptr, l.R, l.K, l.N,
                                 ws.defined() ? ws.data_ptr() : nullptr, ws.defined() ? bytes(ws) : 0, on.stream);
   });
-  return rc ? PyLong_FromLong(rc) : pack({y, pre});
+  if (rc) return PyLong_FromLong(rc);
+  written({out});
+  return pack({y, pre});
   END_HANDLE_TH_ERRORS
 }
 
@@ -793,13 +805,14 @@ PyObject* linear_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+const char* const kState[5] = {"exp_avg", "exp_avg_sq", "scale_avg", "scale_sq", "master"};
+
 // A state dict's buffers for n elements.
 bool adamw_state(PyObject* d, int64_t n, res_adamw_state_t* s) {
   if (!PyDict_CheckExact(d)) return false;
   const Tensor* t[5] = {};
-  static const char* const names[5] = {"exp_avg", "exp_avg_sq", "scale_avg", "scale_sq", "master"};
   for (int k = 0; k < 5; ++k) {
-    PyObject* o = PyDict_GetItemString(d, names[k]);
+    PyObject* o = PyDict_GetItemString(d, kState[k]);
     if (o && !(t[k] = plain(o))) return false;
   }
   if (!t[0] || !t[1]) return false;
@@ -857,6 +870,11 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                 step, fp0(scale), on.stream);
   });
   if (rc) return PyLong_FromLong(rc);
+  for (Py_ssize_t k = 0; k < count; ++k) written({plain(PyList_GET_ITEM(a[2], k))});
+  for (const char* name : kState) {
+    PyObject* o = PyDict_GetItemString(a[4], name);
+    if (o) written({plain(o)});
+  }
   Py_RETURN_TRUE;
   END_HANDLE_TH_ERRORS
 }

@@ -1027,6 +1027,11 @@ def _rows(t, name, dtype, shape):
     return _lib.Rows(t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0)
 
 
+def _written(*tensors):
+    """Tells autograd that a caller's tensors hold new values, so that a graph that kept the old ones says so."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None and not t.is_inference()])
+
+
 def _f32(t, name, shape):
     if t is None:
         return None
@@ -1089,6 +1094,7 @@ def resonator_gated_scan_fwd(x, r, i, gamma, h0=None, lengths=None, return_state
     _f32(h0, "h0", (B, D))
     _gated_lengths(lengths, B)
     y = torch.empty((B, L, D), dtype=x.dtype, device=x.device) if out is None else _given(out, "out", B * L * D, x.dtype)
+    given = out, h_out
     if h_out is not None:
         _f32(h_out, "h_out", (B, D))
     elif return_state:
@@ -1098,6 +1104,7 @@ def resonator_gated_scan_fwd(x, r, i, gamma, h0=None, lengths=None, return_state
     check(_lib.lib().resonator_gated_scan_fwd(
         *rows, _code(x), _ptr(y), B, L, D, _ptr(gamma), _ptr(h0), _ptr(lengths), _ptr(h_out), _ptr(carry), _ptr(ws),
         ws.numel() * ws.element_size(), _stream(x.device)))
+    _written(*given)
     r_ = (y,) + ((h_out,) if return_state else ()) + ((carry,) if save else ())
     return r_ if len(r_) > 1 else y
 
@@ -1125,6 +1132,7 @@ def resonator_gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh_out=N
     _f32(h0, "h0", (B, D))
     _f32(dh_out, "dh_out", (B, D))
     _gated_lengths(lengths, B)
+    given = () if out is None else out
     if out is None:
         out = [torch.empty((B, L, D), dtype=x.dtype, device=x.device) for _ in range(3)]
     dx, dr, di = out
@@ -1144,6 +1152,7 @@ def resonator_gated_scan_bwd(x, r, i, gamma, dy, h0=None, lengths=None, dh_out=N
     check(_lib.lib().resonator_gated_scan_bwd(
         *rows, _code(x), *orows, B, L, D, _ptr(gamma), _ptr(carry), _ptr(lengths), _ptr(dh_out), _ptr(dgamma),
         _ptr(dh0), _ptr(ws), wsb, _stream(x.device)))
+    _written(*given)
     g = {"dx": dx, "dr": dr, "di": di, "dgamma": dgamma}
     if want_dh0:
         g["dh0"] = dh0
@@ -1165,6 +1174,7 @@ def resonator_gated_scan_step(x_t, r_t, i_t, gamma, h, h_out=None, out=None):
     y = torch.empty((B, D), dtype=x_t.dtype, device=x_t.device) if out is None else _given(out, "out", B * D, x_t.dtype)
     check(_lib.lib().resonator_gated_scan_step(*rows, _code(x_t), _ptr(y), B, D, _ptr(gamma), _ptr(h), _ptr(h_out),
                                                _stream(x_t.device)))
+    _written(h_out, out)
     return y
 
 
@@ -1293,6 +1303,7 @@ def resonator_linear_fwd(x, W, bias=None, act="none", residual=None, save=False,
     ws, n = _linear_ws(ws, 0, code, x, ldx, W)
     check(_lib.lib().resonator_linear_fwd(_ptr(x), ldx, _ptr(W), _code(x), _ptr(bias), code, _ptr(residual), _ptr(y),
                                           _ptr(pre), R, K, N, _ptr(ws), n, _stream(x.device)))
+    _written(out)
     return (y, LinearSaved(pre, bias)) if save else y
 
 
@@ -1456,6 +1467,7 @@ def resonator_adamw_step(params, grads, state, step, lr, betas=(0.9, 0.999), eps
     check(_lib.lib().resonator_adamw_step(table, len(params), _code(params[0]), _code(grads[0]), ctypes.byref(old_s),
                                           ctypes.byref(new_s), float(lr), float(betas[0]), float(betas[1]), float(eps),
                                           float(weight_decay), int(step), _ptr(grad_scale), _stream(dev)))
+    _written(*new, *new_state.values())
 
 
 def resonator_adamw_values(state):
