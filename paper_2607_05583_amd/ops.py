@@ -1178,6 +1178,11 @@ def resonator_gated_scan_step(x_t, r_t, i_t, gamma, h, h_out=None, out=None):
     return y
 
 
+def _needs_graph(*tensors):
+    """Whether some gradient may be asked for: else nothing is kept for a backward."""
+    return torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors)
+
+
 class GatedScanFunction(torch.autograd.Function):
     """Autograd wrapper: resonator_gated_scan_fwd (y and the last state) and resonator_gated_scan_bwd."""
 
@@ -1200,6 +1205,8 @@ class GatedScanFunction(torch.autograd.Function):
 
 def resonator_gated_scan(x, r, i, gamma, h0=None, lengths=None):
     """Differentiable gated scan: (y, last state); x, r, i, gamma and h0 receive gradients."""
+    if not _needs_graph(x, r, i, gamma, h0):
+        return resonator_gated_scan_fwd(x, r, i, gamma, h0=h0, lengths=lengths, return_state=True)
     return GatedScanFunction.apply(x, r, i, gamma, h0, lengths)
 
 
@@ -1366,6 +1373,8 @@ class LinearFunction(torch.autograd.Function):
 
 def resonator_linear(x, W, bias=None, act="none", residual=None):
     """Differentiable act(x W + bias) + residual (x, W, bias and residual receive gradients)."""
+    if not _needs_graph(x, W, bias, residual):
+        return resonator_linear_fwd(x, W, bias, act=act, residual=residual)
     return LinearFunction.apply(x, W, bias, act, residual)
 
 
@@ -1573,4 +1582,6 @@ class GatedLayerFunction(torch.autograd.Function):
 
 def resonator_gated_layer(x, p, h0=None, lengths=None, act="gelu_tanh"):
     """Differentiable gated recurrent layer: (out, last state); x, h0 and p's tensors receive gradients."""
+    if not _needs_graph(x, h0, *p):
+        return resonator_gated_layer_fwd(x, p, h0=h0, lengths=lengths, act=act, return_state=True)
     return GatedLayerFunction.apply(x, h0, lengths, act, *p)
