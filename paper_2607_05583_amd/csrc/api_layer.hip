@@ -675,11 +675,15 @@ int resonator_adamw_values(const res_adamw_state_t* state, int64_t n, float* m, 
   if (state->m == nullptr || state->v == nullptr || state->scale_m == nullptr || state->scale_v == nullptr ||
       m == nullptr || v == nullptr)
     return api_error(RES_ERR_INVALID_ARG, "the state's tensors, m and v must be non-null");
-  if (!aligned(state->m, 16) || !aligned(state->v, 16) || !aligned(m, 16) || !aligned(v, 16))
-    return api_error(RES_ERR_MISALIGNED, "the codes, m and v must be 16-byte aligned");
-  if (touch(flat(m, 4 * n), flat(v, 4 * n)) || touch(flat(m, 4 * n), flat(state->m, n)) || touch(flat(v, 4 * n), flat(state->v, n)) ||
-      touch(flat(m, 4 * n), flat(state->v, n)) || touch(flat(v, 4 * n), flat(state->m, n)))
-    return api_error(RES_ERR_INVALID_ARG, "m and v must not overlap each other or the codes");
+  if (!aligned(state->m, 16) || !aligned(state->v, 16) || !aligned(m, 16) || !aligned(v, 16) || !aligned(state->scale_m, 4) ||
+      !aligned(state->scale_v, 4))
+    return api_error(RES_ERR_MISALIGNED, "the codes, m and v must be 16-byte aligned, scales 4-byte");
+  const size_t scales = n / RES_ADAMW_BLOCK * 4;
+  for (float* o : {m, v})
+    if (touch(flat(o, 4 * n), flat(state->m, n)) || touch(flat(o, 4 * n), flat(state->v, n)) ||
+        touch(flat(o, 4 * n), flat(state->scale_m, scales)) || touch(flat(o, 4 * n), flat(state->scale_v, scales)))
+      return api_error(RES_ERR_INVALID_ARG, "m and v must not overlap the codes or their scales");
+  if (touch(flat(m, 4 * n), flat(v, 4 * n))) return api_error(RES_ERR_INVALID_ARG, "m and v must not overlap each other");
   return launched(launch_adamw_values(state->m, state->v, state->scale_m, state->scale_v, n, m, v, (hipStream_t)stream),
                   "AdamW values launch");
 }

@@ -57,3 +57,14 @@ def test_many_tensors_one_of_them_twice():
         t = [(at(1, 4000 * ((37 * j) % 100)), at(2), at(1, 4000 * ((37 * j) % 100)), N, 1024 * j) for j in range(100)]
         t[k + 1] = t[k][:4] + (1024 * (k + 1),)
         assert step(t, ST) == L.RES_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("m,v,scale_m,scale_v,code", [
+    (at(1), at(2), at(1, 512), at(13), L.RES_ERR_INVALID_ARG), (at(1), at(2), at(12), at(1, 1020), L.RES_ERR_INVALID_ARG),
+    (at(1), at(2), at(2, 4), at(13), L.RES_ERR_INVALID_ARG), (at(1), at(2), at(12), at(2), L.RES_ERR_INVALID_ARG),
+    (at(10, 240), at(2), at(12), at(13), L.RES_ERR_INVALID_ARG), (at(1), at(11), at(12), at(13), L.RES_ERR_INVALID_ARG),
+    (at(1), at(2), at(12, 2), at(13), L.RES_ERR_MISALIGNED), (at(1), at(2), at(12), at(13, 1), L.RES_ERR_MISALIGNED)])
+def test_values_over_what_they_are_read_from(m, v, scale_m, scale_v, code):
+    """The values of 256 codes, over the codes or one of their scales, and scales that are not aligned."""
+    s = L.AdamWState(8, at(10), at(11), scale_m, scale_v, None)
+    assert L.lib().resonator_adamw_values(ctypes.byref(s), 256, ctypes.c_void_p(m), ctypes.c_void_p(v), None) == code
