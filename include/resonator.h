@@ -542,10 +542,11 @@ typedef struct {
  *            every RES_GATED_CARRY-th step, which the backward starts from
  *   ws       resonator_gated_scan_workspace_bytes(dt, B, L, D) bytes, 256-byte aligned
  * The workspace must be zero-filled before its first use; every call leaves it
- * ready for the next call, forward or backward, of any sizes whose need it covers.
- * Its first word is a status as the mixing's (resonator_fwd_status reads it): 1 when a
- * wait for other work-groups gave up, whose results are NaN.
- * Calls that share one must not overlap in time.  B, D >= 1, L >= 0.
+ * ready for the next call, forward or backward, of any sizes whose need it covers,
+ * for 2^32 - 1 launches (then it has to be zero-filled again: they are told apart by
+ * their 32-bit number).  Its first word is a status as the mixing's
+ * (resonator_fwd_status reads it): 1 when a wait for other work-groups gave up, whose
+ * results are NaN.  Calls that share one must not overlap in time.  B, D >= 1, L >= 0.
  * Outputs must not overlap inputs or each other.
  */
 #define RES_GATED_CARRY 128

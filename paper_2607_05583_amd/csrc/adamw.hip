@@ -8,8 +8,9 @@
 //
 // A wave takes one block of 256 elements, four consecutive ones a lane, so that a block's largest value is one reduction
 // over the wave and every access 4 to 16 bytes a lane.  Memory bounds it: bfloat16 with float32 copies and states moves
-// 28 bytes an element, 201 M of them in 994 us (5.7 TB/s); float32 with float32 states 28 bytes, 4.7 M in 23 us (out of
-// the last cache); float32 with states of 8 bits 16 bytes, 80 M in 257 us (5.0 TB/s; 300 vector instructions a wave).
+// 28 bytes an element, 201 M of them in 994 to 1035 us on different cards (5.7 to 5.4 TB/s); float32 with float32 states 28
+// bytes, 4.7 M in 22 us (out of the last cache); float32 with states of 8 bits 16 bytes, 80 M in 258 us (5.0 TB/s; 324 vector
+// instructions a wave).
 // Two blocks a wave and element 64 j + lane took 1026, 36 and 345 us.
 #include "layer.h"
 

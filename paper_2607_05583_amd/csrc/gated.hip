@@ -22,7 +22,7 @@
 // ticket counter, so the tiles that one waits for are always at work (one work-group a
 // tile: a loop over tiles took 60 registers more).  A published value is a 64-bit word with
 // the call's number beside it: a word is its own flag, and nothing has to be cleared
-// between calls.
+// between calls.  A call of more than 2^32 threads is several launches of whole batch rows.
 //
 // A step of a channel is 8 bytes forward and 14 backward in bf16, and 36 and 94 vector
 // instructions of a wave, six and ten of them transcendental.

@@ -1510,7 +1510,9 @@ class GatedLayerParams(NamedTuple):
 def resonator_gated_layer_fwd(x, p, h0=None, lengths=None, act="gelu_tanh", return_state=False, save=False, ws=None):
     """A gated recurrent layer: y = gated scan of the columns of x Wp + bp, z = x + y Wo + bo,
     out = z + act(z W1 + b1) W2 + b2.  x [B, L, d]; ``p`` a GatedLayerParams; ``h0``, ``lengths`` and ``ws`` (a
-    gated_scan_workspace) as in resonator_gated_scan_fwd.  Returns out; with ``return_state`` also the state after the
+    gated_scan_workspace) as in resonator_gated_scan_fwd.  The lengths are the scan's alone: the products take every row, so
+    that what x (and, in the backward, dout) holds behind a row's length must be finite, out has rows there, and a dout that
+    is not zero there adds to the gradients.  Returns out; with ``return_state`` also the state after the
     last step, from which resonator_gated_layer_step goes on; with ``save`` also the dict for resonator_gated_layer_bwd.
     Four products and a scan: the biases, the activation and the residuals are part of the products."""
     u = resonator_linear_fwd(x, p.Wp, p.bp)
