@@ -38,12 +38,17 @@ Span flat(const void* p, size_t bytes) {
 }
 bool touch(const Span& a, const Span& b) {
   if (a.lo == a.hi || b.lo == b.hi || a.hi <= b.lo || b.hi <= a.lo) return false;
-  // columns of one wider tensor: the same strides, and columns that do not meet within a step
-  if (a.st == b.st && a.st > 0 && (a.sb == b.sb || (a.B == 1 && b.B == 1)) && (a.B == 1 || a.sb % a.st == 0)) {
-    const int64_t d = (((int64_t)(b.lo - a.lo)) % a.st + a.st) % a.st;  // b's first column after a's
-    if (d >= a.row && d + b.row <= a.st) return false;
-  }
-  return true;
+  // columns of one wider tensor, whichever axis is outermost: every distance between rows is a multiple of the least, and
+  // within that the columns do not meet
+  const int64_t by[4] = {a.B > 1 ? a.sb : 0, a.L > 1 ? a.st : 0, b.B > 1 ? b.sb : 0, b.L > 1 ? b.st : 0};
+  int64_t least = 0;
+  for (int64_t s : by)
+    if (s > 0 && (least == 0 || s < least)) least = s;
+  if (least == 0) return true;
+  for (int64_t s : by)
+    if (s % least != 0) return true;
+  const int64_t d = (((int64_t)(b.lo - a.lo)) % least + least) % least;  // b's first column after a's
+  return !(d >= a.row && d + b.row <= least);
 }
 // whether the rows of an output lie apart from each other
 bool rows_apart(int64_t sb, int64_t st, int64_t B, int64_t L, int64_t D) {
