@@ -516,6 +516,7 @@ int resonator_epilogue_bwd(const void* y, const void* gate, const void* v, const
  * Rows of a [B][L] set of D consecutive elements each: row (b, t) starts at element
  * b sb + t st of p (strides in elements, >= 0).  A contiguous [B][L][D] tensor has
  * sb = L D, st = D; one of three columns of a fused projection [B][L][3 D] has st = 3 D.
+ * sb is at most 2^40 and st 2^21; with one step (L = 1) st plays no part.
  */
 typedef struct {
   const void* p;

@@ -58,11 +58,11 @@ bool rows_apart(int64_t sb, int64_t st, int64_t B, int64_t L, int64_t D) {
   return (st >= D && sb >= (L - 1) * st + D) || (sb >= D && st >= (B - 1) * sb + D);
 }
 
-int check_rows(const char* name, const void* p, int64_t sb, int64_t st, size_t es) {
+int check_rows(const char* name, const void* p, int64_t sb, int64_t st, int64_t L, size_t es) {
   if (p == nullptr) return api_error(RES_ERR_INVALID_ARG, "%s must be non-null", name);
   if (!aligned(p, es)) return api_error(RES_ERR_MISALIGNED, "%s must be aligned to its element", name);
-  // (a tile's bytes have 32-bit offsets)
-  if (sb < 0 || st < 0 || sb > (1LL << 40) || st > (1LL << 21))
+  // (a tile's bytes have 32-bit offsets; one step has no distance to a next one)
+  if (sb < 0 || sb > (1LL << 40) || (L > 1 && (st < 0 || st > (1LL << 21))))
     return api_error(RES_ERR_UNSUPPORTED, "%s: strides must be in [0, 2^40] (rows) and [0, 2^21] (steps) elements", name);
   return RES_OK;
 }
@@ -114,8 +114,8 @@ int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype
   int rc = check_scan(B, L, D, dt);
   if (rc || (rc = check_launch(L, D, GATED_FWD_TILE))) return rc;
   const size_t es = elt(dt);
-  if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, es)) || (rc = check_rows("r", r.p, r.sb, r.st, es)) ||
-                (rc = check_rows("i", i.p, i.sb, i.st, es))))
+  if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, L, es)) || (rc = check_rows("r", r.p, r.sb, r.st, L, es)) ||
+                (rc = check_rows("i", i.p, i.sb, i.st, L, es))))
     return rc;
   if ((rc = check_f32("gamma", gamma, true)) || (rc = check_f32("h0", h0, false)) ||
       (rc = check_f32("h_out", h_out, false)) || (rc = check_f32("carry", carry, false)))
@@ -140,9 +140,9 @@ int resonator_gated_scan_fwd(res_rows_t x, res_rows_t r, res_rows_t i, res_dtype
       if (touch(out[o], out[k])) return api_error(RES_ERR_INVALID_ARG, "outputs must not overlap each other");
   }
   GatedArgs a{};
-  a.x = Rows{x.p, x.sb, x.st};
-  a.r = Rows{r.p, r.sb, r.st};
-  a.i = Rows{i.p, i.sb, i.st};
+  a.x = Rows{x.p, x.sb, L > 1 ? x.st : 0};
+  a.r = Rows{r.p, r.sb, L > 1 ? r.st : 0};
+  a.i = Rows{i.p, i.sb, L > 1 ? i.st : 0};
   a.y = y;
   a.B = B;
   a.L = L;
@@ -168,10 +168,10 @@ int resonator_gated_scan_bwd(res_rows_t x, res_rows_t r, res_rows_t i, res_rows_
   int rc = check_scan(B, L, D, dt);
   if (rc || (rc = check_launch(L, D, GATED_BWD_TILE))) return rc;
   const size_t es = elt(dt);
-  if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, es)) || (rc = check_rows("r", r.p, r.sb, r.st, es)) ||
-                (rc = check_rows("i", i.p, i.sb, i.st, es)) || (rc = check_rows("dy", dy.p, dy.sb, dy.st, es)) ||
-                (rc = check_rows("dx", dx.p, dx.sb, dx.st, es)) || (rc = check_rows("dr", dr.p, dr.sb, dr.st, es)) ||
-                (rc = check_rows("di", di.p, di.sb, di.st, es))))
+  if (L > 0 && ((rc = check_rows("x", x.p, x.sb, x.st, L, es)) || (rc = check_rows("r", r.p, r.sb, r.st, L, es)) ||
+                (rc = check_rows("i", i.p, i.sb, i.st, L, es)) || (rc = check_rows("dy", dy.p, dy.sb, dy.st, L, es)) ||
+                (rc = check_rows("dx", dx.p, dx.sb, dx.st, L, es)) || (rc = check_rows("dr", dr.p, dr.sb, dr.st, L, es)) ||
+                (rc = check_rows("di", di.p, di.sb, di.st, L, es))))
     return rc;
   if ((rc = check_f32("gamma", gamma, true)) || (rc = check_f32("carry", carry, L > 0)) ||
       (rc = check_f32("dh_out", dh_out, false)) || (rc = check_f32("dgamma", dgamma, true)) ||
@@ -198,13 +198,13 @@ int resonator_gated_scan_bwd(res_rows_t x, res_rows_t r, res_rows_t i, res_rows_
   if (L > 0 && !(rows_apart(dx.sb, dx.st, B, L, D) && rows_apart(dr.sb, dr.st, B, L, D) && rows_apart(di.sb, di.st, B, L, D)))
     return api_error(RES_ERR_INVALID_ARG, "the rows of dx, dr and di must not overlap");
   GatedArgs a{};
-  a.x = Rows{x.p, x.sb, x.st};
-  a.r = Rows{r.p, r.sb, r.st};
-  a.i = Rows{i.p, i.sb, i.st};
-  a.dy = Rows{dy.p, dy.sb, dy.st};
-  a.dx = RowsOut{dx.p, dx.sb, dx.st};
-  a.dr = RowsOut{dr.p, dr.sb, dr.st};
-  a.di = RowsOut{di.p, di.sb, di.st};
+  a.x = Rows{x.p, x.sb, L > 1 ? x.st : 0};
+  a.r = Rows{r.p, r.sb, L > 1 ? r.st : 0};
+  a.i = Rows{i.p, i.sb, L > 1 ? i.st : 0};
+  a.dy = Rows{dy.p, dy.sb, L > 1 ? dy.st : 0};
+  a.dx = RowsOut{dx.p, dx.sb, L > 1 ? dx.st : 0};
+  a.dr = RowsOut{dr.p, dr.sb, L > 1 ? dr.st : 0};
+  a.di = RowsOut{di.p, di.sb, L > 1 ? di.st : 0};
   a.B = B;
   a.L = L;
   a.D = (int)D;
@@ -230,8 +230,8 @@ int resonator_gated_scan_step(res_rows_t x, res_rows_t r, res_rows_t i, res_dtyp
   int rc = check_scan(B, 1, D, dt);
   if (rc) return rc;
   const size_t es = elt(dt);
-  if ((rc = check_rows("x", x.p, x.sb, x.st, es)) || (rc = check_rows("r", r.p, r.sb, r.st, es)) ||
-      (rc = check_rows("i", i.p, i.sb, i.st, es)) || (rc = check_f32("gamma", gamma, true)) ||
+  if ((rc = check_rows("x", x.p, x.sb, x.st, 1, es)) || (rc = check_rows("r", r.p, r.sb, r.st, 1, es)) ||
+      (rc = check_rows("i", i.p, i.sb, i.st, 1, es)) || (rc = check_f32("gamma", gamma, true)) ||
       (rc = check_f32("h", h, true)) || (rc = check_f32("h_out", h_out, true)))
     return rc;
   if (y == nullptr) return api_error(RES_ERR_INVALID_ARG, "y must be non-null");

@@ -59,3 +59,22 @@ def test_time_first_columns_that_meet_are_refused(path, B, L, D, shift):
     out = dp[..., :D], dp[..., shift:shift + D], dp[..., 2 * D:]
     with pytest.raises(Exception, match="overlap"):
         ops.resonator_gated_scan_bwd(x, x, x, gamma, x, carry=carry, out=out)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("B,D", [(1400, 512), (700, 1001)])
+def test_one_step_of_many_rows_time_first(path, act, B, D):
+    """One step, whose distance to a next one (2^21 elements and more) plays no part."""
+    say(f"one step time first {path} {act} {B} {D}")
+    p = torch.randn(1, B, 3 * D, device="cuda").to(DT[act]).transpose(0, 1)
+    assert p.stride(1) > 1 << 21
+    gamma, dy = torch.linspace(0.05, 2.0, D, device="cuda"), torch.randn(B, 1, D, device="cuda").to(DT[act])
+    xri = p.split(D, dim=-1)
+    y, carry = ops.resonator_gated_scan_fwd(*xri, gamma, save=True)
+    dp = torch.full((1, B, 3 * D), 7.0, dtype=DT[act], device="cuda").transpose(0, 1)
+    got = ops.resonator_gated_scan_bwd(*xri, gamma, dy, carry=carry, out=dp.split(D, dim=-1))
+    apart = [v.contiguous() for v in xri]
+    y2, carry2 = ops.resonator_gated_scan_fwd(*apart, gamma, save=True)
+    want = ops.resonator_gated_scan_bwd(*apart, gamma, dy, carry=carry2)
+    assert torch.equal(y, y2) and torch.equal(carry, carry2) and torch.equal(got["dgamma"], want["dgamma"])
+    assert torch.equal(dp, torch.cat([want[k] for k in ("dx", "dr", "di")], dim=-1))
