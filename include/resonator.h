@@ -671,6 +671,129 @@ int resonator_adamw_step(const res_adamw_tensor_t* tensors, int64_t count, res_d
 int resonator_adamw_values(const res_adamw_state_t* state, int64_t n, float* m, float* v, void* stream);
 
 /*
+ * Short causal convolution, per channel d, with what a prompt's end leaves for the tokens behind it:
+ *   pre_t = sum_{k<K} w[d][k] x_{t-k} + bias[d],  y_t = act(pre_t)
+ * (tap k multiplies the input k steps back, as in the mixer epilogue's local path).
+ *   x          rows of dt; y [B][L][D] of dt
+ *   w [D][K], bias [D] (or NULL)  float32;  1 <= K <= 16;  act RES_ACT_*
+ *   state      [B][K - 1][D] of dt, oldest first: the inputs before the call, or NULL (zeros)
+ *   lengths    [B] int32 or NULL: row b has its first lengths[b] steps (clamped to 0..L); what x holds
+ *              behind them does not matter and y is 0 there
+ *   state_out  [B][K - 1][D] of dt or NULL: the K - 1 inputs before the row's end (may be state itself)
+ * Arithmetic is float32, rounded once to dt.  B, D >= 1, L >= 0.  Outputs must not overlap inputs or
+ * each other otherwise.  Needs no workspace.
+ */
+int resonator_short_conv_fwd(res_rows_t x, res_dtype_t dt, const float* w, const float* bias, int act, int64_t K,
+                             const void* state, const int32_t* lengths, void* y, void* state_out, int64_t B, int64_t L,
+                             int64_t D, void* stream);
+
+/*
+ * Backward of resonator_short_conv_fwd for the loss sum(dy y) + sum(dstate_out state_out): with
+ * dpre = dy act'(pre) (pre is computed again),
+ *   dx_s = sum_k w[k] dpre_{s+k} (+ dstate_out's),  dw[k] = sum dpre_t x_{t-k},  dbias = sum dpre
+ *   dx         rows of dt, overwritten (0 behind a row's length); dw [D][K], dbias [D] (or NULL) float32
+ *   dstate_out [B][K - 1][D] of dt or NULL (zero); dstate [B][K - 1][D] of dt or NULL
+ *   ws         resonator_short_conv_workspace_bytes(B, L, D, K) bytes, 256-byte aligned
+ * Sums run in a fixed order: calls on the same inputs are bitwise reproducible.
+ */
+size_t resonator_short_conv_workspace_bytes(int64_t B, int64_t L, int64_t D, int64_t K);
+int resonator_short_conv_bwd(res_rows_t x, res_rows_t dy, res_dtype_t dt, const float* w, const float* bias, int act,
+                             int64_t K, const void* state, const int32_t* lengths, const void* dstate_out,
+                             res_rows_out_t dx, float* dw, float* dbias, void* dstate, int64_t B, int64_t L, int64_t D,
+                             void* ws, size_t ws_bytes, void* stream);
+
+/* One step for B sequences: rows x [B] (their st is not used), state [B][K - 1][D] of dt; y [B][D] and state_out (may be
+ * state itself) are written. */
+int resonator_short_conv_step(res_rows_t x, res_dtype_t dt, const float* w, const float* bias, int act, int64_t K,
+                              const void* state, void* y, void* state_out, int64_t B, int64_t D, void* stream);
+
+/*
+ * Selective scan: a causal mixer whose state is written and read by the data.  Head h has a state [P][N]:
+ *   D_t = softplus(dt_t + dt_bias),  a_t = exp(-gamma D_t),  h_t = a_t h_{t-1} + D_t x_t b_t^T,  h_{-1} = h0,
+ *   y_t = h_t c_t + skip x_t,
+ * with gamma >= 0 (a precondition), dt_bias and skip of the head, b and c of its group (H / G heads share them).
+ *   x, y    [B][L] steps of [H][P];  dt [H] a step;  b, c [G][N] a step; all of act_dt
+ *           (x, dt, b, c are rows: they may be columns of one projection); y is contiguous
+ *   gamma, dt_bias, skip  float32 [H]; the last two may be NULL (zero)
+ *   h0, h_out             float32 [B][H][P][N] or NULL (zero; not wanted); h_out may be h0 itself
+ *   lengths               [B] int32 or NULL: row b has its first lengths[b] steps (clamped to 0..L); what the
+ *                         inputs hold behind them does not matter, y is 0 there and the state stays
+ *   carry                 resonator_selective_scan_carry_floats(...) floats or NULL: receives the states
+ *                         that the backward starts from
+ *   ws                    resonator_selective_scan_workspace_bytes(0, ...) bytes, 256-byte aligned; contents
+ *                         need not be initialised
+ * y may be NULL where h_out is and carry is not.  1 <= P, N <= 128, G divides H.  The state is float32; for bf16
+ * the weights of the steps that act on each other within 64 steps are rounded to bf16 (2^-8 of a term, as y's own
+ * rounding), states and what makes them are not.  A step's value that is not finite makes the other steps of its
+ * 64 not finite too, earlier ones among them.  Sums run in an order that depends on the sizes alone.
+ * Outputs must not overlap inputs or each other otherwise.
+ */
+size_t resonator_selective_scan_workspace_bytes(int backward, res_dtype_t act_dt, int64_t B, int64_t L, int64_t H, int64_t P,
+                                                int64_t G, int64_t N);
+int64_t resonator_selective_scan_carry_floats(res_dtype_t act_dt, int64_t B, int64_t L, int64_t H, int64_t P, int64_t G,
+                                              int64_t N);
+int resonator_selective_scan_fwd(res_rows_t x, res_rows_t dt, res_rows_t b, res_rows_t c, res_dtype_t act_dt,
+                                 const float* gamma, const float* dt_bias, const float* skip, const float* h0,
+                                 const int32_t* lengths, void* y, float* h_out, float* carry, int64_t B, int64_t L,
+                                 int64_t H, int64_t P, int64_t G, int64_t N, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward of resonator_selective_scan_fwd for the loss sum(dy y) + sum(dh_out h_out).  With g_t the gradient of h_t
+ * (g_t = dy_t c_t^T + a_{t+1} g_{t+1}):
+ *   dc = h^T dy,  db = D g^T x  (summed over the group's heads),  du = g b,  dx = D du + skip dy,
+ *   dl = <g_t, a_t h_{t-1}>,  dD = x.du - gamma dl,  ddt = dD sigmoid(dt + dt_bias),  dgamma = -sum D dl,
+ *   ddt_bias = sum ddt,  dskip = sum dy.x,  dh0 = a_0 g_0
+ *   dy                    rows of act_dt; dx, ddt, db, dc rows of act_dt, overwritten (0 behind a row's length);
+ *                         they may be columns of one tensor
+ *   carry                 the forward's of the same inputs (may be NULL where it has no floats)
+ *   dgamma [H], ddt_bias, dskip [H] (or NULL), dh0 [B][H][P][N] (or NULL)  float32, overwritten
+ *   ws                    resonator_selective_scan_workspace_bytes(1, ...)
+ * Calls on the same inputs are bitwise reproducible.
+ */
+int resonator_selective_scan_bwd(res_rows_t x, res_rows_t dt, res_rows_t b, res_rows_t c, res_rows_t dy, res_dtype_t act_dt,
+                                 const float* gamma, const float* dt_bias, const float* skip, const float* h0,
+                                 const int32_t* lengths, const float* carry, const float* dh_out, res_rows_out_t dx,
+                                 res_rows_out_t ddt, res_rows_out_t db, res_rows_out_t dc, float* dgamma, float* ddt_bias,
+                                 float* dskip, float* dh0, int64_t B, int64_t L, int64_t H, int64_t P, int64_t G, int64_t N,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/* One step for B sequences: rows x, dt, b, c [B] (their st is not used), state h [B][H][P][N] float32; y [B][H][P] of act_dt
+ * and h_out (may be h itself) are written. */
+int resonator_selective_scan_step(res_rows_t x, res_rows_t dt, res_rows_t b, res_rows_t c, res_dtype_t act_dt,
+                                  const float* gamma, const float* dt_bias, const float* skip, const float* h, void* y,
+                                  float* h_out, int64_t B, int64_t H, int64_t P, int64_t G, int64_t N, void* stream);
+
+/*
+ * Log probabilities of given tokens under softmax(scale logits), per row:
+ *   logp = scale logits[token] - log sum_j exp(scale logits[j])
+ *   entropy = -sum_j p_j log p_j   (a p_j of 0 adds nothing)
+ *   the `top` likeliest tokens, likeliest first (equal logits: the lowest token first), and their log probabilities
+ *   logits     R rows of V consecutive elements of dt, ld >= V elements apart; scale > 0
+ *   tokens     int64 [R]; below 0: an ignored position, whose logp is 0 and gives no gradient; V or more: logp is NaN
+ *   logp [R] float32;  stats [R][2] float32 or NULL: the row's largest logit and log sum_j exp(scale (logit - largest)),
+ *              for the backward;  entropy [R] float32 or NULL
+ *   top_ids int64, top_logp float32  [R][top], 0 <= top <= min(V, 64)
+ * A logit of -inf is a token that cannot come: its log probability is -inf.  A row whose logits are all -inf has log
+ * probabilities of -inf, entropy 0 and no gradient.  In a row with NaN or +inf the results are NaN (NaN ranks above all).
+ * Sums are float32.  R >= 0, V >= 1.  Outputs must not overlap inputs or each other.  Needs no workspace.
+ */
+#define RES_LOGPROBS_TOP_MAX 64
+int resonator_token_logprobs_fwd(const void* logits, int64_t ld, res_dtype_t dt, const int64_t* tokens, int64_t R, int64_t V,
+                                 float scale, float* logp, float* stats, float* entropy, int64_t top, int64_t* top_ids,
+                                 float* top_logp, void* stream);
+
+/*
+ * The logits' gradient for the loss sum(dlogp logp) + sum(dentropy entropy), p = softmax(scale logits):
+ *   dlogits_j = scale (dlogp (1{j = token} - p_j) - dentropy p_j (log p_j + entropy))
+ *   stats from the forward; entropy from the forward where dentropy is given
+ *   dlogp, dentropy [R] float32, each or NULL (zero); dlogits rows of dt, ldd elements apart (may be the logits
+ *   themselves, with ldd = ld).
+ */
+int resonator_token_logprobs_bwd(const void* logits, int64_t ld, res_dtype_t dt, const int64_t* tokens, int64_t R, int64_t V,
+                                 float scale, const float* stats, const float* entropy, const float* dlogp,
+                                 const float* dentropy, void* dlogits, int64_t ldd, void* stream);
+
+/*
  * Measurement hook.  Arms a pair of HIP events (hipEvent_t passed as void*) on the
  * calling thread: the next resonator_mix_fwd or resonator_mix_bwd call on this
  * thread records start_event immediately before and stop_event immediately after

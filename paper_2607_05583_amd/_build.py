@@ -23,7 +23,7 @@ BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libresonator.so")
 HOST = os.path.join(PKG, "_host.so")
 SOURCES = ["fwd.hip", "bwd.hip", "decode.hip", "epilogue.hip", "params.hip", "quadref.hip", "gemm.hip", "proj.hip", "fftref.hip", "gated.hip", "linear.hip", "adamw.hip",
-           "api.hip", "api_layer.hip"]
+           "conv.hip", "selective.hip", "logprobs.hip", "api.hip", "api_layer.hip", "api_select.hip"]
 ARCH = "gfx950"
 
 

@@ -19,6 +19,7 @@ RES_M_MAX = 16
 RES_GATED_CARRY = 128
 RES_ADAMW_BLOCK = 256
 RES_LINEAR_FAR = 1 << 21
+RES_LOGPROBS_TOP_MAX = 64
 
 SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd",
            "resonator_mix_bwd", "resonator_state_init", "resonator_decode_step",
@@ -38,7 +39,11 @@ SYMBOLS = ("resonator_version", "resonator_workspace_bytes", "resonator_mix_fwd"
            "resonator_gated_scan_workspace_bytes", "resonator_gated_scan_fwd", "resonator_gated_scan_bwd",
            "resonator_gated_scan_step",
            "resonator_linear_workspace_bytes", "resonator_linear_keeps_pre", "resonator_linear_fwd", "resonator_linear_bwd",
-           "resonator_adamw_step", "resonator_adamw_values")
+           "resonator_adamw_step", "resonator_adamw_values",
+           "resonator_short_conv_fwd", "resonator_short_conv_bwd", "resonator_short_conv_step", "resonator_short_conv_workspace_bytes",
+           "resonator_selective_scan_workspace_bytes", "resonator_selective_scan_carry_floats", "resonator_selective_scan_fwd",
+           "resonator_selective_scan_bwd", "resonator_selective_scan_step",
+           "resonator_token_logprobs_fwd", "resonator_token_logprobs_bwd")
 
 class Rows(ctypes.Structure):
     """res_rows_t / res_rows_out_t: rows of consecutive elements at p + b sb + t st."""
@@ -182,6 +187,31 @@ def _declare(lib):
                                          ctypes.POINTER(AdamWState), f64, f64, f64, f64, f64, i64, fp, vp]
     lib.resonator_adamw_values.restype = i32
     lib.resonator_adamw_values.argtypes = [ctypes.POINTER(AdamWState), i64, fp, fp, vp]
+    lib.resonator_short_conv_fwd.restype = i32
+    lib.resonator_short_conv_fwd.argtypes = [Rows, i32, fp, fp, i32, i64, vp, vp, vp, vp, i64, i64, i64, vp]
+    lib.resonator_short_conv_workspace_bytes.restype = sz
+    lib.resonator_short_conv_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.resonator_short_conv_bwd.restype = i32
+    lib.resonator_short_conv_bwd.argtypes = [Rows, Rows, i32, fp, fp, i32, i64, vp, vp, vp, Rows, fp, fp, vp, i64, i64, i64, vp,
+                                             sz, vp]
+    lib.resonator_short_conv_step.restype = i32
+    lib.resonator_short_conv_step.argtypes = [Rows, i32, fp, fp, i32, i64, vp, vp, vp, i64, i64, vp]
+    sizes = [i64] * 6
+    lib.resonator_selective_scan_workspace_bytes.restype = sz
+    lib.resonator_selective_scan_workspace_bytes.argtypes = [i32, i32, *sizes]
+    lib.resonator_selective_scan_carry_floats.restype = i64
+    lib.resonator_selective_scan_carry_floats.argtypes = [i32, *sizes]
+    lib.resonator_selective_scan_fwd.restype = i32
+    lib.resonator_selective_scan_fwd.argtypes = [Rows, Rows, Rows, Rows, i32, fp, fp, fp, fp, vp, vp, fp, fp, *sizes, vp, sz, vp]
+    lib.resonator_selective_scan_bwd.restype = i32
+    lib.resonator_selective_scan_bwd.argtypes = [Rows, Rows, Rows, Rows, Rows, i32, fp, fp, fp, fp, vp, fp, fp, Rows, Rows, Rows,
+                                                 Rows, fp, fp, fp, fp, *sizes, vp, sz, vp]
+    lib.resonator_selective_scan_step.restype = i32
+    lib.resonator_selective_scan_step.argtypes = [Rows, Rows, Rows, Rows, i32, fp, fp, fp, fp, vp, fp, i64, i64, i64, i64, i64, vp]
+    lib.resonator_token_logprobs_fwd.restype = i32
+    lib.resonator_token_logprobs_fwd.argtypes = [vp, i64, i32, vp, i64, i64, f32, fp, fp, fp, i64, vp, fp, vp]
+    lib.resonator_token_logprobs_bwd.restype = i32
+    lib.resonator_token_logprobs_bwd.argtypes = [vp, i64, i32, vp, i64, i64, f32, fp, fp, fp, fp, vp, i64, vp]
 
 
 def lib():

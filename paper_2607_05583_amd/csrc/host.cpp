@@ -879,6 +879,360 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------
+// The selective layer and the token probabilities
+// ---------------------------------------------------------------------------
+const int32_t* ip0(const Tensor* t) { return t ? static_cast<const int32_t*>(t->data_ptr()) : nullptr; }
+void* vp0(const Tensor* t) { return t ? t->data_ptr() : nullptr; }
+bool together(std::initializer_list<const Tensor*> ts) {  // on one GPU
+  const Tensor* first = nullptr;
+  for (const Tensor* t : ts) {
+    if (!t) continue;
+    if (!first) first = t;
+    if (t->device() != first->device()) return false;
+  }
+  return true;
+}
+
+struct Conv {
+  const Tensor *x, *w, *bias, *state;
+  int64_t B, L, D, K, act;
+  res_dtype_t dt;
+};
+// x and, in their order, w, bias, act code, state
+bool conv(PyObject* ox, PyObject* ow, PyObject* obias, PyObject* oact, PyObject* ostate, int dims, Conv* c) {
+  c->x = rows(ox);
+  c->w = plain(ow);
+  if (!c->x || !c->w || c->x->dim() != dims || code(*c->x) < 0 || c->w->dim() != 2 || !f32(*c->w) || !integer(oact, &c->act)) return false;
+  c->B = c->x->size(0);
+  c->L = dims == 3 ? c->x->size(1) : 1;
+  c->D = c->x->size(-1);
+  c->K = c->w->size(1);
+  c->dt = (res_dtype_t)code(*c->x);
+  return c->w->size(0) == c->D && c->K >= 1 && maybe(obias, at::kFloat, {c->D}, &c->bias) &&
+         maybe(ostate, c->x->scalar_type(), {c->B, c->K - 1, c->D}, &c->state) && together({c->x, c->w, c->bias, c->state});
+}
+
+// (x, w, bias, act code, state, lengths, return_state, out, state_out) -> y, or (y, the last inputs)
+PyObject* short_conv_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Conv c;
+  const Tensor *len, *out, *so;
+  bool want;
+  if (n != 9 || !conv(a[0], a[1], a[2], a[3], a[4], 3, &c) || !maybe(a[5], at::kInt, {c.B}, &len) || !truth(a[6], &want) ||
+      !maybe(a[7], c.x->scalar_type(), c.x->sizes(), &out) || !maybe(a[8], c.x->scalar_type(), {c.B, c.K - 1, c.D}, &so) ||
+      !together({c.x, len, out, so}))
+    return none();
+  const Tensor y = out ? *out : empty({c.B, c.L, c.D}, *c.x, c.x->scalar_type());
+  Tensor last;
+  if (so) last = *so;
+  else if (want) last = empty({c.B, c.K - 1, c.D}, *c.x, c.x->scalar_type());
+  const OnDevice on(*c.x);
+  const int rc = call([&] {
+    return resonator_short_conv_fwd(as_rows(*c.x), c.dt, fp(*c.w), fp0(c.bias), (int)c.act, c.K, vp0(c.state), ip0(len), y.data_ptr(),
+                                    last.defined() ? last.data_ptr() : nullptr, c.B, c.L, c.D, on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({out, so});
+  return want ? pack({y, last}) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, w, dy, bias, act code, state, lengths, dstate_out, want_dstate, out, ws) -> (dx, dw, dbias, dstate or None)
+PyObject* short_conv_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Conv c;
+  const Tensor *len, *dso, *out = nullptr, *given;
+  bool want;
+  if (n != 11 || !conv(a[0], a[1], a[3], a[4], a[5], 3, &c) || !maybe(a[6], at::kInt, {c.B}, &len) ||
+      !maybe(a[7], c.x->scalar_type(), {c.B, c.K - 1, c.D}, &dso) || !truth(a[8], &want))
+    return none();
+  const Tensor* dy = rows(a[2]);
+  if (!dy || dy->sizes() != c.x->sizes() || dy->scalar_type() != c.x->scalar_type()) return none();
+  if (a[9] != Py_None) {
+    out = rows(a[9]);
+    if (!out || out->sizes() != c.x->sizes() || out->scalar_type() != c.x->scalar_type()) return none();
+  }
+  given = a[10] == Py_None ? nullptr : plain(a[10]);
+  if ((a[10] != Py_None && !given) || !together({c.x, len, dso, dy, out, given})) return none();
+  Tensor ws, dstate;
+  if (given) {
+    ws = *given;
+  } else {
+    const size_t nb = resonator_short_conv_workspace_bytes(c.B, c.L, c.D, c.K);
+    if (nb == 0) return none();
+    ws = empty({(int64_t)nb}, *c.x, at::kByte);
+  }
+  const Tensor dx = out ? *out : empty({c.B, c.L, c.D}, *c.x, c.x->scalar_type()), dw = empty({c.D, c.K}, *c.x, at::kFloat),
+               db = empty({c.D}, *c.x, at::kFloat);
+  if (want) dstate = empty({c.B, c.K - 1, c.D}, *c.x, c.x->scalar_type());
+  const OnDevice on(*c.x);
+  const int rc = call([&] {
+    return resonator_short_conv_bwd(as_rows(*c.x), as_rows(*dy), c.dt, fp(*c.w), fp0(c.bias), (int)c.act, c.K, vp0(c.state), ip0(len),
+                                    vp0(dso), as_rows_out(dx), fpm(dw), fpm(db), want ? dstate.data_ptr() : nullptr, c.B, c.L, c.D,
+                                    ws.data_ptr(), bytes(ws), on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({out});
+  return pack({dx, dw, db, dstate});
+  END_HANDLE_TH_ERRORS
+}
+
+// (x_t, w, state, bias, act code, state_out, out) -> y_t
+PyObject* short_conv_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Conv c;
+  const Tensor *so, *out;
+  if (n != 7 || a[2] == Py_None || !conv(a[0], a[1], a[3], a[4], a[2], 2, &c) ||
+      !maybe(a[5], c.x->scalar_type(), {c.B, c.K - 1, c.D}, &so) || !maybe(a[6], c.x->scalar_type(), c.x->sizes(), &out) ||
+      !together({c.x, so, out}))
+    return none();
+  const Tensor y = out ? *out : empty({c.B, c.D}, *c.x, c.x->scalar_type());
+  const OnDevice on(*c.x);
+  const int rc = call([&] {
+    return resonator_short_conv_step(as_rows(*c.x), c.dt, fp(*c.w), fp0(c.bias), (int)c.act, c.K, c.state->data_ptr(), y.data_ptr(),
+                                     (so ? so : c.state)->data_ptr(), c.B, c.D, on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({so ? so : c.state, out});
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// A tensor [B(, L), heads, n] whose last two dimensions are consecutive.
+const Tensor* heads(PyObject* o, int dims) {
+  const Tensor* t = rows(o);
+  return t && t->dim() == dims && (t->size(-2) <= 1 || t->stride(-2) == t->size(-1)) ? t : nullptr;
+}
+res_rows_t as_heads(const Tensor& t) { return res_rows_t{t.data_ptr(), t.stride(0), t.dim() == 4 ? t.stride(1) : 0}; }
+res_rows_out_t as_heads_out(const Tensor& t) { return res_rows_out_t{t.data_ptr(), t.stride(0), t.stride(1)}; }
+
+struct Selective {
+  const Tensor *x, *dt, *b, *c, *gamma, *bias, *skip;
+  int64_t B, L, H, P, G, N;
+  res_dtype_t code;
+};
+// (x, dt, b, c, gamma), dt_bias and skip
+bool selective(PyObject* const* a, PyObject* obias, PyObject* oskip, int dims, Selective* s) {
+  s->x = heads(a[0], dims);
+  s->dt = rows(a[1]);
+  s->b = heads(a[2], dims);
+  s->c = heads(a[3], dims);
+  s->gamma = plain(a[4]);
+  if (!s->x || !s->dt || !s->b || !s->c || !s->gamma || code(*s->x) < 0 || s->dt->dim() != dims - 1) return false;
+  for (const Tensor* t : {s->dt, s->b, s->c})
+    if (t->scalar_type() != s->x->scalar_type() || t->size(0) != s->x->size(0) || (dims == 4 && t->size(1) != s->x->size(1))) return false;
+  s->B = s->x->size(0);
+  s->L = dims == 4 ? s->x->size(1) : 1;
+  s->H = s->x->size(-2);
+  s->P = s->x->size(-1);
+  s->G = s->b->size(-2);
+  s->N = s->b->size(-1);
+  s->code = (res_dtype_t)code(*s->x);
+  return s->dt->size(-1) == s->H && s->c->sizes() == s->b->sizes() && f32(*s->gamma) && shape(*s->gamma, {s->H}) &&
+         maybe(obias, at::kFloat, {s->H}, &s->bias) && maybe(oskip, at::kFloat, {s->H}, &s->skip) &&
+         together({s->x, s->dt, s->b, s->c, s->gamma, s->bias, s->skip});
+}
+bool selective_ws(PyObject* o, int backward, const Selective& s, Tensor* ws) {
+  if (o != Py_None) {
+    const Tensor* w = plain(o);
+    if (!w || w->device() != s.x->device()) return false;
+    *ws = *w;
+    return true;
+  }
+  const size_t nb = resonator_selective_scan_workspace_bytes(backward, s.code, s.B, s.L, s.H, s.P, s.G, s.N);
+  *ws = empty({(int64_t)(nb > 256 ? nb : 256)}, *s.x, at::kByte);
+  return true;
+}
+
+// (x, dt, b, c, gamma, dt_bias, skip, h0, lengths, return_state, save, out, ws, h_out) -> y, or a tuple of y, the state and the carry
+PyObject* selective_scan_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Selective s;
+  const Tensor *h0, *len, *out, *ho;
+  bool want, save;
+  if (n != 14 || !selective(a, a[5], a[6], 4, &s) || !maybe(a[7], at::kFloat, {s.B, s.H, s.P, s.N}, &h0) ||
+      !maybe(a[8], at::kInt, {s.B}, &len) || !truth(a[9], &want) || !truth(a[10], &save) ||
+      !maybe(a[11], s.x->scalar_type(), s.x->sizes(), &out) || !maybe(a[13], at::kFloat, {s.B, s.H, s.P, s.N}, &ho) ||
+      !together({s.x, h0, len, out, ho}))
+    return none();
+  const int64_t floats = resonator_selective_scan_carry_floats(s.code, s.B, s.L, s.H, s.P, s.G, s.N);
+  Tensor ws, h, carry;
+  if (floats < 0 || !selective_ws(a[12], 0, s, &ws)) return none();
+  const Tensor y = out ? *out : empty({s.B, s.L, s.H, s.P}, *s.x, s.x->scalar_type());
+  if (ho) h = *ho;
+  else if (want) h = empty({s.B, s.H, s.P, s.N}, *s.x, at::kFloat);
+  if (save) carry = empty({floats}, *s.x, at::kFloat);
+  const OnDevice on(*s.x);
+  const int rc = call([&] {
+    return resonator_selective_scan_fwd(as_heads(*s.x), as_rows(*s.dt), as_heads(*s.b), as_heads(*s.c), s.code, fp(*s.gamma), fp0(s.bias),
+                                        fp0(s.skip), fp0(h0), ip0(len), y.data_ptr(), h.defined() ? fpm(h) : nullptr,
+                                        floats > 0 && save ? fpm(carry) : nullptr, s.B, s.L, s.H, s.P, s.G, s.N, ws.data_ptr(), bytes(ws),
+                                        on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({out, ho});
+  if (want) return save ? pack({y, h, carry}) : pack({y, h});
+  return save ? pack({y, carry}) : THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+// (x, dt, b, c, gamma, dy, dt_bias, skip, h0, lengths, dh_out, carry, want_dh0, out, ws) -> the gradients, dh0 or None last
+PyObject* selective_scan_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Selective s;
+  const Tensor *h0, *len, *dh, *carry;
+  bool want;
+  if (n != 15 || !selective(a, a[6], a[7], 4, &s) || !truth(a[12], &want) || a[11] == Py_None) return none();
+  const int64_t floats = resonator_selective_scan_carry_floats(s.code, s.B, s.L, s.H, s.P, s.G, s.N);
+  const Tensor* dy = heads(a[5], 4);
+  if (floats < 0 || !dy || dy->sizes() != s.x->sizes() || dy->scalar_type() != s.x->scalar_type() ||
+      !maybe(a[8], at::kFloat, {s.B, s.H, s.P, s.N}, &h0) || !maybe(a[9], at::kInt, {s.B}, &len) ||
+      !maybe(a[10], at::kFloat, {s.B, s.H, s.P, s.N}, &dh) || !maybe(a[11], at::kFloat, {floats}, &carry) ||
+      !together({s.x, dy, h0, len, dh, carry}))
+    return none();
+  const Tensor* in[4] = {s.x, s.dt, s.b, s.c};
+  Tensor o[4], ws, dh0;
+  if (a[13] != Py_None) {
+    if (!PyTuple_CheckExact(a[13]) && !PyList_CheckExact(a[13])) return none();
+    if (PySequence_Fast_GET_SIZE(a[13]) != 4) return none();
+    for (int k = 0; k < 4; ++k) {
+      PyObject* v = PySequence_Fast_GET_ITEM(a[13], k);
+      const Tensor* t = k == 1 ? rows(v) : heads(v, 4);
+      if (!t || t->sizes() != in[k]->sizes() || t->scalar_type() != s.x->scalar_type() || t->device() != s.x->device()) return none();
+      o[k] = *t;
+    }
+  } else {
+    for (int k = 0; k < 4; ++k) o[k] = empty(in[k]->sizes(), *s.x, s.x->scalar_type());
+  }
+  if (!selective_ws(a[14], 1, s, &ws)) return none();
+  const Tensor dg = empty({s.H}, *s.x, at::kFloat), db = empty({s.H}, *s.x, at::kFloat), ds = empty({s.H}, *s.x, at::kFloat);
+  if (want) dh0 = empty({s.B, s.H, s.P, s.N}, *s.x, at::kFloat);
+  const OnDevice on(*s.x);
+  const int rc = call([&] {
+    return resonator_selective_scan_bwd(as_heads(*s.x), as_rows(*s.dt), as_heads(*s.b), as_heads(*s.c), as_heads(*dy), s.code,
+                                        fp(*s.gamma), fp0(s.bias), fp0(s.skip), fp0(h0), ip0(len), floats > 0 ? fp(*carry) : nullptr,
+                                        fp0(dh), as_heads_out(o[0]), as_rows_out(o[1]), as_heads_out(o[2]), as_heads_out(o[3]), fpm(dg),
+                                        fpm(db), fpm(ds), want ? fpm(dh0) : nullptr, s.B, s.L, s.H, s.P, s.G, s.N, ws.data_ptr(),
+                                        bytes(ws), on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  if (a[13] != Py_None) written({&o[0], &o[1], &o[2], &o[3]});
+  return pack({o[0], o[1], o[2], o[3], dg, db, ds, dh0});
+  END_HANDLE_TH_ERRORS
+}
+
+// (x_t, dt_t, b_t, c_t, gamma, h, dt_bias, skip, h_out, out) -> y_t
+PyObject* selective_scan_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Selective s;
+  const Tensor *h, *ho, *out;
+  if (n != 10 || !selective(a, a[6], a[7], 3, &s) || a[5] == Py_None || !maybe(a[5], at::kFloat, {s.B, s.H, s.P, s.N}, &h) ||
+      !maybe(a[8], at::kFloat, {s.B, s.H, s.P, s.N}, &ho) || !maybe(a[9], s.x->scalar_type(), s.x->sizes(), &out) ||
+      !together({s.x, h, ho, out}))
+    return none();
+  const Tensor y = out ? *out : empty({s.B, s.H, s.P}, *s.x, s.x->scalar_type());
+  const OnDevice on(*s.x);
+  const int rc = call([&] {
+    return resonator_selective_scan_step(as_heads(*s.x), as_rows(*s.dt), as_heads(*s.b), as_heads(*s.c), s.code, fp(*s.gamma),
+                                         fp0(s.bias), fp0(s.skip), fp(*h), y.data_ptr(), fpm(ho ? *ho : *h), s.B, s.H, s.P, s.G, s.N,
+                                         on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({ho ? ho : h, out});
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+struct Logits {
+  const Tensor *x, *tokens;
+  int64_t R, V, ld;
+  float scale;
+};
+// contiguous logits [..., V], or [R, V] with rows apart; tokens [...]
+bool logits_of(PyObject* ox, PyObject* otok, PyObject* oscale, Logits* l) {
+  l->x = rows(ox);
+  l->tokens = plain(otok);
+  if (!l->x || !l->tokens || code(*l->x) < 0 || l->tokens->scalar_type() != at::kLong || l->tokens->dim() != l->x->dim() - 1 ||
+      l->tokens->sizes() != l->x->sizes().slice(0, l->x->dim() - 1) || !number(oscale, &l->scale) || !together({l->x, l->tokens}))
+    return false;
+  l->V = l->x->size(-1);
+  if (l->V < 1) return false;
+  l->R = l->tokens->numel();
+  l->ld = l->V;
+  if (!l->x->is_contiguous()) {
+    if (l->x->dim() != 2 || l->x->stride(0) < l->V) return false;
+    l->ld = l->x->stride(0);
+  }
+  return true;
+}
+
+// (logits, tokens, top, entropy, scale) -> (logp, entropy or None, top_ids or None, top_logp or None, stats)
+PyObject* token_logprobs_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Logits l;
+  int64_t top;
+  bool ent;
+  if (n != 5 || !logits_of(a[0], a[1], a[4], &l) || !integer(a[2], &top) || !truth(a[3], &ent) || top < 0 || top > RES_LOGPROBS_TOP_MAX ||
+      top > l.V)
+    return none();
+  const auto s = l.tokens->sizes().vec();
+  auto s2 = s, st = s;
+  s2.push_back(2);
+  st.push_back(top);
+  const Tensor logp = empty(s, *l.x, at::kFloat), stats = empty(s2, *l.x, at::kFloat);
+  Tensor entropy, ids, tlp;
+  if (ent) entropy = empty(s, *l.x, at::kFloat);
+  if (top > 0) {
+    ids = empty(st, *l.x, at::kLong);
+    tlp = empty(st, *l.x, at::kFloat);
+  }
+  const OnDevice on(*l.x);
+  const int rc = call([&] {
+    return resonator_token_logprobs_fwd(l.x->data_ptr(), l.ld, (res_dtype_t)code(*l.x), static_cast<const int64_t*>(l.tokens->data_ptr()),
+                                        l.R, l.V, l.scale, fpm(logp), fpm(stats), ent ? fpm(entropy) : nullptr, top,
+                                        top > 0 ? static_cast<int64_t*>(ids.data_ptr()) : nullptr, top > 0 ? fpm(tlp) : nullptr,
+                                        on.stream);
+  });
+  return rc ? PyLong_FromLong(rc) : pack({logp, entropy, ids, tlp, stats});
+  END_HANDLE_TH_ERRORS
+}
+
+// (logits, tokens, stats, entropy, dlogp, dentropy, scale, out) -> dlogits
+PyObject* token_logprobs_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  Logits l;
+  const Tensor *stats, *entropy, *dl, *de, *out = nullptr;
+  if (n != 8 || !logits_of(a[0], a[1], a[6], &l) || a[2] == Py_None) return none();
+  const auto s = l.tokens->sizes().vec();
+  auto s2 = s;
+  s2.push_back(2);
+  if (!maybe(a[2], at::kFloat, s2, &stats) || !maybe(a[3], at::kFloat, s, &entropy) || !maybe(a[4], at::kFloat, s, &dl) ||
+      !maybe(a[5], at::kFloat, s, &de) || (de && !entropy))
+    return none();
+  int64_t ldd = l.V;
+  if (a[7] != Py_None) {
+    out = rows(a[7]);
+    if (!out || out->sizes() != l.x->sizes() || out->scalar_type() != l.x->scalar_type()) return none();
+    if (!out->is_contiguous()) {
+      if (out->dim() != 2 || out->stride(0) < l.V) return none();
+      ldd = out->stride(0);
+    }
+  }
+  if (!together({l.x, stats, entropy, dl, de, out})) return none();
+  const Tensor dx = out ? *out : empty(l.x->sizes(), *l.x, l.x->scalar_type());
+  const OnDevice on(*l.x);
+  const int rc = call([&] {
+    return resonator_token_logprobs_bwd(l.x->data_ptr(), l.ld, (res_dtype_t)code(*l.x), static_cast<const int64_t*>(l.tokens->data_ptr()),
+                                        l.R, l.V, l.scale, fp(*stats), de ? fp(*entropy) : nullptr, fp0(dl), fp0(de), dx.data_ptr(), ldd,
+                                        on.stream);
+  });
+  if (rc) return PyLong_FromLong(rc);
+  written({out});
+  return THPVariable_Wrap(dx);
+  END_HANDLE_TH_ERRORS
+}
+
 #define RES_FN(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RES_FN("mix_fwd", mix_fwd),
                          RES_FN("mix_bwd", mix_bwd),
@@ -900,6 +1254,14 @@ PyMethodDef methods[] = {RES_FN("mix_fwd", mix_fwd),
                          RES_FN("linear_fwd", linear_fwd),
                          RES_FN("linear_bwd", linear_bwd),
                          RES_FN("adamw_step", adamw_step),
+                         RES_FN("short_conv_fwd", short_conv_fwd),
+                         RES_FN("short_conv_bwd", short_conv_bwd),
+                         RES_FN("short_conv_step", short_conv_step),
+                         RES_FN("selective_scan_fwd", selective_scan_fwd),
+                         RES_FN("selective_scan_bwd", selective_scan_bwd),
+                         RES_FN("selective_scan_step", selective_scan_step),
+                         RES_FN("token_logprobs_fwd", token_logprobs_fwd),
+                         RES_FN("token_logprobs_bwd", token_logprobs_bwd),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "Native marshalling of the hot entry points.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -1022,7 +1022,7 @@ def _rows(t, name, dtype, shape):
         raise ValueError(f"{name} must be on the GPU (got {t.device})")
     if t.dtype != dtype or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {dtype} {list(shape)} (got {t.dtype} {list(t.shape)})")
-    if t.dim() and t.shape[-1] > 1 and t.stride(-1) != 1:
+    if t.numel() and t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError(f"{name}'s last dimension must be consecutive in memory")
     return _lib.Rows(t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 3 else 0)
 
@@ -1587,3 +1587,579 @@ def resonator_gated_layer(x, p, h0=None, lengths=None, act="gelu_tanh"):
     if not _needs_graph(x, h0, *p):
         return resonator_gated_layer_fwd(x, p, h0=h0, lengths=lengths, act=act, return_state=True)
     return GatedLayerFunction.apply(x, h0, lengths, act, *p)
+
+
+# ---------------------------------------------------------------------------
+# Selective layer: short causal convolution
+# ---------------------------------------------------------------------------
+def _together(*tensors):
+    """Refuses tensors of several GPUs; the context in which theirs is the current one."""
+    devices = {t.device for t in tensors if isinstance(t, torch.Tensor)}
+    if len(devices) > 1:
+        raise ValueError(f"the tensors must be on one device (got {', '.join(sorted(map(str, devices)))})")
+    return torch.cuda.device(devices.pop())
+
+
+def _conv_inputs(x, w, bias, state, dims):
+    if not isinstance(x, torch.Tensor) or x.dim() != dims:
+        raise ValueError(f"x must be a [{'B, L, D' if dims == 3 else 'B, D'}] tensor")
+    _code(x)
+    rows = _rows(x, "x", x.dtype, x.shape)
+    B, D = x.shape[0], x.shape[-1]
+    if not isinstance(w, torch.Tensor) or w.dim() != 2:
+        raise ValueError("w must be a float32 [D, K] tensor")
+    _f32(w, "w", (D, w.shape[1]))
+    _f32(bias, "bias", (D,))
+    _like(state, "state", x.dtype, (B, w.shape[1] - 1, D))
+    return rows, w.shape[1]
+
+
+def resonator_short_conv_fwd(x, w, bias=None, act="silu", state=None, lengths=None, return_state=False, out=None,
+                             state_out=None):
+    """Short causal convolution per channel: y_t = act(sum_k w[d, k] x_{t-k} + bias[d]).
+
+    x: [B, L, D], the last dimension consecutive (columns of a fused projection are taken as they are); w [D, K] and
+    bias [D] float32, K at most 16; ``act`` as resonator_linear_fwd's; ``state`` [B, K - 1, D] of x's type: the inputs
+    before the call, oldest first (None: zeros); ``lengths`` [B] int32: row b has its first lengths[b] steps.  Returns y;
+    with ``return_state`` also the K - 1 inputs before each row's end (written to ``state_out`` where given, which may be
+    the state itself)."""
+    code = _act_code(act)
+    done = (_NATIVE or _native()).short_conv_fwd(x, w, bias, code, state, lengths, return_state, out, state_out)
+    if done is not None:
+        return _done(done)
+    rows, K = _conv_inputs(x, w, bias, state, 3)
+    B, L, D = x.shape
+    _gated_lengths(lengths, B)
+    y = torch.empty((B, L, D), dtype=x.dtype, device=x.device) if out is None else _like(out, "out", x.dtype, x.shape)
+    given = out, state_out
+    if state_out is not None:
+        _like(state_out, "state_out", x.dtype, (B, K - 1, D))
+    elif return_state:
+        state_out = torch.empty((B, K - 1, D), dtype=x.dtype, device=x.device)
+    with _together(x, w, bias, state, lengths, out, state_out):
+        check(_lib.lib().resonator_short_conv_fwd(rows, _code(x), _ptr(w), _ptr(bias), code, K, _ptr(state), _ptr(lengths), _ptr(y),
+                                                  _ptr(state_out), B, L, D, _stream(x.device)))
+    _written(*given)
+    return (y, state_out) if return_state else y
+
+
+def resonator_short_conv_bwd(x, w, dy, bias=None, act="silu", state=None, lengths=None, dstate_out=None, want_dstate=False,
+                             out=None, ws=None):
+    """Gradients of sum(dy y) + sum(dstate_out state_out): dict with dx, dw, dbias (, dstate).  dy: [B, L, D] like x;
+    ``dstate_out`` [B, K - 1, D]: the gradient of the state that the forward returned.  ``out`` receives dx (it may be
+    columns of a wider tensor)."""
+    code = _act_code(act)
+    done = (_NATIVE or _native()).short_conv_bwd(x, w, dy, bias, code, state, lengths, dstate_out, want_dstate, out, ws)
+    if done is not None:
+        return {k: v for k, v in zip(("dx", "dw", "dbias", "dstate"), _done(done)) if v is not None}
+    rows, K = _conv_inputs(x, w, bias, state, 3)
+    B, L, D = x.shape
+    drows = _rows(dy, "dy", x.dtype, x.shape)
+    _gated_lengths(lengths, B)
+    _like(dstate_out, "dstate_out", x.dtype, (B, K - 1, D))
+    dx = torch.empty((B, L, D), dtype=x.dtype, device=x.device) if out is None else out
+    orows = _rows(dx, "out", x.dtype, x.shape)
+    dw, db = torch.empty_like(w), torch.empty((D,), dtype=torch.float32, device=x.device)
+    dstate = torch.empty((B, K - 1, D), dtype=x.dtype, device=x.device) if want_dstate else None
+    if ws is None:
+        n = int(_lib.lib().resonator_short_conv_workspace_bytes(B, L, D, K))
+        ws = torch.empty(n, dtype=torch.uint8, device=x.device)
+    _dev(ws, "ws")
+    with _together(x, w, dy, bias, state, lengths, dstate_out, out, ws):
+        check(_lib.lib().resonator_short_conv_bwd(
+            rows, drows, _code(x), _ptr(w), _ptr(bias), code, K, _ptr(state), _ptr(lengths), _ptr(dstate_out), orows, _ptr(dw),
+            _ptr(db), _ptr(dstate), B, L, D, _ptr(ws), ws.numel() * ws.element_size(), _stream(x.device)))
+    _written(out)
+    g = {"dx": dx, "dw": dw, "dbias": db}
+    if want_dstate:
+        g["dstate"] = dstate
+    return g
+
+
+def resonator_short_conv_step(x_t, w, state, bias=None, act="silu", state_out=None, out=None):
+    """One step: x_t [B, D], state [B, K - 1, D] of x_t's type, moved on in place unless ``state_out`` receives the new one;
+    returns y_t [B, D]."""
+    code = _act_code(act)
+    done = (_NATIVE or _native()).short_conv_step(x_t, w, state, bias, code, state_out, out)
+    if done is not None:
+        return _done(done)
+    if state is None:
+        raise TypeError("state must be a torch.Tensor")
+    rows, K = _conv_inputs(x_t, w, bias, state, 2)
+    B, D = x_t.shape
+    state_out = state if state_out is None else _like(state_out, "state_out", x_t.dtype, (B, K - 1, D))
+    y = torch.empty((B, D), dtype=x_t.dtype, device=x_t.device) if out is None else _like(out, "out", x_t.dtype, x_t.shape)
+    with _together(x_t, w, state, bias, state_out, out):
+        check(_lib.lib().resonator_short_conv_step(rows, _code(x_t), _ptr(w), _ptr(bias), code, K, _ptr(state), _ptr(y),
+                                                   _ptr(state_out), B, D, _stream(x_t.device)))
+    _written(state_out, out)
+    return y
+
+
+class ShortConvFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_short_conv_fwd (y and the last inputs) and resonator_short_conv_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, w, bias=None, act="silu", state=None, lengths=None):
+        y, last = resonator_short_conv_fwd(x, w, bias, act=act, state=state, lengths=lengths, return_state=True)
+        ctx.save_for_backward(x, w, bias, state, lengths)
+        ctx.act = act
+        ctx.set_materialize_grads(False)
+        return y, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dlast):
+        x, w, bias, state, lengths = ctx.saved_tensors
+        dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None else dy.contiguous()
+        g = resonator_short_conv_bwd(x, w, dy, bias, act=ctx.act, state=state, lengths=lengths,
+                                     dstate_out=None if dlast is None else dlast.contiguous(),
+                                     want_dstate=ctx.needs_input_grad[4])
+        return g["dx"], g["dw"], None if bias is None else g["dbias"], None, g.get("dstate"), None
+
+
+def resonator_short_conv(x, w, bias=None, act="silu", state=None, lengths=None):
+    """Differentiable short convolution: (y, the inputs before each row's end); x, w, bias and state receive gradients."""
+    if not _needs_graph(x, w, bias, state):
+        return resonator_short_conv_fwd(x, w, bias, act=act, state=state, lengths=lengths, return_state=True)
+    return ShortConvFunction.apply(x, w, bias, act, state, lengths)
+
+
+# ---------------------------------------------------------------------------
+# Selective layer: selective scan
+# ---------------------------------------------------------------------------
+def _heads(t, name, dtype, shape):
+    """A GPU tensor [B(, L), heads, n] whose last two dimensions are consecutive, as rows of the library."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU (got {t.device})")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {dtype} {list(shape)} (got {t.dtype} {list(t.shape)})")
+    if t.numel() and ((t.shape[-1] > 1 and t.stride(-1) != 1) or (t.shape[-2] > 1 and t.stride(-2) != t.shape[-1])):
+        raise ValueError(f"{name}'s last two dimensions must be consecutive in memory")
+    return _lib.Rows(t.data_ptr(), t.stride(0), t.stride(1) if t.dim() == 4 else 0)
+
+
+def _selective_inputs(x, dt, b, c, gamma, dt_bias, skip, dims):
+    """(rows of x, dt, b, c; (B, L, H, P, G, N))"""
+    lead = "B, L" if dims == 4 else "B"
+    if not isinstance(x, torch.Tensor) or x.dim() != dims:
+        raise ValueError(f"x must be a [{lead}, H, P] tensor")
+    if not isinstance(b, torch.Tensor) or b.dim() != dims:
+        raise ValueError(f"b must be a [{lead}, G, N] tensor")
+    _code(x)
+    H, P = x.shape[-2:]
+    G, N = b.shape[-2:]
+    head = tuple(x.shape[:-2])
+    rows = [_heads(x, "x", x.dtype, x.shape), _rows(dt, "dt", x.dtype, head + (H,)), _heads(b, "b", x.dtype, head + (G, N)),
+            _heads(c, "c", x.dtype, head + (G, N))]
+    if gamma is None:
+        raise TypeError("gamma must be a torch.Tensor")
+    for name, t in (("gamma", gamma), ("dt_bias", dt_bias), ("skip", skip)):
+        _f32(t, name, (H,))
+    return rows, (head[0], head[1] if dims == 4 else 1, H, P, G, N)
+
+
+def selective_scan_workspace(act_dtype, B, L, H, P, G, N, device, backward=True):
+    """A workspace of the selective scan's calls of these sizes on one stream; ``backward`` False: of the forward alone."""
+    n = max(int(_lib.lib().resonator_selective_scan_workspace_bytes(k, _DT[act_dtype], B, L, H, P, G, N))
+            for k in ((0, 1) if backward else (0,)))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _selective_ws(ws, backward, act_dtype, sizes, device):
+    if ws is None:
+        n = int(_lib.lib().resonator_selective_scan_workspace_bytes(backward, _DT[act_dtype], *sizes))
+        ws = torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+    return _dev(ws, "ws")
+
+
+def _selective_carry(act_dtype, sizes, device):
+    n = int(_lib.lib().resonator_selective_scan_carry_floats(_DT[act_dtype], *sizes))
+    return torch.empty(max(n, 0), dtype=torch.float32, device=device)
+
+
+def resonator_selective_scan_fwd(x, dt, b, c, gamma, dt_bias=None, skip=None, h0=None, lengths=None, return_state=False,
+                                 save=False, out=None, ws=None, h_out=None):
+    """Selective scan, per head a state [P, N]: D = softplus(dt_t + dt_bias), a = exp(-gamma D),
+    h_t = a h_{t-1} + D x_t b_t^T, y_t = h_t c_t + skip x_t.
+
+    x [B, L, H, P], dt [B, L, H], b and c [B, L, G, N] of one type, the last two dimensions consecutive (columns of a
+    projection are taken as they are); G divides H; P and N at most 128; gamma (>= 0), dt_bias, skip [H] and
+    h0 [B, H, P, N] float32; ``lengths`` [B] int32: row b has its first lengths[b] steps (y is 0 behind them, the state
+    stays, and what the inputs hold there does not matter).  Returns y; with ``return_state`` also the last state
+    (written to ``h_out`` where given, which may be h0 itself); with ``save`` also what resonator_selective_scan_bwd
+    starts from.  ``ws``: a selective_scan_workspace, else one is made for the call."""
+    done = (_NATIVE or _native()).selective_scan_fwd(x, dt, b, c, gamma, dt_bias, skip, h0, lengths, return_state, save, out, ws,
+                                                     h_out)
+    if done is not None:
+        return _done(done)
+    rows, sizes = _selective_inputs(x, dt, b, c, gamma, dt_bias, skip, 4)
+    B, L, H, P, G, N = sizes
+    _f32(h0, "h0", (B, H, P, N))
+    _gated_lengths(lengths, B)
+    y = torch.empty((B, L, H, P), dtype=x.dtype, device=x.device) if out is None else _like(out, "out", x.dtype, x.shape)
+    given = out, h_out
+    if h_out is not None:
+        _f32(h_out, "h_out", (B, H, P, N))
+    elif return_state:
+        h_out = torch.empty((B, H, P, N), dtype=torch.float32, device=x.device)
+    carry = _selective_carry(x.dtype, sizes, x.device) if save else None
+    ws = _selective_ws(ws, 0, x.dtype, sizes, x.device)
+    with _together(x, dt, b, c, gamma, dt_bias, skip, h0, lengths, out, ws, h_out):
+        check(_lib.lib().resonator_selective_scan_fwd(
+            *rows, _code(x), _ptr(gamma), _ptr(dt_bias), _ptr(skip), _ptr(h0), _ptr(lengths), _ptr(y), _ptr(h_out),
+            _ptr(carry) if save and carry.numel() else None, *sizes, _ptr(ws), ws.numel() * ws.element_size(), _stream(x.device)))
+    _written(*given)
+    r = (y,) + ((h_out,) if return_state else ()) + ((carry,) if save else ())
+    return r if len(r) > 1 else y
+
+
+def resonator_selective_scan_bwd(x, dt, b, c, gamma, dy, dt_bias=None, skip=None, h0=None, lengths=None, dh_out=None, carry=None,
+                                 want_dh0=False, out=None, ws=None):
+    """Gradients of sum(dy y) + sum(dh_out h_out): dict with dx, ddt, db, dc, dgamma, ddt_bias, dskip (, dh0).
+
+    ``carry``: what a forward with ``save`` on the same inputs returned, else it is computed again.  ``out`` = (dx, ddt, db,
+    dc) receives the gradients (they may be columns of one tensor)."""
+    done = (_NATIVE or _native()).selective_scan_bwd(x, dt, b, c, gamma, dy, dt_bias, skip, h0, lengths, dh_out, carry, want_dh0,
+                                                     out, ws)
+    names = ("dx", "ddt", "db", "dc", "dgamma", "ddt_bias", "dskip", "dh0")
+    if done is not None:
+        return {k: v for k, v in zip(names, _done(done)) if v is not None}
+    rows, sizes = _selective_inputs(x, dt, b, c, gamma, dt_bias, skip, 4)
+    B, L, H, P, G, N = sizes
+    drow = _heads(dy, "dy", x.dtype, x.shape)
+    _f32(h0, "h0", (B, H, P, N))
+    _f32(dh_out, "dh_out", (B, H, P, N))
+    _gated_lengths(lengths, B)
+    given = () if out is None else out
+    if out is None:
+        out = [torch.empty(t.shape, dtype=x.dtype, device=x.device) for t in (x, dt, b, c)]
+    dx, ddt, db, dc = out
+    orows = [_heads(dx, "dx", x.dtype, x.shape), _rows(ddt, "ddt", x.dtype, dt.shape), _heads(db, "db", x.dtype, b.shape),
+             _heads(dc, "dc", x.dtype, b.shape)]
+    lib = _lib.lib()
+    ws = _selective_ws(ws, 1, x.dtype, sizes, x.device)
+    here = _together(x, dt, b, c, gamma, dy, dt_bias, skip, h0, lengths, dh_out, carry, *out, ws)
+    n = int(lib.resonator_selective_scan_carry_floats(_code(x), *sizes))
+    if carry is not None:
+        _f32(carry, "carry", (max(n, 0),))
+    elif n > 0:
+        carry = _selective_carry(x.dtype, sizes, x.device)
+        with here:
+            check(lib.resonator_selective_scan_fwd(
+                *rows, _code(x), _ptr(gamma), _ptr(dt_bias), _ptr(skip), _ptr(h0), _ptr(lengths), None, None, _ptr(carry), *sizes,
+                _ptr(ws), ws.numel() * ws.element_size(), _stream(x.device)))
+    f32 = dict(dtype=torch.float32, device=x.device)
+    dgamma, dbias, dskip = (torch.empty((H,), **f32) for _ in range(3))
+    dh0 = torch.empty((B, H, P, N), **f32) if want_dh0 else None
+    with here:
+        check(lib.resonator_selective_scan_bwd(
+            *rows, drow, _code(x), _ptr(gamma), _ptr(dt_bias), _ptr(skip), _ptr(h0), _ptr(lengths), _ptr(carry) if n > 0 else None,
+            _ptr(dh_out), *orows, _ptr(dgamma), _ptr(dbias), _ptr(dskip), _ptr(dh0), *sizes, _ptr(ws),
+            ws.numel() * ws.element_size(), _stream(x.device)))
+    _written(*given)
+    return {k: v for k, v in zip(names, (dx, ddt, db, dc, dgamma, dbias, dskip, dh0)) if v is not None}
+
+
+def resonator_selective_scan_step(x_t, dt_t, b_t, c_t, gamma, h, dt_bias=None, skip=None, h_out=None, out=None):
+    """One step of the selective scan: x_t [B, H, P], dt_t [B, H], b_t and c_t [B, G, N], state h [B, H, P, N] float32,
+    advanced in place unless ``h_out`` receives the new one; returns y_t [B, H, P]."""
+    done = (_NATIVE or _native()).selective_scan_step(x_t, dt_t, b_t, c_t, gamma, h, dt_bias, skip, h_out, out)
+    if done is not None:
+        return _done(done)
+    rows, (B, _, H, P, G, N) = _selective_inputs(x_t, dt_t, b_t, c_t, gamma, dt_bias, skip, 3)
+    if h is None:
+        raise TypeError("h must be a torch.Tensor")
+    _f32(h, "h", (B, H, P, N))
+    h_out = h if h_out is None else _f32(h_out, "h_out", (B, H, P, N))
+    y = torch.empty((B, H, P), dtype=x_t.dtype, device=x_t.device) if out is None else _like(out, "out", x_t.dtype, x_t.shape)
+    with _together(x_t, dt_t, b_t, c_t, gamma, h, dt_bias, skip, h_out, out):
+        check(_lib.lib().resonator_selective_scan_step(*rows, _code(x_t), _ptr(gamma), _ptr(dt_bias), _ptr(skip), _ptr(h), _ptr(y),
+                                                       _ptr(h_out), B, H, P, G, N, _stream(x_t.device)))
+    _written(h_out, out)
+    return y
+
+
+class SelectiveScanFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_selective_scan_fwd (y and the last state) and resonator_selective_scan_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, dt, b, c, gamma, dt_bias=None, skip=None, h0=None, lengths=None):
+        y, h, carry = resonator_selective_scan_fwd(x, dt, b, c, gamma, dt_bias, skip, h0=h0, lengths=lengths, return_state=True,
+                                                   save=True)
+        ctx.save_for_backward(x, dt, b, c, gamma, dt_bias, skip, h0, lengths, carry)
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh):
+        x, dt, b, c, gamma, dt_bias, skip, h0, lengths, carry = ctx.saved_tensors
+        dy = torch.zeros_like(x, memory_format=torch.contiguous_format) if dy is None else dy.contiguous()
+        g = resonator_selective_scan_bwd(x, dt, b, c, gamma, dy, dt_bias, skip, h0=h0, lengths=lengths,
+                                         dh_out=None if dh is None else dh.contiguous(), carry=carry,
+                                         want_dh0=ctx.needs_input_grad[7])
+        return (g["dx"], g["ddt"], g["db"], g["dc"], g["dgamma"], None if dt_bias is None else g["ddt_bias"],
+                None if skip is None else g["dskip"], g.get("dh0"), None)
+
+
+def resonator_selective_scan(x, dt, b, c, gamma, dt_bias=None, skip=None, h0=None, lengths=None):
+    """Differentiable selective scan: (y, last state); x, dt, b, c, gamma, dt_bias, skip and h0 receive gradients."""
+    if not _needs_graph(x, dt, b, c, gamma, dt_bias, skip, h0):
+        return resonator_selective_scan_fwd(x, dt, b, c, gamma, dt_bias, skip, h0=h0, lengths=lengths, return_state=True)
+    return SelectiveScanFunction.apply(x, dt, b, c, gamma, dt_bias, skip, h0, lengths)
+
+
+# ---------------------------------------------------------------------------
+# Selective layer: projection, short convolution, selective scan, output projection, MLP
+# ---------------------------------------------------------------------------
+class SelectiveLayerParams(NamedTuple):
+    """One layer's tensors for H heads of P channels and G groups of N states, C = H P + 2 G N: Wp [d, C + H] (the drive, b, c
+    and the steps' logits side by side), Wo [H P, d], W1 [d, f], W2 [f, d] of the activations' type; bp [C + H], the
+    convolution's w [C, K] and wb [C], gamma, dt_bias, skip [H], bo [d], b1 [f], b2 [d] float32."""
+
+    Wp: torch.Tensor
+    bp: torch.Tensor
+    w: torch.Tensor
+    wb: torch.Tensor
+    gamma: torch.Tensor
+    dt_bias: torch.Tensor
+    skip: torch.Tensor
+    Wo: torch.Tensor
+    bo: torch.Tensor
+    W1: torch.Tensor
+    b1: torch.Tensor
+    W2: torch.Tensor
+    b2: torch.Tensor
+
+    def split(self, v, groups):
+        """The drive [..., H, P], b and c [..., G, N] of the convolution's columns [..., C]."""
+        H, HP, C = self.gamma.shape[0], self.Wo.shape[0], self.w.shape[0]
+        if HP % H or (C - HP) % (2 * groups) or C <= HP:
+            raise ValueError(f"{C} columns are not {H} heads of {HP // H} and b and c of {groups} groups")
+        x, b, c = v.split((HP, (C - HP) // 2, (C - HP) // 2), dim=-1)
+        return x.unflatten(-1, (H, HP // H)), b.unflatten(-1, (groups, -1)), c.unflatten(-1, (groups, -1))
+
+
+class SelectiveState(NamedTuple):
+    """What a selective layer carries from token to token: the convolution's last inputs [B, K - 1, C] of the activations'
+    type and the scan's state [B, H, P, N] float32."""
+
+    conv: torch.Tensor
+    h: torch.Tensor
+
+
+def resonator_selective_layer_fwd(x, p, groups=1, state=None, lengths=None, act="gelu_tanh", return_state=False, save=False, ws=None):
+    """A selective layer: of u = x Wp + bp, v = silu(short convolution of u's first C columns), y = selective scan of v's columns
+    with steps from u's last H, z = x + y Wo + bo, out = z + act(z W1 + b1) W2 + b2.  x [B, L, d]; ``p`` a
+    SelectiveLayerParams; ``state`` a SelectiveState (None: nothing came before).  The lengths are the convolution's and the
+    scan's alone, as in resonator_gated_layer_fwd.  Returns out; with ``return_state`` also the SelectiveState behind each
+    row's last step, from which resonator_selective_layer_step goes on; with ``save`` also the dict for
+    resonator_selective_layer_bwd."""
+    C = p.w.shape[0]
+    first, h0 = (None, None) if state is None else state
+    u = resonator_linear_fwd(x, p.Wp, p.bp)
+    v, last = resonator_short_conv_fwd(u[..., :C], p.w, p.wb, state=first, lengths=lengths, return_state=True)
+    vx, vb, vc = p.split(v, groups)
+    keep = resonator_selective_scan_fwd(vx, u[..., C:], vb, vc, p.gamma, p.dt_bias, p.skip, h0=h0, lengths=lengths,
+                                        return_state=True, save=save, ws=ws)
+    y, h = keep[0].flatten(-2), keep[1]
+    z = resonator_linear_fwd(y, p.Wo, p.bo, residual=x)
+    m, pre = resonator_linear_fwd(z, p.W1, p.b1, act=act, save=True) if save else (
+        resonator_linear_fwd(z, p.W1, p.b1, act=act), None)
+    out = resonator_linear_fwd(m, p.W2, p.b2, residual=z)
+    r = (out,) + ((SelectiveState(last, h),) if return_state else ()) + (
+        (dict(u=u, v=v, y=y, carry=keep[2], z=z, m=m, pre=pre),) if save else ())
+    return r if len(r) > 1 else out
+
+
+def resonator_selective_layer_bwd(x, p, dout, saved, groups=1, state=None, lengths=None, dstate=None, act="gelu_tanh",
+                                  want_dstate=False, ws=None):
+    """Gradients of sum(dout out) + sum(dstate state): dict with dx, ``dp`` (a SelectiveLayerParams: weights of the activations'
+    type, the rest float32) and, where wanted, ``dstate`` (a SelectiveState: of the state before the call).  ``saved`` is what
+    the forward with ``save`` returned."""
+    u, v, C = saved["u"], saved["v"], p.w.shape[0]
+    first, h0 = (None, None) if state is None else state
+    dlast, dh = (None, None) if dstate is None else dstate
+    g2 = resonator_linear_bwd(saved["m"], p.W2, dout, want_db=True)
+    g1 = resonator_linear_bwd(saved["z"], p.W1, g2["dx"], pre=saved["pre"], act=act, residual=dout, want_db=True)
+    go = resonator_linear_bwd(saved["y"], p.Wo, g1["dx"], want_db=True)
+    du, dv = torch.empty_like(u), torch.empty_like(v)
+    vx, vb, vc = p.split(v, groups)
+    dx, db, dc = p.split(dv, groups)
+    gs = resonator_selective_scan_bwd(vx, u[..., C:], vb, vc, p.gamma, go["dx"].view(vx.shape), p.dt_bias, p.skip, h0=h0,
+                                      lengths=lengths, dh_out=dh, carry=saved["carry"], want_dh0=want_dstate,
+                                      out=(dx, du[..., C:], db, dc), ws=ws)
+    gc = resonator_short_conv_bwd(u[..., :C], p.w, dv, p.wb, state=first, lengths=lengths, dstate_out=dlast,
+                                  want_dstate=want_dstate, out=du[..., :C])
+    gp = resonator_linear_bwd(x, p.Wp, du, residual=g1["dx"], want_db=True)
+    r = {"dx": gp["dx"], "dp": SelectiveLayerParams(gp["dW"], gp["db"], gc["dw"], gc["dbias"], gs["dgamma"], gs["ddt_bias"],
+                                                    gs["dskip"], go["dW"], go["db"], g1["dW"], g1["db"], g2["dW"], g2["db"])}
+    if want_dstate:
+        r["dstate"] = SelectiveState(gc["dstate"], gs["dh0"])
+    return r
+
+
+def resonator_selective_layer_step(x_t, p, state, groups=1, act="gelu_tanh", state_out=None):
+    """The layer for one token of every sequence: x_t [B, d], ``state`` a SelectiveState, advanced in place unless ``state_out``
+    receives the new one; returns [B, d].  Six launches; a caller may capture them into a graph."""
+    C = p.w.shape[0]
+    conv_out, h_out = (None, None) if state_out is None else state_out
+    u = resonator_linear_fwd(x_t, p.Wp, p.bp)
+    v = resonator_short_conv_step(u[..., :C], p.w, state.conv, p.wb, state_out=conv_out)
+    vx, vb, vc = p.split(v, groups)
+    y = resonator_selective_scan_step(vx, u[..., C:], vb, vc, p.gamma, state.h, p.dt_bias, p.skip, h_out=h_out)
+    z = resonator_linear_fwd(y.flatten(-2), p.Wo, p.bo, residual=x_t)
+    m = resonator_linear_fwd(z, p.W1, p.b1, act=act)
+    return resonator_linear_fwd(m, p.W2, p.b2, residual=z)
+
+
+class SelectiveLayerFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_selective_layer_fwd (the output and both parts of the last state) and
+    resonator_selective_layer_bwd."""
+
+    @staticmethod
+    def forward(ctx, x, first, h0, lengths, groups, act, *p):
+        p = SelectiveLayerParams(*p)
+        ctx.started = first is not None
+        state = SelectiveState(first, h0) if ctx.started else None
+        out, last, saved = resonator_selective_layer_fwd(x, p, groups, state=state, lengths=lengths, act=act, return_state=True,
+                                                         save=True)
+        pre = saved.pop("pre")
+        ctx.names, ctx.act, ctx.groups = tuple(saved), act, groups
+        ctx.save_for_backward(x, first, h0, lengths, pre.pre, *p, *saved.values())
+        ctx.set_materialize_grads(False)
+        return out, last.conv, last.h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dout, dlast, dh):
+        x, first, h0, lengths, pre, *rest = ctx.saved_tensors
+        n = len(SelectiveLayerParams._fields)
+        p, saved = SelectiveLayerParams(*rest[:n]), dict(zip(ctx.names, rest[n:]))
+        saved["pre"] = LinearSaved(pre, p.b1)
+        dout = torch.zeros_like(x, memory_format=torch.contiguous_format) if dout is None else dout.contiguous()
+        want = ctx.started and (ctx.needs_input_grad[1] or ctx.needs_input_grad[2])
+        g = resonator_selective_layer_bwd(x, p, dout, saved, ctx.groups, state=SelectiveState(first, h0) if ctx.started else None,
+                                          lengths=lengths, dstate=SelectiveState(*(None if t is None else t.contiguous() for t in (dlast, dh))),
+                                          act=ctx.act, want_dstate=want)
+        back = g["dstate"] if want else (None, None)
+        return g["dx"], *back, None, None, None, *g["dp"]
+
+
+def resonator_selective_layer(x, p, groups=1, state=None, lengths=None, act="gelu_tanh"):
+    """Differentiable selective layer: (out, SelectiveState behind the last steps); x, the state and p's tensors receive
+    gradients."""
+    first, h0 = (None, None) if state is None else state
+    if not _needs_graph(x, first, h0, *p):
+        return resonator_selective_layer_fwd(x, p, groups, state=state, lengths=lengths, act=act, return_state=True)
+    out, last, h = SelectiveLayerFunction.apply(x, first, h0, lengths, groups, act, *p)
+    return out, SelectiveState(last, h)
+
+
+# ---------------------------------------------------------------------------
+# Log probabilities of tokens
+# ---------------------------------------------------------------------------
+class TokenLogprobs(NamedTuple):
+    """logp [...] float32; entropy [...] float32, top_ids [..., top] int64 and top_logp [..., top] float32 or None; stats
+    [..., 2] float32: the largest logit and log sum exp(scale (logit - largest)), which the backward starts from."""
+
+    logp: torch.Tensor
+    entropy: torch.Tensor | None
+    top_ids: torch.Tensor | None
+    top_logp: torch.Tensor | None
+    stats: torch.Tensor
+
+
+def _logits(logits, tokens):
+    R, ld = _rows2(logits, "logits")
+    _dev(tokens, "tokens")
+    if tokens.dtype != torch.int64 or tuple(tokens.shape) != tuple(logits.shape[:-1]):
+        raise ValueError(f"tokens must be int64 {list(logits.shape[:-1])} (got {tokens.dtype} {list(tokens.shape)})")
+    if tokens.device != logits.device:
+        raise ValueError("tokens must be on the logits' device")
+    return R, ld
+
+
+def resonator_token_logprobs_fwd(logits, tokens, top=0, entropy=False, scale=1.0):
+    """Log probabilities of given tokens under softmax(scale logits), with the entropy and the likeliest tokens: TokenLogprobs.
+
+    logits [..., V] float32 or bfloat16 (rows at one distance); tokens [...] int64, negative where a position is ignored
+    (logp 0 and no gradient there; V or more gives NaN).  ``top``: how many of the likeliest tokens, at most 64, likeliest
+    first, equal logits by the lowest token.  ``scale`` > 0 is the inverse temperature.  A logit of -inf is a token that
+    cannot come; a row of nothing else has log probabilities of -inf, entropy 0 and no gradient."""
+    done = (_NATIVE or _native()).token_logprobs_fwd(logits, tokens, top, entropy, scale)
+    if done is not None:
+        return TokenLogprobs(*_done(done))
+    R, ld = _logits(logits, tokens)
+    V = logits.shape[-1]
+    top = int(top)
+    lead, f32 = tuple(tokens.shape), dict(dtype=torch.float32, device=logits.device)
+    logp, stats = torch.empty(lead, **f32), torch.empty(lead + (2,), **f32)
+    ent = torch.empty(lead, **f32) if entropy else None
+    if not 0 <= top <= min(V, _lib.RES_LOGPROBS_TOP_MAX):
+        raise ValueError(f"top must be in [0, min(V, {_lib.RES_LOGPROBS_TOP_MAX})] (got {top})")
+    ids = torch.empty(lead + (top,), dtype=torch.int64, device=logits.device) if top else None
+    tlp = torch.empty(lead + (top,), **f32) if top else None
+    with _together(logits, tokens):
+        check(_lib.lib().resonator_token_logprobs_fwd(_ptr(logits), ld, _code(logits), _ptr(tokens), R, V, float(scale), _ptr(logp),
+                                                      _ptr(stats), _ptr(ent), top, _ptr(ids), _ptr(tlp), _stream(logits.device)))
+    return TokenLogprobs(logp, ent, ids, tlp, stats)
+
+
+def resonator_token_logprobs_bwd(logits, tokens, saved, dlogp=None, dentropy=None, scale=1.0, out=None):
+    """The logits' gradient of sum(dlogp logp) + sum(dentropy entropy), of the logits' type.  ``saved``: the forward's
+    TokenLogprobs (with its entropy where dentropy is given); dlogp, dentropy [...] float32 or None.  ``out`` may be the
+    logits themselves."""
+    done = (_NATIVE or _native()).token_logprobs_bwd(logits, tokens, saved.stats, saved.entropy, dlogp, dentropy, scale, out)
+    if done is not None:
+        return _done(done)
+    R, ld = _logits(logits, tokens)
+    V, lead = logits.shape[-1], tuple(tokens.shape)
+    _f32(saved.stats, "stats", lead + (2,))
+    for name, t in (("dlogp", dlogp), ("dentropy", dentropy)):
+        _f32(t, name, lead)
+    if dentropy is not None:
+        if saved.entropy is None:
+            raise TypeError("dentropy needs a forward with entropy")
+        _f32(saved.entropy, "entropy", lead)
+    dx = torch.empty(tuple(logits.shape), dtype=logits.dtype, device=logits.device) if out is None else out
+    if dx.dtype != logits.dtype or dx.shape != logits.shape:
+        raise ValueError(f"out must be {logits.dtype} {list(logits.shape)}")
+    _, ldd = _rows2(dx, "out")
+    with _together(logits, tokens, saved.stats, saved.entropy, dlogp, dentropy, out):
+        check(_lib.lib().resonator_token_logprobs_bwd(_ptr(logits), ld, _code(logits), _ptr(tokens), R, V, float(scale),
+                                                      _ptr(saved.stats), _ptr(saved.entropy) if dentropy is not None else None,
+                                                      _ptr(dlogp), _ptr(dentropy), _ptr(dx), ldd, _stream(logits.device)))
+    _written(out)
+    return dx
+
+
+class TokenLogprobsFunction(torch.autograd.Function):
+    """Autograd wrapper: resonator_token_logprobs_fwd (logp, and the entropy where asked for) and _bwd."""
+
+    @staticmethod
+    def forward(ctx, logits, tokens, entropy=False, scale=1.0):
+        r = resonator_token_logprobs_fwd(logits, tokens, entropy=entropy, scale=scale)
+        ctx.save_for_backward(logits, tokens, r.stats, r.entropy)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return (r.logp, r.entropy) if entropy else r.logp
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dlogp, dentropy=None):
+        logits, tokens, stats, entropy = ctx.saved_tensors
+        dlogp, dentropy = (None if t is None else t.contiguous() for t in (dlogp, dentropy))
+        return resonator_token_logprobs_bwd(logits, tokens, TokenLogprobs(None, entropy, None, None, stats), dlogp, dentropy,
+                                            scale=ctx.scale), None, None, None
+
+
+def resonator_token_logprobs(logits, tokens, entropy=False, scale=1.0):
+    """Differentiable log probabilities of given tokens: logp, or (logp, entropy); the logits receive a gradient."""
+    if not _needs_graph(logits):
+        r = resonator_token_logprobs_fwd(logits, tokens, entropy=entropy, scale=scale)
+        return (r.logp, r.entropy) if entropy else r.logp
+    return TokenLogprobsFunction.apply(logits, tokens, entropy, scale)
