@@ -4,6 +4,8 @@
 //   dx_j = scale [ dlogp (1{j = token} - p_j) - dH p_j (log p_j + H) ],   p_j = e_j / S.
 // m and log S are kept apart: their sum loses what the difference z - m keeps, and overflows where z does.
 // The forward reads V elements a row and the backward reads and writes them: memory bounds both.
+#include <type_traits>
+
 #include "select.h"
 
 namespace res {
@@ -21,6 +23,9 @@ __device__ __forceinline__ uint32_t order_of(float v) {
 __device__ __forceinline__ float value_of(uint32_t o) {
   return __uint_as_float((o & 0x80000000u) != 0 ? o & 0x7fffffffu : ~o);  // (0xffffffff: a NaN)
 }
+
+// The order of a bf16 value from its upper half: the lower one is zeros, below zero ones (and NaN's all ones).
+__device__ __forceinline__ uint32_t whole_order(uint32_t o) { return (o & 0x80000000u) == 0 || o == 0xffff0000u ? o | 0xffffu : o; }
 
 // The running maximum, the sum of e^(scale (x - m)) and that of d e^d, with d in units of ln 2.
 struct Stats {
@@ -42,108 +47,137 @@ __device__ __forceinline__ void join(Stats& a, Stats b, float c) {
   a.w += b.w;
 }
 
-constexpr int LIST = 2048;  // candidates kept in LDS: those not below the threshold that the first elements give
+constexpr int LIST = 1536, EQUAL = 512;  // alternatives' candidates kept in LDS; those of them at the border itself
 
 struct Shared {
-  Stats part[16];
-  float top[16];
-  int count, finite;
-  uint64_t best[16];
-  uint32_t order[LIST];
-  int at[LIST];
+  uint32_t kth[16], share[16], border;
+  uint32_t tops[1024];  // lanes' maxima not below the first border
+  int lane[1024];       // the lanes whose elements are looked at again
+  int count, above, equal, lanes, again;
+  uint64_t list[LIST];  // order << 32 | ~place: the larger one comes first
 };
 
-// The k-th largest of a wave's 64 values (k <= 64), as an order: bit after bit, how many are not below.
-__device__ __forceinline__ uint32_t kth_of_wave(uint32_t o, int k) {
-  uint32_t t = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t u = t | 1u << bit;
-    if (__popcll(__ballot(o >= u)) >= k) t = u;
+__device__ __forceinline__ uint64_t entry_of(float v, int64_t at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~(uint32_t)at; }
+
+// The k-th and the j-th largest of a wave's 64 orders (k, j <= 64), bit after bit: how many are not below.  (A loop: run once
+// by each wave, unrolled it took 0.7 us more of 18 for 64 rows of 50304.)  HALF: the orders are of bf16 values.
+template <bool HALF>
+__device__ __forceinline__ void kth_of_wave(uint32_t o, int k, int j, uint32_t* kth, uint32_t* jth) {
+  uint32_t t = 0, s = 0;
+#pragma unroll 1
+  for (int bit = 31; bit >= (HALF ? 16 : 0); --bit) {
+    const uint32_t u = t | 1u << bit, v = s | 1u << bit;
+    const int above = __popcll(__ballot(o >= u)), also = __popcll(__ballot(o >= v));
+    t = above >= k ? u : t;
+    s = also >= j ? v : s;
   }
-  return t;
+  *kth = HALF ? whole_order(t) : t;
+  *jth = HALF ? whole_order(s) : s;
 }
 
-// One work-group a row.  Elements go through in one pass, 4 vectors a thread at a time: their maximum first, so that the sums
-// are rescaled at most once for them.  For the alternatives the pass keeps those not below a threshold: the largest over the
-// waves of the k-th largest of a wave's lanes' maxima over the first vectors, below which no alternative can be.  The list is
-// ranked at the end.  Rows whose list overflows (many equal values, values that rise along the row) take one more pass for
-// each alternative.
-template <typename T, int NT, bool TOP>
+// A row's elements, some vectors a thread at a time.
+template <typename T, int NT, int UV> struct RowPiece {
+  static constexpr int V = 16 / (int)sizeof(T), U = UV, STEP = NT * V * U;
+  T q[U][V];
+  __device__ __forceinline__ static int64_t at(int64_t base, int u) { return base + ((int64_t)u * NT + threadIdx.x) * V; }
+  // -inf behind the row's end
+  __device__ __forceinline__ void load(const T* x, int64_t base, int64_t N) {
+    if (base + STEP <= N) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_part<T, V>(x + at(base, u), V, q[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t j = at(base, u);
+#pragma unroll
+        for (int e = 0; e < V; ++e) q[u][e] = from_f32<T>(-INFINITY);
+        if (j + V <= N)
+          load_part<T, V>(x + j, V, q[u]);
+        else
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (j + e < N) q[u][e] = x[j + e];
+      }
+    }
+  }
+};
+
+// One work-group a row, whose elements go through in one pass, the next ones loaded while these are added: their maximum first,
+// so that the sums are rescaled at most once for them.
+// Alternatives: no alternative is below the k-th largest of the lanes' maxima (the border), and only the lanes whose maximum is
+// not below it, some k of them, have any, so that their elements alone are looked at again (k of 256 lanes: 8 % of the row for 20
+// alternatives).  The lanes are few from the start: not below the largest of the waves' own k-th
+// largest, nor below the least of their (k / waves)-th largest.  What is found is
+// ranked in LDS.  Many elements at the border itself (a mask's value) are not all listed: those missing are its lowest places.
+// Rows with NaN or infinity, or with more than LIST elements above the border, find the k-th largest by counting.
+template <typename T, int NT, bool TOP, bool ENT>
 __global__ __launch_bounds__(NT) void logprobs_fwd_kernel(LogprobsArgs a) {
-  constexpr int V = 16 / (int)sizeof(T), U = 4, W = NT / 64;
-  __shared__ Shared sh;
+  typedef RowPiece<T, NT, 4> Piece;
+  constexpr int V = Piece::V, U = Piece::U, W = NT / 64;
+  __shared__ Stats part[16];
+  extern __shared__ __align__(16) char raw[];
+  Shared& sh = *reinterpret_cast<Shared*>(raw);  // (with alternatives only)
   const int64_t r = a.r0 + blockIdx.x;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const T* x = static_cast<const T*>(a.logits) + r * a.ld;
   const float c = a.scale * LOG2E;
   const int64_t N = a.V;
   Stats st{LOWEST, 0.0f, 0.0f};
-  float threshold = -INFINITY;
-  if (TOP && tid == 0) sh.count = sh.finite = 0;
-  for (int64_t base = 0; base < N; base += (int64_t)NT * V * U) {
-    T q[U][V];
-    int n[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t j = base + ((int64_t)u * NT + tid) * V;
-      n[u] = (int)(j >= N ? 0 : N - j < V ? N - j : V);
-      load_part<T, V>(x + (n[u] > 0 ? j : 0), n[u], q[u]);
-    }
+  float most = -INFINITY;
+  if (TOP && tid == 0) sh.count = sh.above = sh.equal = sh.lanes = sh.again = 0;
+  Piece next;
+  next.load(x, 0, N);
+  for (int64_t base = 0; base < N; base += Piece::STEP) {
+    const Piece p = next;
+    if (base + Piece::STEP < N) next.load(x, base + Piece::STEP, N);
     float v[U][V], top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        v[u][e] = e < n[u] ? to_f32(q[u][e]) : -INFINITY;
+        v[u][e] = to_f32(p.q[u][e]);
         top = fmaxf(top, v[u][e]);
       }
+    most = fmaxf(most, top);
     rescale(st, fmaxf(st.m, top), c);
+    // d = c x - c m with one rounding of its own; that of c m is taken out of the sums at once, since it is the same for all.
+    // (Where c m is next to float32's end, or is none, the difference is taken first.)
+    const float cm = st.m * c;
+    const bool far = !(fabsf(cm) < 1e30f);
+    const float mc = far ? 0.0f : cm, fix = far ? 0.0f : fmaf(st.m, c, -mc);
     float s = 0.0f, w = 0.0f;
+    auto add = [&](float d) {
+      const float f = exp2_fast(d);
+      s += f;
+      if (ENT) w = fmaf(f, fmaxf(d, -1024.0f), w);  // (f is 0 there)
+    };
+    if (far) {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int e = 0; e < V; ++e) {
-        const float d = (v[u][e] - st.m) * c, p = exp2_fast(d);
-        s += p;
-        w = fmaf(p, fmaxf(d, -1024.0f), w);  // (p is 0 there)
-      }
-    st.s += s;
-    st.w += w;
-    if constexpr (TOP) {
-      if (base == 0) {
-        const uint32_t k = kth_of_wave(order_of(top), a.top);
-        if (lane == 0) sh.top[wave] = value_of(k);
-        __syncthreads();
+        for (int e = 0; e < V; ++e) add((v[u][e] - st.m) * c);
+    } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) threshold = fmaxf(threshold, sh.top[i]);  // (a NaN is left out)
-      }
-      // (a NaN is among what is not below; -inf is never listed)
-      if (__any(!(top < threshold) || s != s)) {
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-          for (int e = 0; e < V; ++e)
-            if (e < n[u] && !(v[u][e] < threshold) && v[u][e] != -INFINITY) {
-              const int k = atomicAdd(&sh.count, 1);
-              if (k < LIST) {
-                sh.order[k] = order_of(v[u][e]);
-                sh.at[k] = (int)(base + ((int64_t)u * NT + tid) * V + e);
-              }
-            }
-      }
+        for (int e = 0; e < V; ++e) add(fmaf(v[u][e], c, -mc));
     }
+    const float by = exp2_fast(-fix);
+    s *= by;
+    st.s += s;
+    if (ENT) st.w += fmaf(-fix, s, w * by);
   }
   // the work-group's sums: every lane of the wave, then every wave, in a fixed order
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
-    Stats b{__shfl_xor(st.m, o), __shfl_xor(st.s, o), __shfl_xor(st.w, o)};
+    Stats b{__shfl_xor(st.m, o), __shfl_xor(st.s, o), ENT ? __shfl_xor(st.w, o) : 0.0f};
     join(st, b, c);
   }
-  if (lane == 0) sh.part[wave] = st;
+  if (lane == 0) part[wave] = st;
   __syncthreads();
-  st = sh.part[0];
+  st = part[0];
 #pragma unroll
-  for (int i = 1; i < W; ++i) join(st, sh.part[i], c);
+  for (int i = 1; i < W; ++i) join(st, part[i], c);
   const bool empty = st.s == 0.0f;  // every logit is -inf: no token has a probability
   const float logs = empty ? 0.0f : logf(st.s), m = empty ? -INFINITY : st.m;
   if (tid == 0) {
@@ -158,64 +192,120 @@ __global__ __launch_bounds__(NT) void logprobs_fwd_kernel(LogprobsArgs a) {
       a.stats[2 * r] = m;
       a.stats[2 * r + 1] = logs;
     }
-    if (a.entropy != nullptr) a.entropy[r] = empty ? 0.0f : fmaxf(fmaf(-LN2, st.w / st.s, logs), st.s != st.s ? NAN : 0.0f);
+    if (ENT) a.entropy[r] = empty ? 0.0f : fmaxf(fmaf(-LN2, st.w / st.s, logs), st.s != st.s ? NAN : 0.0f);
   }
   if constexpr (TOP) {
     int64_t* ids = a.top_ids + r * a.top;
     float* lps = a.top_logp + r * a.top;
     auto lp_of = [&](uint32_t o) { return empty ? -INFINITY : fmaf(a.scale, value_of(o) - m, -logs); };
-    const int count = sh.count;
-    if (count <= LIST) {
-      // an entry's rank: how many are larger, or equal and at a lower place
-      for (int i = tid; i < count; i += NT) {
-        const uint32_t o = sh.order[i];
-        const int at = sh.at[i];
-        int rank = 0;
-        for (int k = 0; k < count; ++k) rank += sh.order[k] > o || (sh.order[k] == o && sh.at[k] < at);
-        if (rank < a.top) {
-          ids[rank] = at;
-          lps[rank] = lp_of(o);
-        }
-      }
-      // fewer than asked for: then all but -inf are listed, and the lowest places of -inf follow
-      if (count < a.top && wave == 0) {
-        int have = count;
-        for (int64_t j = 0; j < N && have < a.top; j += 64) {
-          const bool is = j + lane < N && to_f32(x[j + lane]) == -INFINITY;
-          const uint64_t who = __ballot(is);
-          const int k = have + __popcll(who & ((1ull << lane) - 1));
-          if (is && k < a.top) {
-            ids[k] = j + lane;
-            lps[k] = lp_of(order_of(-INFINITY));
-          }
-          have += __popcll(who);
-        }
-      }
-    } else {
-      // each time the largest (order, then lowest place) behind the last one found
-      uint64_t last = ~0ull;
-      for (int k = 0; k < a.top; ++k) {
-        uint64_t best = 0;
-        for (int64_t j = tid; j < N; j += NT) {
-          const uint64_t e = (uint64_t)order_of(to_f32(x[j])) << 32 | (uint32_t)~(uint32_t)j;
-          if ((k == 0 || e < last) && e > best) best = e;
-        }
+    const uint32_t mine = order_of(most);
+    uint32_t own, share;
+    kth_of_wave<sizeof(T) == 2>(mine, a.top, (a.top + W - 1) / W, &own, &share);
+    if (lane == 0) {
+      sh.kth[wave] = own;
+      sh.share[wave] = share;
+    }
+    __syncthreads();
+    uint32_t first = 0, every = ~0u;
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) {
-          const uint64_t b = (uint64_t)__shfl_xor((uint32_t)(best >> 32), o) << 32 | __shfl_xor((uint32_t)best, o);
-          best = b > best ? b : best;
-        }
-        if (lane == 0) sh.best[wave] = best;
-        __syncthreads();
-        best = sh.best[0];
+    for (int i = 0; i < W; ++i) {
+      first = sh.kth[i] > first ? sh.kth[i] : first;
+      every = sh.share[i] < every ? sh.share[i] : every;
+    }
+    first = every > first ? every : first;
+    if (mine >= first) sh.tops[atomicAdd(&sh.lanes, 1)] = mine;
+    __syncthreads();
+    if (mine >= first) {
+      int more = 0, least = 0;  // lanes above this one's maximum, and not below it
+      const int lanes = sh.lanes;
+      for (int i = 0; i < lanes; i += 8)
 #pragma unroll
-        for (int i = 1; i < W; ++i) best = sh.best[i] > best ? sh.best[i] : best;
-        last = best;
-        if (tid == 0) {
-          ids[k] = (uint32_t)~(uint32_t)best;
-          lps[k] = lp_of((uint32_t)(best >> 32));
+        for (int u = 0; u < 8; ++u) {
+          const uint32_t t = i + u < lanes ? sh.tops[i + u] : 0;
+          more += t > mine;
+          least += t >= mine;
         }
+      if (more < a.top && a.top <= least) sh.border = mine;  // (all that write, write the same)
+    }
+    __syncthreads();
+    uint32_t border = sh.border;
+    if (mine >= border) sh.lane[atomicAdd(&sh.again, 1)] = tid;
+    __syncthreads();
+    const uint32_t again = (uint32_t)sh.again, each = (uint32_t)((N + NT * V - 1) / (NT * V));  // vectors of a lane
+    for (uint32_t i = tid; i < again * each; i += NT) {
+      const int64_t j = ((int64_t)(i % each) * NT + sh.lane[i / each]) * V;
+      T q[V];
+      const int n = (int)(j >= N ? 0 : N - j < V ? N - j : V);
+      load_part<T, V>(x + (n > 0 ? j : 0), n, q);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float v = to_f32(q[e]);
+        const uint32_t o = order_of(v);
+        if (o < border || e >= n) continue;
+        if (o == border ? atomicAdd(&sh.equal, 1) >= EQUAL : (atomicAdd(&sh.above, 1), false)) continue;
+        const int k = atomicAdd(&sh.count, 1);
+        if (k < LIST) sh.list[k] = entry_of(v, j + e);
+      }
+    }
+    __syncthreads();
+    int count = sh.count, above = sh.above, equal = sh.equal;
+    if (count > LIST || st.s != st.s) {
+      // the k-th largest, bit after bit, by counting what is not below; then what is above it and as many as fit at it
+      uint32_t t = 0;
+      for (int bit = 31; bit >= (sizeof(T) == 2 ? 16 : 0); --bit) {
+        const uint32_t u = t | 1u << bit;
+        int n = 0;
+        for (int64_t j = tid; j < N; j += NT) n += order_of(to_f32(x[j])) >= u;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
         __syncthreads();
+        if (lane == 0) sh.kth[wave] = (uint32_t)n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int i = 0; i < W; ++i) n += (int)sh.kth[i];
+        if (n >= a.top) t = u;
+      }
+      border = sizeof(T) == 2 ? whole_order(t) : t;
+      __syncthreads();
+      if (tid == 0) sh.count = sh.above = sh.equal = 0;
+      __syncthreads();
+      for (int64_t j = tid; j < N; j += NT) {
+        const float v = to_f32(x[j]);
+        const uint32_t o = order_of(v);
+        if (o < border) continue;
+        if (o == border ? atomicAdd(&sh.equal, 1) >= EQUAL : (atomicAdd(&sh.above, 1), false)) continue;
+        sh.list[atomicAdd(&sh.count, 1)] = entry_of(v, j);  // (fewer than k are above)
+      }
+      __syncthreads();
+      count = sh.count;
+      above = sh.above;
+      equal = sh.equal;
+    }
+    const bool cut = equal > EQUAL;  // not all at the threshold are listed: only what is above it is ranked
+    for (int i = tid; i < count; i += NT) {
+      const uint64_t o = sh.list[i];
+      if (cut && (uint32_t)(o >> 32) == border) continue;
+      int rank = 0;
+      for (int k = 0; k < count; k += 8)
+#pragma unroll
+        for (int u = 0; u < 8; ++u) rank += (k + u < count ? sh.list[k + u] : 0) > o;
+      if (rank < a.top) {
+        ids[rank] = (uint32_t)~(uint32_t)o;
+        lps[rank] = lp_of((uint32_t)(o >> 32));
+      }
+    }
+    if (cut && above < a.top && wave == 0) {  // the lowest places of the threshold
+      int have = above;
+      for (int64_t j = 0; j < N && have < a.top; j += 64) {
+        const bool is = j + lane < N && order_of(to_f32(x[j + lane])) == border;
+        const uint64_t who = __ballot(is);
+        const int k = have + __popcll(who & ((1ull << lane) - 1));
+        if (is && k < a.top) {
+          ids[k] = j + lane;
+          lps[k] = lp_of(border);
+        }
+        have += __popcll(who);
       }
     }
   }
@@ -264,23 +354,24 @@ __global__ __launch_bounds__(BWD_THREADS) void logprobs_bwd_kernel(LogprobsArgs 
 template <typename T, int NT>
 hipError_t fwd(LogprobsArgs a, hipStream_t st) {
   const int64_t most = LAUNCH_THREADS / NT, R = a.R;
-  for (a.r0 = 0; a.r0 < R; a.r0 += most) {
-    const uint32_t n = (uint32_t)(R - a.r0 < most ? R - a.r0 : most);
-    if (a.top > 0)
-      logprobs_fwd_kernel<T, NT, true><<<n, NT, 0, st>>>(a);
-    else
-      logprobs_fwd_kernel<T, NT, false><<<n, NT, 0, st>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
+  auto go = [&](auto top, auto ent) {
+    for (a.r0 = 0; a.r0 < R; a.r0 += most) {
+      const uint32_t n = (uint32_t)(R - a.r0 < most ? R - a.r0 : most);
+      logprobs_fwd_kernel<T, NT, top, ent><<<n, NT, top ? sizeof(Shared) : 0, st>>>(a);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+  };
+  if (a.top > 0) return a.entropy != nullptr ? go(std::true_type{}, std::true_type{}) : go(std::true_type{}, std::false_type{});
+  return a.entropy != nullptr ? go(std::false_type{}, std::true_type{}) : go(std::false_type{}, std::false_type{});
 }
 
 }  // namespace
 
 template <typename T>
 hipError_t launch_logprobs_fwd(LogprobsArgs a, hipStream_t st) {
-  return a.V <= 8192 ? fwd<T, 256>(a, st) : fwd<T, 1024>(a, st);
+  return a.V <= 8192 || a.R >= 512 ? fwd<T, 256>(a, st) : fwd<T, 1024>(a, st);
 }
 template <typename T>
 hipError_t launch_logprobs_bwd(LogprobsArgs a, hipStream_t st) {
