@@ -188,9 +188,9 @@ int check_selective(const Sizes& z, res_dtype_t dt) {
   if (z.B < 1 || z.L < 0 || z.H < 1 || z.P < 1 || z.G < 1 || z.N < 1 || z.H % z.G != 0)
     return api_error(RES_ERR_INVALID_ARG, "B, H, P, G and N must be >= 1, L >= 0 and G divide H (got B=%lld L=%lld H=%lld P=%lld G=%lld N=%lld)",
                      (long long)z.B, (long long)z.L, (long long)z.H, (long long)z.P, (long long)z.G, (long long)z.N);
-  // (a launch begins with any work-group, but their number and the elements of states and partial sums are 64-bit products)
+  // (work-groups are 32-bit counts)
   if (z.P > SEL_MAX || z.N > SEL_MAX || z.H > (1 << 16) || z.H * z.P > (1 << 21) || z.G * z.N > (1 << 21) || z.B > (1LL << 31) ||
-      z.L >= (1LL << 31) - 65536 || z.B * z.H * (z.L / SEL_Q + 1) >= (1LL << 40))
+      z.L >= (1LL << 31) - 65536 || z.B * z.H >= (1LL << 29) || z.B * z.H * (z.L / SEL_Q + 1) >= (1LL << 40))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld H=%lld P=%lld G=%lld N=%lld)", (long long)z.B,
                      (long long)z.L, (long long)z.H, (long long)z.P, (long long)z.G, (long long)z.N);
   return RES_OK;
@@ -216,7 +216,7 @@ size_t lay_out(const Sizes& z, bool backward, bool carry, char* base, SelArgs* a
   }
   a->leave = border;
   const size_t wgs = (size_t)(z.B * p.segs * z.G * ((p.HG + p.HR - 1) / p.HR)), state = (size_t)p.HR * 4 * ((p.NT + 3) / 4) * 4 * 64 * 16;
-  a->hs = (f4*)take(wgs * (size_t)(p.seg + 1) * state);
+  a->hs = (f4*)take(wgs * (size_t)p.seg * state);
   a->gs = (f4*)take(wgs * state);
   const int64_t blocks = (p.HG + p.HR - 1) / p.HR;
   a->part = (float*)take(blocks > 1 ? (size_t)(blocks * 2 * z.B * z.L * z.G * z.N) * 4 : 0);

@@ -80,7 +80,7 @@ constexpr int SEL_BWD_HEADS = 8;  // row blocks of a work-group of the backward 
 
 struct SelPlan {
   int NT;            // tiles of 16 states, padded: 2, 4 or 8
-  int PB;            // row blocks of a head
+  int PB, PS;        // row blocks of a head: 1 or 2; PB - 1
   int HV, HG;        // row blocks of a batch row, of a group
   int HF, HR;        // row blocks of a work-group, forward and backward
   int64_t chunks, seg, segs;  // chunks of a row; chunks of a segment; segments
@@ -98,7 +98,7 @@ struct SelArgs {
   float* enter;   // [B][HV][segs][SEL_P][NP]: the state before each segment (with several)
   float* leave;   // the gradient of the state behind each segment, likewise
   float* decay;   // [B][HV][segs]: a segment's sum of gamma D in units of ln 2
-  f4* hs;         // backward: a work-group's states before each chunk and behind the last
+  f4* hs;         // backward: a work-group's states before each chunk
   f4* gs;         // backward: its states' gradients
   float* part;    // backward: db and dc of each block of heads of a group [blocks][2][B][L][G N], with more than one
   float* params;  // backward: [B][segs][HV][3], sums for dgamma, ddt_bias, dskip

@@ -16,6 +16,8 @@
 // two bf16 parts, hi + lo, 2^-16 relative, where float32 results depend on it (states, dl); the weights (c.b) E D and E K
 // that only make bf16 outputs, and g in db, go in as one bf16 (2^-8 a term, as much as the output's own rounding).
 // float32 inputs use float32 MFMA throughout.  Sums and states are float32.
+#include <type_traits>
+
 #include "select.h"
 
 namespace res {
@@ -113,13 +115,14 @@ template <typename T, int COLS> struct Tile {
   static constexpr int V = 16 / (int)sizeof(T), PR = COLS / V, RT = SEL_THREADS / PR, U = Q / RT, LD = COLS + Mx<T>::PAD;
   static constexpr int BYTES = Q * LD * (int)sizeof(T);
   T v[U][V];
-  __device__ __forceinline__ void load(const T* p, int64_t st, int rows, int cols) {
-    const int r0 = threadIdx.x / PR, c = threadIdx.x % PR * V;
+  // rows at distance st (elements; below 2^21, so that a lane's offset has 32 bits) from p, which is the same in all lanes
+  __device__ __forceinline__ void load(const T* p, uint32_t st, int rows, int cols, int tid) {
+    const int r0 = tid / PR, c = tid % PR * V, n = cols - c;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int r = r0 + u * RT, n = r < rows ? cols - c : 0;
-      if (n > 0)
-        load_part<T, V>(p + r * st + c, n, v[u]);
+      const T* at = reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) + ((uint32_t)(r0 + u * RT) * st + (uint32_t)c) * (uint32_t)sizeof(T));
+      if (r0 + u * RT < rows && n > 0)
+        load_part<T, V>(at, n, v[u]);
       else {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[u][e] = T(0);
@@ -139,34 +142,98 @@ template <typename T, int COLS> struct Tile {
   }
 };
 
-// A chunk's steps, one a lane (by one wave): D, s (inclusive sums of gamma D, base 2), what follows a step (exclusive), the total.
+// Sums over lanes that stay in the vector unit.  (Through LDS, as a general shuffle goes, each step waits some 130 cycles.)
+template <int CTRL>
+__device__ __forceinline__ float lanes_add(float v) {  // v and that of another lane of the 16; 0 where there is none
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float sum_lanes(float v) {  // over the 16 lanes of a row
+  v = lanes_add<0xB1>(v);         // neighbours
+  v = lanes_add<0x4E>(v);         // pairs
+  v = lanes_add<0x141>(v);        // halves of eight, mirrored
+  return lanes_add<0x140>(v);     // halves of sixteen, mirrored
+}
+__device__ __forceinline__ float sum_rows(float v) {  // over the 4 lanes i, i + 16, i + 32, i + 48
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const unsigned a = __float_as_uint(v);
+  const u2 p = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+  const float s = __uint_as_float(p[0]) + __uint_as_float(p[1]);
+  const unsigned b = __float_as_uint(s);
+  const u2 q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+__device__ __forceinline__ float sum_wave(float v) { return sum_rows(sum_lanes(v)); }
+__device__ __forceinline__ float prefix_lanes(float v) {  // over the lanes of a row up to this one
+  v = lanes_add<0x111>(v);
+  v = lanes_add<0x112>(v);
+  v = lanes_add<0x114>(v);
+  return lanes_add<0x118>(v);
+}
+__device__ __forceinline__ float suffix_lanes(float v) {  // from this one on
+  v = lanes_add<0x101>(v);
+  v = lanes_add<0x102>(v);
+  v = lanes_add<0x104>(v);
+  return lanes_add<0x108>(v);
+}
+__device__ __forceinline__ float of_lane(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+}
+
+// A chunk's steps, one a lane (by one wave).  Sums of gamma D (base 2): s up to and with a step, after behind it, and the same
+// within its tile of 16 steps (in, behind): what decays between two steps is summed from these, since a difference of s loses
+// what is small beside s (2^-24 of up to some hundred).
 struct Steps {
-  float d, s, after, total, slope;
+  float d, s, after, in, behind, total, slope;
 };
+// the step's logit, loaded ahead of its use
 template <typename T>
-__device__ __forceinline__ Steps steps_of(const SelArgs& a, int64_t b, int64_t t, int64_t n, int h, int lane) {
-  Steps o{0, 0, 0, 0, 0};
+__device__ __forceinline__ float load_step(const SelArgs& a, int64_t b, int64_t t, int64_t n, int h, int lane) {
+  return t + lane < n ? to_f32(static_cast<const T*>(a.dt.p)[b * a.dt.sb + (t + lane) * a.dt.st + h]) : 0.0f;
+}
+__device__ __forceinline__ Steps steps_of(const SelArgs& a, float v, bool inside, int h, int lane) {
+  Steps o{0, 0, 0, 0, 0, 0, 0};
   float ld = 0.0f;
-  if (t + lane < n) {
-    const float v = to_f32(static_cast<const T*>(a.dt.p)[b * a.dt.sb + (t + lane) * a.dt.st + h]) + (a.dt_bias != nullptr ? a.dt_bias[h] : 0.0f);
+  if (inside) {
+    v += a.dt_bias != nullptr ? a.dt_bias[h] : 0.0f;
     o.d = fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v)));
     if (v != v) o.d = v;
     o.slope = 1.0f / (1.0f + expf(-v));
     ld = o.d * a.gamma[h] * LOG2E;
     ld = ld > NO_MORE ? NO_MORE : ld;
   }
-  o.s = ld;
-  float back = ld;
+  const float next = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, ld), 0x101, 0xF, 0xF, true));
+  o.in = prefix_lanes(ld);
+  o.behind = suffix_lanes(next);  // (the next lane's on; nothing behind the last)
+  o.s = o.in;
+  o.after = o.behind;
 #pragma unroll
-  for (int k = 1; k < 64; k <<= 1) {
-    const float up = __shfl_up(o.s, k), down = __shfl_down(back, k);
-    if (lane >= k) o.s += up;
-    if (lane + k < 64) back += down;
+  for (int t = 0; t < 4; ++t) {
+    const float all = of_lane(o.in, 16 * t + 15);
+    o.total += all;
+    if (t < lane >> 4) o.s += all;
+    if (t > lane >> 4) o.after += all;
   }
-  o.total = __shfl(o.s, 63);
-  const float next = __shfl_down(back, 1);
-  o.after = lane < 63 ? next : 0.0f;
   return o;
+}
+// what a tile's steps decay, from s and in of its first step's lane on: sums of whole tiles between tiles si and ti
+struct Between {
+  float in[Q], behind[Q], tile[4];  // (behind: negative)
+  __device__ __forceinline__ void put(const Steps& s, int lane) {
+    in[lane] = s.in;
+    behind[lane] = -s.behind;
+    if ((lane & 15) == 15) tile[lane >> 4] = s.in;
+  }
+  // exponents of E over 4 steps t of a tile from step s (in its lane), or 4 steps s to step t: to[] + from
+  __device__ __forceinline__ float gap(int si, int ti) const {  // whole tiles between
+    return ti - si < 2 ? 0.0f : ti - si < 3 ? tile[si + 1] : tile[1] + tile[2];
+  }
+};
+
+// The value again, as one that the compiler does not know: what is computed from it stays where it is used.  (Hoisted out of the
+// loops, the backward's addresses took more registers than there are.)
+__device__ __forceinline__ int here(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // Which rows a work-group has: its batch row, segment, group and row blocks hv0 .. hv0 + heads (of the batch row's HV).
@@ -174,16 +241,20 @@ struct Place {
   int64_t b, seg;
   int g, block, hv0, heads;
 };
-__device__ __forceinline__ Place place_of(const SelArgs& a, int per) {
-  const int blocks = (a.p.HG + per - 1) / per;
-  int64_t id = a.wg0 + blockIdx.x;
+__device__ __forceinline__ Place place_of(const SelArgs& a, int per, uint32_t* index) {
+  const uint32_t blocks = (uint32_t)((a.p.HG + per - 1) / per), G = (uint32_t)a.G, segs = (uint32_t)a.p.segs;
+  // Work-groups go to the eight dies in turn: die d takes the d-th eighth of the launch's, so that the blocks of a group, which
+  // read the same b and c, run together on one die and share them in its cache.  (Fewer than 2^31 work-groups.)
+  const uint32_t n = gridDim.x, d = blockIdx.x % 8, q = n / 8, r = n % 8;
+  uint32_t id = (uint32_t)a.wg0 + d * q + (d < r ? d : r) + blockIdx.x / 8;
+  *index = id;
   Place o;
   o.block = (int)(id % blocks);
   id /= blocks;
-  o.g = (int)(id % a.G);
-  id /= a.G;
-  o.seg = id % a.p.segs;
-  o.b = id / a.p.segs;
+  o.g = (int)(id % G);
+  id /= G;
+  o.seg = id % segs;
+  o.b = id / segs;
   o.hv0 = o.g * a.p.HG + o.block * per;
   o.heads = a.p.HG - o.block * per < per ? a.p.HG - o.block * per : per;
   return o;
@@ -192,10 +263,6 @@ __device__ __forceinline__ int64_t length_of(const SelArgs& a, int64_t b) {
   if (a.lengths == nullptr) return a.L;
   const int64_t n = a.lengths[b];
   return n < 0 ? 0 : n > a.L ? a.L : n;
-}
-__device__ __forceinline__ float sum_rows(float v) {  // over the 4 lanes of one column
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
 }
 
 // A state [P][N] of a caller's tensor (or none: zeros) or a padded one of the workspace.
@@ -209,20 +276,32 @@ struct StateAt {
   }
 };
 __device__ __forceinline__ StateAt state_at(const SelArgs& a, const float* ext, const float* pad, int64_t b, int hv, int64_t seg) {
-  const int h = hv / a.p.PB, NP = 16 * a.p.NT;
-  StateAt s{ext, nullptr, a.P, a.N, hv % a.p.PB * SEL_P, NP};
+  const int h = (hv >> a.p.PS), NP = 16 * a.p.NT;
+  StateAt s{ext, nullptr, a.P, a.N, (hv & a.p.PS) * SEL_P, NP};
   if (ext != nullptr) s.ext = ext + (b * a.H + h) * (int64_t)a.P * a.N;
   if (pad != nullptr) s.pad = pad + ((b * a.p.HV + hv) * a.p.segs + seg) * (int64_t)(SEL_P * NP);
   return s;
 }
+
+// The tiles on and below the diagonal: of the 10, wave w has w, w + 4 and w + 8, the last one again where there are no more.
+struct TileId {
+  int t, s;
+};
+__device__ __forceinline__ TileId tile_id(int w, int e) {
+  const int id = w + 4 * e < 10 ? w + 4 * e : 9, t = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3;
+  return TileId{t, id - t * (t + 1) / 2};
+}
+// What is loaded before stays before, what is computed behind stays behind: loads of a product go together, and it waits once.
+__device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0); }
 
 // ---------------------------------------------------------------------------
 // Forward: a wave owns 16 of a row block's 64 rows.  Its states are in registers, transposed: lane (p, q) holds
 // n = 16 v + 4 q .. + 3.  STATES: only the segment's end state from a zero start (and REV: the gradient that the segment
 // gives to the state before it: dy, c and exp(-s_t) in the place of x, b and the weights, from the last chunk back).
 // ---------------------------------------------------------------------------
+// The next head's x (the next chunk's b, c and steps) are loaded to registers while a head's products run.
 template <typename T, int NT, int HF, bool STATES, bool REV>
-__global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
+__global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective_fwd_kernel(SelArgs a) {
   typedef Mx<T> M;
   constexpr int NP = 16 * NT, KS = NT / 2;
   typedef Tile<T, NP> TB;
@@ -231,15 +310,19 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
   __shared__ __align__(16) T ct[STATES ? 8 : Q * TB::LD];
   __shared__ __align__(16) T xt[2][Q * TX::LD];
   __shared__ __align__(16) T mt[STATES ? 1 : 2][STATES ? 8 : 6 * 64 * 8];
-  __shared__ __align__(16) float ss[HF][Q], sd[HF][Q], sw[HF][Q], st[HF];  // s, D, D exp(what follows), the chunk's total
-  const Place o = place_of(a, HF);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lq = lane >> 4;
+  __shared__ __align__(16) Between gap[STATES ? 1 : HF];
+  __shared__ __align__(16) float sd[HF][Q], sw[HF][Q], sp[HF][Q], st[HF];  // D, D exp(what follows), exp(-s), the chunk's total
+  uint32_t index;
+  const Place o = place_of(a, HF, &index);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, lq = lane >> 4;
   const int64_t n = length_of(a, o.b);
   const int64_t c0 = o.seg * a.p.seg, c1 = c0 + a.p.seg < a.p.chunks ? c0 + a.p.seg : a.p.chunks;
+  const int64_t some = (n + Q - 1) / Q - c0, active = some < 0 ? 0 : some < c1 - c0 ? some : c1 - c0;  // chunks with steps
   const Rows rx = REV ? a.dy : a.x, rb = REV ? a.c : a.b;
   const T* px = static_cast<const T*>(rx.p) + o.b * rx.sb;
   const T* pb = static_cast<const T*>(rb.p) + o.b * rb.sb + o.g * a.N;
   const T* pc = static_cast<const T*>(a.c.p) + o.b * a.c.sb + o.g * a.N;
+  const int64_t hp = (int64_t)a.H * a.P;
 
   f4 h[HF][NT];
   float total[HF];
@@ -260,83 +343,89 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
     // the tiles above the diagonal that share a fragment with one on it stay zero
     for (int i = tid; i < 2 * 6 * 64 * 8; i += SEL_THREADS) mt[0][i] = T(0);
   }
-  for (int64_t ci = c0; ci < c1; ++ci) {
-    const int64_t ch = REV ? c1 - 1 - (ci - c0) : ci, t0 = ch * Q;
-    const int rows = (int)(n - t0 < 0 ? 0 : n - t0 < Q ? n - t0 : Q);
-    const int held = (int)(a.L - t0 < Q ? a.L - t0 : Q);
-    if (rows == 0) {  // behind the row's end: the state stays
-      if constexpr (!STATES) {
-        T* y = static_cast<T*>(a.y) + (o.b * a.L + t0) * a.H * a.P;
-        for (int k = 0; k < o.heads; ++k) {
-          const int hv = o.hv0 + k, p0 = hv % a.p.PB * SEL_P;
-          const int cols = a.P - p0 < SEL_P ? a.P - p0 : SEL_P;
-          for (int i = tid; i < held * SEL_P; i += SEL_THREADS)
-            if (i % SEL_P < cols) y[(int64_t)(i / SEL_P) * a.H * a.P + hv / a.p.PB * a.P + p0 + i % SEL_P] = T(0);
-        }
-      }
-      continue;
-    }
+  auto start_of = [&](int64_t ci) { return (REV ? c0 + active - 1 - ci : c0 + ci) * Q; };
+  auto rows_at = [&](int64_t t0) { return (int)(n - t0 < Q ? n - t0 : Q); };
+  TB rb0, rc0;
+  TX rx0;
+  float step = 0.0f;
+  auto load_chunk = [&](int64_t ci) {  // (a wave has at most one head)
+    const int64_t t0 = start_of(ci);
+    rb0.load(pb + t0 * rb.st, (uint32_t)rb.st, rows_at(t0), a.N, tid);
+    if constexpr (!STATES) rc0.load(pc + t0 * a.c.st, (uint32_t)a.c.st, rows_at(t0), a.N, tid);
+    if (w < o.heads) step = load_step<T>(a, o.b, t0, n, (o.hv0 + w) >> a.p.PS, lane);
+  };
+  auto load_x = [&](int64_t ci, int k) {
+    const int64_t t0 = start_of(ci);
+    const int hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
+    rx0.load(px + t0 * rx.st + (hv >> a.p.PS) * a.P + p0, (uint32_t)rx.st, rows_at(t0), a.P - p0, tid);
+  };
+  if (active > 0) {
+    load_chunk(0);
+    load_x(0, 0);
+  }
+  int turn = 0;  // which of two buffers a head's x and weights are in
+  for (int64_t ci = 0; ci < active; ++ci) {
+    const int64_t t0 = start_of(ci);
+    const int rows = rows_at(t0), held = (int)(a.L - t0 < Q ? a.L - t0 : Q);
     __syncthreads();  // the last chunk's readers are through
-    {
-      TB t;
-      t.load(pb + t0 * rb.st, rb.st, rows, a.N);
-      t.put(bt);
-      if constexpr (!STATES) {
-        t.load(pc + t0 * a.c.st, a.c.st, rows, a.N);
-        t.put(ct);
-      }
+    rb0.put(bt);
+    if constexpr (!STATES) rc0.put(ct);
+    if (w < o.heads) {
+      const Steps s = steps_of(a, step, lane < rows, (o.hv0 + w) >> a.p.PS, lane);
+      sd[w][lane] = s.d;
+      sp[w][lane] = exp2_fast(-s.s);
+      sw[w][lane] = REV ? exp2_fast(-s.s) : s.d * exp2_fast(-s.after);
+      if constexpr (!STATES) gap[w].put(s, lane);
+      if (lane == 0) st[w] = s.total;
     }
-    for (int k = w; k < o.heads; k += 4) {
-      const Steps s = steps_of<T>(a, o.b, t0, n, (o.hv0 + k) / a.p.PB, lane);
-      ss[k][lane] = s.s;
-      sd[k][lane] = s.d;
-      sw[k][lane] = REV ? exp2_fast(-s.s) : s.d * exp2_fast(-s.after);
-      if (lane == 0) st[k] = s.total;
-    }
-    auto load_x = [&](int k) {
-      const int hv = o.hv0 + k, p0 = hv % a.p.PB * SEL_P;
-      TX t;
-      t.load(px + t0 * rx.st + hv / a.p.PB * a.P + p0, rx.st, rows, a.P - p0);
-      t.put(xt[k & 1]);
-    };
-    load_x(0);
+    if (ci + 1 < active) load_chunk(ci + 1);
     __syncthreads();
-    // G^T [s][t] = b c^T: tile e of 10 (and this wave's are e = w, w + 4, w + 8) is t tile ti, s tile si <= ti
+    // G^T [s][t] = b c^T: tile e of 10 (this wave's are w, w + 4, w + 8) is t tile ti, s tile si <= ti
     f4 g[3];
     if constexpr (!STATES) {
 #pragma unroll
       for (int e = 0; e < 3; ++e) {
-        const int id = w + 4 * e, ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
-        g[e] = f4{0, 0, 0, 0};
-        if (id < 10)
+        const TileId id = tile_id(w, e);
+        typename M::Frag fb[KS], fc[KS];
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
-            g[e] = M::mma(M::row(bt + (16 * si + li) * TB::LD + 32 * k + 4 * lq), M::row(ct + (16 * ti + li) * TB::LD + 32 * k + 4 * lq), g[e]);
+        for (int k = 0; k < KS; ++k) {
+          fb[k] = M::row(bt + (16 * id.s + li) * TB::LD + 32 * k + 4 * lq);
+          fc[k] = M::row(ct + (16 * id.t + li) * TB::LD + 32 * k + 4 * lq);
+        }
+        loads_first();
+        g[e] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < KS; ++k) g[e] = M::mma(fb[k], fc[k], g[e]);
       }
     }
 #pragma unroll
     for (int k = 0; k < HF; ++k) {
       if (k >= o.heads) break;
-      const int hv = o.hv0 + k, hd = hv / a.p.PB, p0 = hv % a.p.PB * SEL_P;
+      const int hv = o.hv0 + k, hd = (hv >> a.p.PS), p0 = (hv & a.p.PS) * SEL_P;
+      T* const xk = xt[turn];
+      T* const mk = mt[STATES ? 0 : turn];
+      turn ^= 1;
+      rx0.put(xk);  // (its readers, two heads ago, were through before the last barrier)
+      if (k + 1 < o.heads)
+        load_x(ci, k + 1);
+      else if (ci + 1 < active)
+        load_x(ci + 1, 0);
       if constexpr (!STATES) {
 #pragma unroll
         for (int e = 0; e < 3; ++e) {
-          const int id = w + 4 * e, ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
-          if (id < 10) {
-            const float s_t = ss[k][16 * ti + li];
-            const f4 s_s = load_f4(&ss[k][16 * si + 4 * lq]), d = load_f4(&sd[k][16 * si + 4 * lq]);
-            f4 m;
+          const TileId id = tile_id(w, e);
+          const Between& b = gap[k];
+          const float to = -(b.in[16 * id.t + li] + b.gap(id.s, id.t));
+          const f4 from = load_f4((id.s == id.t ? b.in : b.behind) + 16 * id.s + 4 * lq), d = load_f4(&sd[k][16 * id.s + 4 * lq]);
+          f4 m;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) m[r] = si < ti || 4 * lq + r <= li ? g[e][r] * (exp2_fast(s_s[r] - s_t) * d[r]) : 0.0f;
-            // fragment (t tile, 32 steps s): 0, 1, 2 and 3, 4 and 5 of t tiles 0, 1, 2, 3
-            const int f = ti < 2 ? ti : 2 * ti - 2 + (si >> 1);
-            put_quad(&mt[k & 1][(f * 64 + lane) * 8 + (si & 1) * 4], m);
-          }
+          for (int r = 0; r < 4; ++r) m[r] = id.s < id.t || 4 * lq + r <= li ? g[e][r] * (exp2_fast(from[r] + to) * d[r]) : 0.0f;
+          // fragment (t tile, 32 steps s): 0, 1, 2 and 3, 4 and 5 of t tiles 0, 1, 2, 3
+          const int f = id.t < 2 ? id.t : 2 * id.t - 2 + (id.s >> 1);
+          put_quad(&mk[(f * 64 + lane) * 8 + (id.s & 1) * 4], m);
         }
       }
       __syncthreads();
-      if (k + 1 < o.heads) load_x(k + 1);  // (its buffer's readers were through before the barrier)
-      const T* xk = xt[k & 1];
       typename M::Frag xf[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) xf[j] = M::col(xk + 32 * j * TX::LD + 16 * w, TX::LD, li, lq);
@@ -346,31 +435,44 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
         for (int t = 0; t < 4; ++t) y[t] = f4{0, 0, 0, 0};
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
+          typename M::Frag cf[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) cf[t] = M::row(ct + (16 * t + li) * TB::LD + 32 * j + 4 * lq);
           float hf[8];
 #pragma unroll
           for (int r = 0; r < 8; ++r) hf[r] = h[k][2 * j + (r >> 2)][r & 3];
           const typename M::Split hp = M::split(hf);
+          loads_first();
 #pragma unroll
-          for (int t = 0; t < 4; ++t) y[t] = M::mma(hp, M::row(ct + (16 * t + li) * TB::LD + 32 * j + 4 * lq), y[t]);
+          for (int t = 0; t < 4; ++t) y[t] = M::mma(hp, cf[t], y[t]);
         }
-        const float skip = a.skip != nullptr ? a.skip[hd] : 0.0f;
-        T* yp = static_cast<T*>(a.y) + (o.b * a.L + t0) * a.H * a.P + hd * a.P + p0 + 16 * w + 4 * lq;
+        typename M::Frag mf[6];
+        f4 xr[4];
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) mf[i] = *reinterpret_cast<const typename M::Frag*>(&mk[(i * 64 + lane) * 8]);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const float f = exp2_fast(-ss[k][16 * t + li]);
+          f[t] = sp[k][16 * t + li];
+          xr[t] = quad(xk + (16 * t + li) * TX::LD + 16 * w + 4 * lq);
+        }
+        loads_first();
+        const float skip = a.skip != nullptr ? a.skip[hd] : 0.0f;
+        T* yp = static_cast<T*>(a.y) + (o.b * a.L + t0) * hp + hd * a.P + p0 + 16 * w;
+        const int cols = a.P - p0 - 16 * w - 4 * lq;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[t][r] *= f;
+        for (int t = 0; t < 4; ++t) {
 #pragma unroll
-          for (int j = 0; j <= t / 2; ++j) {
-            const int fr = t < 2 ? t : 2 * t - 2 + j;
-            const typename M::Frag mf = *reinterpret_cast<const typename M::Frag*>(&mt[k & 1][(fr * 64 + lane) * 8]);
-            y[t] = M::mma(xf[j], mf, y[t]);
-          }
+          for (int r = 0; r < 4; ++r) y[t][r] *= f[t];
+#pragma unroll
+          for (int j = 0; j <= t / 2; ++j) y[t] = M::mma(xf[j], mf[t < 2 ? t : 2 * t - 2 + j], y[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
           const int row = 16 * t + li;
-          const f4 xr = quad(xk + row * TX::LD + 16 * w + 4 * lq);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) y[t][r] = row < rows ? fmaf(skip, xr[r], y[t][r]) : 0.0f;
-          if (row < held) store_quad(yp + (int64_t)row * a.H * a.P, a.P - p0 - 16 * w - 4 * lq, y[t]);
+          for (int r = 0; r < 4; ++r) y[t][r] = row < rows ? fmaf(skip, xr[t][r], y[t][r]) : 0.0f;
+          if (row < held) store_quad(yp + ((uint32_t)row * (uint32_t)hp + 4 * lq), cols, y[t]);
         }
       }
       const float keep = exp2_fast(-st[k]);
@@ -381,13 +483,30 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
         for (int r = 0; r < 4; ++r) h[k][v][r] *= keep;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
+        typename M::Frag bf[NT];
+#pragma unroll
+        for (int v = 0; v < NT; ++v) bf[v] = M::col(bt + 32 * j * TB::LD + 16 * v, TB::LD, li, lq);
         const f4 w0 = load_f4(&sw[k][32 * j + 4 * lq]), w1 = load_f4(&sw[k][32 * j + 16 + 4 * lq]);
         float xw[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) xw[r] = M::at(xf[j], r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
         const typename M::Split xp = M::split(xw);
+        loads_first();
 #pragma unroll
-        for (int v = 0; v < NT; ++v) h[k][v] = M::mma(M::col(bt + 32 * j * TB::LD + 16 * v, TB::LD, li, lq), xp, h[k][v]);
+        for (int v = 0; v < NT; ++v) h[k][v] = M::mma(bf[v], xp, h[k][v]);
+      }
+    }
+  }
+  if constexpr (!STATES) {  // behind the row's end: the state stays
+    for (int64_t ch = c0 + active; ch < c1; ++ch) {
+      const int64_t t0 = ch * Q;
+      const int held = (int)(a.L - t0 < Q ? a.L - t0 : Q);
+      T* y = static_cast<T*>(a.y) + (o.b * a.L + t0) * hp;
+      for (int k = 0; k < o.heads; ++k) {
+        const int hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
+        const int cols = a.P - p0 < SEL_P ? a.P - p0 : SEL_P;
+        for (int i = tid; i < held * SEL_P; i += SEL_THREADS)
+          if (i % SEL_P < cols) y[(i / SEL_P) * hp + (hv >> a.p.PS) * a.P + p0 + i % SEL_P] = T(0);
       }
     }
   }
@@ -402,8 +521,8 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_fwd_kernel(SelArgs a) {
       for (int v = 0; v < NT; ++v) put_quad(s + 16 * v, h[k][v]);
       if (tid == 0) a.decay[at] = total[k];
     } else if (a.p.segs == 1 && a.h_out != nullptr) {
-      const int p0 = hv % a.p.PB * SEL_P;
-      float* s = a.h_out + ((o.b * a.H + hv / a.p.PB) * (int64_t)a.P + p0 + p) * a.N;
+      const int p0 = (hv & a.p.PS) * SEL_P;
+      float* s = a.h_out + ((o.b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p0 + p) * a.N;
 #pragma unroll
       for (int v = 0; v < NT; ++v)
 #pragma unroll
@@ -425,250 +544,317 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
   f4 e{s.get(p, n), s.get(p, n + 1), s.get(p, n + 2), s.get(p, n + 3)};
   float* buf = (REV ? a.leave : a.enter) + bh * a.p.segs * (int64_t)(SEL_P * NP) + at;
   const float* decay = a.decay + bh * a.p.segs;
-  for (int64_t i = 0; i < a.p.segs; ++i) {
-    const int64_t k = REV ? a.p.segs - 1 - i : i;
-    float* q = buf + k * (int64_t)(SEL_P * NP);
-    const f4 own = load_f4(q);
-    const float keep = exp2_fast(-decay[k]);
-    put_quad(q, e);
+  constexpr int U = 8;  // segments loaded together
+  for (int64_t i = 0; i < a.p.segs; i += U) {
+    f4 own[U];
+    float keep[U];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) e[r] = fmaf(keep, e[r], own[r]);
+    for (int u = 0; u < U; ++u)
+      if (i + u < a.p.segs) {
+        const int64_t k = REV ? a.p.segs - 1 - i - u : i + u;
+        own[u] = load_f4(buf + k * (int64_t)(SEL_P * NP));
+        keep[u] = exp2_fast(-decay[k]);
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (i + u < a.p.segs) {
+        const int64_t k = REV ? a.p.segs - 1 - i - u : i + u;
+        put_quad(buf + k * (int64_t)(SEL_P * NP), e);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) e[r] = fmaf(keep[u], e[r], own[u][r]);
+      }
   }
   float* out = REV ? a.dh0 : a.h_out;
-  const int p1 = hv % a.p.PB * SEL_P + p;
+  const int p1 = (hv & a.p.PS) * SEL_P + p;
   if (out != nullptr && p1 < a.P)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (n + r < a.N) out[((b * a.H + hv / a.p.PB) * (int64_t)a.P + p1) * a.N + n + r] = e[r];
+      if (n + r < a.N) out[((b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p1) * a.N + n + r] = e[r];
 }
 
 // ---------------------------------------------------------------------------
 // Backward: a work-group takes a segment of up to SEL_BWD_HEADS row blocks of a group, so that db and dc are summed over them
-// in registers.  First the states before each chunk are made again (to hs); then the chunks from the last one back, head after
-// head.  A wave owns the 16-state tiles w, w + 4: there states and their gradients are lanes (n, q) with p = 16 v + 4 q .. + 3,
-// as their products with x and dy need them; du, which needs a row's states, takes them through LDS.
+// in registers.  First the states before each chunk are made again (to hs), a head after the other; then the chunks from the
+// last one back, in each head after head.  A wave owns the 16-state tiles w, w + 4: there states and their gradients are
+// lanes (n, q) with p = 16 v + 4 q .. + 3, as their products with x and dy need them; du, which needs a row's states, takes
+// them through LDS.  What the next head needs is loaded to registers meanwhile.
 // ---------------------------------------------------------------------------
 template <typename T, int NT> struct BwdLds {
   static constexpr int SL = NT < 4 ? NT : 4, NS = 16 * SL;  // state tiles of a slice, which goes through LDS at once
   typedef Tile<T, 16 * NT> TB;
   typedef Tile<T, SEL_P> TX;
-  __align__(16) T bt[Q * TB::LD];
-  __align__(16) T ct[Q * TB::LD];
-  __align__(16) T xt[Q * TX::LD];
-  __align__(16) T dt[Q * TX::LD];
-  __align__(16) T ek[Q * TX::LD];              // row s: E[t,s] D_s K[t,s] over t
-  __align__(16) T eg[Q * TX::LD];              // row s: E[t,s] (c_t.b_s)
+  __align__(16) T bc[2][Q * TB::LD];  // b, c
+  __align__(16) T xd[2][Q * TX::LD];  // x, dy
+  __align__(16) T ek[Q * TX::LD];     // row s: E[t,s] D_s K[t,s] over t
+  __align__(16) T eg[Q * TX::LD];     // row s: E[t,s] (c_t.b_s)
   __align__(16) T gx[2][sizeof(T) == 2 ? NS * TX::LD : NS * TX::LD / 2];  // row n: g over p (two parts; float32: one)
-  __align__(16) float s[Q], d[Q], suf[Q], pre[Q], slope[Q];  // s, D, exp(-what follows), exp(-s), dD/d dt
-  float rowz[4][Q], colz[4][Q], ic[4][Q], ig[4][Q];  // by s tile, by t tile, by wave, by wave
-  float lam[SEL_BWD_HEADS][4], sums[SEL_BWD_HEADS][3], skip[4], total;
+  __align__(16) Between gap;
+  __align__(16) float d[Q], suf[Q], pre[Q], slope[Q];  // D, exp(-what follows), exp(-s), dD / d dt
+  __align__(16) float rowz[4][Q], colz[4][Q], ic[4][Q], ig[4][Q];  // by s tile, by t tile, by wave, by wave
+  float lam[2][SEL_BWD_HEADS][4], sums[SEL_BWD_HEADS][3], skip[4], total[2];
 };
 
 template <typename T, int NT>
-__global__ __launch_bounds__(SEL_THREADS) void selective_bwd_kernel(SelArgs a) {
+__global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) void selective_bwd_kernel(SelArgs a) {
   typedef Mx<T> M;
   typedef BwdLds<T, NT> Lds;
   typedef typename Lds::TB TB;
   typedef typename Lds::TX TX;
-  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL;
+  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL, STATE = 4 * NW * 4 * 64;
   extern __shared__ __align__(16) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
-  const Place o = place_of(a, a.p.HR);
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, li = lane & 15, lq = lane >> 4;
+  T *const bt = l.bc[0], *const ct = l.bc[1], *const xt = l.xd[0], *const dt = l.xd[1];
+  uint32_t index;
+  const Place o = place_of(a, a.p.HR, &index);
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), li = lane & 15, lq = lane >> 4;
   const int64_t n = length_of(a, o.b);
-  const int64_t c0 = o.seg * a.p.seg, c1 = c0 + a.p.seg < a.p.chunks ? c0 + a.p.seg : a.p.chunks;
-  const T* px = static_cast<const T*>(a.x.p) + o.b * a.x.sb;
-  const T* pd = static_cast<const T*>(a.dy.p) + o.b * a.dy.sb;
-  const T* pb = static_cast<const T*>(a.b.p) + o.b * a.b.sb + o.g * a.N;
-  const T* pc = static_cast<const T*>(a.c.p) + o.b * a.c.sb + o.g * a.N;
+  const int64_t c0 = o.seg * a.p.seg;
+  const int all = (int)(a.p.chunks - c0 < a.p.seg ? a.p.chunks - c0 : a.p.seg);  // chunks of the segment
+  const int64_t some = (n + Q - 1) / Q - c0;
+  const int active = (int)(some < 0 ? 0 : some < all ? some : all);              // those with steps
+  // where the segment's rows begin, and the distance of their steps
+  const uint32_t sx = (uint32_t)a.x.st, sy = (uint32_t)a.dy.st, sb = (uint32_t)a.b.st, sc = (uint32_t)a.c.st, sd = (uint32_t)a.dt.st;
+  const T* px = static_cast<const T*>(a.x.p) + o.b * a.x.sb + c0 * Q * a.x.st;
+  const T* pd = static_cast<const T*>(a.dy.p) + o.b * a.dy.sb + c0 * Q * a.dy.st;
+  const T* pb = static_cast<const T*>(a.b.p) + o.b * a.b.sb + c0 * Q * a.b.st + o.g * a.N;
+  const T* pc = static_cast<const T*>(a.c.p) + o.b * a.c.sb + c0 * Q * a.c.st + o.g * a.N;
+  const T* pt = static_cast<const T*>(a.dt.p) + o.b * a.dt.sb + c0 * Q * a.dt.st;
+  const int left = (int)(n - c0 * Q < (int64_t)active * Q ? n - c0 * Q : (int64_t)active * Q);  // steps of the segment (with active chunks)
+  auto step_at = [&](int ci, int hd) { return ci * Q + lane < left ? to_f32(pt[(int64_t)(ci * Q) * sd + (uint32_t)lane * sd + hd]) : 0.0f; };
   const bool mine = w < NT;  // the wave has state tiles
-  // states of a work-group: [chunk (one more)][head][wave][own tile][p tile][lane]
-  const int64_t wg = a.wg0 + blockIdx.x;
-  f4* hs = a.hs + wg * (a.p.seg + 1) * a.p.HR * (4 * NW * 4 * 64) + w * (NW * 4 * 64) + lane;
-  f4* gs = a.gs + wg * a.p.HR * (4 * NW * 4 * 64) + w * (NW * 4 * 64) + lane;
-  auto hs_at = [&](int64_t c, int k) { return hs + (c * a.p.HR + k) * (4 * NW * 4 * 64); };
-  auto gs_at = [&](int k) { return gs + k * (4 * NW * 4 * 64); };
+  // states of a work-group before its chunks, but for the first: [chunk][head][wave][own tile][p tile][lane]
+  f4* const hs = a.hs + (int64_t)index * a.p.seg * a.p.HR * STATE + w * (NW * 4 * 64);
+  f4* const gs = a.gs + (int64_t)index * a.p.HR * STATE + w * (NW * 4 * 64);
+  auto hs_at = [&](int c, int k) { return hs + (int64_t)(c * a.p.HR + k) * STATE; };
+  auto gs_at = [&](int k) { return gs + k * STATE; };
+  auto rows_at = [&](int ci) { return left - ci * Q < Q ? left - ci * Q : Q; };
+  auto held_at = [&](int ci) { const int64_t h = a.L - (c0 + ci) * Q; return (int)(h < Q ? h : Q); };  // rows of the chunk at all
+  auto at_of = [&](int k) { return ((o.hv0 + k) >> a.p.PS) * a.P + ((o.hv0 + k) & a.p.PS) * SEL_P; };  // a row block's columns
+  auto cols_of = [&](int k) { return a.P - ((o.hv0 + k) & a.p.PS) * SEL_P; };
 
   for (int i = tid; i < Q * TX::LD; i += SEL_THREADS) l.ek[i] = l.eg[i] = T(0);
+  if (tid < SEL_BWD_HEADS * 3) l.sums[tid / 3][tid % 3] = 0.0f;
   if (tid < 4) l.skip[tid] = 0.0f;
-  // the states entering and the gradients behind the segment
-  for (int k = 0; k < o.heads; ++k) {
-    const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
-    const StateAt e = state_at(a, a.dh_out, a.p.segs > 1 ? a.leave : nullptr, o.b, o.hv0 + k, o.seg);
-    if (mine)
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          f4 hv, gv;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            hv[r] = s.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
-            gv[r] = e.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
-          }
-          hs_at(0, k)[(m * 4 + v) * 64] = hv;
-          gs_at(k)[(m * 4 + v) * 64] = gv;
-        }
-  }
-  auto put_steps = [&](int64_t t0, int k) {  // by one wave
-    const Steps s = steps_of<T>(a, o.b, t0, n, (o.hv0 + k) / a.p.PB, lane);
-    l.s[lane] = s.s;
-    l.d[lane] = s.d;
-    l.suf[lane] = exp2_fast(-s.after);
-    l.pre[lane] = exp2_fast(-s.s);
-    l.slope[lane] = s.slope;
-    if (lane == 0) l.total = s.total;
-  };
-  auto cols_of = [&](int k, int64_t* at) {  // a row block's columns within a step
-    const int hv = o.hv0 + k, p0 = hv % a.p.PB * SEL_P;
-    *at = hv / a.p.PB * a.P + p0;
-    return a.P - p0;
-  };
 
-  // the states before each chunk, and behind the last
-  for (int64_t ci = 0; ci < c1 - c0; ++ci) {
-    const int64_t t0 = (c0 + ci) * Q;
-    const int rows = (int)(n - t0 < 0 ? 0 : n - t0 < Q ? n - t0 : Q);
-    __syncthreads();
-    if (rows > 0) {
-      TB t;
-      t.load(pb + t0 * a.b.st, a.b.st, rows, a.N);
-      t.put(l.bt);
-    }
+  // The states before each chunk, and behind the last: b's and x's tiles in two buffers each (bc, xd), the weights D exp(-what
+  // follows) in ic[0], ic[1].
+  {
+    TB rb;
+    TX rx;
+    float step = 0.0f;
+    auto load = [&](int k, int ci) {
+      rb.load(pb + (int64_t)(ci * Q) * sb, sb, rows_at(ci), a.N, here(tid));
+      rx.load(px + (int64_t)(ci * Q) * sx + at_of(k), sx, rows_at(ci), cols_of(k), here(tid));
+      if (w == (ci & 3)) step = step_at(ci, (o.hv0 + k) >> a.p.PS);
+    };
+    if (active > 0) load(0, 0);
+    int turn = 0;
     for (int k = 0; k < o.heads; ++k) {
-      __syncthreads();
-      if (rows > 0) {
-        int64_t at;
-        const int cols = cols_of(k, &at);
-        TX t;
-        t.load(px + t0 * a.x.st + at, a.x.st, rows, cols);
-        t.put(l.xt);
-        if (w == 0) put_steps(t0, k);
-      }
-      __syncthreads();
-      if (!mine) continue;
       f4 h[NW][4];
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) h[m][v] = hs_at(ci, k)[(m * 4 + v) * 64];
-      if (rows > 0) {
-        const float keep = exp2_fast(-l.total);
+      const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
+      if (mine)
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
-          for (int v = 0; v < 4; ++v)
+          for (int v = 0; v < 4; ++v) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) h[m][v][r] *= keep;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float ws[8];
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            const int t = 32 * j + 16 * (r >> 2) + 4 * lq + (r & 3);
-            ws[r] = l.d[t] * l.suf[t];
+            for (int r = 0; r < 4; ++r) h[m][v][r] = s.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
           }
-          typename M::Split bs[NW];
+      for (int ci = 0; ci < active; ++ci) {
+        const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
+        rb.put(l.bc[turn]);
+        rx.put(l.xd[turn]);
+        if (w == (ci & 3)) {
+          const Steps p = steps_of(a, step, lane < rows_at(ci), (o.hv0 + k) >> a.p.PS, lane);
+          l.ic[turn][lane] = p.d * exp2_fast(-p.after);
+          if (lane == 0) l.total[turn] = p.total;
+        }
+        if (ci + 1 < active)
+          load(k, ci + 1);
+        else if (k + 1 < o.heads)
+          load(k + 1, 0);
+        __syncthreads();
+        if (mine) {
+          const T *b = l.bc[turn], *x = l.xd[turn];
+          const float keep = exp2_fast(-l.total[turn]);
 #pragma unroll
-          for (int m = 0; m < NW; ++m) {
-            const typename M::Frag bf = M::col(l.bt + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
-            float bw[8];
+          for (int m = 0; m < NW; ++m)
 #pragma unroll
-            for (int r = 0; r < 8; ++r) bw[r] = M::at(bf, r) * ws[r];
-            bs[m] = M::split(bw);
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) h[m][v][r] *= keep;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const f4 w0 = load_f4(&l.ic[turn][32 * j + 4 * lq]), w1 = load_f4(&l.ic[turn][32 * j + 16 + 4 * lq]);
+            typename M::Frag xf[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) xf[v] = M::col(x + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
+            typename M::Split bs[NW];
+#pragma unroll
+            for (int m = 0; m < NW; ++m) {
+              const typename M::Frag bf = M::col(b + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
+              float bw[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) bw[r] = M::at(bf, r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
+              bs[m] = M::split(bw);
+            }
+            loads_first();
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+              for (int m = 0; m < NW; ++m) h[m][v] = M::mma(xf[v], bs[m], h[m][v]);
           }
+          if (ci + 1 < active)
+#pragma unroll
+            for (int m = 0; m < NW; ++m)
+#pragma unroll
+              for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 4 + v) * 64 + lane] = h[m][v];
+        }
+        turn ^= 1;
+      }
+      // <g, h> behind the segment
+      float dot = 0.0f;
+      const StateAt e = state_at(a, a.dh_out, a.p.segs > 1 ? a.leave : nullptr, o.b, o.hv0 + k, o.seg);
+      if (mine)
+#pragma unroll
+        for (int m = 0; m < NW; ++m)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            const typename M::Frag xf = M::col(l.xt + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
 #pragma unroll
-            for (int m = 0; m < NW; ++m) h[m][v] = M::mma(xf, bs[m], h[m][v]);
+            for (int r = 0; r < 4; ++r) dot = fmaf(h[m][v][r], e.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li), dot);
           }
-        }
-      }
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 4 + v) * 64] = h[m][v];
+      dot = sum_wave(dot);
+      if (lane == 0) l.lam[(active - 1) & 1][k][w] = dot;
     }
   }
-  // <g, h> behind the segment
-  for (int k = 0; k < o.heads; ++k) {
-    float dot = 0.0f;
-    if (mine)
+
+  TB rb, rc;
+  TX rx, rd;
+  float step = 0.0f;
+  f4 g[NW][4], h[NW][4], gn[NW][4];  // a head's, and the next one's
+  auto load_g = [&](int ci, int k, int lane, f4(&g)[NW][4]) {
+    if (!mine) return;
+    const int li = lane & 15, lq = lane >> 4;
+    if (ci == active - 1) {
+      const StateAt e = state_at(a, a.dh_out, a.p.segs > 1 ? a.leave : nullptr, o.b, o.hv0 + k, o.seg);
 #pragma unroll
       for (int m = 0; m < NW; ++m)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const f4 h = hs_at(c1 - c0, k)[(m * 4 + v) * 64], g = gs_at(k)[(m * 4 + v) * 64];
+        for (int v = 0; v < 4; ++v)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dot = fmaf(h[r], g[r], dot);
-        }
+          for (int r = 0; r < 4; ++r) g[m][v][r] = e.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
+    } else {
 #pragma unroll
-    for (int s = 1; s < 64; s <<= 1) dot += __shfl_xor(dot, s);
-    if (lane == 0) l.lam[k][w] = dot;
+      for (int m = 0; m < NW; ++m)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) g[m][v] = gs_at(k)[(m * 4 + v) * 64 + lane];
+    }
+  };
+  auto load_h = [&](int ci, int k, int lane, f4(&h)[NW][4]) {
+    if (!mine) return;
+    const int li = lane & 15, lq = lane >> 4;
+    if (ci == 0) {
+      const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
+#pragma unroll
+      for (int m = 0; m < NW; ++m)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) h[m][v][r] = s.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
+    } else {
+#pragma unroll
+      for (int m = 0; m < NW; ++m)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) h[m][v] = hs_at(ci, k)[(m * 4 + v) * 64 + lane];
+    }
+  };
+  auto put_dh0 = [&](int k, int lane, const f4(&g)[NW][4]) {
+    if (!mine || a.dh0 == nullptr) return;
+    const int li = lane & 15, lq = lane >> 4, hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
+    float* s = a.dh0 + ((o.b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p0) * a.N;
+#pragma unroll
+    for (int m = 0; m < NW; ++m)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int c = 16 * (w + 4 * m) + li, p = 16 * v + 4 * lq;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (c < a.N && p0 + p + r < a.P) s[(p + r) * a.N + c] = g[m][v][r];
+      }
+  };
+  // (a head alone has its gradient only when its chunk is through)
+  const bool ahead = o.heads > 1;
+  auto steps_wave = [&](int k) { return (k + 2) & 3; };  // which wave makes a head's steps
+  auto load_chunk = [&](int ci) {
+    rb.load(pb + (int64_t)(ci * Q) * sb, sb, rows_at(ci), a.N, here(tid));
+    rc.load(pc + (int64_t)(ci * Q) * sc, sc, rows_at(ci), a.N, here(tid));
+  };
+  auto load_head = [&](int ci, int k) {
+    rx.load(px + (int64_t)(ci * Q) * sx + at_of(k), sx, rows_at(ci), cols_of(k), here(tid));
+    rd.load(pd + (int64_t)(ci * Q) * sy + at_of(k), sy, rows_at(ci), cols_of(k), here(tid));
+    if (w == steps_wave(k)) step = step_at(ci, (o.hv0 + k) >> a.p.PS);
+  };
+  if (active > 0) {
+    load_chunk(active - 1);
+    load_head(active - 1, 0);
+    if (ahead) load_g(active - 1, 0, lane, gn);
   }
-  if (tid < SEL_BWD_HEADS * 3) l.sums[tid / 3][tid % 3] = 0.0f;
-
-  for (int64_t ci = c1 - c0 - 1; ci >= 0; --ci) {
+  for (int ci = active - 1; ci >= 0; --ci) {
     const int64_t t0 = (c0 + ci) * Q;
-    const int rows = (int)(n - t0 < 0 ? 0 : n - t0 < Q ? n - t0 : Q);
-    const int held = (int)(a.L - t0 < Q ? a.L - t0 : Q);
+    const int rows = rows_at(ci), held = held_at(ci);
     f4 db[NW][4], dc[NW][4], g0[3];
 #pragma unroll
     for (int m = 0; m < NW; ++m)
 #pragma unroll
       for (int v = 0; v < 4; ++v) db[m][v] = dc[m][v] = f4{0, 0, 0, 0};
     __syncthreads();
-    if (rows > 0) {
-      TB t;
-      t.load(pb + t0 * a.b.st, a.b.st, rows, a.N);
-      t.put(l.bt);
-      t.load(pc + t0 * a.c.st, a.c.st, rows, a.N);
-      t.put(l.ct);
-      __syncthreads();
-      // (c.b)[t][s], by the tiles on and below the diagonal: tile e of 10 is t tile ti, s tile si
+    rb.put(bt);
+    rc.put(ct);
+    if (ci > 0) load_chunk(ci - 1);
+    __syncthreads();
+    // (c.b)[t][s], by the tiles on and below the diagonal
 #pragma unroll
-      for (int e = 0; e < 3; ++e) {
-        const int id = w + 4 * e, ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
-        g0[e] = f4{0, 0, 0, 0};
-        if (id < 10)
+    for (int e = 0; e < 3; ++e) {
+      const TileId id = tile_id(w, e);
+      typename M::Frag fb[KS], fc[KS];
 #pragma unroll
-          for (int k = 0; k < KS; ++k)
-            g0[e] = M::mma(M::row(l.ct + (16 * ti + li) * TB::LD + 32 * k + 4 * lq), M::row(l.bt + (16 * si + li) * TB::LD + 32 * k + 4 * lq), g0[e]);
+      for (int k = 0; k < KS; ++k) {
+        fb[k] = M::row(bt + (16 * id.s + li) * TB::LD + 32 * k + 4 * lq);
+        fc[k] = M::row(ct + (16 * id.t + li) * TB::LD + 32 * k + 4 * lq);
       }
+      loads_first();
+      g0[e] = f4{0, 0, 0, 0};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) g0[e] = M::mma(fc[k], fb[k], g0[e]);
     }
-    float ddt = 0.0f;  // wave 0: a step's, over a head's row blocks
+    float ddt = 0.0f;  // a step's, over a head's row blocks (of the wave that has the head)
     for (int k = 0; k < o.heads; ++k) {
-      const int hv = o.hv0 + k, hd = hv / a.p.PB;
-      int64_t at;
-      const int cols = cols_of(k, &at);
-      T* pdx = static_cast<T*>(a.dx.p) + o.b * a.dx.sb + t0 * a.dx.st + at;
-      T* pdd = static_cast<T*>(a.ddt.p) + o.b * a.ddt.sb + t0 * a.ddt.st + hd;
-      if (rows == 0) {
-        for (int i = tid; i < held * SEL_P; i += SEL_THREADS)
-          if (i % SEL_P < cols) pdx[(int64_t)(i / SEL_P) * a.dx.st + i % SEL_P] = T(0);
-        if (tid < held) pdd[tid * a.ddt.st] = T(0);
-        continue;
-      }
+      const int hv = o.hv0 + k, hd = (hv >> a.p.PS);
+      const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
+      const int cols = cols_of(k);
       const float skip = a.skip != nullptr ? a.skip[hd] : 0.0f;
-      f4 g[NW][4], h[NW][4];
-      if (mine)
+      if (!ahead) load_g(ci, k, lane, gn);
 #pragma unroll
-        for (int m = 0; m < NW; ++m)
+      for (int m = 0; m < NW; ++m)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            g[m][v] = gs_at(k)[(m * 4 + v) * 64];
-            h[m][v] = hs_at(ci, k)[(m * 4 + v) * 64];
-          }
+        for (int v = 0; v < 4; ++v) g[m][v] = gn[m][v];
+      load_h(ci, k, lane, h);
       __syncthreads();  // the last head's readers are through
-      {
-        TX t;
-        t.load(px + t0 * a.x.st + at, a.x.st, rows, cols);
-        t.put(l.xt);
-        t.load(pd + t0 * a.dy.st + at, a.dy.st, rows, cols);
-        t.put(l.dt);
+      rx.put(xt);
+      rd.put(dt);
+      if (w == steps_wave(k)) {
+        const Steps s = steps_of(a, step, lane < rows, hd, lane);
+        l.gap.put(s, lane);
+        l.d[lane] = s.d;
+        l.suf[lane] = exp2_fast(-s.after);
+        l.pre[lane] = exp2_fast(-s.s);
+        l.slope[lane] = s.slope;
+        if (lane == 0) l.total[0] = s.total;
       }
-      if (w == 0) put_steps(t0, k);
+      if (k + 1 < o.heads)
+        load_head(ci, k + 1);
+      else if (ci > 0)
+        load_head(ci - 1, 0);
       // du = exp(-what follows) g b, this wave's 16 rows p: g's slices through LDS
       f4 du[4];
 #pragma unroll
@@ -694,6 +880,7 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_bwd_kernel(SelArgs a) {
 #pragma unroll
         for (int j = 0; j < SL / 2; ++j) {
           typename M::Split gf;
+          typename M::Frag bf[4];
           if constexpr (sizeof(T) == 2) {
             gf.hi = M::col(&l.gx[0][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
             gf.lo = M::col(&l.gx[1][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
@@ -701,170 +888,217 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_bwd_kernel(SelArgs a) {
             gf = M::col(&l.gx[0][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
           }
 #pragma unroll
-          for (int v = 0; v < 4; ++v) du[v] = M::mma(gf, M::row(l.bt + (16 * v + li) * TB::LD + 64 * m + 32 * j + 4 * lq), du[v]);
+          for (int v = 0; v < 4; ++v) bf[v] = M::row(bt + (16 * v + li) * TB::LD + 64 * m + 32 * j + 4 * lq);
+          loads_first();
+#pragma unroll
+          for (int v = 0; v < 4; ++v) du[v] = M::mma(gf, bf[v], du[v]);
         }
       }
       {  // its part of x.du
+        f4 x[4];
+        float f[4];
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          const f4 x = quad(l.xt + (16 * v + li) * TX::LD + 16 * w + 4 * lq);
-          const float f = l.suf[16 * v + li];
-          float dot = 0.0f;
+          x[v] = quad(xt + (16 * v + li) * TX::LD + 16 * w + 4 * lq);
+          f[v] = l.suf[16 * v + li];
+        }
+        loads_first();
+        float dot[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            du[v][r] *= f;
-            dot = fmaf(x[r], du[v][r], dot);
+            du[v][r] *= f[v];
+            dot[v] = fmaf(x[v][r], du[v][r], dot[v]);
           }
-          dot = sum_rows(dot);
-          if (lq == 0) l.ig[w][16 * v + li] = dot;
+          dot[v] = sum_rows(dot[v]);
         }
+        l.ig[w][lane] = lq == 0 ? dot[0] : lq == 1 ? dot[1] : lq == 2 ? dot[2] : dot[3];
       }
       // K = dy.x; Z = (c.b) E K; the weights of the products within the chunk
 #pragma unroll
       for (int e = 0; e < 3; ++e) {
-        const int id = w + 4 * e, ti = id < 1 ? 0 : id < 3 ? 1 : id < 6 ? 2 : 3, si = id - ti * (ti + 1) / 2;
-        if (id >= 10) continue;
+        const TileId id = tile_id(w, e);
+        typename M::Frag fy[2], fx[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          fy[j] = M::row(dt + (16 * id.t + li) * TX::LD + 32 * j + 4 * lq);
+          fx[j] = M::row(xt + (16 * id.s + li) * TX::LD + 32 * j + 4 * lq);
+        }
+        const float from = (id.s == id.t ? l.gap.in : l.gap.behind)[16 * id.s + li] - l.gap.gap(id.s, id.t), d_s = l.d[16 * id.s + li];
+        const f4 to = load_f4(&l.gap.in[16 * id.t + 4 * lq]);
+        loads_first();
         f4 kk{0, 0, 0, 0};
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          kk = M::mma(M::row(l.dt + (16 * ti + li) * TX::LD + 32 * j + 4 * lq), M::row(l.xt + (16 * si + li) * TX::LD + 32 * j + 4 * lq), kk);
-        const float s_s = l.s[16 * si + li], d_s = l.d[16 * si + li];
-        const f4 s_t = load_f4(&l.s[16 * ti + 4 * lq]);
+        for (int j = 0; j < 2; ++j) kk = M::mma(fy[j], fx[j], kk);
         f4 ek, eg, z;
         float col = 0.0f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool in = si < ti || li <= 4 * lq + r;
-          const float f = exp2_fast(s_s - s_t[r]);
+          const bool in = id.s < id.t || li <= 4 * lq + r;
+          const float f = exp2_fast(from - to[r]);
           eg[r] = in ? f * g0[e][r] : 0.0f;
-          const float kf = in ? f * kk[r] : 0.0f;
-          ek[r] = kf * d_s;
+          ek[r] = in ? f * kk[r] * d_s : 0.0f;
           col = fmaf(eg[r], kk[r], col);
-          z[r] = ek[r] * g0[e][r];
+          z[r] = sum_lanes(ek[r] * g0[e][r]);
         }
-        put_quad(l.ek + (16 * si + li) * TX::LD + 16 * ti + 4 * lq, ek);
-        put_quad(l.eg + (16 * si + li) * TX::LD + 16 * ti + 4 * lq, eg);
+        put_quad(l.ek + (16 * id.s + li) * TX::LD + 16 * id.t + 4 * lq, ek);
+        put_quad(l.eg + (16 * id.s + li) * TX::LD + 16 * id.t + 4 * lq, eg);
         col = sum_rows(col);
-        if (lq == 0) l.colz[ti][16 * si + li] = col;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-#pragma unroll
-          for (int sft = 1; sft < 16; sft <<= 1) z[r] += __shfl_xor(z[r], sft);
-        }
-        if (li == 0) *reinterpret_cast<f4*>(&l.rowz[si][16 * ti + 4 * lq]) = z;
-        if (si == ti) {  // the diagonal: dy_t.x_t
+        if (lq == 0) l.colz[id.t][16 * id.s + li] = col;
+        if (li == 0) put_quad(&l.rowz[id.s][16 * id.t + 4 * lq], z);
+        if (id.s == id.t) {  // the diagonal: dy_t.x_t
           float dg = 0.0f;
 #pragma unroll
           for (int r = 0; r < 4; ++r) dg += li == 4 * lq + r ? kk[r] : 0.0f;
-#pragma unroll
-          for (int sft = 1; sft < 64; sft <<= 1) dg += __shfl_xor(dg, sft);
-          if (lane == 0) l.skip[ti] = dg;
+          dg = sum_wave(dg);
+          if (lane == 0) l.skip[id.t] = dg;
         }
       }
       // dc's part from the states: exp(-s_t) h^T dy_t, and with c_t its part of dy.y
       if (mine) {
-        float ic[4] = {0, 0, 0, 0};
+        float ic[4] = {0, 0, 0, 0}, f[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) f[t] = l.pre[16 * t + li];
 #pragma unroll
         for (int m = 0; m < NW; ++m) {
-          f4 acc[4];
+          f4 acc[4], c[4];
 #pragma unroll
-          for (int t = 0; t < 4; ++t) acc[t] = f4{0, 0, 0, 0};
+          for (int t = 0; t < 4; ++t) {
+            acc[t] = f4{0, 0, 0, 0};
+            c[t] = quad(ct + (16 * t + li) * TB::LD + 16 * (w + 4 * m) + 4 * lq);
+          }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
+            typename M::Frag yf[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) yf[t] = M::row(dt + (16 * t + li) * TX::LD + 32 * j + 4 * lq);
             float hf[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) hf[r] = h[m][2 * j + (r >> 2)][r & 3];
             const typename M::Split hp = M::split(hf);
+            loads_first();
 #pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = M::mma(hp, M::row(l.dt + (16 * t + li) * TX::LD + 32 * j + 4 * lq), acc[t]);
+            for (int t = 0; t < 4; ++t) acc[t] = M::mma(hp, yf[t], acc[t]);
           }
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
-            const float f = l.pre[16 * t + li];
-            const f4 c = quad(l.ct + (16 * t + li) * TB::LD + 16 * (w + 4 * m) + 4 * lq);
+          for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-              const float v = acc[t][r] * f;
-              ic[t] = fmaf(c[r], v, ic[t]);
+              const float v = acc[t][r] * f[t];
+              ic[t] = fmaf(c[t][r], v, ic[t]);
               dc[m][t][r] += v;
             }
-          }
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const float v = sum_rows(ic[t]);
-          if (lq == 0) l.ic[w][16 * t + li] = v;
-        }
-      } else if (lane < 16) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) l.ic[w][16 * t + lane] = 0.0f;
+        for (int t = 0; t < 4; ++t) ic[t] = sum_rows(ic[t]);
+        l.ic[w][lane] = lq == 0 ? ic[0] : lq == 1 ? ic[1] : lq == 2 ? ic[2] : ic[3];
+      } else {
+        l.ic[w][lane] = 0.0f;
       }
       __syncthreads();
-      if (w == 0) {  // dl, dD and the parameters' sums; one step a lane
+      if (ahead) {
+        if (k + 1 < o.heads)
+          load_g(ci, k + 1, lane, gn);
+        else if (ci > 0)
+          load_g(ci - 1, 0, lane, gn);
+      }
+      if (w == ((k >> a.p.PS) & 3)) {  // dl, dD and the parameters' sums; one step a lane
         const int tile = lane >> 4;
-        float ry = 0.0f, cu = 0.0f;
-        for (int v = 0; v <= tile; ++v) ry += l.rowz[v][lane];
-        for (int v = tile; v < 4; ++v) cu += l.colz[v][lane];
+        float rz[4], cz[4], ic[4], ig[4], lam = 0.0f;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          ry += l.ic[v][lane];
-          cu += l.ig[v][lane];
+          rz[v] = l.rowz[v][lane];
+          cz[v] = l.colz[v][lane];
+          ic[v] = l.ic[v][lane];
+          ig[v] = l.ig[v][lane];
+          lam += l.lam[ci & 1][k][v];
         }
-        const float d = l.d[lane];
-        float dl = ry - d * cu;
+        const float d = l.d[lane], slope = l.slope[lane], gamma = a.gamma[hd];
+        loads_first();
+        float ry = 0.0f, cu = 0.0f;
 #pragma unroll
-        for (int sft = 1; sft < 64; sft <<= 1) {
-          const float v = __shfl_down(dl, sft);
-          if (lane + sft < 64) dl += v;
+        for (int v = 0; v < 4; ++v) {
+          ry += ic[v] + (v <= tile ? rz[v] : 0.0f);
+          cu += ig[v] + (v >= tile ? cz[v] : 0.0f);
         }
-        dl += l.lam[k][0] + l.lam[k][1] + l.lam[k][2] + l.lam[k][3];
-        const float v = (cu - a.gamma[hd] * dl) * l.slope[lane];
-        float sg = -d * dl, sb = v;
+        float dl = suffix_lanes(ry - d * cu);
+        float later = lam;
 #pragma unroll
-        for (int sft = 1; sft < 64; sft <<= 1) {
-          sg += __shfl_xor(sg, sft);
-          sb += __shfl_xor(sb, sft);
+        for (int v = 3; v > 0; --v) {
+          const float all = of_lane(dl, 16 * v);
+          later += tile < v ? all : 0.0f;
         }
+        dl += later;
+        const float v = (cu - gamma * dl) * slope;
+        const float sg = sum_wave(-d * dl), sb = sum_wave(v);
         if (lane == 0) {
           l.sums[k][0] += sg;
           l.sums[k][1] += sb;
           l.sums[k][2] += l.skip[0] + l.skip[1] + l.skip[2] + l.skip[3];
         }
-        ddt = hv % a.p.PB == 0 ? v : ddt + v;
-        if (hv % a.p.PB == a.p.PB - 1 && lane < held) pdd[lane * a.ddt.st] = from_f32<T>(lane < rows ? ddt : 0.0f);
+        ddt = (hv & a.p.PS) == 0 ? v : ddt + v;
+        if ((hv & a.p.PS) == a.p.PS && lane < held)
+          static_cast<T*>(a.ddt.p)[o.b * a.ddt.sb + (t0 + lane) * a.ddt.st + hd] = from_f32<T>(lane < rows ? ddt : 0.0f);
       }
-      // within the chunk: dc, db, du
+      // within the chunk: dc, db, du (6 fragments of 32 steps: of tiles 0, 1 one, of the others two; the other way round for s)
+      if (mine) {
+        typename M::Frag ef[6];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
+        for (int i = 0; i < 6; ++i) ef[i] = M::col(l.ek + 32 * (i < 2 ? 0 : i & 1) * TX::LD + 16 * (i < 2 ? i : (i + 2) / 2), TX::LD, li, lq);
 #pragma unroll
-        for (int j = 0; j <= t / 2; ++j)
-          if (mine) {
-            const typename M::Frag f = M::col(l.ek + 32 * j * TX::LD + 16 * t, TX::LD, li, lq);
+        for (int m = 0; m < NW; ++m) {
+          typename M::Frag bf[2];
 #pragma unroll
-            for (int m = 0; m < NW; ++m) dc[m][t] = M::mma(M::col(l.bt + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq), f, dc[m][t]);
-          }
+          for (int j = 0; j < 2; ++j) bf[j] = M::col(bt + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
+          loads_first();
 #pragma unroll
-      for (int v = 0; v < 4; ++v)
-#pragma unroll
-        for (int j = v / 2; j < 2; ++j) {
-          if (mine) {
-            const typename M::Frag f = M::row(l.ek + (16 * v + li) * TX::LD + 32 * j + 4 * lq);
-#pragma unroll
-            for (int m = 0; m < NW; ++m) db[m][v] = M::mma(M::col(l.ct + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq), f, db[m][v]);
-          }
-          du[v] = M::mma(M::col(l.dt + 32 * j * TX::LD + 16 * w, TX::LD, li, lq), M::row(l.eg + (16 * v + li) * TX::LD + 32 * j + 4 * lq), du[v]);
+          for (int i = 0; i < 6; ++i) dc[m][i < 2 ? i : (i + 2) / 2] = M::mma(bf[i < 2 ? 0 : i & 1], ef[i], dc[m][i < 2 ? i : (i + 2) / 2]);
         }
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int row = 16 * v + li;
-        const float d = l.d[row];
-        const f4 y = quad(l.dt + row * TX::LD + 16 * w + 4 * lq);
+        for (int i = 0; i < 6; ++i) ef[i] = M::row(l.ek + (16 * (i < 4 ? i / 2 : i - 2) + li) * TX::LD + 32 * (i < 4 ? i & 1 : 1) + 4 * lq);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) du[v][r] = row < rows ? fmaf(skip, y[r], d * du[v][r]) : 0.0f;
-        if (row < held) store_quad(pdx + (int64_t)row * a.dx.st + 16 * w + 4 * lq, cols - 16 * w - 4 * lq, du[v]);
+        for (int m = 0; m < NW; ++m) {
+          typename M::Frag cf[2];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) cf[j] = M::col(ct + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
+          loads_first();
+#pragma unroll
+          for (int i = 0; i < 6; ++i) db[m][i < 4 ? i / 2 : i - 2] = M::mma(cf[i < 4 ? i & 1 : 1], ef[i], db[m][i < 4 ? i / 2 : i - 2]);
+        }
       }
+      {
+        typename M::Frag ef[6], yf[2];
+#pragma unroll
+        for (int i = 0; i < 6; ++i) ef[i] = M::row(l.eg + (16 * (i < 4 ? i / 2 : i - 2) + li) * TX::LD + 32 * (i < 4 ? i & 1 : 1) + 4 * lq);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) yf[j] = M::col(dt + 32 * j * TX::LD + 16 * w, TX::LD, li, lq);
+        f4 y[4];
+        float d[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          y[v] = quad(dt + (16 * v + li) * TX::LD + 16 * w + 4 * lq);
+          d[v] = l.d[16 * v + li];
+        }
+        loads_first();
+#pragma unroll
+        for (int i = 0; i < 6; ++i) du[i < 4 ? i / 2 : i - 2] = M::mma(yf[i < 4 ? i & 1 : 1], ef[i], du[i < 4 ? i / 2 : i - 2]);
+        T* pdx = static_cast<T*>(a.dx.p) + o.b * a.dx.sb + t0 * a.dx.st + at_of(k) + 16 * w;
+        const uint32_t sdx = (uint32_t)a.dx.st;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const int row = 16 * v + li;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) du[v][r] = row < rows ? fmaf(skip, y[v][r], d[v] * du[v][r]) : 0.0f;
+          if (row < held) store_quad(pdx + ((uint32_t)row * sdx + 4 * lq), cols - 16 * w - 4 * lq, du[v]);
+        }
+      }
+      float dot = 0.0f;
       if (mine) {
         // db's part from the states' gradients
+        float f[4];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) f[v] = l.d[16 * v + li] * l.suf[16 * v + li];
 #pragma unroll
         for (int m = 0; m < NW; ++m) {
           f4 acc[4];
@@ -872,22 +1106,24 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_bwd_kernel(SelArgs a) {
           for (int v = 0; v < 4; ++v) acc[v] = f4{0, 0, 0, 0};
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
+            typename M::Frag xf[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) xf[v] = M::row(xt + (16 * v + li) * TX::LD + 32 * j + 4 * lq);
             float gf[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) gf[r] = g[m][2 * j + (r >> 2)][r & 3];
             const typename M::Frag go = M::one(gf);
+            loads_first();
 #pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] = M::mma(go, M::row(l.xt + (16 * v + li) * TX::LD + 32 * j + 4 * lq), acc[v]);
+            for (int v = 0; v < 4; ++v) acc[v] = M::mma(go, xf[v], acc[v]);
           }
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const float f = l.d[16 * v + li] * l.suf[16 * v + li];
+          for (int v = 0; v < 4; ++v)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) db[m][v][r] = fmaf(f, acc[v][r], db[m][v][r]);
-          }
+            for (int r = 0; r < 4; ++r) db[m][v][r] = fmaf(f[v], acc[v][r], db[m][v][r]);
         }
         // g before the chunk, and its product with the state there
-        const float keep = exp2_fast(-l.total);
+        const float keep = exp2_fast(-l.total[0]);
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
@@ -897,76 +1133,87 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_bwd_kernel(SelArgs a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const f4 w0 = load_f4(&l.pre[32 * j + 4 * lq]), w1 = load_f4(&l.pre[32 * j + 16 + 4 * lq]);
+          typename M::Frag yf[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) yf[v] = M::col(dt + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
           typename M::Split cs[NW];
 #pragma unroll
           for (int m = 0; m < NW; ++m) {
-            const typename M::Frag cf = M::col(l.ct + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
+            const typename M::Frag cf = M::col(ct + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
             float cw[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) cw[r] = M::at(cf, r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
             cs[m] = M::split(cw);
           }
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const typename M::Frag yf = M::col(l.dt + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
-#pragma unroll
-            for (int m = 0; m < NW; ++m) g[m][v] = M::mma(yf, cs[m], g[m][v]);
-          }
-        }
-#pragma unroll
-        for (int m = 0; m < NW; ++m)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) gs_at(k)[(m * 4 + v) * 64] = g[m][v];
-      }
-      float dot = 0.0f;
-      if (mine)
-#pragma unroll
-        for (int m = 0; m < NW; ++m)
+          loads_first();
 #pragma unroll
           for (int v = 0; v < 4; ++v)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dot = fmaf(g[m][v][r], h[m][v][r], dot);
+            for (int m = 0; m < NW; ++m) g[m][v] = M::mma(yf[v], cs[m], g[m][v]);
+        }
 #pragma unroll
-      for (int sft = 1; sft < 64; sft <<= 1) dot += __shfl_xor(dot, sft);
-      __syncthreads();  // (wave 0 has read the head's earlier value)
-      if (lane == 0) l.lam[k][w] = dot;
+        for (int m = 0; m < NW; ++m)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            if (ci > 0) gs_at(k)[(m * 4 + v) * 64 + lane] = g[m][v];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot = fmaf(g[m][v][r], h[m][v][r], dot);
+          }
+      }
+      dot = sum_wave(dot);
+      if (lane == 0) l.lam[(ci - 1) & 1][k][w] = dot;
+      if (ci == 0 && a.p.segs == 1) put_dh0(k, lane, g);
     }
     if (mine) {
-      const int64_t gn = (int64_t)a.G * a.N;
+      auto put = [&](auto* pb, auto* pc, uint32_t sb, uint32_t sc) {
 #pragma unroll
-      for (int m = 0; m < NW; ++m)
+        for (int m = 0; m < NW; ++m)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const int row = 16 * v + li, c = 16 * (w + 4 * m) + 4 * lq;
-          if (row >= held) continue;
-          if (row >= rows) db[m][v] = dc[m][v] = f4{0, 0, 0, 0};
-          if (a.part != nullptr) {
-            float* p = a.part + (((int64_t)o.block * 2 * a.B + o.b) * a.L + t0 + row) * gn + o.g * a.N + c;
-            store_quad(p, a.N - c, db[m][v]);
-            store_quad(p + a.B * a.L * gn, a.N - c, dc[m][v]);
-          } else {
-            store_quad(static_cast<T*>(a.db.p) + o.b * a.db.sb + (t0 + row) * a.db.st + o.g * a.N + c, a.N - c, db[m][v]);
-            store_quad(static_cast<T*>(a.dc.p) + o.b * a.dc.sb + (t0 + row) * a.dc.st + o.g * a.N + c, a.N - c, dc[m][v]);
+          for (int v = 0; v < 4; ++v) {
+            const int row = 16 * v + li, c = 16 * (w + 4 * m) + 4 * lq;
+            if (row >= held) continue;
+            if (row >= rows) db[m][v] = dc[m][v] = f4{0, 0, 0, 0};
+            store_quad(pb + ((uint32_t)row * sb + (uint32_t)c), a.N - c, db[m][v]);
+            store_quad(pc + ((uint32_t)row * sc + (uint32_t)c), a.N - c, dc[m][v]);
           }
-        }
+      };
+      if (a.part != nullptr) {
+        const uint32_t gn = (uint32_t)(a.G * a.N);
+        float* p = a.part + (((int64_t)o.block * 2 * a.B + o.b) * a.L + t0) * gn + o.g * a.N;
+        put(p, p + a.B * a.L * gn, gn, gn);
+      } else {
+        put(static_cast<T*>(a.db.p) + o.b * a.db.sb + t0 * a.db.st + o.g * a.N, static_cast<T*>(a.dc.p) + o.b * a.dc.sb + t0 * a.dc.st + o.g * a.N,
+            (uint32_t)a.db.st, (uint32_t)a.dc.st);
+      }
     }
   }
-  for (int k = 0; k < o.heads; ++k) {
-    if (mine && a.p.segs == 1 && a.dh0 != nullptr) {
-      const int hv = o.hv0 + k, p0 = hv % a.p.PB * SEL_P;
-      float* s = a.dh0 + ((o.b * a.H + hv / a.p.PB) * (int64_t)a.P + p0) * a.N;
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          const f4 g = gs_at(k)[(m * 4 + v) * 64];
-          const int c = 16 * (w + 4 * m) + li;
-#pragma unroll
-          for (int r = 0; r < 4; ++r)
-            if (c < a.N && p0 + 16 * v + 4 * lq + r < a.P) s[(int64_t)(16 * v + 4 * lq + r) * a.N + c] = g[r];
-        }
+  // behind the row's end
+  for (int ci = active; ci < all; ++ci) {
+    const int64_t t0 = (c0 + ci) * Q, gn = (int64_t)a.G * a.N;
+    const int held = held_at(ci);
+    for (int k = 0; k < o.heads; ++k) {
+      const int cols = cols_of(k), hv = o.hv0 + k;
+      T* pdx = static_cast<T*>(a.dx.p) + o.b * a.dx.sb + t0 * a.dx.st + at_of(k);
+      for (int i = tid; i < held * SEL_P; i += SEL_THREADS)
+        if (i % SEL_P < cols) pdx[(int64_t)(i / SEL_P) * a.dx.st + i % SEL_P] = T(0);
+      if ((hv & a.p.PS) == 0 && tid < held) static_cast<T*>(a.ddt.p)[o.b * a.ddt.sb + (t0 + tid) * a.ddt.st + (hv >> a.p.PS)] = T(0);
+    }
+    for (int i = tid; i < held * a.N; i += SEL_THREADS) {
+      const int64_t t = t0 + i / a.N, c = (int64_t)o.g * a.N + i % a.N;
+      if (a.part != nullptr) {
+        float* p = a.part + (((int64_t)o.block * 2 * a.B + o.b) * a.L + t) * gn + c;
+        p[0] = p[a.B * a.L * gn] = 0.0f;
+      } else {
+        static_cast<T*>(a.db.p)[o.b * a.db.sb + t * a.db.st + c] = T(0);
+        static_cast<T*>(a.dc.p)[o.b * a.dc.sb + t * a.dc.st + c] = T(0);
+      }
     }
   }
+  if (active == 0 && a.p.segs == 1)
+    for (int k = 0; k < o.heads; ++k) {
+      load_g(-1, k, lane, gn);  // (ci == active - 1: the gradient behind the segment)
+      put_dh0(k, lane, gn);
+    }
   __syncthreads();
   if (tid < o.heads * 3) a.params[((o.b * a.p.segs + o.seg) * a.p.HV + o.hv0) * 3 + tid] = l.sums[tid / 3][tid % 3];
 }
@@ -1095,10 +1342,11 @@ SelPlan sel_plan(bool bf16, int64_t B, int64_t L, int64_t H, int64_t P, int64_t 
   SelPlan p{};
   p.NT = N <= 32 ? 2 : N <= 64 ? 4 : 8;
   p.PB = (int)((P + SEL_P - 1) / SEL_P);
+  p.PS = p.PB - 1;
   p.HV = (int)(H * p.PB);
   p.HG = (int)(H / G * p.PB);
   p.HF = p.NT > 4 ? 2 : 4;
-  p.HR = SEL_BWD_HEADS;
+  p.HR = 4;
   p.chunks = (L + SEL_Q - 1) / SEL_Q;
   // segments: enough work-groups of the forward for the chip, each with two chunks at least
   const int64_t rows = B * G * ((p.HG + p.HF - 1) / p.HF);
