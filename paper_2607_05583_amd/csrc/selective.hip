@@ -99,9 +99,16 @@ __device__ __forceinline__ void put_quad(bf16_t* p, const f4& v) {
   typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
   *reinterpret_cast<bf4*>(p) = __builtin_convertvector(v, bf4);
 }
-// 4 results to a row of memory, n of them
-template <typename T>
+// 4 results to a row of memory, n of them (WHOLE: all or none)
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void store_quad(T* p, int n, const f4& v) {
+  if constexpr (WHOLE) {
+    T q[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) q[r] = from_f32<T>(v[r]);
+    if (n > 0) store_part<T, 4>(p, 4, q);
+    return;
+  }
   T q[4];
 #pragma unroll
   for (int r = 0; r < 4; ++r) q[r] = from_f32<T>(v[r]);
@@ -109,9 +116,11 @@ __device__ __forceinline__ void store_quad(T* p, int n, const f4& v) {
 }
 
 // ---------------------------------------------------------------------------
-// Tiles: Q rows of COLS elements from memory to registers (zeros outside) and on to LDS rows of COLS + PAD
+// Tiles: Q rows of COLS elements from memory to registers (zeros outside) and on to LDS rows of COLS + PAD.  WHOLE: P and N are
+// whole numbers of 16-byte vectors, so that no vector is cut.  (Both in one kernel, the paths of cut vectors were a third of its
+// code, and their addresses spilled the scalar registers.)
 // ---------------------------------------------------------------------------
-template <typename T, int COLS> struct Tile {
+template <typename T, int COLS, bool WHOLE> struct Tile {
   static constexpr int V = 16 / (int)sizeof(T), PR = COLS / V, RT = SEL_THREADS / PR, U = Q / RT, LD = COLS + Mx<T>::PAD;
   static constexpr int BYTES = Q * LD * (int)sizeof(T);
   T v[U][V];
@@ -122,7 +131,7 @@ template <typename T, int COLS> struct Tile {
     for (int u = 0; u < U; ++u) {
       const T* at = reinterpret_cast<const T*>(reinterpret_cast<const char*>(p) + ((uint32_t)(r0 + u * RT) * st + (uint32_t)c) * (uint32_t)sizeof(T));
       if (r0 + u * RT < rows && n > 0)
-        load_part<T, V>(at, n, v[u]);
+        load_part<T, V>(at, WHOLE ? V : n, v[u]);
       else {
 #pragma unroll
         for (int e = 0; e < V; ++e) v[u][e] = T(0);
@@ -265,22 +274,16 @@ __device__ __forceinline__ int64_t length_of(const SelArgs& a, int64_t b) {
   return n < 0 ? 0 : n > a.L ? a.L : n;
 }
 
-// A state [P][N] of a caller's tensor (or none: zeros) or a padded one of the workspace.
-struct StateAt {
-  const float* ext;
-  const float* pad;
-  int P, N, p0, NP;
-  __device__ __forceinline__ float get(int p, int n) const {
-    if (pad != nullptr) return pad[p * NP + n];
-    return ext != nullptr && p0 + p < P && n < N ? ext[(int64_t)(p0 + p) * N + n] : 0.0f;
-  }
-};
-__device__ __forceinline__ StateAt state_at(const SelArgs& a, const float* ext, const float* pad, int64_t b, int hv, int64_t seg) {
-  const int h = (hv >> a.p.PS), NP = 16 * a.p.NT;
-  StateAt s{ext, nullptr, a.P, a.N, (hv & a.p.PS) * SEL_P, NP};
-  if (ext != nullptr) s.ext = ext + (b * a.H + h) * (int64_t)a.P * a.N;
-  if (pad != nullptr) s.pad = pad + ((b * a.p.HV + hv) * a.p.segs + seg) * (int64_t)(SEL_P * NP);
-  return s;
+// A state of the workspace: tiles of 16 x 16, of 4 row tiles v for each state tile m, with lane (n, q) holding p = 4 q .. + 3 of it, as
+// the backward's waves need them.
+__device__ __forceinline__ int state_index(int p, int n) { return (((n >> 4) * 4 + (p >> 4)) * 64 + ((p >> 2) & 3) * 16 + (n & 15)) * 4 + (p & 3); }
+__device__ __forceinline__ int64_t border(const SelArgs& a, int64_t b, int hv, int64_t seg) {
+  return ((b * a.p.HV + hv) * a.p.segs + seg) * (int64_t)(SEL_P * 16 * a.p.NT);
+}
+// An element of a caller's state [B][H][P][N] (none: zero), of a row block
+__device__ __forceinline__ float state_of(const SelArgs& a, const float* s, int64_t b, int hv, int p, int n) {
+  p += (hv & a.p.PS) * SEL_P;
+  return s != nullptr && p < a.P && n < a.N ? s[((b * a.H + (hv >> a.p.PS)) * a.P + p) * (int64_t)a.N + n] : 0.0f;
 }
 
 // The tiles on and below the diagonal: of the 10, wave w has w, w + 4 and w + 8, the last one again where there are no more.
@@ -296,16 +299,16 @@ __device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0
 
 // ---------------------------------------------------------------------------
 // Forward: a wave owns 16 of a row block's 64 rows.  Its states are in registers, transposed: lane (p, q) holds
-// n = 16 v + 4 q .. + 3.  STATES: only the segment's end state from a zero start (and REV: the gradient that the segment
+// n = 16 v + 4 q .. + 3.  STATES: only the segment's end state from a zero start, the other way round (and REV: the gradient that the segment
 // gives to the state before it: dy, c and exp(-s_t) in the place of x, b and the weights, from the last chunk back).
 // ---------------------------------------------------------------------------
 // The next head's x (the next chunk's b, c and steps) are loaded to registers while a head's products run.
-template <typename T, int NT, int HF, bool STATES, bool REV>
+template <typename T, int NT, int HF, bool WHOLE, bool STATES, bool REV>
 __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective_fwd_kernel(SelArgs a) {
   typedef Mx<T> M;
   constexpr int NP = 16 * NT, KS = NT / 2;
-  typedef Tile<T, NP> TB;
-  typedef Tile<T, SEL_P> TX;
+  typedef Tile<T, NP, WHOLE> TB;
+  typedef Tile<T, SEL_P, WHOLE> TX;
   __shared__ __align__(16) T bt[Q * TB::LD];
   __shared__ __align__(16) T ct[STATES ? 8 : Q * TB::LD];
   __shared__ __align__(16) T xt[2][Q * TX::LD];
@@ -332,11 +335,14 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
 #pragma unroll
     for (int v = 0; v < NT; ++v) h[k][v] = f4{0, 0, 0, 0};
     if (!STATES && k < o.heads) {
-      const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
+      const float* e = a.enter + border(a, o.b, o.hv0 + k, o.seg);
 #pragma unroll
       for (int v = 0; v < NT; ++v)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) h[k][v][r] = s.get(16 * w + li, 16 * v + 4 * lq + r);
+        for (int r = 0; r < 4; ++r) {
+          const int p = 16 * w + li, n = 16 * v + 4 * lq + r;
+          h[k][v][r] = a.p.segs > 1 ? e[state_index(p, n)] : state_of(a, a.h0, o.b, o.hv0 + k, p, n);
+        }
     }
   }
   if constexpr (!STATES) {
@@ -472,7 +478,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
           const int row = 16 * t + li;
 #pragma unroll
           for (int r = 0; r < 4; ++r) y[t][r] = row < rows ? fmaf(skip, xr[t][r], y[t][r]) : 0.0f;
-          if (row < held) store_quad(yp + ((uint32_t)row * (uint32_t)hp + 4 * lq), cols, y[t]);
+          if (row < held) store_quad<WHOLE>(yp + ((uint32_t)row * (uint32_t)hp + 4 * lq), cols, y[t]);
         }
       }
       const float keep = exp2_fast(-st[k]);
@@ -493,7 +499,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
         const typename M::Split xp = M::split(xw);
         loads_first();
 #pragma unroll
-        for (int v = 0; v < NT; ++v) h[k][v] = M::mma(bf[v], xp, h[k][v]);
+        for (int v = 0; v < NT; ++v) h[k][v] = STATES ? M::mma(xp, bf[v], h[k][v]) : M::mma(bf[v], xp, h[k][v]);
       }
     }
   }
@@ -516,9 +522,9 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
     const int hv = o.hv0 + k, p = 16 * w + li;
     if constexpr (STATES) {
       const int64_t at = (o.b * a.p.HV + hv) * a.p.segs + o.seg;
-      float* s = (REV ? a.leave : a.enter) + (at * SEL_P + p) * NP + 4 * lq;
+      f4* s = reinterpret_cast<f4*>((REV ? a.leave : a.enter) + at * (SEL_P * NP)) + w * 64 + lane;
 #pragma unroll
-      for (int v = 0; v < NT; ++v) put_quad(s + 16 * v, h[k][v]);
+      for (int v = 0; v < NT; ++v) s[v * 256] = h[k][v];
       if (tid == 0) a.decay[at] = total[k];
     } else if (a.p.segs == 1 && a.h_out != nullptr) {
       const int p0 = (hv & a.p.PS) * SEL_P;
@@ -538,10 +544,12 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
   const int NP = 16 * a.p.NT, per = SEL_P * NP / 4;
   const int64_t id = (int64_t)blockIdx.x * SEL_THREADS + threadIdx.x, bh = a.wg0 + id / per;
   if (bh >= a.B * a.p.HV) return;
-  const int at = (int)(id % per) * 4, p = at / NP, n = at % NP, hv = (int)(bh % a.p.HV);
+  const int at = (int)(id % per) * 4, lane = (at >> 2) & 63, tile = at >> 8, hv = (int)(bh % a.p.HV);
+  const int p = 16 * (tile & 3) + 4 * (lane >> 4), n = 16 * (tile >> 2) + (lane & 15);
   const int64_t b = bh / a.p.HV;
-  const StateAt s = state_at(a, REV ? a.dh_out : a.h0, nullptr, b, hv, 0);
-  f4 e{s.get(p, n), s.get(p, n + 1), s.get(p, n + 2), s.get(p, n + 3)};
+  f4 e;
+#pragma unroll
+  for (int r = 0; r < 4; ++r) e[r] = state_of(a, REV ? a.dh_out : a.h0, b, hv, p + r, n);
   float* buf = (REV ? a.leave : a.enter) + bh * a.p.segs * (int64_t)(SEL_P * NP) + at;
   const float* decay = a.decay + bh * a.p.segs;
   constexpr int U = 8;  // segments loaded together
@@ -566,10 +574,10 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
   }
   float* out = REV ? a.dh0 : a.h_out;
   const int p1 = (hv & a.p.PS) * SEL_P + p;
-  if (out != nullptr && p1 < a.P)
+  if (out != nullptr && n < a.N)
 #pragma unroll
     for (int r = 0; r < 4; ++r)
-      if (n + r < a.N) out[((b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p1) * a.N + n + r] = e[r];
+      if (p1 + r < a.P) out[((b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p1 + r) * a.N + n] = e[r];
 }
 
 // ---------------------------------------------------------------------------
@@ -579,10 +587,10 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
 // lanes (n, q) with p = 16 v + 4 q .. + 3, as their products with x and dy need them; du, which needs a row's states, takes
 // them through LDS.  What the next head needs is loaded to registers meanwhile.
 // ---------------------------------------------------------------------------
-template <typename T, int NT> struct BwdLds {
+template <typename T, int NT, bool WHOLE> struct BwdLds {
   static constexpr int SL = NT < 4 ? NT : 4, NS = 16 * SL;  // state tiles of a slice, which goes through LDS at once
-  typedef Tile<T, 16 * NT> TB;
-  typedef Tile<T, SEL_P> TX;
+  typedef Tile<T, 16 * NT, WHOLE> TB;
+  typedef Tile<T, SEL_P, WHOLE> TX;
   __align__(16) T bc[2][Q * TB::LD];  // b, c
   __align__(16) T xd[2][Q * TX::LD];  // x, dy
   __align__(16) T ek[Q * TX::LD];     // row s: E[t,s] D_s K[t,s] over t
@@ -594,13 +602,13 @@ template <typename T, int NT> struct BwdLds {
   float lam[2][SEL_BWD_HEADS][4], sums[SEL_BWD_HEADS][3], skip[4], total[2];
 };
 
-template <typename T, int NT>
+template <typename T, int NT, bool WHOLE>
 __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) void selective_bwd_kernel(SelArgs a) {
   typedef Mx<T> M;
-  typedef BwdLds<T, NT> Lds;
+  typedef BwdLds<T, NT, WHOLE> Lds;
   typedef typename Lds::TB TB;
   typedef typename Lds::TX TX;
-  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL, STATE = 4 * NW * 4 * 64;
+  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL, STATE = 4 * NW * 4 * 64;  // (f4 of a state, of all waves)
   extern __shared__ __align__(16) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   T *const bt = l.bc[0], *const ct = l.bc[1], *const xt = l.xd[0], *const dt = l.xd[1];
@@ -622,11 +630,17 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   const int left = (int)(n - c0 * Q < (int64_t)active * Q ? n - c0 * Q : (int64_t)active * Q);  // steps of the segment (with active chunks)
   auto step_at = [&](int ci, int hd) { return ci * Q + lane < left ? to_f32(pt[(int64_t)(ci * Q) * sd + (uint32_t)lane * sd + hd]) : 0.0f; };
   const bool mine = w < NT;  // the wave has state tiles
-  // states of a work-group before its chunks, but for the first: [chunk][head][wave][own tile][p tile][lane]
-  f4* const hs = a.hs + (int64_t)index * a.p.seg * a.p.HR * STATE + w * (NW * 4 * 64);
-  f4* const gs = a.gs + (int64_t)index * a.p.HR * STATE + w * (NW * 4 * 64);
-  auto hs_at = [&](int c, int k) { return hs + (int64_t)(c * a.p.HR + k) * STATE; };
-  auto gs_at = [&](int k) { return gs + k * STATE; };
+  // states of a work-group before its chunks, and their gradients: [chunk][head][wave][own tile][p tile][lane].  Before the first
+  // chunk and behind the last they are those at the segment's borders, or the caller's, which are put here first.
+  f4* const hs = a.hs + (int64_t)index * a.p.seg * a.p.HR * STATE + w * 256;
+  f4* const gs = a.gs + (int64_t)index * a.p.HR * STATE + w * 256;
+  const bool several = a.p.segs > 1;
+  const f4* const enter = reinterpret_cast<const f4*>(several ? a.enter + border(a, o.b, o.hv0, o.seg) : nullptr) + w * 256;
+  const f4* const leave = reinterpret_cast<const f4*>(several ? a.leave + border(a, o.b, o.hv0, o.seg) : nullptr) + w * 256;
+  const int64_t next = a.p.segs * (int64_t)(SEL_P * 16 * NT / 4);  // from a row block's to the next one's, in f4
+  // (own tile m is the work-group's tile w + 4 m: four waves' tiles further in both layouts)
+  auto hs_at = [&](int c, int k) { return c > 0 || !several ? hs + (int64_t)(c * a.p.HR + k) * STATE : const_cast<f4*>(enter) + k * next; };
+  auto gs_at = [&](int k, bool last) { return last && several ? const_cast<f4*>(leave) + k * next : gs + k * STATE; };
   auto rows_at = [&](int ci) { return left - ci * Q < Q ? left - ci * Q : Q; };
   auto held_at = [&](int ci) { const int64_t h = a.L - (c0 + ci) * Q; return (int)(h < Q ? h : Q); };  // rows of the chunk at all
   auto at_of = [&](int k) { return ((o.hv0 + k) >> a.p.PS) * a.P + ((o.hv0 + k) & a.p.PS) * SEL_P; };  // a row block's columns
@@ -651,15 +665,25 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
     int turn = 0;
     for (int k = 0; k < o.heads; ++k) {
       f4 h[NW][4];
-      const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
-      if (mine)
+      if (mine) {
+        if (!several)
+#pragma unroll 1
+          for (int i = 0; i < NW * 4; ++i) {
+            f4 h, g;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int p = 16 * (i & 3) + 4 * lq + r, n = 16 * (w + (i & ~3)) + li;
+              h[r] = state_of(a, a.h0, o.b, o.hv0 + k, p, n);
+              g[r] = state_of(a, a.dh_out, o.b, o.hv0 + k, p, n);
+            }
+            hs_at(0, k)[((i & ~3) * 4 + (i & 3)) * 64 + lane] = h;
+            gs_at(k, false)[((i & ~3) * 4 + (i & 3)) * 64 + lane] = g;
+          }
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r) h[m][v][r] = s.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
-          }
+          for (int v = 0; v < 4; ++v) h[m][v] = hs_at(0, k)[(m * 16 + v) * 64 + lane];
+      }
       for (int ci = 0; ci < active; ++ci) {
         const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
         rb.put(l.bc[turn]);
@@ -708,20 +732,20 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
 #pragma unroll
             for (int m = 0; m < NW; ++m)
 #pragma unroll
-              for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 4 + v) * 64 + lane] = h[m][v];
+              for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 16 + v) * 64 + lane] = h[m][v];
         }
         turn ^= 1;
       }
       // <g, h> behind the segment
       float dot = 0.0f;
-      const StateAt e = state_at(a, a.dh_out, a.p.segs > 1 ? a.leave : nullptr, o.b, o.hv0 + k, o.seg);
       if (mine)
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
+            const f4 g = gs_at(k, true)[(m * 16 + v) * 64 + lane];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) dot = fmaf(h[m][v][r], e.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li), dot);
+            for (int r = 0; r < 4; ++r) dot = fmaf(h[m][v][r], g[r], dot);
           }
       dot = sum_wave(dot);
       if (lane == 0) l.lam[(active - 1) & 1][k][w] = dot;
@@ -732,55 +756,13 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   TX rx, rd;
   float step = 0.0f;
   f4 g[NW][4], h[NW][4], gn[NW][4];  // a head's, and the next one's
-  auto load_g = [&](int ci, int k, int lane, f4(&g)[NW][4]) {
-    if (!mine) return;
-    const int li = lane & 15, lq = lane >> 4;
-    if (ci == active - 1) {
-      const StateAt e = state_at(a, a.dh_out, a.p.segs > 1 ? a.leave : nullptr, o.b, o.hv0 + k, o.seg);
+  auto load_g = [&](int ci, int k, int lane) {
+    const f4* p = gs_at(k, ci == active - 1);
+    if (mine)
 #pragma unroll
       for (int m = 0; m < NW; ++m)
 #pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) g[m][v][r] = e.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
-    } else {
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) g[m][v] = gs_at(k)[(m * 4 + v) * 64 + lane];
-    }
-  };
-  auto load_h = [&](int ci, int k, int lane, f4(&h)[NW][4]) {
-    if (!mine) return;
-    const int li = lane & 15, lq = lane >> 4;
-    if (ci == 0) {
-      const StateAt s = state_at(a, a.h0, a.p.segs > 1 ? a.enter : nullptr, o.b, o.hv0 + k, o.seg);
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) h[m][v][r] = s.get(16 * v + 4 * lq + r, 16 * (w + 4 * m) + li);
-    } else {
-#pragma unroll
-      for (int m = 0; m < NW; ++m)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) h[m][v] = hs_at(ci, k)[(m * 4 + v) * 64 + lane];
-    }
-  };
-  auto put_dh0 = [&](int k, int lane, const f4(&g)[NW][4]) {
-    if (!mine || a.dh0 == nullptr) return;
-    const int li = lane & 15, lq = lane >> 4, hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
-    float* s = a.dh0 + ((o.b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p0) * a.N;
-#pragma unroll
-    for (int m = 0; m < NW; ++m)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int c = 16 * (w + 4 * m) + li, p = 16 * v + 4 * lq;
-#pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (c < a.N && p0 + p + r < a.P) s[(p + r) * a.N + c] = g[m][v][r];
-      }
+        for (int v = 0; v < 4; ++v) gn[m][v] = p[(m * 16 + v) * 64 + lane];
   };
   // (a head alone has its gradient only when its chunk is through)
   const bool ahead = o.heads > 1;
@@ -797,7 +779,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   if (active > 0) {
     load_chunk(active - 1);
     load_head(active - 1, 0);
-    if (ahead) load_g(active - 1, 0, lane, gn);
+    if (ahead) load_g(active - 1, 0, lane);
   }
   for (int ci = active - 1; ci >= 0; --ci) {
     const int64_t t0 = (c0 + ci) * Q;
@@ -833,12 +815,18 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
       const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
       const int cols = cols_of(k);
       const float skip = a.skip != nullptr ? a.skip[hd] : 0.0f;
-      if (!ahead) load_g(ci, k, lane, gn);
+      if (!ahead) load_g(ci, k, lane);
 #pragma unroll
       for (int m = 0; m < NW; ++m)
 #pragma unroll
         for (int v = 0; v < 4; ++v) g[m][v] = gn[m][v];
-      load_h(ci, k, lane, h);
+      if (mine) {
+        const f4* p = hs_at(ci, k);
+#pragma unroll
+        for (int m = 0; m < NW; ++m)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) h[m][v] = p[(m * 16 + v) * 64 + lane];
+      }
       __syncthreads();  // the last head's readers are through
       rx.put(xt);
       rd.put(dt);
@@ -999,9 +987,9 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
       __syncthreads();
       if (ahead) {
         if (k + 1 < o.heads)
-          load_g(ci, k + 1, lane, gn);
+          load_g(ci, k + 1, lane);
         else if (ci > 0)
-          load_g(ci - 1, 0, lane, gn);
+          load_g(ci - 1, 0, lane);
       }
       if (w == ((k >> a.p.PS) & 3)) {  // dl, dD and the parameters' sums; one step a lane
         const int tile = lane >> 4;
@@ -1090,7 +1078,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           const int row = 16 * v + li;
 #pragma unroll
           for (int r = 0; r < 4; ++r) du[v][r] = row < rows ? fmaf(skip, y[v][r], d[v] * du[v][r]) : 0.0f;
-          if (row < held) store_quad(pdx + ((uint32_t)row * sdx + 4 * lq), cols - 16 * w - 4 * lq, du[v]);
+          if (row < held) store_quad<WHOLE>(pdx + ((uint32_t)row * sdx + 4 * lq), cols - 16 * w - 4 * lq, du[v]);
         }
       }
       float dot = 0.0f;
@@ -1155,14 +1143,13 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         for (int m = 0; m < NW; ++m)
 #pragma unroll
           for (int v = 0; v < 4; ++v) {
-            if (ci > 0) gs_at(k)[(m * 4 + v) * 64 + lane] = g[m][v];
+            if (ci > 0 || !several) gs[k * STATE + (m * 16 + v) * 64 + lane] = g[m][v];
 #pragma unroll
             for (int r = 0; r < 4; ++r) dot = fmaf(g[m][v][r], h[m][v][r], dot);
           }
       }
       dot = sum_wave(dot);
       if (lane == 0) l.lam[(ci - 1) & 1][k][w] = dot;
-      if (ci == 0 && a.p.segs == 1) put_dh0(k, lane, g);
     }
     if (mine) {
       auto put = [&](auto* pb, auto* pc, uint32_t sb, uint32_t sc) {
@@ -1173,8 +1160,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
             const int row = 16 * v + li, c = 16 * (w + 4 * m) + 4 * lq;
             if (row >= held) continue;
             if (row >= rows) db[m][v] = dc[m][v] = f4{0, 0, 0, 0};
-            store_quad(pb + ((uint32_t)row * sb + (uint32_t)c), a.N - c, db[m][v]);
-            store_quad(pc + ((uint32_t)row * sc + (uint32_t)c), a.N - c, dc[m][v]);
+            store_quad<WHOLE>(pb + ((uint32_t)row * sb + (uint32_t)c), a.N - c, db[m][v]);
+            store_quad<WHOLE>(pc + ((uint32_t)row * sc + (uint32_t)c), a.N - c, dc[m][v]);
           }
       };
       if (a.part != nullptr) {
@@ -1209,10 +1196,18 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
       }
     }
   }
-  if (active == 0 && a.p.segs == 1)
+  if (mine && !several && a.dh0 != nullptr)
     for (int k = 0; k < o.heads; ++k) {
-      load_g(-1, k, lane, gn);  // (ci == active - 1: the gradient behind the segment)
-      put_dh0(k, lane, gn);
+      const int hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
+      float* s = a.dh0 + ((o.b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p0) * a.N;
+#pragma unroll 1
+      for (int i = 0; i < NW * 4; ++i) {
+        const f4 g = gs[k * STATE + ((i & ~3) * 4 + (i & 3)) * 64 + lane];
+        const int c = 16 * (w + (i & ~3)) + li, p = 16 * (i & 3) + 4 * lq;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (c < a.N && p0 + p + r < a.P) s[(p + r) * a.N + c] = g[r];
+      }
     }
   __syncthreads();
   if (tid < o.heads * 3) a.params[((o.b * a.p.segs + o.seg) * a.p.HV + o.hv0) * 3 + tid] = l.sums[tid / 3][tid % 3];
@@ -1235,7 +1230,7 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_bc_kernel(SelArgs a, in
     for (int r = 0; r < 4; ++r) s[r] += q[r];
   }
   const RowsOut& o = second ? a.dc : a.db;
-  store_quad(static_cast<T*>(o.p) + b * o.sb + t * o.st + c, nc, s);
+  store_quad<false>(static_cast<T*>(o.p) + b * o.sb + t * o.st + c, nc, s);
 }
 
 // dgamma, ddt_bias, dskip of a head: a work-group sums its row blocks' parts, each thread every 256th, in a fixed order.
@@ -1311,11 +1306,30 @@ hipError_t over(SelArgs& a, int64_t all, F&& launch) {
   }
   return hipSuccess;
 }
+template <typename T>
+bool whole(const SelArgs& a) {
+  constexpr int V = 16 / (int)sizeof(T);
+  return a.P % V == 0 && a.N % V == 0;
+}
 template <typename T, int NT, bool STATES, bool REV>
 hipError_t forward(SelArgs a, hipStream_t st) {
   constexpr int HF = NT > 4 ? 2 : 4;
   const int64_t wgs = a.B * a.p.segs * a.G * ((a.p.HG + HF - 1) / HF);
-  return over(a, wgs, [&](uint32_t grid) { selective_fwd_kernel<T, NT, HF, STATES, REV><<<grid, SEL_THREADS, 0, st>>>(a); });
+  return over(a, wgs, [&](uint32_t grid) {
+    if (whole<T>(a))
+      selective_fwd_kernel<T, NT, HF, true, STATES, REV><<<grid, SEL_THREADS, 0, st>>>(a);
+    else
+      selective_fwd_kernel<T, NT, HF, false, STATES, REV><<<grid, SEL_THREADS, 0, st>>>(a);
+  });
+}
+template <typename T, int NT, bool WHOLE>
+hipError_t backward(SelArgs a, hipStream_t st) {
+  constexpr int lds = (int)sizeof(BwdLds<T, NT, WHOLE>);
+  static_assert(lds <= 163840, "a compute unit's LDS");
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(selective_bwd_kernel<T, NT, WHOLE>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (e != hipSuccess) return e;
+  const int64_t wgs = a.B * a.p.segs * a.G * ((a.p.HG + a.p.HR - 1) / a.p.HR);
+  return over(a, wgs, [&](uint32_t grid) { selective_bwd_kernel<T, NT, WHOLE><<<grid, SEL_THREADS, lds, st>>>(a); });
 }
 template <bool REV>
 hipError_t join(SelArgs a, hipStream_t st) {
@@ -1379,13 +1393,7 @@ hipError_t launch_selective_bwd(const SelArgs& a, hipStream_t st) {
       if (e == hipSuccess) e = join<true>(a, st);
       if (e != hipSuccess) return e;
     }
-    constexpr int lds = (int)sizeof(BwdLds<T, nt>);
-    static_assert(lds <= 163840, "a compute unit's LDS");
-    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(selective_bwd_kernel<T, nt>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    SelArgs c = a;
-    const int64_t wgs = a.B * a.p.segs * a.G * ((a.p.HG + a.p.HR - 1) / a.p.HR);
-    return over(c, wgs, [&](uint32_t grid) { selective_bwd_kernel<T, nt><<<grid, SEL_THREADS, lds, st>>>(c); });
+    return whole<T>(a) ? backward<T, nt, true>(a, st) : backward<T, nt, false>(a, st);
   });
   if (e != hipSuccess) return e;
   SelArgs c = a;
