@@ -356,14 +356,14 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
   float step = 0.0f;
   auto load_chunk = [&](int64_t ci) {  // (a wave has at most one head)
     const int64_t t0 = start_of(ci);
-    rb0.load(pb + t0 * rb.st, (uint32_t)rb.st, rows_at(t0), a.N, tid);
-    if constexpr (!STATES) rc0.load(pc + t0 * a.c.st, (uint32_t)a.c.st, rows_at(t0), a.N, tid);
+    rb0.load(pb + t0 * rb.st, (uint32_t)rb.st, rows_at(t0), a.N, here(tid));
+    if constexpr (!STATES) rc0.load(pc + t0 * a.c.st, (uint32_t)a.c.st, rows_at(t0), a.N, here(tid));
     if (w < o.heads) step = load_step<T>(a, o.b, t0, n, (o.hv0 + w) >> a.p.PS, lane);
   };
   auto load_x = [&](int64_t ci, int k) {
     const int64_t t0 = start_of(ci);
     const int hv = o.hv0 + k, p0 = (hv & a.p.PS) * SEL_P;
-    rx0.load(px + t0 * rx.st + (hv >> a.p.PS) * a.P + p0, (uint32_t)rx.st, rows_at(t0), a.P - p0, tid);
+    rx0.load(px + t0 * rx.st + (hv >> a.p.PS) * a.P + p0, (uint32_t)rx.st, rows_at(t0), a.P - p0, here(tid));
   };
   if (active > 0) {
     load_chunk(0);
@@ -407,6 +407,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
 #pragma unroll
     for (int k = 0; k < HF; ++k) {
       if (k >= o.heads) break;
+      const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
       const int hv = o.hv0 + k, hd = (hv >> a.p.PS), p0 = (hv & a.p.PS) * SEL_P;
       T* const xk = xt[turn];
       T* const mk = mt[STATES ? 0 : turn];
@@ -538,46 +539,40 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
   }
 }
 
-// The segments' states one after the other: each segment's own end state makes way for the state that enters it.
+// The segments' states one after the other: each segment's own end state makes way for the state that enters it.  An element a
+// thread, so that there are enough of them for the latency of the segments' loads, some of which go together.
 template <bool REV>
 __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) {
-  const int NP = 16 * a.p.NT, per = SEL_P * NP / 4;
+  const int per = SEL_P * 16 * a.p.NT;
   const int64_t id = (int64_t)blockIdx.x * SEL_THREADS + threadIdx.x, bh = a.wg0 + id / per;
   if (bh >= a.B * a.p.HV) return;
-  const int at = (int)(id % per) * 4, lane = (at >> 2) & 63, tile = at >> 8, hv = (int)(bh % a.p.HV);
-  const int p = 16 * (tile & 3) + 4 * (lane >> 4), n = 16 * (tile >> 2) + (lane & 15);
+  const int at = (int)(id % per), lane = (at >> 2) & 63, tile = at >> 8, hv = (int)(bh % a.p.HV);
+  const int p = 16 * (tile & 3) + 4 * (lane >> 4) + (at & 3), n = 16 * (tile >> 2) + (lane & 15);
   const int64_t b = bh / a.p.HV;
-  f4 e;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) e[r] = state_of(a, REV ? a.dh_out : a.h0, b, hv, p + r, n);
-  float* buf = (REV ? a.leave : a.enter) + bh * a.p.segs * (int64_t)(SEL_P * NP) + at;
+  float e = state_of(a, REV ? a.dh_out : a.h0, b, hv, p, n);
+  float* buf = (REV ? a.leave : a.enter) + bh * a.p.segs * (int64_t)per + at;
   const float* decay = a.decay + bh * a.p.segs;
-  constexpr int U = 8;  // segments loaded together
+  constexpr int U = 16;  // segments loaded together
   for (int64_t i = 0; i < a.p.segs; i += U) {
-    f4 own[U];
-    float keep[U];
+    float own[U], keep[U];
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i + u < a.p.segs) {
         const int64_t k = REV ? a.p.segs - 1 - i - u : i + u;
-        own[u] = load_f4(buf + k * (int64_t)(SEL_P * NP));
-        keep[u] = exp2_fast(-decay[k]);
+        own[u] = buf[k * per];
+        keep[u] = decay[k];
       }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (i + u < a.p.segs) {
         const int64_t k = REV ? a.p.segs - 1 - i - u : i + u;
-        put_quad(buf + k * (int64_t)(SEL_P * NP), e);
-#pragma unroll
-        for (int r = 0; r < 4; ++r) e[r] = fmaf(keep[u], e[r], own[u][r]);
+        buf[k * per] = e;
+        e = fmaf(exp2_fast(-keep[u]), e, own[u]);
       }
   }
   float* out = REV ? a.dh0 : a.h_out;
   const int p1 = (hv & a.p.PS) * SEL_P + p;
-  if (out != nullptr && n < a.N)
-#pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (p1 + r < a.P) out[((b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p1 + r) * a.N + n] = e[r];
+  if (out != nullptr && n < a.N && p1 < a.P) out[((b * a.H + (hv >> a.p.PS)) * (int64_t)a.P + p1) * a.N + n] = e;
 }
 
 // ---------------------------------------------------------------------------
@@ -1334,7 +1329,7 @@ hipError_t backward(SelArgs a, hipStream_t st) {
 template <bool REV>
 hipError_t join(SelArgs a, hipStream_t st) {
   // (a launch begins with a whole row block)
-  const int64_t per = SEL_P * 16 * a.p.NT / 4, all = a.B * a.p.HV, most = LAUNCH_THREADS / per;
+  const int64_t per = SEL_P * 16 * a.p.NT, all = a.B * a.p.HV, most = LAUNCH_THREADS / per;
   for (a.wg0 = 0; a.wg0 < all; a.wg0 += most) {
     const int64_t n = all - a.wg0 < most ? all - a.wg0 : most;
     selective_join_kernel<REV><<<(uint32_t)((n * per + SEL_THREADS - 1) / SEL_THREADS), SEL_THREADS, 0, st>>>(a);
