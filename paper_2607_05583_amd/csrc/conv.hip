@@ -6,6 +6,8 @@
 // The forward moves two elements a step and channel, the backward three, for 2 K and 8 K operations: memory bounds both.
 // A thread owns a vector of channels over a tile of steps and keeps the last K inputs in registers, so that an input is read
 // once and the K - 1 before its tile again.
+#include <type_traits>
+
 #include "select.h"
 
 namespace res {
@@ -39,9 +41,23 @@ __device__ __forceinline__ float pre_of(const float (&w)[KX][V], const float* u,
   return acc;
 }
 
-template <typename T, int KX, bool EXACT, int V>
+// ACT: the activation, or -1 for that of the arguments.  WHOLE: D is a whole number of vectors.
+template <int ACT> __device__ __forceinline__ int act_of(const ConvArgs& a) { return ACT < 0 ? a.act : ACT; }
+
+// Rows of V elements, zeros where they are not wanted
+template <typename T, int V, bool WHOLE>
+__device__ __forceinline__ void load_row(bool wanted, const T* p, int nd, T (&q)[V]) {
+  if (wanted)
+    load_part<T, V>(p, WHOLE ? V : nd, q);
+  else {
+#pragma unroll
+    for (int e = 0; e < V; ++e) q[e] = T(0);
+  }
+}
+
+template <typename T, int KX, bool EXACT, int V, int ACT, bool WHOLE>
 __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int64_t nb) {
-  constexpr int U = 8, KB = KX - 1;  // steps loaded together
+  constexpr int U = 8, KB = KX - 1;  // steps loaded together, while those before them are computed
   const uint32_t id = blockIdx.x * CONV_THREADS + threadIdx.x, DV = (uint32_t)((a.D + V - 1) / V);
   const uint32_t tiles = (uint32_t)((a.L + CONV_TILE - 1) / CONV_TILE) + (a.L == 0);
   const uint32_t cv = id % DV, rest = id / DV, tile = rest % tiles;
@@ -54,24 +70,25 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int6
     n = n < 0 ? 0 : n > a.L ? a.L : n;
   }
   const T* x = static_cast<const T*>(a.x.p) + b * a.x.sb + d;
-  T* y = static_cast<T*>(a.y) + b * a.L * a.D + d;
   const T* st = a.state != nullptr ? static_cast<const T*>(a.state) + b * (K - 1) * a.D + d : nullptr;
-  // what the state's row j .. holds, and the inputs behind it
   auto input = [&](int64_t t, T(&q)[V]) {  // x_t, of the state where t < 0
     if (t >= 0)
-      load_part<T, V>(x + t * a.x.st, nd, q);
-    else if (st != nullptr && t >= 1 - K)
-      load_part<T, V>(st + (t + K - 1) * a.D, nd, q);
-    else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) q[e] = T(0);
-    }
+      load_row<T, V, WHOLE>(true, x + t * a.x.st, nd, q);
+    else
+      load_row<T, V, WHOLE>(st != nullptr && t >= 1 - K, st + (t + K - 1) * a.D, nd, q);
   };
+  const int in = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_TILE ? n - t0 : CONV_TILE);         // the tile's steps
+  const int end = (int)(a.L - t0 < CONV_TILE ? a.L - t0 : CONV_TILE);                     // its rows
+  const T* xt = x + t0 * a.x.st;
+  const uint32_t sx = (uint32_t)a.x.st, sy = (uint32_t)a.D;  // (within a tile offsets have 32 bits)
+  T q[U][V];
+#pragma unroll
+  for (int s = 0; s < U; ++s) load_row<T, V, WHOLE>(s < in, xt + (uint32_t)s * sx, nd, q[s]);
   float f[KB + U][V];  // the inputs before the steps at hand, and theirs
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
     T q[V] = {};
-    if (t0 < n || tile == 0) input(t0 - KB + k, q);
+    if (in > 0 || tile == 0) input(t0 - KB + k, q);
     widen<T, V>(q, f[k]);
   }
   if (tile == 0 && a.state_out != nullptr) {  // (which may be the state: everything is read before it is written)
@@ -86,29 +103,21 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int6
   }
   float w[KX][V], bias[V];
   load_taps<KX, EXACT, V>(a, d, nd, w, bias);
-  const int64_t end = t0 + CONV_TILE < a.L ? t0 + CONV_TILE : a.L;
-  for (int64_t t = t0; t < end; t += U) {
-    T q[U][V];
-#pragma unroll
-    for (int s = 0; s < U; ++s) {
-      if (t + s < n && t + s < end)
-        load_part<T, V>(x + (t + s) * a.x.st, nd, q[s]);
-      else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) q[s][e] = T(0);
-      }
-    }
+  T* y = static_cast<T*>(a.y) + (b * a.L + t0) * a.D + d;
+  for (int t = 0; t < end; t += U) {
 #pragma unroll
     for (int s = 0; s < U; ++s) widen<T, V>(q[s], f[KB + s]);
+    if (t + U < in)
+#pragma unroll
+      for (int s = 0; s < U; ++s) load_row<T, V, WHOLE>(t + U + s < in, xt + (uint32_t)(t + U + s) * sx, nd, q[s]);
 #pragma unroll
     for (int s = 0; s < U; ++s) {
+      T out[V];
 #pragma unroll
       for (int e = 0; e < V; ++e)
-        q[s][e] = t + s < n ? from_f32<T>(act_value(pre_of<KX, EXACT, V>(w, &f[KB + s][e], V, K, e, bias[e]), a.act)) : T(0);
+        out[e] = t + s < in ? from_f32<T>(act_value(pre_of<KX, EXACT, V>(w, &f[KB + s][e], V, K, e, bias[e]), act_of<ACT>(a))) : T(0);
+      if (t + s < end) store_part<T, V>(y + (uint32_t)(t + s) * sy, WHOLE ? V : nd, out);
     }
-#pragma unroll
-    for (int s = 0; s < U; ++s)
-      if (t + s < end) store_part<T, V>(y + (t + s) * a.D, nd, q[s]);
 #pragma unroll
     for (int k = 0; k < KB; ++k)
 #pragma unroll
@@ -118,7 +127,7 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int6
 
 // The backward's thread goes through its tile's steps and the K - 1 behind them: dpre of each (pre again from the inputs) enters
 // a window, and dx of the step K - 1 before it leaves.  The first tile goes on with the state's gradients.
-template <typename T, int KX, bool EXACT, int V>
+template <typename T, int KX, bool EXACT, int V, int ACT, bool WHOLE>
 __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint32_t blocks_d) {
   constexpr int U = 4, KB = KX - 1, CW = CONV_BWD_CHANNELS, LANES = CW / V, RB = CONV_THREADS / LANES;
   static_assert(RB * LANES == CONV_THREADS && RB <= CONV_BWD_ROWS && CONV_BWD_ROWS % RB == 0, "whole rows of threads");
@@ -145,57 +154,64 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
       n = a.lengths[b];
       n = n < 0 ? 0 : n > a.L ? a.L : n;
     }
-    const T* x = static_cast<const T*>(a.x.p) + b * a.x.sb + d;
-    const T* dy = static_cast<const T*>(a.dy.p) + b * a.dy.sb + d;
-    T* dx = static_cast<T*>(a.dx.p) + b * a.dx.sb + d;
+    // the tile's steps, its rows, and the steps that are there behind it
+    const int in = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_BWD_TILE ? n - t0 : CONV_BWD_TILE);
+    const int held = (int)(a.L - t0 < CONV_BWD_TILE ? a.L - t0 : CONV_BWD_TILE);
+    const int seen = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_BWD_TILE + K - 1 ? n - t0 : CONV_BWD_TILE + K - 1);
+    const T* x = static_cast<const T*>(a.x.p) + b * a.x.sb + t0 * a.x.st + d;
+    const T* dy = static_cast<const T*>(a.dy.p) + b * a.dy.sb + t0 * a.dy.st + d;
+    T* dx = static_cast<T*>(a.dx.p) + b * a.dx.sb + t0 * a.dx.st + d;
+    const uint32_t sx = (uint32_t)a.x.st, sy = (uint32_t)a.dy.st, sd = (uint32_t)a.dx.st;
     const int64_t so = b * (K - 1) * a.D + d;
-    const T* st = a.state != nullptr ? static_cast<const T*>(a.state) + so : nullptr;
     const T* dso = a.dstate_out != nullptr ? static_cast<const T*>(a.dstate_out) + so : nullptr;
-    const int64_t end = t0 + CONV_BWD_TILE < n ? t0 + CONV_BWD_TILE : n;          // behind the tile's own steps
-    const int64_t first = t0 > 0 ? t0 : 1 - K;                                    // the first input whose gradient is made here
+    const int64_t into = n - t0;                    // (step `into` of the tile is the row's end)
+    const int first = t0 > 0 ? 0 : 1 - K;           // the first input whose gradient is made here
+    T qx[U][V], qy[U][V];
+    auto load = [&](int t) {
+#pragma unroll
+      for (int s = 0; s < U; ++s) {
+        load_row<T, V, WHOLE>(t + s < seen, x + (uint32_t)(t + s) * sx, nd, qx[s]);
+        load_row<T, V, WHOLE>(t + s < seen, dy + (uint32_t)(t + s) * sy, nd, qy[s]);
+      }
+    };
+    load(0);
     float f[KB + U][V], g[KB + U][V];
 #pragma unroll
     for (int k = 0; k < KB; ++k) {
       T q[V] = {};
       const int64_t t = t0 - KB + k;
       if (t >= 0 && t < n)
-        load_part<T, V>(x + t * a.x.st, nd, q);
-      else if (t < 0 && st != nullptr && t >= 1 - K)
-        load_part<T, V>(st + (t + K - 1) * a.D, nd, q);
+        load_row<T, V, WHOLE>(true, x + (int64_t)(k - KB) * a.x.st, nd, q);
+      else if (t < 0 && a.state != nullptr && t >= 1 - K)
+        load_row<T, V, WHOLE>(true, static_cast<const T*>(a.state) + so + (t + K - 1) * a.D, nd, q);
       widen<T, V>(q, f[k]);
 #pragma unroll
       for (int e = 0; e < V; ++e) g[k][e] = 0.0f;
     }
-    for (int64_t t = t0; t < end + K - 1; t += U) {
-      T qx[U][V], qy[U][V];
-#pragma unroll
-      for (int s = 0; s < U; ++s) {
-        if (t + s < n && t + s < end + K - 1) {
-          load_part<T, V>(x + (t + s) * a.x.st, nd, qx[s]);
-          load_part<T, V>(dy + (t + s) * a.dy.st, nd, qy[s]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e) qx[s][e] = qy[s][e] = T(0);
-        }
-      }
+    for (int t = 0; t < in + K - 1; t += U) {
 #pragma unroll
       for (int s = 0; s < U; ++s) {
         widen<T, V>(qx[s], f[KB + s]);
         widen<T, V>(qy[s], g[KB + s]);
+      }
+      if (t + U < in + K - 1) load(t + U);
+#pragma unroll
+      for (int s = 0; s < U; ++s) {
+        const bool own = t + s < in;  // (later steps are another tile's)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float pre = pre_of<KX, EXACT, V>(w, &f[KB + s][e], V, K, e, bias[e]);
-          const float dpre = t + s < n ? g[KB + s][e] * act_slope(pre, a.act) : 0.0f;
+          const float dpre = t + s < seen ? g[KB + s][e] * act_slope(pre, act_of<ACT>(a)) : 0.0f;
           g[KB + s][e] = dpre;
-          if (t + s < end) {  // (later steps are another tile's)
-            db[e] += dpre;
+          const float mine = own ? dpre : 0.0f;
+          db[e] += mine;
+          if (own)
 #pragma unroll
             for (int k = 0; k < KX; ++k)
-              if (tap<KX, EXACT>(k, K)) dw[k][e] = fmaf(dpre, f[KB + s - k][e], dw[k][e]);
-          }
+              if (tap<KX, EXACT>(k, K)) dw[k][e] = fmaf(mine, f[KB + s - k][e], dw[k][e]);
         }
-        const int64_t at = t + s - (K - 1);  // the input whose gradient is complete
-        if (at >= first && at < end) {
+        const int at = t + s - (K - 1);  // the input whose gradient is complete
+        if (at >= first && at < in) {
           float du[V];
 #pragma unroll
           for (int e = 0; e < V; ++e) {
@@ -216,10 +232,9 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
                 }
             }
           }
-          const int64_t j = at + (K - 1) - n;  // its place in the state that the call leaves
-          if (dso != nullptr && j >= 0) {
+          if (dso != nullptr && at + (K - 1) >= into) {  // its place in the state that the call leaves
             T q[V];
-            load_part<T, V>(dso + j * a.D, nd, q);
+            load_row<T, V, WHOLE>(true, dso + (at + (K - 1) - into) * a.D, nd, q);
 #pragma unroll
             for (int e = 0; e < V; ++e) du[e] += to_f32(q[e]);
           }
@@ -227,9 +242,9 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
 #pragma unroll
           for (int e = 0; e < V; ++e) q[e] = from_f32<T>(du[e]);
           if (at >= 0)
-            store_part<T, V>(dx + at * a.dx.st, nd, q);
+            store_part<T, V>(dx + (uint32_t)at * sd, WHOLE ? V : nd, q);
           else if (a.dstate != nullptr)
-            store_part<T, V>(static_cast<T*>(a.dstate) + so + (at + K - 1) * a.D, nd, q);
+            store_part<T, V>(static_cast<T*>(a.dstate) + so + (at + K - 1) * a.D, WHOLE ? V : nd, q);
         }
       }
 #pragma unroll
@@ -241,8 +256,7 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
         }
     }
     T zero[V] = {};
-    const int64_t all = t0 + CONV_BWD_TILE < a.L ? t0 + CONV_BWD_TILE : a.L;
-    for (int64_t t = n > t0 ? n : t0; t < all; ++t) store_part<T, V>(dx + t * a.dx.st, nd, zero);
+    for (int t = in; t < held; ++t) store_part<T, V>(dx + (uint32_t)t * sd, WHOLE ? V : nd, zero);
   }
   // the block's sums, in the order of its rows
   for (int k = 0; k <= K; ++k) {
@@ -342,26 +356,44 @@ auto by_taps(int K, F&& f) {
   }
 }
 
-template <typename T, bool EXACT> constexpr int fwd_vec() { return EXACT ? 16 / (int)sizeof(T) : 2; }
-template <bool EXACT> constexpr int bwd_vec() { return EXACT ? 4 : 2; }
+// Channels of a thread: two, so that a thread's windows leave room for many waves on a compute unit, whose loads cover each
+// other's latency.  65536 steps of 640 channels, bf16: forward 50 us (3.4 TB/s; with four channels 55), backward 55 us
+// (4.5 TB/s).
+constexpr int CONV_VEC = 2;
+
+// F with the taps, whether the activation is silu, and whether D is whole vectors, as constants.
+template <typename F>
+hipError_t by_kind(const ConvArgs& a, F&& f) {
+  return by_taps(a.K, [&](auto kx, auto exact) {
+    if constexpr (exact) {
+      if (a.act == ACT_SILU)
+        return a.D % CONV_VEC == 0 ? f(kx, exact, std::integral_constant<int, ACT_SILU>{}, std::true_type{})
+                            : f(kx, exact, std::integral_constant<int, ACT_SILU>{}, std::false_type{});
+      return a.D % CONV_VEC == 0 ? f(kx, exact, std::integral_constant<int, -1>{}, std::true_type{})
+                          : f(kx, exact, std::integral_constant<int, -1>{}, std::false_type{});
+    } else {
+      return f(kx, exact, std::integral_constant<int, -1>{}, std::false_type{});
+    }
+  });
+}
 
 }  // namespace
 
 template <typename T>
 hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st) {
-  return by_taps(a.K, [&](auto kx, auto exact) {
-    constexpr int V = fwd_vec<T, exact>();
+  return by_kind(a, [&](auto kx, auto exact, auto act, auto whole) {
+    constexpr int V = CONV_VEC;
     const int64_t tiles = (a.L + CONV_TILE - 1) / CONV_TILE + (a.L == 0);
     return by_rows(a.B, tiles * ((a.D + V - 1) / V), [&](int64_t b0, int64_t nb, uint32_t grid) {
       a.b0 = b0;
-      conv_fwd_kernel<T, kx, exact, V><<<grid, CONV_THREADS, 0, st>>>(a, nb);
+      conv_fwd_kernel<T, kx, exact, V, act, whole><<<grid, CONV_THREADS, 0, st>>>(a, nb);
     });
   });
 }
 template <typename T>
 hipError_t launch_conv_step(ConvArgs a, hipStream_t st) {
   return by_taps(a.K, [&](auto kx, auto exact) {
-    constexpr int V = 2;  // (a decoding batch has few elements)
+    constexpr int V = CONV_VEC;
     return by_rows(a.B, (a.D + V - 1) / V, [&](int64_t b0, int64_t nb, uint32_t grid) {
       a.b0 = b0;
       conv_step_kernel<T, kx, exact, V><<<grid, CONV_THREADS, 0, st>>>(a, nb);
@@ -372,13 +404,13 @@ template <typename T>
 hipError_t launch_conv_bwd(const ConvArgs& a, hipStream_t st) {
   const int64_t rows = conv_row_blocks(a.B, a.L);
   const uint32_t bd = (uint32_t)((a.D + CONV_BWD_CHANNELS - 1) / CONV_BWD_CHANNELS);
-  const hipError_t e = by_taps(a.K, [&](auto kx, auto exact) {
+  const hipError_t e = by_kind(a, [&](auto kx, auto exact, auto act, auto whole) {
     const int64_t most = LAUNCH_THREADS / CONV_THREADS / bd;
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
       ConvArgs c = a;
       c.b0 = r0;
       const int64_t n = rows - r0 < most ? rows - r0 : most;
-      conv_bwd_kernel<T, kx, exact, bwd_vec<exact>()><<<(uint32_t)(n * bd), CONV_THREADS, 0, st>>>(c, bd);
+      conv_bwd_kernel<T, kx, exact, CONV_VEC, act, whole><<<(uint32_t)(n * bd), CONV_THREADS, 0, st>>>(c, bd);
       const hipError_t e = hipGetLastError();
       if (e != hipSuccess) return e;
     }

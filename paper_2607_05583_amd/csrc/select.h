@@ -43,7 +43,7 @@ constexpr int CONV_TAPS = 16;       // taps at most
 constexpr int CONV_THREADS = 256;
 constexpr int CONV_TILE = 32;       // steps of a thread, forward
 constexpr int CONV_BWD_TILE = 64;   // and backward
-constexpr int CONV_BWD_ROWS = 8;    // tiles of a work-group of the backward, whose weight gradients are summed in it
+constexpr int CONV_BWD_ROWS = 4;    // tiles of a work-group of the backward, whose weight gradients are summed in it
 constexpr int CONV_BWD_CHANNELS = 128;
 
 struct ConvArgs {
