@@ -92,7 +92,7 @@ def train(model, steps, B=32, L=128, vocab=32, rules=4, lr=2e-3, bits=32, seed=1
     losses = []
     for step in range(1, steps + 1):
         t = sequences(B, L + 1, vocab, rules, g)
-        loss = F.cross_entropy(model.logits(t[:, :-1]).float().flatten(0, 1), t[:, 1:].flatten())
+        loss = -ops.resonator_token_logprobs(model.logits(t[:, :-1]), t[:, 1:].contiguous()).mean()
         loss.backward()
         grads = [[p.grad for p in group] for group in model.groups]
         norm = torch.stack([v.float().norm() for group in grads for v in group]).norm()
@@ -113,11 +113,17 @@ def generate(model, prompt, n):
     """``n`` further tokens, the likeliest ones."""
     logits, states = model.prefill(prompt)
     layers = model.damped()
-    out, t = [], logits[:, -1].argmax(-1)
+    out, t = [], likeliest(logits[:, -1])
     for _ in range(n):
         out.append(t)
-        t = model.step(t, states, layers).argmax(-1)
+        t = likeliest(model.step(t, states, layers))
     return torch.stack(out, 1)
+
+
+def likeliest(logits):
+    """[B] tokens of logits [B, vocab] (no token is given whose probability is asked for)."""
+    none = torch.full(logits.shape[:1], -1, device=logits.device)
+    return ops.resonator_token_logprobs_fwd(logits, none, top=1).top_ids[:, 0]
 
 
 def main():
