@@ -7,14 +7,16 @@
 // which are matrix products (MFMA).  The backward, with g the gradient of the state behind the chunk and K[t,s] = dy_t.x_s:
 //   dc_t = sum_s E D_s K b_s + exp(-s_t) h^T dy_t,      db_s = D_s (sum_t E K c_t + exp(s_s - s_Q) g^T x_s),
 //   du_s = sum_t E (c_t.b_s) dy_t + exp(s_s - s_Q) g b_s,  dx_s = D_s du_s + skip dy_s,
-//   dl_t = <g, h'> + sum_{u>=t} (dy_u.y_u - D_u x_u.du_u)   (the gradient of log a_t; y without the skip),
+//   dl_t = exp(-s_Q) <g, h> + sum_{u>=t} exp(-s_u) dy_u.(h c_u) + sum_{s<t} (D_s exp(s_s - s_Q) x_s.(g b_s) + sum_{u>=t} Z[u,s])
+//   (the gradient of log a_t; Z = (c.b) E D K),
 //   dD_s = x_s.du_s - gamma dl_s,  dgamma = -sum D dl,  g' = exp(-s_Q) g + sum_t exp(-s_t) dy_t c_t^T.
-// dy.y and x.du need no rounded products: their parts within the chunk are the row and column sums of Z = (c.b) E K in
-// float32, those of the states are products of two-part operands.
+// dl and x.du need no rounded products: their parts within the chunk are sums of Z in float32, those of the states are products
+// of operands in three parts.
 //
-// Rounding, bf16 inputs: products of two inputs are exact.  An operand that is computed (states, weighted b, c, x) goes in as
-// two bf16 parts, hi + lo, 2^-16 relative, where float32 results depend on it (states, dl); the weights (c.b) E D and E K
-// that only make bf16 outputs, and g in db, go in as one bf16 (2^-8 a term, as much as the output's own rounding).
+// Rounding, bf16 inputs: products of two inputs are exact.  An operand that is computed goes in as three bf16 parts (2^-24 of it is
+// lost) where float32 results depend on it: the weighted x, b and c that make states and their gradients, and those in dl.
+// States that are read for y go in as two parts (2^-16); the weights (c.b) E D and E D K that only make bf16 outputs, and g
+// in du, as one (2^-8 a term, as much as the output's own rounding).
 // float32 inputs use float32 MFMA throughout.  Sums and states are float32.
 #include <type_traits>
 
@@ -34,12 +36,35 @@ constexpr float NO_MORE = 512.0f;  // an exponent (base 2) behind which nothing 
 template <typename T> struct Mx;
 template <> struct Mx<bf16_t> {
   typedef bf8 Frag;
-  struct Split { bf8 hi, lo; };
+  struct Split { bf8 hi, lo; };       // two parts: 2^-16 of a value is lost
+  struct Whole { bf8 hi, mid, lo; };  // three: 2^-24
   struct Quad { uint32_t v[2]; } __attribute__((aligned(8)));
   static constexpr int PAD = 8;
   __device__ static __forceinline__ f4 mma(const Frag& a, const Frag& b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   __device__ static __forceinline__ f4 mma(const Split& a, const Frag& b, f4 c) { return mma(a.hi, b, mma(a.lo, b, c)); }
-  __device__ static __forceinline__ f4 mma(const Frag& a, const Split& b, f4 c) { return mma(a, b.hi, mma(a, b.lo, c)); }
+  __device__ static __forceinline__ f4 mma(const Whole& a, const Frag& b, f4 c) { return mma(a.hi, b, mma(a.mid, b, mma(a.lo, b, c))); }
+  __device__ static __forceinline__ f4 mma(const Frag& a, const Whole& b, f4 c) { return mma(a, b.hi, mma(a, b.mid, mma(a, b.lo, c))); }
+  __device__ static __forceinline__ f4 mma_even(const Frag (&a)[2], const Frag (&b)[2]) {
+    return mma(a[0], b[0], f4{0, 0, 0, 0}) - mma(minus(a[1]), b[1], f4{0, 0, 0, 0});
+  }
+  // The unit's bf16 sums are low by some 2^-28 of their terms on average, whatever their sign (measured: 10^7 products of normal
+  // values, off by up to 2^-20 either way).  In dgamma, which sums millions of them, that stands out (5e-6 of it), so
+  // half of each sum is made of the other sign: the second half of a product over a row block, and every other chunk's g.
+  __device__ static __forceinline__ Frag minus(const Frag& a) {
+    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+    return __builtin_bit_cast(Frag, __builtin_bit_cast(u4, a) ^ 0x80008000u);
+  }
+  __device__ static __forceinline__ Whole whole(const float (&v)[8]) {
+    Whole s;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s.hi[j] = (__bf16)v[j];
+      const float left = v[j] - (float)s.hi[j];
+      s.mid[j] = (__bf16)left;
+      s.lo[j] = (__bf16)(left - (float)s.mid[j]);
+    }
+    return s;
+  }
   __device__ static __forceinline__ Frag one(const float (&v)[8]) {
     Frag f;
 #pragma unroll
@@ -73,11 +98,14 @@ template <> struct Mx<bf16_t> {
 };
 template <> struct Mx<float> {
   struct Frag { f4 v[2]; };
-  typedef Frag Split;
+  typedef Frag Split, Whole;
+  __device__ static __forceinline__ Frag minus(const Frag& a) { return Frag{{-a.v[0], -a.v[1]}}; }
   static constexpr int PAD = 4;
   __device__ static __forceinline__ f4 mma(const Frag& a, const Frag& b, f4 c) { return mma_f32(a.v[1], b.v[1], mma_f32(a.v[0], b.v[0], c)); }
+  __device__ static __forceinline__ f4 mma_even(const Frag (&a)[2], const Frag (&b)[2]) { return mma(a[1], b[1], mma(a[0], b[0], f4{0, 0, 0, 0})); }
   __device__ static __forceinline__ Frag one(const float (&v)[8]) { return Frag{{f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]}}}; }
   __device__ static __forceinline__ Frag split(const float (&v)[8]) { return one(v); }
+  __device__ static __forceinline__ Frag whole(const float (&v)[8]) { return one(v); }
   __device__ static __forceinline__ float at(const Frag& f, int j) { return f.v[j >> 2][j & 3]; }
   __device__ static __forceinline__ Frag row(const float* p) { return Frag{{load_f4(p), load_f4(p + 16)}}; }
   __device__ static __forceinline__ Frag col(const float* p, int ld, int i, int q) {
@@ -171,6 +199,14 @@ __device__ __forceinline__ float sum_rows(float v) {  // over the 4 lanes i, i +
   const u2 q = __builtin_amdgcn_permlane32_swap(b, b, false, false);
   return __uint_as_float(q[0]) + __uint_as_float(q[1]);
 }
+__device__ __forceinline__ float rows_behind(float v, int row) {  // over the lanes i + 16 r with r > row
+  typedef unsigned u2 __attribute__((ext_vector_type(2)));
+  const unsigned a = __float_as_uint(v);
+  const u2 p = __builtin_amdgcn_permlane16_swap(a, a, false, false);  // rows 0 0 2 2, rows 1 1 3 3
+  const unsigned b = __float_as_uint(__uint_as_float(p[0]) + __uint_as_float(p[1]));
+  const u2 q = __builtin_amdgcn_permlane32_swap(b, b, false, false);  // rows 0 + 1, rows 2 + 3
+  return ((row & 1) == 0 ? __uint_as_float(p[1]) : 0.0f) + (row < 2 ? __uint_as_float(q[1]) : 0.0f);
+}
 __device__ __forceinline__ float sum_wave(float v) { return sum_rows(sum_lanes(v)); }
 __device__ __forceinline__ float prefix_lanes(float v) {  // over the lanes of a row up to this one
   v = lanes_add<0x111>(v);
@@ -189,18 +225,27 @@ __device__ __forceinline__ float of_lane(float v, int lane) {
 }
 
 // A chunk's steps, one a lane (by one wave).  Sums of gamma D (base 2): s up to and with a step, after behind it, and the same
-// within its tile of 16 steps (in, behind): what decays between two steps is summed from these, since a difference of s loses
-// what is small beside s (2^-24 of up to some hundred).
+// within its tile of 16 steps (in, behind): what decays between steps of two tiles is summed from these, since a difference of s
+// loses what is small beside s (2^-24 of up to some hundred).  Between steps of one tile it is a difference of in, which has a
+// second word for that (rest: what in lost to rounding).
 struct Steps {
-  float d, s, after, in, behind, total, slope;
+  float d, s, after, in, rest, behind, total, slope;
 };
+template <int CTRL>
+__device__ __forceinline__ void lanes_add(float& v, float& rest) {  // with what each sum loses, exactly (the sum's error is a float)
+  const float u = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+  rest = lanes_add<CTRL>(rest);
+  const float s = v + u, of_u = s - v;
+  rest += (v - (s - of_u)) + (u - of_u);
+  v = s;
+}
 // the step's logit, loaded ahead of its use
 template <typename T>
 __device__ __forceinline__ float load_step(const SelArgs& a, int64_t b, int64_t t, int64_t n, int h, int lane) {
   return t + lane < n ? to_f32(static_cast<const T*>(a.dt.p)[b * a.dt.sb + (t + lane) * a.dt.st + h]) : 0.0f;
 }
 __device__ __forceinline__ Steps steps_of(const SelArgs& a, float v, bool inside, int h, int lane) {
-  Steps o{0, 0, 0, 0, 0, 0, 0};
+  Steps o{0, 0, 0, 0, 0, 0, 0, 0};
   float ld = 0.0f;
   if (inside) {
     v += a.dt_bias != nullptr ? a.dt_bias[h] : 0.0f;
@@ -211,7 +256,11 @@ __device__ __forceinline__ Steps steps_of(const SelArgs& a, float v, bool inside
     ld = ld > NO_MORE ? NO_MORE : ld;
   }
   const float next = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, ld), 0x101, 0xF, 0xF, true));
-  o.in = prefix_lanes(ld);
+  o.in = ld;
+  lanes_add<0x111>(o.in, o.rest);
+  lanes_add<0x112>(o.in, o.rest);
+  lanes_add<0x114>(o.in, o.rest);
+  lanes_add<0x118>(o.in, o.rest);
   o.behind = suffix_lanes(next);  // (the next lane's on; nothing behind the last)
   o.s = o.in;
   o.after = o.behind;
@@ -226,9 +275,10 @@ __device__ __forceinline__ Steps steps_of(const SelArgs& a, float v, bool inside
 }
 // what a tile's steps decay, from s and in of its first step's lane on: sums of whole tiles between tiles si and ti
 struct Between {
-  float in[Q], behind[Q], tile[4];  // (behind: negative)
+  float in[Q], rest[Q], behind[Q], tile[4];  // (behind: negative)
   __device__ __forceinline__ void put(const Steps& s, int lane) {
     in[lane] = s.in;
+    rest[lane] = s.rest;
     behind[lane] = -s.behind;
     if ((lane & 15) == 15) tile[lane >> 4] = s.in;
   }
@@ -380,7 +430,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
       const Steps s = steps_of(a, step, lane < rows, (o.hv0 + w) >> a.p.PS, lane);
       sd[w][lane] = s.d;
       sp[w][lane] = exp2_fast(-s.s);
-      sw[w][lane] = REV ? exp2_fast(-s.s) : s.d * exp2_fast(-s.after);
+      sw[w][lane] = REV ? ((ci & 1) != 0 ? exp2_fast(-s.s) : -exp2_fast(-s.s)) : s.d * exp2_fast(-s.after);
       if constexpr (!STATES) gap[w].put(s, lane);
       if (lane == 0) st[w] = s.total;
     }
@@ -423,10 +473,14 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
           const TileId id = tile_id(w, e);
           const Between& b = gap[k];
           const float to = -(b.in[16 * id.t + li] + b.gap(id.s, id.t));
+          // (rest: what it changes is below a bf16 y's rounding)
+          constexpr bool REST = sizeof(T) == 4;
+          const float to_rest = REST ? b.rest[16 * id.t + li] : 0.0f;
+          const f4 rest = REST ? load_f4(&b.rest[16 * id.s + 4 * lq]) : f4{0, 0, 0, 0};
           const f4 from = load_f4((id.s == id.t ? b.in : b.behind) + 16 * id.s + 4 * lq), d = load_f4(&sd[k][16 * id.s + 4 * lq]);
           f4 m;
 #pragma unroll
-          for (int r = 0; r < 4; ++r) m[r] = id.s < id.t || 4 * lq + r <= li ? g[e][r] * (exp2_fast(from[r] + to) * d[r]) : 0.0f;
+          for (int r = 0; r < 4; ++r) m[r] = id.s < id.t || 4 * lq + r <= li ? g[e][r] * (exp2_fast((from[r] + to) + (REST && id.s == id.t ? rest[r] - to_rest : 0.0f)) * d[r]) : 0.0f;
           // fragment (t tile, 32 steps s): 0, 1, 2 and 3, 4 and 5 of t tiles 0, 1, 2, 3
           const int f = id.t < 2 ? id.t : 2 * id.t - 2 + (id.s >> 1);
           put_quad(&mk[(f * 64 + lane) * 8 + (id.s & 1) * 4], m);
@@ -482,7 +536,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
           if (row < held) store_quad<WHOLE>(yp + ((uint32_t)row * (uint32_t)hp + 4 * lq), cols, y[t]);
         }
       }
-      const float keep = exp2_fast(-st[k]);
+      const float keep = REV ? -exp2_fast(-st[k]) : exp2_fast(-st[k]);  // (a gradient's sign turns with each chunk: see Mx::minus)
       total[k] += st[k];
 #pragma unroll
       for (int v = 0; v < NT; ++v)
@@ -497,7 +551,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
         float xw[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) xw[r] = M::at(xf[j], r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
-        const typename M::Split xp = M::split(xw);
+        const typename M::Whole xp = M::whole(xw);
         loads_first();
 #pragma unroll
         for (int v = 0; v < NT; ++v) h[k][v] = STATES ? M::mma(xp, bf[v], h[k][v]) : M::mma(bf[v], xp, h[k][v]);
@@ -525,7 +579,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
       const int64_t at = (o.b * a.p.HV + hv) * a.p.segs + o.seg;
       f4* s = reinterpret_cast<f4*>((REV ? a.leave : a.enter) + at * (SEL_P * NP)) + w * 64 + lane;
 #pragma unroll
-      for (int v = 0; v < NT; ++v) s[v * 256] = h[k][v];
+      for (int v = 0; v < NT; ++v) s[v * 256] = REV && (active & 1) != 0 ? -h[k][v] : h[k][v];
       if (tid == 0) a.decay[at] = total[k];
     } else if (a.p.segs == 1 && a.h_out != nullptr) {
       const int p0 = (hv & a.p.PS) * SEL_P;
@@ -590,11 +644,11 @@ template <typename T, int NT, bool WHOLE> struct BwdLds {
   __align__(16) T xd[2][Q * TX::LD];  // x, dy
   __align__(16) T ek[Q * TX::LD];     // row s: E[t,s] D_s K[t,s] over t
   __align__(16) T eg[Q * TX::LD];     // row s: E[t,s] (c_t.b_s)
-  __align__(16) T gx[2][sizeof(T) == 2 ? NS * TX::LD : NS * TX::LD / 2];  // row n: g over p (two parts; float32: one)
+  __align__(16) T gx[NS * TX::LD];    // row n: g over p
   __align__(16) Between gap;
   __align__(16) float d[Q], suf[Q], pre[Q], slope[Q];  // D, exp(-what follows), exp(-s), dD / d dt
   __align__(16) float rowz[4][Q], colz[4][Q], ic[4][Q], ig[4][Q];  // by s tile, by t tile, by wave, by wave
-  float lam[2][SEL_BWD_HEADS][4], sums[SEL_BWD_HEADS][3], skip[4], total[2];
+  float zd[Q], lam[4], sums[SEL_BWD_HEADS][3], skip[4], total[2];  // Z's diagonal; <g, h> by wave
 };
 
 template <typename T, int NT, bool WHOLE>
@@ -645,8 +699,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   if (tid < SEL_BWD_HEADS * 3) l.sums[tid / 3][tid % 3] = 0.0f;
   if (tid < 4) l.skip[tid] = 0.0f;
 
-  // The states before each chunk, and behind the last: b's and x's tiles in two buffers each (bc, xd), the weights D exp(-what
-  // follows) in ic[0], ic[1].
+  // The states before each chunk: b's and x's tiles in two buffers each (bc, xd), the weights D exp(-what follows) in ic[0], ic[1].
   {
     TB rb;
     TX rx;
@@ -656,7 +709,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
       rx.load(px + (int64_t)(ci * Q) * sx + at_of(k), sx, rows_at(ci), cols_of(k), here(tid));
       if (w == (ci & 3)) step = step_at(ci, (o.hv0 + k) >> a.p.PS);
     };
-    if (active > 0) load(0, 0);
+    if (active > 1) load(0, 0);
     int turn = 0;
     for (int k = 0; k < o.heads; ++k) {
       f4 h[NW][4];
@@ -679,7 +732,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
 #pragma unroll
           for (int v = 0; v < 4; ++v) h[m][v] = hs_at(0, k)[(m * 16 + v) * 64 + lane];
       }
-      for (int ci = 0; ci < active; ++ci) {
+      for (int ci = 0; ci + 1 < active; ++ci) {
         const int lane = here(tid & 63), li = lane & 15, lq = lane >> 4;
         rb.put(l.bc[turn]);
         rx.put(l.xd[turn]);
@@ -688,7 +741,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           l.ic[turn][lane] = p.d * exp2_fast(-p.after);
           if (lane == 0) l.total[turn] = p.total;
         }
-        if (ci + 1 < active)
+        if (ci + 2 < active)
           load(k, ci + 1);
         else if (k + 1 < o.heads)
           load(k + 1, 0);
@@ -708,14 +761,14 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
             typename M::Frag xf[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) xf[v] = M::col(x + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
-            typename M::Split bs[NW];
+            typename M::Whole bs[NW];
 #pragma unroll
             for (int m = 0; m < NW; ++m) {
               const typename M::Frag bf = M::col(b + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
               float bw[8];
 #pragma unroll
               for (int r = 0; r < 8; ++r) bw[r] = M::at(bf, r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
-              bs[m] = M::split(bw);
+              bs[m] = M::whole(bw);
             }
             loads_first();
 #pragma unroll
@@ -723,27 +776,13 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
 #pragma unroll
               for (int m = 0; m < NW; ++m) h[m][v] = M::mma(xf[v], bs[m], h[m][v]);
           }
-          if (ci + 1 < active)
 #pragma unroll
-            for (int m = 0; m < NW; ++m)
+          for (int m = 0; m < NW; ++m)
 #pragma unroll
-              for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 16 + v) * 64 + lane] = h[m][v];
+            for (int v = 0; v < 4; ++v) hs_at(ci + 1, k)[(m * 16 + v) * 64 + lane] = h[m][v];
         }
         turn ^= 1;
       }
-      // <g, h> behind the segment
-      float dot = 0.0f;
-      if (mine)
-#pragma unroll
-        for (int m = 0; m < NW; ++m)
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const f4 g = gs_at(k, true)[(m * 16 + v) * 64 + lane];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dot = fmaf(h[m][v][r], g[r], dot);
-          }
-      dot = sum_wave(dot);
-      if (lane == 0) l.lam[(active - 1) & 1][k][w] = dot;
     }
   }
 
@@ -779,6 +818,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   for (int ci = active - 1; ci >= 0; --ci) {
     const int64_t t0 = (c0 + ci) * Q;
     const int rows = rows_at(ci), held = held_at(ci);
+    const float sign = ((active - 1 - ci) & 1) != 0 ? -1.0f : 1.0f;  // of g in registers and gs
     f4 db[NW][4], dc[NW][4], g0[3];
 #pragma unroll
     for (int m = 0; m < NW; ++m)
@@ -829,8 +869,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         const Steps s = steps_of(a, step, lane < rows, hd, lane);
         l.gap.put(s, lane);
         l.d[lane] = s.d;
-        l.suf[lane] = exp2_fast(-s.after);
-        l.pre[lane] = exp2_fast(-s.s);
+        l.suf[lane] = sign * exp2_fast(-s.after);
+        l.pre[lane] = -sign * exp2_fast(-s.s);
         l.slope[lane] = s.slope;
         if (lane == 0) l.total[0] = s.total;
       }
@@ -847,29 +887,12 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         if (m > 0) __syncthreads();
         if (mine)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            T* row = &l.gx[0][(16 * w + li) * TX::LD + 16 * v + 4 * lq];
-            if constexpr (sizeof(T) == 2) {
-              typedef __bf16 bf4 __attribute__((ext_vector_type(4)));
-              const bf4 hi = __builtin_convertvector(g[m][v], bf4);
-              const f4 back = __builtin_convertvector(hi, f4);
-              *reinterpret_cast<bf4*>(row) = hi;
-              put_quad(&l.gx[1][(16 * w + li) * TX::LD + 16 * v + 4 * lq], g[m][v] - back);
-            } else {
-              put_quad(row, g[m][v]);
-            }
-          }
+          for (int v = 0; v < 4; ++v) put_quad(&l.gx[(16 * w + li) * TX::LD + 16 * v + 4 * lq], g[m][v]);
         __syncthreads();
 #pragma unroll
         for (int j = 0; j < SL / 2; ++j) {
-          typename M::Split gf;
           typename M::Frag bf[4];
-          if constexpr (sizeof(T) == 2) {
-            gf.hi = M::col(&l.gx[0][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
-            gf.lo = M::col(&l.gx[1][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
-          } else {
-            gf = M::col(&l.gx[0][32 * j * TX::LD + 16 * w], TX::LD, li, lq);
-          }
+          const typename M::Frag gf = M::col(&l.gx[32 * j * TX::LD + 16 * w], TX::LD, li, lq);
 #pragma unroll
           for (int v = 0; v < 4; ++v) bf[v] = M::row(bt + (16 * v + li) * TB::LD + 64 * m + 32 * j + 4 * lq);
           loads_first();
@@ -877,26 +900,11 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           for (int v = 0; v < 4; ++v) du[v] = M::mma(gf, bf[v], du[v]);
         }
       }
-      {  // its part of x.du
-        f4 x[4];
-        float f[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          x[v] = quad(xt + (16 * v + li) * TX::LD + 16 * w + 4 * lq);
-          f[v] = l.suf[16 * v + li];
-        }
-        loads_first();
-        float dot[4] = {0, 0, 0, 0};
+      for (int v = 0; v < 4; ++v) {
+        const float f = l.suf[16 * v + li];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            du[v][r] *= f[v];
-            dot[v] = fmaf(x[v][r], du[v][r], dot[v]);
-          }
-          dot[v] = sum_rows(dot[v]);
-        }
-        l.ig[w][lane] = lq == 0 ? dot[0] : lq == 1 ? dot[1] : lq == 2 ? dot[2] : dot[3];
+        for (int r = 0; r < 4; ++r) du[v][r] *= f;
       }
       // K = dy.x; Z = (c.b) E K; the weights of the products within the chunk
 #pragma unroll
@@ -909,75 +917,107 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           fx[j] = M::row(xt + (16 * id.s + li) * TX::LD + 32 * j + 4 * lq);
         }
         const float from = (id.s == id.t ? l.gap.in : l.gap.behind)[16 * id.s + li] - l.gap.gap(id.s, id.t), d_s = l.d[16 * id.s + li];
-        const f4 to = load_f4(&l.gap.in[16 * id.t + 4 * lq]);
+        const float from_rest = l.gap.rest[16 * id.s + li];
+        const f4 to = load_f4(&l.gap.in[16 * id.t + 4 * lq]), to_rest = load_f4(&l.gap.rest[16 * id.t + 4 * lq]);
         loads_first();
-        f4 kk{0, 0, 0, 0};
-#pragma unroll
-        for (int j = 0; j < 2; ++j) kk = M::mma(fy[j], fx[j], kk);
+        const f4 kk = M::mma_even(fy, fx);
         f4 ek, eg, z;
         float col = 0.0f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const bool in = id.s < id.t || li <= 4 * lq + r;
-          const float f = exp2_fast(from - to[r]);
+          const bool in = id.s < id.t || li <= 4 * lq + r, below = id.s < id.t || li < 4 * lq + r;
+          const float f = exp2_fast((from - to[r]) + (id.s == id.t ? from_rest - to_rest[r] : 0.0f));
           eg[r] = in ? f * g0[e][r] : 0.0f;
           ek[r] = in ? f * kk[r] * d_s : 0.0f;
-          col = fmaf(eg[r], kk[r], col);
-          z[r] = sum_lanes(ek[r] * g0[e][r]);
+          col += below ? eg[r] * kk[r] : 0.0f;
+          z[r] = below ? ek[r] * g0[e][r] : 0.0f;
         }
         put_quad(l.ek + (16 * id.s + li) * TX::LD + 16 * id.t + 4 * lq, ek);
         put_quad(l.eg + (16 * id.s + li) * TX::LD + 16 * id.t + 4 * lq, eg);
         col = sum_rows(col);
         if (lq == 0) l.colz[id.t][16 * id.s + li] = col;
-        if (li == 0) put_quad(&l.rowz[id.s][16 * id.t + 4 * lq], z);
-        if (id.s == id.t) {  // the diagonal: dy_t.x_t
-          float dg = 0.0f;
+        if (id.s == id.t) {  // what passes step t within its tile: from s < t to the rows from t on
+          z[2] += z[3];
+          z[1] += z[2];
+          z[0] += z[1];
+          const float rows = rows_behind(z[0], lq);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) dg += li == 4 * lq + r ? kk[r] : 0.0f;
+          for (int r = 0; r < 4; ++r) z[r] = li < 4 * lq + r ? z[r] + rows : 0.0f;
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[r] = sum_lanes(z[r]);
+        if (li == 0) put_quad(&l.rowz[id.s][16 * id.t + 4 * lq], z);
+        if (id.s == id.t) {  // the diagonal: (c.b) dy.x of a step, and dy.x
+          float zd = 0.0f, dg = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            dg += li == 4 * lq + r ? kk[r] : 0.0f;
+            zd += li == 4 * lq + r ? kk[r] * g0[e][r] : 0.0f;
+          }
+          zd = sum_rows(zd);
           dg = sum_wave(dg);
+          if (lq == 0) l.zd[16 * id.t + li] = zd;
           if (lane == 0) l.skip[id.t] = dg;
         }
       }
-      // dc's part from the states: exp(-s_t) h^T dy_t, and with c_t its part of dy.y
+      // dc's part from the states, exp(-s_t) h^T dy_t, and with c_t its part of dy.y; db's, D exp(-what follows) g^T x, and with b its part of
+      // x.du; <g, h>
       if (mine) {
-        float ic[4] = {0, 0, 0, 0}, f[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) f[t] = l.pre[16 * t + li];
-#pragma unroll
-        for (int m = 0; m < NW; ++m) {
-          f4 acc[4], c[4];
+        auto inter = [&](const f4(&st)[NW][4], const T* act, const T* read, const float* by, float sign, const float* also, f4(&to)[NW][4], float* dots) {
+          float dot[4] = {0, 0, 0, 0}, f[4], d[4];
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
-            acc[t] = f4{0, 0, 0, 0};
-            c[t] = quad(ct + (16 * t + li) * TB::LD + 16 * (w + 4 * m) + 4 * lq);
+            f[t] = sign * by[16 * t + li];
+            d[t] = also != nullptr ? also[16 * t + li] : 1.0f;
           }
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            typename M::Frag yf[4];
+          for (int m = 0; m < NW; ++m) {
+            f4 acc[4], c[4];
 #pragma unroll
-            for (int t = 0; t < 4; ++t) yf[t] = M::row(dt + (16 * t + li) * TX::LD + 32 * j + 4 * lq);
-            float hf[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) hf[r] = h[m][2 * j + (r >> 2)][r & 3];
-            const typename M::Split hp = M::split(hf);
-            loads_first();
-#pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = M::mma(hp, yf[t], acc[t]);
-          }
-#pragma unroll
-          for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const float v = acc[t][r] * f[t];
-              ic[t] = fmaf(c[t][r], v, ic[t]);
-              dc[m][t][r] += v;
+            for (int t = 0; t < 4; ++t) {
+              acc[t] = f4{0, 0, 0, 0};
+              c[t] = quad(read + (16 * t + li) * TB::LD + 16 * (w + 4 * m) + 4 * lq);
             }
-        }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) ic[t] = sum_rows(ic[t]);
-        l.ic[w][lane] = lq == 0 ? ic[0] : lq == 1 ? ic[1] : lq == 2 ? ic[2] : ic[3];
+            for (int j = 0; j < 2; ++j) {
+              typename M::Frag yf[4];
+#pragma unroll
+              for (int t = 0; t < 4; ++t) yf[t] = M::row(act + (16 * t + li) * TX::LD + 32 * j + 4 * lq);
+              float hf[8];
+#pragma unroll
+              for (int r = 0; r < 8; ++r) hf[r] = st[m][2 * j + (r >> 2)][r & 3];
+              const typename M::Whole hp = M::whole(hf);
+              loads_first();
+#pragma unroll
+              for (int t = 0; t < 4; ++t) acc[t] = j == 0 ? M::mma(hp, yf[t], acc[t]) : M::mma(hp, M::minus(yf[t]), -acc[t]);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) {
+                const float v = acc[t][r] * f[t];
+                dot[t] = fmaf(c[t][r], v, dot[t]);
+                to[m][t][r] = fmaf(d[t], v, to[m][t][r]);
+              }
+          }
+#pragma unroll
+          for (int t = 0; t < 4; ++t) dot[t] = sum_rows(dot[t]);
+          dots[lane] = lq == 0 ? dot[0] : lq == 1 ? dot[1] : lq == 2 ? dot[2] : dot[3];
+        };
+        inter(h, dt, ct, l.pre, sign, nullptr, dc, l.ic[w]);
+        inter(g, xt, bt, l.suf, -1.0f, l.d, db, l.ig[w]);
+        float dot = 0.0f;
+#pragma unroll
+        for (int m = 0; m < NW; ++m)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) dot = fmaf(g[m][v][r], h[m][v][r], dot);
+        dot = sum_wave(dot);
+        if (lane == 0) l.lam[w] = dot;
       } else {
-        l.ic[w][lane] = 0.0f;
+        l.ic[w][lane] = l.ig[w][lane] = 0.0f;
+        if (lane == 0) l.lam[w] = 0.0f;
       }
       __syncthreads();
       if (ahead) {
@@ -995,24 +1035,39 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           cz[v] = l.colz[v][lane];
           ic[v] = l.ic[v][lane];
           ig[v] = l.ig[v][lane];
-          lam += l.lam[ci & 1][k][v];
+          lam += l.lam[v];
         }
-        const float d = l.d[lane], slope = l.slope[lane], gamma = a.gamma[hd];
+        const float d = l.d[lane], slope = l.slope[lane], zd = l.zd[lane], gamma = a.gamma[hd];
+        lam *= sign * exp2_fast(-l.total[0]);
         loads_first();
-        float ry = 0.0f, cu = 0.0f;
+        // What passes step t, from the steps before it and the state to those from it on and the gradient behind the chunk, as a sum of
+        // only that: whole tiles beyond t's, rows and columns of its tile with those, and the tile's own.  (Sums of all that leaves and
+        // all that arrives up to t are the same less what cancels; it left errors up to 2e-5 of dgamma and of dt_bias's gradient.)
+        float after = 0.0f, before = 0.0f, row = 0.0f, col = 0.0f, own = 0.0f;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          ry += ic[v] + (v <= tile ? rz[v] : 0.0f);
-          cu += ig[v] + (v >= tile ? cz[v] : 0.0f);
+          after += ic[v];
+          before += ig[v];
+          row += v < tile ? rz[v] : 0.0f;
+          col += v > tile ? cz[v] : 0.0f;
+          own = v == tile ? rz[v] : own;
         }
-        float dl = suffix_lanes(ry - d * cu);
-        float later = lam;
+        float cu = before + zd;
 #pragma unroll
-        for (int v = 3; v > 0; --v) {
-          const float all = of_lane(dl, 16 * v);
-          later += tile < v ? all : 0.0f;
+        for (int v = 0; v < 4; ++v) cu += v >= tile ? cz[v] : 0.0f;
+        before *= d;
+        const float arrive = suffix_lanes(after), leave = sum_lanes(before), z0 = sum_lanes(rz[0]), z1 = sum_lanes(rz[1]);
+        const float sent = prefix_lanes(
+            __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, fmaf(d, col, before)), 0x111, 0xF, 0xF, true)));
+        float dl = lam + own + (arrive + suffix_lanes(row)) + sent;
+        // (read in all lanes: in a branch the sums would be those of the branch's lanes)
+        const float z20 = of_lane(z0, 32), z30 = of_lane(z0, 48), z31 = of_lane(z1, 48);
+        dl += tile == 1 ? z20 + z30 : tile == 2 ? z30 + z31 : 0.0f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float a0 = of_lane(leave, 16 * v), a1 = of_lane(arrive, 16 * v);
+          dl += v < tile ? a0 : v > tile ? a1 : 0.0f;
         }
-        dl += later;
         const float v = (cu - gamma * dl) * slope;
         const float sg = sum_wave(-d * dl), sb = sum_wave(v);
         if (lane == 0) {
@@ -1076,37 +1131,9 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           if (row < held) store_quad<WHOLE>(pdx + ((uint32_t)row * sdx + 4 * lq), cols - 16 * w - 4 * lq, du[v]);
         }
       }
-      float dot = 0.0f;
       if (mine) {
-        // db's part from the states' gradients
-        float f[4];
-#pragma unroll
-        for (int v = 0; v < 4; ++v) f[v] = l.d[16 * v + li] * l.suf[16 * v + li];
-#pragma unroll
-        for (int m = 0; m < NW; ++m) {
-          f4 acc[4];
-#pragma unroll
-          for (int v = 0; v < 4; ++v) acc[v] = f4{0, 0, 0, 0};
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            typename M::Frag xf[4];
-#pragma unroll
-            for (int v = 0; v < 4; ++v) xf[v] = M::row(xt + (16 * v + li) * TX::LD + 32 * j + 4 * lq);
-            float gf[8];
-#pragma unroll
-            for (int r = 0; r < 8; ++r) gf[r] = g[m][2 * j + (r >> 2)][r & 3];
-            const typename M::Frag go = M::one(gf);
-            loads_first();
-#pragma unroll
-            for (int v = 0; v < 4; ++v) acc[v] = M::mma(go, xf[v], acc[v]);
-          }
-#pragma unroll
-          for (int v = 0; v < 4; ++v)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) db[m][v][r] = fmaf(f[v], acc[v][r], db[m][v][r]);
-        }
-        // g before the chunk, and its product with the state there
-        const float keep = exp2_fast(-l.total[0]);
+        // g before the chunk, with the other sign
+        const float keep = -exp2_fast(-l.total[0]);
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
@@ -1119,14 +1146,14 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           typename M::Frag yf[4];
 #pragma unroll
           for (int v = 0; v < 4; ++v) yf[v] = M::col(dt + 32 * j * TX::LD + 16 * v, TX::LD, li, lq);
-          typename M::Split cs[NW];
+          typename M::Whole cs[NW];
 #pragma unroll
           for (int m = 0; m < NW; ++m) {
             const typename M::Frag cf = M::col(ct + 32 * j * TB::LD + 16 * (w + 4 * m), TB::LD, li, lq);
             float cw[8];
 #pragma unroll
             for (int r = 0; r < 8; ++r) cw[r] = M::at(cf, r) * (r < 4 ? w0[r & 3] : w1[r & 3]);
-            cs[m] = M::split(cw);
+            cs[m] = M::whole(cw);
           }
           loads_first();
 #pragma unroll
@@ -1137,14 +1164,12 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
 #pragma unroll
         for (int m = 0; m < NW; ++m)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            if (ci > 0 || !several) gs[k * STATE + (m * 16 + v) * 64 + lane] = g[m][v];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) dot = fmaf(g[m][v][r], h[m][v][r], dot);
-          }
+          for (int v = 0; v < 4; ++v)
+            if (ci > 0)
+              gs[k * STATE + (m * 16 + v) * 64 + lane] = g[m][v];
+            else if (!several)
+              gs[k * STATE + (m * 16 + v) * 64 + lane] = -sign * g[m][v];
       }
-      dot = sum_wave(dot);
-      if (lane == 0) l.lam[(ci - 1) & 1][k][w] = dot;
     }
     if (mine) {
       auto put = [&](auto* pb, auto* pc, uint32_t sb, uint32_t sc) {

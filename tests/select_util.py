@@ -72,8 +72,7 @@ class Scan:
         most = np.concatenate([ld, pad], 1).reshape(B, -1, 64, H).sum(2).max() if L else 0.0
         # at most some thousand float32 roundings in a row: sums over 64 steps, 128 states or rows, over chunks, twice nested
         e = 2.0 ** -24 * (1024 + 4 * most)
-        two = e + (4 * 2.0 ** -16 if self.act == "bf16" else 0.0)  # and operands of two bf16 parts
-        one = two + (2.0 ** -8 if self.act == "bf16" else 0.0)     # and a weight rounded to bf16
+        one = e + (2.0 ** -8 + 4 * 2.0 ** -16 if self.act == "bf16" else 0.0)  # and a weight of one bf16 part, states of two
         half = HALF[self.act]
         dl = np.zeros((B, L, H))
         if L:
@@ -84,10 +83,10 @@ class Scan:
         du_x = np.where(D > 0, (x * g0["dx"]).sum(-1) / np.where(D > 0, D, 1), 0)
         ddt = slope * (du_x + self.gamma * dl)
         self.bound = dict(
-            y=half * np.abs(self.y) + one * y, h=two * hs[-1], dx=half * np.abs(self.grads["dx"]) + one * g["dx"],
+            y=half * np.abs(self.y) + one * y, h=e * hs[-1], dx=half * np.abs(self.grads["dx"]) + one * g["dx"],
             db=half * np.abs(self.grads["db"]) + one * g["db"], dc=half * np.abs(self.grads["dc"]) + one * g["dc"],
-            ddt=half * np.abs(self.grads["ddt"]) + two * ddt, dgamma=two * (D * dl).sum((0, 1)), ddt_bias=two * ddt.sum((0, 1)),
-            dskip=two * (x * dy).sum((0, 1, 3)), dh0=two * g["dh0"])
+            ddt=half * np.abs(self.grads["ddt"]) + e * ddt, dgamma=e * (D * dl).sum((0, 1)), ddt_bias=e * ddt.sum((0, 1)),
+            dskip=e * (x * dy).sum((0, 1, 3)), dh0=e * g["dh0"])
 
     def tensors(self, fused=False):
         """x, dt, b, c, gamma on the GPU; behind the rows' ends NaN; `fused`: columns of one tensor."""
