@@ -50,9 +50,9 @@ __device__ __forceinline__ void join(Stats& a, Stats b, float c) {
 constexpr int LIST = 1536, EQUAL = 512;  // alternatives' candidates kept in LDS; those of them at the border itself
 
 struct Shared {
-  uint32_t kth[16], share[16], border;
-  uint32_t tops[1024];  // lanes' maxima not below the first border
-  int lane[1024];       // the lanes whose elements are looked at again
+  uint32_t kth[8], share[8], border;
+  uint32_t tops[512];  // lanes' maxima not below the first border
+  int lane[512];       // the lanes whose elements are looked at again
   int count, above, equal, lanes, again;
   uint64_t list[LIST];  // order << 32 | ~place: the larger one comes first
 };
@@ -60,7 +60,7 @@ struct Shared {
 __device__ __forceinline__ uint64_t entry_of(float v, int64_t at) { return (uint64_t)order_of(v) << 32 | (uint32_t)~(uint32_t)at; }
 
 // The k-th and the j-th largest of a wave's 64 orders (k, j <= 64), bit after bit: how many are not below.  (A loop: run once
-// by each wave, unrolled it took 0.7 us more of 18 for 64 rows of 50304.)  HALF: the orders are of bf16 values.
+// by each wave, unrolled it took 0.7 us more of 18 for 64 rows of 50304 with 1024 threads.)  HALF: the orders are of bf16 values.
 template <bool HALF>
 __device__ __forceinline__ void kth_of_wave(uint32_t o, int k, int j, uint32_t* kth, uint32_t* jth) {
   uint32_t t = 0, s = 0;
@@ -114,7 +114,8 @@ template <typename T, int NT, bool TOP, bool ENT>
 __global__ __launch_bounds__(NT) void logprobs_fwd_kernel(LogprobsArgs a) {
   typedef RowPiece<T, NT, 4> Piece;
   constexpr int V = Piece::V, U = Piece::U, W = NT / 64;
-  __shared__ Stats part[16];
+  static_assert(NT <= 512 && W <= 8, "the shared arrays");
+  __shared__ Stats part[W];
   extern __shared__ __align__(16) char raw[];
   Shared& sh = *reinterpret_cast<Shared*>(raw);  // (with alternatives only)
   const int64_t r = a.r0 + blockIdx.x;
@@ -371,7 +372,10 @@ hipError_t fwd(LogprobsArgs a, hipStream_t st) {
 
 template <typename T>
 hipError_t launch_logprobs_fwd(LogprobsArgs a, hipStream_t st) {
-  return a.V <= 8192 || a.R >= 512 ? fwd<T, 256>(a, st) : fwd<T, 1024>(a, st);
+  // Threads of a row: more share its elements, but join their results and find the border over more lanes.  bf16 with the entropy and
+  // 8 alternatives, 256, 512 and 1024 threads: 64 x 50304 13.9, 14.1 and 17.9 us, 512 x 50304 19.3, 22.2 and 37.3, 8 x 131072 19.9,
+  // 17.4 and 19.7; with 20 of them 64 x 128000 25.7, 20.9 and 26.2.
+  return a.V <= 65536 || a.R >= 512 ? fwd<T, 256>(a, st) : fwd<T, 512>(a, st);
 }
 template <typename T>
 hipError_t launch_logprobs_bwd(LogprobsArgs a, hipStream_t st) {
