@@ -351,8 +351,12 @@ __device__ __forceinline__ void loads_first() { __builtin_amdgcn_sched_barrier(0
 // Forward: a wave owns 16 of a row block's 64 rows.  Its states are in registers, transposed: lane (p, q) holds
 // n = 16 v + 4 q .. + 3.  STATES: only the segment's end state from a zero start, the other way round (and REV: the gradient that the segment
 // gives to the state before it: dy, c and exp(-s_t) in the place of x, b and the weights, from the last chunk back).
-// ---------------------------------------------------------------------------
 // The next head's x (the next chunk's b, c and steps) are loaded to registers while a head's products run.
+// Some heads share a work-group's b, c and (c.b): four, or two where 128 states leave registers for no more.  Two passes over x and b
+// instead of a wait for the segment before: 8 x 8192, 8 heads of 64 x 64, bf16: states 40 us, forward 95 (134 MB, a seventh of the
+// matrix rate); 4 x 32768, 128 states: 90 and 224.  Vector instructions and their latency bound both: two waves a SIMD, whose
+// registers are full, half of whose cycles they take; the matrix unit is busy for a fifth of the time.
+// ---------------------------------------------------------------------------
 template <typename T, int NT, int HF, bool WHOLE, bool STATES, bool REV>
 __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective_fwd_kernel(SelArgs a) {
   typedef Mx<T> M;
@@ -594,7 +598,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
 }
 
 // The segments' states one after the other: each segment's own end state makes way for the state that enters it.  An element a
-// thread, so that there are enough of them for the latency of the segments' loads, some of which go together.
+// thread, so that there are enough of them for the latency of the segments' loads, some of which go together.  64 rows of 64 x 64 states in
+// 32 segments: 15 us (67 MB).
 template <bool REV>
 __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) {
   const int per = SEL_P * 16 * a.p.NT;
@@ -635,6 +640,8 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
 // last one back, in each head after head.  A wave owns the 16-state tiles w, w + 4: there states and their gradients are
 // lanes (n, q) with p = 16 v + 4 q .. + 3, as their products with x and dy need them; du, which needs a row's states, takes
 // them through LDS.  What the next head needs is loaded to registers meanwhile.
+// 8 x 8192, 8 heads of 64 x 64, bf16: 300 us, of which the states' second making some 45 and their way through memory 30.  Vector
+// instructions bound it (half of all cycles, some 2000 of a wave for a head's chunk; the matrix unit a tenth), at two waves a SIMD.
 // ---------------------------------------------------------------------------
 template <typename T, int NT, bool WHOLE> struct BwdLds {
   static constexpr int SL = NT < 4 ? NT : 4, NS = 16 * SL;  // state tiles of a slice, which goes through LDS at once
@@ -1233,7 +1240,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   if (tid < o.heads * 3) a.params[((o.b * a.p.segs + o.seg) * a.p.HV + o.hv0) * 3 + tid] = l.sums[tid / 3][tid % 3];
 }
 
-// db and dc of a group from its blocks of heads, in their order: 4 elements of a step a thread.
+// db and dc of a group from its blocks of heads, in their order: 4 elements of a step a thread.  Two blocks of 65536 steps with 64
+// states: 21 us (84 MB).
 template <typename T>
 __global__ __launch_bounds__(SEL_THREADS) void selective_bc_kernel(SelArgs a, int blocks) {
   const int64_t gn = (int64_t)a.G * a.N, per = (gn + 3) / 4, id = a.wg0 + (int64_t)blockIdx.x * SEL_THREADS + threadIdx.x;
@@ -1274,7 +1282,8 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_params_kernel(SelArgs a
 }
 
 // ---------------------------------------------------------------------------
-// One step: a group of LN lanes takes a row p of a state, 4 states a lane.  The states are read and written once; that bounds it.
+// One step: a group of LN lanes takes a row p of a state, 4 states a lane.  The states are read and written once; that bounds it
+// (64 sequences of 8 heads of 64 x 64: 17 MB in 7.2 us, 2 of them a launch's).
 // ---------------------------------------------------------------------------
 template <typename T, int LN>
 __global__ __launch_bounds__(SEL_THREADS) void selective_step_kernel(SelArgs a, const float* h, int64_t rows) {
