@@ -72,7 +72,7 @@ def check(x, tok, dt, scale=1.0, top=0, pad=0, seed=0):
     return t, tk, o
 
 
-# vectors that end inside, one work-group of 256 and of 1024 threads, several passes of its loop
+# vectors that end inside, one work-group of 256 and of 512 threads, several passes of its loop
 @pytest.mark.parametrize("dt", ACTS)
 @pytest.mark.parametrize("R,V,top", [(1, 1, 1), (3, 2, 2), (5, 63, 7), (4, 257, 64), (7, 1000, 20), (2, 8192, 1), (3, 8193, 20), (2, 32768, 64),
                                      (2, 50305, 8), (1, 131073, 20)])
