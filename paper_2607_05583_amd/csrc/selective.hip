@@ -18,6 +18,9 @@
 // States that are read for y go in as two parts (2^-16); the weights (c.b) E D and E D K that only make bf16 outputs, and g
 // in du, as one (2^-8 a term, as much as the output's own rounding).
 // float32 inputs use float32 MFMA throughout.  Sums and states are float32.
+// The matrix unit's bf16 sums are low by some 2^-28 of their terms on average, whatever their sign (measured: 5 million products of
+// normal values, each off by up to 2^-20 either way).  In dgamma, a sum over all steps, that stands out (5e-6 of it): every other
+// chunk's states and gradients are held with the other sign in the backward, so that what is low there makes up for it.
 #include <type_traits>
 
 #include "select.h"
@@ -44,16 +47,6 @@ template <> struct Mx<bf16_t> {
   __device__ static __forceinline__ f4 mma(const Split& a, const Frag& b, f4 c) { return mma(a.hi, b, mma(a.lo, b, c)); }
   __device__ static __forceinline__ f4 mma(const Whole& a, const Frag& b, f4 c) { return mma(a.hi, b, mma(a.mid, b, mma(a.lo, b, c))); }
   __device__ static __forceinline__ f4 mma(const Frag& a, const Whole& b, f4 c) { return mma(a, b.hi, mma(a, b.mid, mma(a, b.lo, c))); }
-  __device__ static __forceinline__ f4 mma_even(const Frag (&a)[2], const Frag (&b)[2]) {
-    return mma(a[0], b[0], f4{0, 0, 0, 0}) - mma(minus(a[1]), b[1], f4{0, 0, 0, 0});
-  }
-  // The unit's bf16 sums are low by some 2^-28 of their terms on average, whatever their sign (measured: 10^7 products of normal
-  // values, off by up to 2^-20 either way).  In dgamma, which sums millions of them, that stands out (5e-6 of it), so
-  // half of each sum is made of the other sign: the second half of a product over a row block, and every other chunk's g.
-  __device__ static __forceinline__ Frag minus(const Frag& a) {
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-    return __builtin_bit_cast(Frag, __builtin_bit_cast(u4, a) ^ 0x80008000u);
-  }
   __device__ static __forceinline__ Whole whole(const float (&v)[8]) {
     Whole s;
 #pragma unroll
@@ -99,10 +92,8 @@ template <> struct Mx<bf16_t> {
 template <> struct Mx<float> {
   struct Frag { f4 v[2]; };
   typedef Frag Split, Whole;
-  __device__ static __forceinline__ Frag minus(const Frag& a) { return Frag{{-a.v[0], -a.v[1]}}; }
   static constexpr int PAD = 4;
   __device__ static __forceinline__ f4 mma(const Frag& a, const Frag& b, f4 c) { return mma_f32(a.v[1], b.v[1], mma_f32(a.v[0], b.v[0], c)); }
-  __device__ static __forceinline__ f4 mma_even(const Frag (&a)[2], const Frag (&b)[2]) { return mma(a[1], b[1], mma(a[0], b[0], f4{0, 0, 0, 0})); }
   __device__ static __forceinline__ Frag one(const float (&v)[8]) { return Frag{{f4{v[0], v[1], v[2], v[3]}, f4{v[4], v[5], v[6], v[7]}}}; }
   __device__ static __forceinline__ Frag split(const float (&v)[8]) { return one(v); }
   __device__ static __forceinline__ Frag whole(const float (&v)[8]) { return one(v); }
@@ -540,7 +531,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 ? 2 : 1) void selective
           if (row < held) store_quad<WHOLE>(yp + ((uint32_t)row * (uint32_t)hp + 4 * lq), cols, y[t]);
         }
       }
-      const float keep = REV ? -exp2_fast(-st[k]) : exp2_fast(-st[k]);  // (a gradient's sign turns with each chunk: see Mx::minus)
+      const float keep = REV ? -exp2_fast(-st[k]) : exp2_fast(-st[k]);  // (a gradient's sign turns with each chunk)
       total[k] += st[k];
 #pragma unroll
       for (int v = 0; v < NT; ++v)
@@ -745,7 +736,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         rx.put(l.xd[turn]);
         if (w == (ci & 3)) {
           const Steps p = steps_of(a, step, lane < rows_at(ci), (o.hv0 + k) >> a.p.PS, lane);
-          l.ic[turn][lane] = p.d * exp2_fast(-p.after);
+          l.ic[turn][lane] = ((ci & 1) != 0 ? p.d : -p.d) * exp2_fast(-p.after);
           if (lane == 0) l.total[turn] = p.total;
         }
         if (ci + 2 < active)
@@ -755,7 +746,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         __syncthreads();
         if (mine) {
           const T *b = l.bc[turn], *x = l.xd[turn];
-          const float keep = exp2_fast(-l.total[turn]);
+          const float keep = -exp2_fast(-l.total[turn]);  // (the other sign)
 #pragma unroll
           for (int m = 0; m < NW; ++m)
 #pragma unroll
@@ -825,7 +816,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   for (int ci = active - 1; ci >= 0; --ci) {
     const int64_t t0 = (c0 + ci) * Q;
     const int rows = rows_at(ci), held = held_at(ci);
-    const float sign = ((active - 1 - ci) & 1) != 0 ? -1.0f : 1.0f;  // of g in registers and gs
+    // of g in registers and gs, of h there and in hs
+    const float sign = ((active - 1 - ci) & 1) != 0 ? -1.0f : 1.0f, hsign = (ci & 1) != 0 ? -1.0f : 1.0f;
     f4 db[NW][4], dc[NW][4], g0[3];
 #pragma unroll
     for (int m = 0; m < NW; ++m)
@@ -927,7 +919,9 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
         const float from_rest = l.gap.rest[16 * id.s + li];
         const f4 to = load_f4(&l.gap.in[16 * id.t + 4 * lq]), to_rest = load_f4(&l.gap.rest[16 * id.t + 4 * lq]);
         loads_first();
-        const f4 kk = M::mma_even(fy, fx);
+        f4 kk{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < 2; ++j) kk = M::mma(fy[j], fx[j], kk);
         f4 ek, eg, z;
         float col = 0.0f;
 #pragma unroll
@@ -996,7 +990,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
               const typename M::Whole hp = M::whole(hf);
               loads_first();
 #pragma unroll
-              for (int t = 0; t < 4; ++t) acc[t] = j == 0 ? M::mma(hp, yf[t], acc[t]) : M::mma(hp, M::minus(yf[t]), -acc[t]);
+              for (int t = 0; t < 4; ++t) acc[t] = M::mma(hp, yf[t], acc[t]);
             }
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -1011,8 +1005,8 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           for (int t = 0; t < 4; ++t) dot[t] = sum_rows(dot[t]);
           dots[lane] = lq == 0 ? dot[0] : lq == 1 ? dot[1] : lq == 2 ? dot[2] : dot[3];
         };
-        inter(h, dt, ct, l.pre, sign, nullptr, dc, l.ic[w]);
-        inter(g, xt, bt, l.suf, -1.0f, l.d, db, l.ig[w]);
+        inter(h, dt, ct, l.pre, -sign * hsign, nullptr, dc, l.ic[w]);
+        inter(g, xt, bt, l.suf, 1.0f, l.d, db, l.ig[w]);
         float dot = 0.0f;
 #pragma unroll
         for (int m = 0; m < NW; ++m)
@@ -1045,7 +1039,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
           lam += l.lam[v];
         }
         const float d = l.d[lane], slope = l.slope[lane], zd = l.zd[lane], gamma = a.gamma[hd];
-        lam *= sign * exp2_fast(-l.total[0]);
+        lam *= sign * hsign * exp2_fast(-l.total[0]);
         loads_first();
         // What passes step t, from the steps before it and the state to those from it on and the gradient behind the chunk, as a sum of
         // only that: whole tiles beyond t's, rows and columns of its tile with those, and the tile's own.  (Sums of all that leaves and
