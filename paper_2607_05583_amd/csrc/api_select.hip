@@ -53,8 +53,8 @@ int check_conv(int64_t B, int64_t L, int64_t D, int64_t K, res_dtype_t dt, int a
     return api_error(RES_ERR_INVALID_ARG, "B, D and K must be >= 1 and L >= 0 (got B=%lld L=%lld D=%lld K=%lld)", (long long)B,
                      (long long)L, (long long)D, (long long)K);
   // (a row's threads fit one launch: 16 steps of two channels each at least)
-  if (K > CONV_TAPS || D > (1 << 21) || B > (1LL << 31) || L >= (1LL << 31) - 65536 || (L / CONV_TILE + 1) * ((D + 1) / 2) >= (1LL << 31) ||
-      B * (L / CONV_BWD_TILE + 1) >= (1LL << 40))
+  if (K > CONV_TAPS || D > (1 << 21) || B > (1LL << 31) || L >= (1LL << 31) - 65536 || (L / (1 << CONV_SHIFT) + 1) * ((D + 1) / 2) >= (1LL << 31) ||
+      B * (L / (1 << CONV_BWD_SHIFT) + 1) >= (1LL << 40))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld D=%lld K=%lld)", (long long)B,
                      (long long)L, (long long)D, (long long)K);
   return RES_OK;
@@ -98,7 +98,7 @@ int resonator_short_conv_fwd(res_rows_t x, res_dtype_t dt, const float* w, const
 
 size_t resonator_short_conv_workspace_bytes(int64_t B, int64_t L, int64_t D, int64_t K) {
   if (check_conv(B, L, D, K, RES_F32, RES_ACT_NONE)) return 0;
-  return up256((size_t)(conv_row_blocks(B, L) * (K + 1) * D) * 4);
+  return up256((size_t)(conv_row_blocks(B, L, conv_bwd_shift(B, L, D)) * (K + 1) * D) * 4);
 }
 
 int resonator_short_conv_bwd(res_rows_t x, res_rows_t dy, res_dtype_t dt, const float* w, const float* bias, int act,

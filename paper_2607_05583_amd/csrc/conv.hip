@@ -59,10 +59,10 @@ template <typename T, int KX, bool EXACT, int V, int ACT, bool WHOLE>
 __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int64_t nb) {
   constexpr int U = 8, KB = KX - 1;  // steps loaded together, while those before them are computed
   const uint32_t id = blockIdx.x * CONV_THREADS + threadIdx.x, DV = (uint32_t)((a.D + V - 1) / V);
-  const uint32_t tiles = (uint32_t)((a.L + CONV_TILE - 1) / CONV_TILE) + (a.L == 0);
+  const uint32_t tiles = (uint32_t)((a.L + a.tile - 1) >> a.shift) + (a.L == 0);
   const uint32_t cv = id % DV, rest = id / DV, tile = rest % tiles;
   if (rest / tiles >= (uint64_t)nb) return;
-  const int64_t b = a.b0 + rest / tiles, d = (int64_t)cv * V, t0 = (int64_t)tile * CONV_TILE;
+  const int64_t b = a.b0 + rest / tiles, d = (int64_t)cv * V, t0 = (int64_t)tile << a.shift;
   const int nd = (int)(a.D - d < V ? a.D - d : V), K = EXACT ? KX : a.K;
   int64_t n = a.L;
   if (a.lengths != nullptr) {
@@ -77,8 +77,8 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int6
     else
       load_row<T, V, WHOLE>(st != nullptr && t >= 1 - K, st + (t + K - 1) * a.D, nd, q);
   };
-  const int in = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_TILE ? n - t0 : CONV_TILE);         // the tile's steps
-  const int end = (int)(a.L - t0 < CONV_TILE ? a.L - t0 : CONV_TILE);                     // its rows
+  const int in = (int)(n - t0 < 0 ? 0 : n - t0 < a.tile ? n - t0 : a.tile);         // the tile's steps
+  const int end = (int)(a.L - t0 < a.tile ? a.L - t0 : a.tile);                     // its rows
   const T* xt = x + t0 * a.x.st;
   const uint32_t sx = (uint32_t)a.x.st, sy = (uint32_t)a.D;  // (within a tile offsets have 32 bits)
   T q[U][V];
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
   const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
   const uint32_t bd = blockIdx.x % blocks_d;
   const int64_t by = a.b0 + blockIdx.x / blocks_d;  // (b0: the launch's first block of rows)
-  const int64_t tiles = (a.L + CONV_BWD_TILE - 1) / CONV_BWD_TILE + (a.L == 0);
+  const int64_t tiles = ((a.L + a.tile - 1) >> a.shift) + (a.L == 0);
   const int64_t d = (int64_t)bd * CW + lane * V;
   const int nd = (int)(d >= a.D ? 0 : a.D - d < V ? a.D - d : V), K = EXACT ? KX : a.K;
   float w[KX][V], bias[V], dw[KX][V], db[V];
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
     for (int k = 0; k < KX; ++k) dw[k][e] = 0.0f;
   }
   for (int r = sub; r < CONV_BWD_ROWS; r += RB) {
-    const int64_t row = by * CONV_BWD_ROWS + r, b = row / tiles, t0 = row % tiles * CONV_BWD_TILE;
+    const int64_t row = by * CONV_BWD_ROWS + r, b = row / tiles, t0 = (row % tiles) << a.shift;
     if (nd == 0 || b >= a.B) continue;
     int64_t n = a.L;
     if (a.lengths != nullptr) {
@@ -155,9 +155,9 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_bwd_kernel(ConvArgs a, uint
       n = n < 0 ? 0 : n > a.L ? a.L : n;
     }
     // the tile's steps, its rows, and the steps that are there behind it
-    const int in = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_BWD_TILE ? n - t0 : CONV_BWD_TILE);
-    const int held = (int)(a.L - t0 < CONV_BWD_TILE ? a.L - t0 : CONV_BWD_TILE);
-    const int seen = (int)(n - t0 < 0 ? 0 : n - t0 < CONV_BWD_TILE + K - 1 ? n - t0 : CONV_BWD_TILE + K - 1);
+    const int in = (int)(n - t0 < 0 ? 0 : n - t0 < a.tile ? n - t0 : a.tile);
+    const int held = (int)(a.L - t0 < a.tile ? a.L - t0 : a.tile);
+    const int seen = (int)(n - t0 < 0 ? 0 : n - t0 < a.tile + K - 1 ? n - t0 : a.tile + K - 1);
     const T* x = static_cast<const T*>(a.x.p) + b * a.x.sb + t0 * a.x.st + d;
     const T* dy = static_cast<const T*>(a.dy.p) + b * a.dy.sb + t0 * a.dy.st + d;
     T* dx = static_cast<T*>(a.dx.p) + b * a.dx.sb + t0 * a.dx.st + d;
@@ -360,6 +360,8 @@ auto by_taps(int K, F&& f) {
 // other's latency.  65536 steps of 640 channels, bf16: forward 50 us (3.4 TB/s; with four channels 55), backward 55 us
 // (4.5 TB/s).
 constexpr int CONV_VEC = 2;
+// Steps of a thread: many read few inputs twice and make few partial sums; with too few threads for the chip a thread's chain of loads
+// is the call's time.  5 x 2001 steps of 203 channels, float32: 32 forward and 64 backward 13 and 29 us, 8 and 8 take 8 and 11 us.
 
 // F with the taps, whether the activation is silu, and whether D is whole vectors, as constants.
 template <typename F>
@@ -381,9 +383,12 @@ hipError_t by_kind(const ConvArgs& a, F&& f) {
 
 template <typename T>
 hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st) {
+  const int64_t threads = a.B * ((a.D + CONV_VEC - 1) / CONV_VEC);
+  a.shift = conv_shift(CONV_SHIFT, a.L, [&](int64_t tiles) { return threads * tiles / CONV_THREADS; });
+  a.tile = 1 << a.shift;
   return by_kind(a, [&](auto kx, auto exact, auto act, auto whole) {
     constexpr int V = CONV_VEC;
-    const int64_t tiles = (a.L + CONV_TILE - 1) / CONV_TILE + (a.L == 0);
+    const int64_t tiles = conv_tiles(a.L, a.shift);
     return by_rows(a.B, tiles * ((a.D + V - 1) / V), [&](int64_t b0, int64_t nb, uint32_t grid) {
       a.b0 = b0;
       conv_fwd_kernel<T, kx, exact, V, act, whole><<<grid, CONV_THREADS, 0, st>>>(a, nb);
@@ -402,13 +407,16 @@ hipError_t launch_conv_step(ConvArgs a, hipStream_t st) {
 }
 template <typename T>
 hipError_t launch_conv_bwd(const ConvArgs& a, hipStream_t st) {
-  const int64_t rows = conv_row_blocks(a.B, a.L);
+  const int shift = conv_bwd_shift(a.B, a.L, a.D);
+  const int64_t rows = conv_row_blocks(a.B, a.L, shift);
   const uint32_t bd = (uint32_t)((a.D + CONV_BWD_CHANNELS - 1) / CONV_BWD_CHANNELS);
   const hipError_t e = by_kind(a, [&](auto kx, auto exact, auto act, auto whole) {
     const int64_t most = LAUNCH_THREADS / CONV_THREADS / bd;
     for (int64_t r0 = 0; r0 < rows; r0 += most) {
       ConvArgs c = a;
       c.b0 = r0;
+      c.shift = shift;
+      c.tile = 1 << shift;
       const int64_t n = rows - r0 < most ? rows - r0 : most;
       conv_bwd_kernel<T, kx, exact, CONV_VEC, act, whole><<<(uint32_t)(n * bd), CONV_THREADS, 0, st>>>(c, bd);
       const hipError_t e = hipGetLastError();

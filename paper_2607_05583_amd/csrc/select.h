@@ -41,8 +41,10 @@ __device__ __forceinline__ void store_part(T* p, int n, const T (&v)[V]) {
 // ---------------------------------------------------------------------------
 constexpr int CONV_TAPS = 16;       // taps at most
 constexpr int CONV_THREADS = 256;
-constexpr int CONV_TILE = 32;       // steps of a thread, forward
-constexpr int CONV_BWD_TILE = 64;   // and backward
+constexpr int CONV_SHIFT = 5;       // steps of a thread at most: 32 forward
+constexpr int CONV_BWD_SHIFT = 6;   // and 64 backward
+constexpr int CONV_LEAST = 3;       // 8 at least
+constexpr int CONV_ENOUGH = 512;    // work-groups that are enough for the chip: with fewer, threads take fewer steps
 constexpr int CONV_BWD_ROWS = 4;    // tiles of a work-group of the backward, whose weight gradients are summed in it
 constexpr int CONV_BWD_CHANNELS = 128;
 
@@ -61,9 +63,18 @@ struct ConvArgs {
   float *dw, *dbias;
   int64_t B, L, D, b0;   // b0: the launch's first batch row
   int K, act;
+  int tile, shift;       // steps of a thread, and their binary logarithm
 };
-inline int64_t conv_row_blocks(int64_t B, int64_t L) {
-  return (B * ((L + CONV_BWD_TILE - 1) / CONV_BWD_TILE + (L == 0)) + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS;
+inline int64_t conv_tiles(int64_t L, int shift) { return ((L + (1 << shift) - 1) >> shift) + (L == 0); }
+template <typename F> int conv_shift(int most, int64_t L, F&& work_groups) {
+  int shift = most;
+  while (shift > CONV_LEAST && work_groups(conv_tiles(L, shift)) < CONV_ENOUGH) --shift;
+  return shift;
+}
+inline int64_t conv_row_blocks(int64_t B, int64_t L, int shift) { return (B * conv_tiles(L, shift) + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS; }
+inline int conv_bwd_shift(int64_t B, int64_t L, int64_t D) {
+  const int64_t across = (D + CONV_BWD_CHANNELS - 1) / CONV_BWD_CHANNELS;
+  return conv_shift(CONV_BWD_SHIFT, L, [&](int64_t tiles) { return (B * tiles + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS * across; });
 }
 template <typename T> hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st);
 template <typename T> hipError_t launch_conv_bwd(const ConvArgs& a, hipStream_t st);

@@ -64,13 +64,24 @@ class Conv:
         return y, last, g
 
 
-# vectors that end inside, tiles of 32 and 64 steps that end inside, steps fewer than taps, every constant number of taps and others
+# vectors that end inside, tiles of steps that end inside, steps fewer than taps, every constant number of taps and others
 @pytest.mark.parametrize("dt", ACTS)
 @pytest.mark.parametrize("sizes", [(1, 1, 1, 1), (2, 1, 5, 4), (1, 2, 8, 4), (2, 33, 16, 4), (3, 65, 17, 3), (1, 200, 130, 4), (2, 100, 64, 2),
                                    (1, 70, 40, 7), (2, 130, 9, 16), (1, 64, 3, 5), (2, 31, 12, 1), (9, 70, 24, 4), (1, 10, 6, 16)])
 def test_forward_and_backward(sizes, dt):
     say(f"conv {dt} {sizes}")
     Conv(dt, *sizes, seed=sum(sizes)).check(pad=sum(sizes) % 4)
+
+
+# calls that fill the chip, whose threads take more steps: forward 8, 32, 16 and 8 of them, backward 64, 32, 32 and 16
+@pytest.mark.parametrize("dt", ACTS)
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("sizes", [(700, 150, 3, 16), (150, 700, 90, 4), (100, 700, 90, 3), (60, 700, 90, 2)])
+def test_large_calls(sizes, ragged, dt):
+    say(f"conv {dt} {sizes} ragged {ragged}")
+    B, L = sizes[:2]
+    lengths = [int(v) for v in np.random.default_rng(7).integers(0, L + 1, B)] if ragged else None
+    Conv(dt, *sizes, lengths=lengths, seed=sum(sizes)).check(pad=2)
 
 
 @pytest.mark.parametrize("dt", ACTS)
