@@ -43,7 +43,7 @@ constexpr int CONV_TAPS = 16;       // taps at most
 constexpr int CONV_THREADS = 256;
 constexpr int CONV_SHIFT = 5;       // steps of a thread at most: 32 forward
 constexpr int CONV_BWD_SHIFT = 6;   // and 64 backward
-constexpr int CONV_LEAST = 3;       // 8 at least
+constexpr int CONV_LEAST = 3;       // 8 at least (forward: 16 with more than nine taps)
 constexpr int CONV_ENOUGH = 512;    // work-groups that are enough for the chip: with fewer, threads take fewer steps
 constexpr int CONV_BWD_ROWS = 4;    // tiles of a work-group of the backward, whose weight gradients are summed in it
 constexpr int CONV_BWD_CHANNELS = 128;
@@ -66,15 +66,23 @@ struct ConvArgs {
   int tile, shift;       // steps of a thread, and their binary logarithm
 };
 inline int64_t conv_tiles(int64_t L, int shift) { return ((L + (1 << shift) - 1) >> shift) + (L == 0); }
-template <typename F> int conv_shift(int most, int64_t L, F&& work_groups) {
+// A forward tile has K - 1 steps at least: no tile but the first needs an input before the call.  That is in the state, which the first
+// tile's threads may overwrite at any time (state_out may be the state).
+inline int conv_least(int K) {
+  int shift = CONV_LEAST;
+  while (1 << shift < K - 1) ++shift;
+  return shift;
+}
+static_assert(CONV_TAPS - 1 <= 1 << CONV_SHIFT, "a tile of the most steps reaches over the taps");
+template <typename F> int conv_shift(int most, int least, int64_t L, F&& work_groups) {
   int shift = most;
-  while (shift > CONV_LEAST && work_groups(conv_tiles(L, shift)) < CONV_ENOUGH) --shift;
+  while (shift > least && work_groups(conv_tiles(L, shift)) < CONV_ENOUGH) --shift;
   return shift;
 }
 inline int64_t conv_row_blocks(int64_t B, int64_t L, int shift) { return (B * conv_tiles(L, shift) + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS; }
 inline int conv_bwd_shift(int64_t B, int64_t L, int64_t D) {
   const int64_t across = (D + CONV_BWD_CHANNELS - 1) / CONV_BWD_CHANNELS;
-  return conv_shift(CONV_BWD_SHIFT, L, [&](int64_t tiles) { return (B * tiles + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS * across; });
+  return conv_shift(CONV_BWD_SHIFT, CONV_LEAST, L, [&](int64_t tiles) { return (B * tiles + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS * across; });
 }
 template <typename T> hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st);
 template <typename T> hipError_t launch_conv_bwd(const ConvArgs& a, hipStream_t st);
