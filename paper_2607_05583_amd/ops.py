@@ -2045,7 +2045,8 @@ class SelectiveLayerFunction(torch.autograd.Function):
         g = resonator_selective_layer_bwd(x, p, dout, saved, ctx.groups, state=SelectiveState(first, h0) if ctx.started else None,
                                           lengths=lengths, dstate=SelectiveState(*(None if t is None else t.contiguous() for t in (dlast, dh))),
                                           act=ctx.act, want_dstate=want)
-        back = g["dstate"] if want else (None, None)
+        # (a part that was not given has no gradient)
+        back = (t if n else None for t, n in zip(g["dstate"], ctx.needs_input_grad[1:3])) if want else (None, None)
         return g["dx"], *back, None, None, None, *g["dp"]
 
 
