@@ -1954,9 +1954,9 @@ class SelectiveState(NamedTuple):
 def resonator_selective_layer_fwd(x, p, groups=1, state=None, lengths=None, act="gelu_tanh", return_state=False, save=False, ws=None):
     """A selective layer: of u = x Wp + bp, v = silu(short convolution of u's first C columns), y = selective scan of v's columns
     with steps from u's last H, z = x + y Wo + bo, out = z + act(z W1 + b1) W2 + b2.  x [B, L, d]; ``p`` a
-    SelectiveLayerParams; ``state`` a SelectiveState (None: nothing came before).  The lengths are the convolution's and the
-    scan's alone, as in resonator_gated_layer_fwd.  Returns out; with ``return_state`` also the SelectiveState behind each
-    row's last step, from which resonator_selective_layer_step goes on; with ``save`` also the dict for
+    SelectiveLayerParams; ``state`` a SelectiveState (None, or None for one of its parts: nothing came before).  The lengths are
+    the convolution's and the scan's alone, as in resonator_gated_layer_fwd.  Returns out; with ``return_state`` also the
+    SelectiveState behind each row's last step, from which resonator_selective_layer_step goes on; with ``save`` also the dict for
     resonator_selective_layer_bwd."""
     C = p.w.shape[0]
     first, h0 = (None, None) if state is None else state
@@ -2023,10 +2023,8 @@ class SelectiveLayerFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, first, h0, lengths, groups, act, *p):
         p = SelectiveLayerParams(*p)
-        ctx.started = first is not None
-        state = SelectiveState(first, h0) if ctx.started else None
-        out, last, saved = resonator_selective_layer_fwd(x, p, groups, state=state, lengths=lengths, act=act, return_state=True,
-                                                         save=True)
+        out, last, saved = resonator_selective_layer_fwd(x, p, groups, state=SelectiveState(first, h0), lengths=lengths, act=act,
+                                                         return_state=True, save=True)
         pre = saved.pop("pre")
         ctx.names, ctx.act, ctx.groups = tuple(saved), act, groups
         ctx.save_for_backward(x, first, h0, lengths, pre.pre, *p, *saved.values())
@@ -2041,9 +2039,9 @@ class SelectiveLayerFunction(torch.autograd.Function):
         p, saved = SelectiveLayerParams(*rest[:n]), dict(zip(ctx.names, rest[n:]))
         saved["pre"] = LinearSaved(pre, p.b1)
         dout = torch.zeros_like(x, memory_format=torch.contiguous_format) if dout is None else dout.contiguous()
-        want = ctx.started and (ctx.needs_input_grad[1] or ctx.needs_input_grad[2])
-        g = resonator_selective_layer_bwd(x, p, dout, saved, ctx.groups, state=SelectiveState(first, h0) if ctx.started else None,
-                                          lengths=lengths, dstate=SelectiveState(*(None if t is None else t.contiguous() for t in (dlast, dh))),
+        want = ctx.needs_input_grad[1] or ctx.needs_input_grad[2]
+        g = resonator_selective_layer_bwd(x, p, dout, saved, ctx.groups, state=SelectiveState(first, h0), lengths=lengths,
+                                          dstate=SelectiveState(*(None if t is None else t.contiguous() for t in (dlast, dh))),
                                           act=ctx.act, want_dstate=want)
         # (a part that was not given has no gradient)
         back = (t if n else None for t, n in zip(g["dstate"], ctx.needs_input_grad[1:3])) if want else (None, None)

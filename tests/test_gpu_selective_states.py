@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("act", ["bf16", "f32"])
-@pytest.mark.parametrize("given", [(True, False)])
+@pytest.mark.parametrize("given", [(True, False), (False, True)])
 def test_part_of_a_state(given, act):
     """What is not given is zero: the same bits forward, and the same gradients of all that is given."""
     say(f"selective layer, state {given} {act}")

@@ -86,7 +86,7 @@ def problem():
     return t(2, 5, 3), p, t(2, 2, 8), t(2, 2, 2, 2)
 
 
-GIVEN = [(True, True), (True, False), (False, False)]
+GIVEN = [(True, True), (True, False), (False, True), (False, False)]
 
 
 @pytest.mark.parametrize("given", GIVEN)
@@ -120,3 +120,16 @@ def test_gradients_go_to_what_is_given(given, leaf):
             t += 1e-6 * v
         want, size = (above - below) / 2e-6, (g.abs() * v.abs()).sum().item() + abs(above)
         assert abs((g * v).sum().item() - want) <= 1e-8 * size
+
+
+@pytest.mark.parametrize("train", ["x", "state", "all"])
+def test_state_without_a_convolution(train):
+    """(None, h0): the same output as the form without gradients, which is not the one without a state."""
+    x, p, _, h0 = problem()
+    want, last = ops.resonator_selective_layer(x, p, state=ops.SelectiveState(None, h0))
+    none, _ = ops.resonator_selective_layer(x, p)
+    assert not torch.equal(want, none)
+    x.requires_grad_(train != "state")
+    h0.requires_grad_(train != "x")
+    out, end = ops.resonator_selective_layer(x, p, state=ops.SelectiveState(None, h0))
+    assert out.requires_grad and torch.equal(out, want) and torch.equal(end.conv, last.conv) and torch.equal(end.h, last.h)
