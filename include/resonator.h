@@ -693,7 +693,8 @@ int resonator_short_conv_fwd(res_rows_t x, res_dtype_t dt, const float* w, const
  *   dx_s = sum_k w[k] dpre_{s+k} (+ dstate_out's),  dw[k] = sum dpre_t x_{t-k},  dbias = sum dpre
  *   dx         rows of dt, overwritten (0 behind a row's length); dw [D][K], dbias [D] (or NULL) float32
  *   dstate_out [B][K - 1][D] of dt or NULL (zero); dstate [B][K - 1][D] of dt or NULL
- *   ws         resonator_short_conv_workspace_bytes(B, L, D, K) bytes, 256-byte aligned
+ *   ws         resonator_short_conv_workspace_bytes(B, L, D, K) bytes, 256-byte aligned; one of the largest sizes
+ *              serves every smaller call (the bytes never fall where a size grows)
  * Sums run in a fixed order: calls on the same inputs are bitwise reproducible.
  */
 size_t resonator_short_conv_workspace_bytes(int64_t B, int64_t L, int64_t D, int64_t K);

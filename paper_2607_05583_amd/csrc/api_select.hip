@@ -98,7 +98,7 @@ int resonator_short_conv_fwd(res_rows_t x, res_dtype_t dt, const float* w, const
 
 size_t resonator_short_conv_workspace_bytes(int64_t B, int64_t L, int64_t D, int64_t K) {
   if (check_conv(B, L, D, K, RES_F32, RES_ACT_NONE)) return 0;
-  return up256((size_t)(conv_row_blocks(B, L, conv_bwd_shift(B, L, D)) * (K + 1) * D) * 4);
+  return up256((size_t)conv_part_floats(B, L, D, K) * 4);
 }
 
 int resonator_short_conv_bwd(res_rows_t x, res_rows_t dy, res_dtype_t dt, const float* w, const float* bias, int act,

@@ -3,6 +3,8 @@
 // probabilities (logprobs.hip), between their C entry points (api_select.hip) and the kernels.
 #pragma once
 
+#include <algorithm>
+
 #include "layer.h"
 
 namespace res {
@@ -83,6 +85,13 @@ inline int64_t conv_row_blocks(int64_t B, int64_t L, int shift) { return (B * co
 inline int conv_bwd_shift(int64_t B, int64_t L, int64_t D) {
   const int64_t across = (D + CONV_BWD_CHANNELS - 1) / CONV_BWD_CHANNELS;
   return conv_shift(CONV_BWD_SHIFT, CONV_LEAST, L, [&](int64_t tiles) { return (B * tiles + CONV_BWD_ROWS - 1) / CONV_BWD_ROWS * across; });
+}
+// Floats of the sums of all blocks, of the largest call of up to these sizes.  A call with CONV_ENOUGH work-groups of the most steps has
+// as many blocks as these make.  Any other takes half the steps only while the work-groups were fewer than CONV_ENOUGH, so that it has
+// fewer than 2 CONV_ENOUGH work-groups of CONV_BWD_CHANNELS channels each, and no more blocks than tiles of the least steps make.
+inline int64_t conv_part_floats(int64_t B, int64_t L, int64_t D, int64_t K) {
+  const int64_t most = 2 * (CONV_ENOUGH - 1) * CONV_BWD_CHANNELS;
+  return (K + 1) * std::max(conv_row_blocks(B, L, CONV_BWD_SHIFT) * D, std::min(conv_row_blocks(B, L, CONV_LEAST) * D, most));
 }
 template <typename T> hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st);
 template <typename T> hipError_t launch_conv_bwd(const ConvArgs& a, hipStream_t st);

@@ -1647,7 +1647,8 @@ def resonator_short_conv_bwd(x, w, dy, bias=None, act="silu", state=None, length
                              out=None, ws=None):
     """Gradients of sum(dy y) + sum(dstate_out state_out): dict with dx, dw, dbias (, dstate).  dy: [B, L, D] like x;
     ``dstate_out`` [B, K - 1, D]: the gradient of the state that the forward returned.  ``out`` receives dx (it may be
-    columns of a wider tensor)."""
+    columns of a wider tensor); ``ws``: a workspace of resonator_short_conv_workspace_bytes for these or larger sizes, else one
+    is made for the call."""
     code = _act_code(act)
     done = (_NATIVE or _native()).short_conv_bwd(x, w, dy, bias, code, state, lengths, dstate_out, want_dstate, out, ws)
     if done is not None:
