@@ -104,7 +104,7 @@ template <typename T> hipError_t launch_conv_step(ConvArgs a, hipStream_t st);
 // ---------------------------------------------------------------------------
 constexpr int SEL_Q = 64, SEL_P = 64, SEL_THREADS = 256;
 constexpr int SEL_MAX = 128;   // P and N at most
-constexpr int SEL_BWD_HEADS = 8;  // row blocks of a work-group of the backward at most
+constexpr int SEL_BWD_HEADS = 4;  // row blocks of a work-group of the backward at most
 
 struct SelPlan {
   int NT;            // tiles of 16 states, padded: 2, 4 or 8

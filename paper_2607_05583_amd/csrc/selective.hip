@@ -1384,8 +1384,9 @@ SelPlan sel_plan(bool bf16, int64_t B, int64_t L, int64_t H, int64_t P, int64_t 
   p.HG = (int)(H / G * p.PB);
   p.HF = p.NT > 4 ? 2 : 4;
   // row blocks of a group that a backward work-group has: more sum more of db and dc in registers and read b and c less often, fewer
-  // keep more work-groups (8 x 8192, 8 heads of 64 x 64, bf16, a training step: 2, 4 and 8 took 521, 487 and 577 us)
-  p.HR = 4;
+  // keep more work-groups (8 x 8192, 8 heads of 64 x 64, bf16, a training step: 2, 4 and 8 took 521, 487 and 577 us).
+  // The workspace counts the states of as many.
+  p.HR = p.HG < SEL_BWD_HEADS ? p.HG : SEL_BWD_HEADS;
   p.chunks = (L + SEL_Q - 1) / SEL_Q;
   // segments: work-groups of the forward for two on each CU; a chunk at least.  (Half of that, it, twice that: the training step above
   // 656, 487 and 525 us, a forward of 4 x 32768 with 128 states 431, 295 and 330.  One row of 777 steps, 32 heads of 64 x 128: at

@@ -20,3 +20,23 @@ def test_conv_workspace_serves_smaller_calls(D, K):
     for T in (1, 300, 6528, 8192):
         for wider in ([conv(B, T, D, K) for B in range(1, 200)], [conv(3, T, d, K) for d in range(D, D + 300)], [conv(3, T, D, k) for k in range(1, 17)]):
             assert wider == sorted(wider), (T, D, K)
+
+
+def scan_kept(act, B, T, H, P, G, N):
+    """Bytes of the states that a backward has to keep: before every chunk of 64 steps, and two for each segment (the gradient that leaves
+    it and the one that goes through its chunks), in rows of 64 channels and 32, 64 or 128 states."""
+    state = 64 * (32 if N <= 32 else 64 if N <= 64 else 128) * 4
+    rows = B * H * -(-P // 64)
+    floats = L.lib().resonator_selective_scan_carry_floats(act, B, T, H, P, G, N)
+    segments = max(1, 4 * floats // (rows * state))
+    chunks = segments * -(-(-(-T // 64)) // segments)  # (of whole segments)
+    return rows * state * (chunks + segments + (segments if segments > 1 else 0)), rows * segments * 4 * 4
+
+
+@pytest.mark.parametrize("act", [L.RES_F32, L.RES_BF16])
+@pytest.mark.parametrize("sizes", [(8, 8192, 32, 64, 32, 64), (2, 8192, 6, 40, 2, 128), (1, 777, 4, 128, 4, 100), (4, 1024, 16, 64, 8, 50)])
+def test_scan_workspace_of_few_heads_a_group(sizes, act):
+    """One to three rows of 64 channels a group: the states are counted for these alone."""
+    kept, sums = scan_kept(act, *sizes)
+    n = L.lib().resonator_selective_scan_workspace_bytes(1, act, *sizes)
+    assert kept + sums <= n <= kept + sums + 6 * 256, (n / kept, sizes)
