@@ -215,7 +215,7 @@ size_t lay_out(const Sizes& z, bool backward, bool carry, char* base, SelArgs* a
     return off;
   }
   a->leave = border;
-  const size_t wgs = (size_t)(z.B * p.segs * z.G * ((p.HG + p.HR - 1) / p.HR)), state = (size_t)p.HR * 4 * ((p.NT + 3) / 4) * 4 * 64 * 16;
+  const size_t wgs = (size_t)(z.B * p.segs * z.G * ((p.HG + p.HR - 1) / p.HR)), state = (size_t)p.HR * SEL_P * 16 * p.NT * 4;
   a->hs = (f4*)take(wgs * (size_t)p.seg * state);
   a->gs = (f4*)take(wgs * state);
   const int64_t blocks = (p.HG + p.HR - 1) / p.HR;

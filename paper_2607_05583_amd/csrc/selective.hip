@@ -655,7 +655,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   typedef BwdLds<T, NT, WHOLE> Lds;
   typedef typename Lds::TB TB;
   typedef typename Lds::TX TX;
-  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL, STATE = 4 * NW * 4 * 64;  // (f4 of a state, of all waves)
+  constexpr int KS = NT / 2, NW = (NT + 3) / 4, SL = Lds::SL, STATE = NT * 4 * 64;  // (f4 of a state, of the waves that have tiles)
   extern __shared__ __align__(16) char raw[];
   Lds& l = *reinterpret_cast<Lds*>(raw);
   T *const bt = l.bc[0], *const ct = l.bc[1], *const xt = l.xd[0], *const dt = l.xd[1];
@@ -677,7 +677,7 @@ __global__ __launch_bounds__(SEL_THREADS, sizeof(T) == 2 && NT <= 4 ? 2 : 1) voi
   const int left = (int)(n - c0 * Q < (int64_t)active * Q ? n - c0 * Q : (int64_t)active * Q);  // steps of the segment (with active chunks)
   auto step_at = [&](int ci, int hd) { return ci * Q + lane < left ? to_f32(pt[(int64_t)(ci * Q) * sd + (uint32_t)lane * sd + hd]) : 0.0f; };
   const bool mine = w < NT;  // the wave has state tiles
-  // states of a work-group before its chunks, and their gradients: [chunk][head][wave][own tile][p tile][lane].  Before the first
+  // states of a work-group before its chunks, and their gradients: [chunk][head][own tile][wave][p tile][lane].  Before the first
   // chunk and behind the last they are those at the segment's borders, or the caller's, which are put here first.
   f4* const hs = a.hs + (int64_t)index * a.p.seg * a.p.HR * STATE + w * 256;
   f4* const gs = a.gs + (int64_t)index * a.p.HR * STATE + w * 256;

@@ -24,7 +24,8 @@ def test_convolution_of_shorter_rows_in_the_longest_ones_workspace():
 
 
 @pytest.mark.parametrize("act", ["bf16", "f32"])
-@pytest.mark.parametrize("sizes", [(2, 300, 6, 40, 2, 50), (2, 300, 3, 64, 3, 64), (1, 200, 2, 128, 2, 128), (1, 130, 5, 20, 5, 100), (2, 300, 10, 16, 1, 40)])
+@pytest.mark.parametrize("sizes", [(2, 300, 6, 40, 2, 50), (2, 300, 3, 64, 3, 64), (1, 200, 2, 128, 2, 128), (1, 130, 5, 20, 5, 100), (2, 300, 10, 16, 1, 40),
+                                   (2, 300, 6, 40, 2, 24), (1, 200, 3, 64, 3, 32), (2, 130, 1, 100, 1, 1), (1, 70, 9, 30, 1, 16)])
 def test_scan_of_few_heads_a_group_stays_in_its_workspace(sizes, act):
     """The backward with a workspace of just the bytes that it asks for: what lies around them is left alone."""
     say(f"scan backward {act} {sizes} in its own bytes")

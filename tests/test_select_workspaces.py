@@ -40,3 +40,12 @@ def test_scan_workspace_of_few_heads_a_group(sizes, act):
     kept, sums = scan_kept(act, *sizes)
     n = L.lib().resonator_selective_scan_workspace_bytes(1, act, *sizes)
     assert kept + sums <= n <= kept + sums + 6 * 256, (n / kept, sizes)
+
+
+@pytest.mark.parametrize("act", [L.RES_F32, L.RES_BF16])
+@pytest.mark.parametrize("sizes", [(8, 8192, 32, 64, 32, 16), (2, 4096, 8, 40, 2, 32), (5, 2001, 4, 64, 1, 24), (1, 300, 2, 100, 1, 1)])
+def test_scan_workspace_of_few_states(sizes, act):
+    """Up to 32 states are kept as 32."""
+    kept, sums = scan_kept(act, *sizes)
+    n = L.lib().resonator_selective_scan_workspace_bytes(1, act, *sizes)
+    assert kept + sums <= n <= kept + sums + 6 * 256, (n / kept, sizes)
