@@ -769,7 +769,7 @@ int resonator_selective_scan_step(res_rows_t x, res_rows_t dt, res_rows_t b, res
  *   logp = scale logits[token] - log sum_j exp(scale logits[j])
  *   entropy = -sum_j p_j log p_j   (a p_j of 0 adds nothing)
  *   the `top` likeliest tokens, likeliest first (equal logits: the lowest token first), and their log probabilities
- *   logits     R rows of V consecutive elements of dt, ld >= V elements apart; scale > 0
+ *   logits     R rows of V consecutive elements of dt, ld >= V elements apart; 0 < scale <= 2^127
  *   tokens     int64 [R]; below 0: an ignored position, whose logp is 0 and gives no gradient; V or more: logp is NaN
  *   logp [R] float32;  stats [R][2] float32 or NULL: the row's largest logit and log sum_j exp(scale (logit - largest)),
  *              for the backward;  entropy [R] float32 or NULL

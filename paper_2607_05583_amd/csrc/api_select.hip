@@ -1,6 +1,5 @@
 // C ABI of the selective layer's operators and of the token probabilities: argument checks and dispatch.
 // Declared in include/resonator.h.
-#include <cmath>
 #include <cstdint>
 
 #include "../../include/resonator.h"
@@ -401,7 +400,8 @@ int check_logprobs(const void* logits, int64_t ld, res_dtype_t dt, const int64_t
   if (R < 0 || V < 1 || ld < V)
     return api_error(RES_ERR_INVALID_ARG, "R must be >= 0, V >= 1 and ld >= V (got R=%lld V=%lld ld=%lld)", (long long)R, (long long)V,
                      (long long)ld);
-  if (!(scale > 0.0f) || !std::isfinite(scale)) return api_error(RES_ERR_INVALID_ARG, "scale must be positive and finite (got %g)", (double)scale);
+  // (the kernels take it times log2 e: the largest logit's difference from itself times an infinite one would be none)
+  if (!(scale > 0.0f) || !(scale <= 0x1p127f)) return api_error(RES_ERR_INVALID_ARG, "scale must be positive and at most 2^127 (got %g)", (double)scale);
   if (V > (1LL << 30) || ld > (1LL << 40) || R > (1LL << 31))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (R=%lld V=%lld ld=%lld)", (long long)R, (long long)V, (long long)ld);
   if ((rc = check_elt("logits", logits, R > 0, elt(dt))) || (rc = check_elt("tokens", tokens, R > 0, 8))) return rc;

@@ -2088,7 +2088,7 @@ def resonator_token_logprobs_fwd(logits, tokens, top=0, entropy=False, scale=1.0
 
     logits [..., V] float32 or bfloat16 (rows at one distance); tokens [...] int64, negative where a position is ignored
     (logp 0 and no gradient there; V or more gives NaN).  ``top``: how many of the likeliest tokens, at most 64, likeliest
-    first, equal logits by the lowest token.  ``scale`` > 0 is the inverse temperature.  A logit of -inf is a token that
+    first, equal logits by the lowest token.  ``scale`` > 0 (at most 2^127) is the inverse temperature.  A logit of -inf is a token that
     cannot come; a row of nothing else has log probabilities of -inf, entropy 0 and no gradient."""
     done = (_NATIVE or _native()).token_logprobs_fwd(logits, tokens, top, entropy, scale)
     if done is not None:
