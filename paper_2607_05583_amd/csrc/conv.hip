@@ -88,11 +88,11 @@ __global__ __launch_bounds__(CONV_THREADS) void conv_fwd_kernel(ConvArgs a, int6
 #pragma unroll
   for (int k = 0; k < KB; ++k) {
     T q[V] = {};
-    if ((in > 0 || tile == 0) && tap<KX, EXACT>(KB - k, K)) input(t0 - KB + k, q);  // (the K - 1 before: none of a later tile is the state's)
+    if ((in > 0 || tile == 0) && tap<KX, EXACT>(KB - k, K)) input(t0 - KB + k, q);  // (the K - 1 before)
     widen<T, V>(q, f[k]);
   }
-  // state_out may be the state: a thread has read its channels of it before it writes them, and the first tile's threads alone read it
-  // (a.tile >= K - 1).
+  // state_out may be the state: a thread has read its channels of it before it writes them, and then the first tile's threads alone
+  // read it (a.tile >= K - 1).
   if (tile == 0 && a.state_out != nullptr) {
     T last[KB > 0 ? KB : 1][V];
 #pragma unroll
@@ -386,7 +386,8 @@ hipError_t by_kind(const ConvArgs& a, F&& f) {
 template <typename T>
 hipError_t launch_conv_fwd(ConvArgs a, hipStream_t st) {
   const int64_t threads = a.B * ((a.D + CONV_VEC - 1) / CONV_VEC);
-  a.shift = conv_shift(CONV_SHIFT, conv_least(a.K), a.L, [&](int64_t tiles) { return threads * tiles / CONV_THREADS; });
+  const int least = a.state != nullptr && a.state_out == a.state ? conv_least(a.K) : CONV_LEAST;
+  a.shift = conv_shift(CONV_SHIFT, least, a.L, [&](int64_t tiles) { return threads * tiles / CONV_THREADS; });
   a.tile = 1 << a.shift;
   return by_kind(a, [&](auto kx, auto exact, auto act, auto whole) {
     constexpr int V = CONV_VEC;
