@@ -722,7 +722,7 @@ int resonator_short_conv_step(res_rows_t x, res_dtype_t dt, const float* w, cons
  *   carry                 resonator_selective_scan_carry_floats(...) floats or NULL: receives the states
  *                         that the backward starts from
  *   ws                    resonator_selective_scan_workspace_bytes(0, ...) bytes, 256-byte aligned; contents
- *                         need not be initialised
+ *                         need not be initialised (for these sizes alone: smaller ones may need more)
  * y may be NULL where h_out is and carry is not.  1 <= P, N <= 128, G divides H.  The state is float32; for bf16
  * the weights of the steps that act on each other within 64 steps are rounded to bf16 (2^-8 of a term, as y's own
  * rounding), states and what makes them are not.  A step's value that is not finite makes the other steps of its
@@ -749,7 +749,7 @@ int resonator_selective_scan_fwd(res_rows_t x, res_rows_t dt, res_rows_t b, res_
  *   carry                 the forward's of the same inputs (may be NULL where it has no floats)
  *   dgamma [H], ddt_bias, dskip [H] (or NULL), dh0 [B][H][P][N] (or NULL)  float32, overwritten
  *   ws                    resonator_selective_scan_workspace_bytes(1, ...)
- * Calls on the same inputs are bitwise reproducible.
+ * Calls on the same inputs are bitwise reproducible.  Values that are not finite act on their 64 steps as in the forward.
  */
 int resonator_selective_scan_bwd(res_rows_t x, res_rows_t dt, res_rows_t b, res_rows_t c, res_rows_t dy, res_dtype_t act_dt,
                                  const float* gamma, const float* dt_bias, const float* skip, const float* h0,

@@ -51,7 +51,8 @@ int check_conv(int64_t B, int64_t L, int64_t D, int64_t K, res_dtype_t dt, int a
   if (B < 1 || D < 1 || L < 0 || K < 1)
     return api_error(RES_ERR_INVALID_ARG, "B, D and K must be >= 1 and L >= 0 (got B=%lld L=%lld D=%lld K=%lld)", (long long)B,
                      (long long)L, (long long)D, (long long)K);
-  // (a row's threads fit one launch: 16 steps of two channels each at least)
+  // (A row's threads fit one launch, here counted with tiles of the most steps.  A call takes shorter ones only while its work-groups are
+  // fewer than CONV_ENOUGH, so that it has no more than twice as many.)
   if (K > CONV_TAPS || D > (1 << 21) || B > (1LL << 31) || L >= (1LL << 31) - 65536 || (L / (1 << CONV_SHIFT) + 1) * ((D + 1) / 2) >= (1LL << 31) ||
       B * (L / (1 << CONV_BWD_SHIFT) + 1) >= (1LL << 40))
     return api_error(RES_ERR_UNSUPPORTED, "sizes beyond the supported range (B=%lld L=%lld D=%lld K=%lld)", (long long)B,

@@ -632,7 +632,9 @@ __global__ __launch_bounds__(SEL_THREADS) void selective_join_kernel(SelArgs a) 
 // lanes (n, q) with p = 16 v + 4 q .. + 3, as their products with x and dy need them; du, which needs a row's states, takes
 // them through LDS.  What the next head needs is loaded to registers meanwhile.
 // 8 x 8192, 8 heads of 64 x 64, bf16: 300 us, of which the states' second making some 45 and their way through memory 30.  Vector
-// instructions bound it (half of all cycles, some 2000 of a wave for a head's chunk; the matrix unit a tenth), at two waves a SIMD.
+// instructions take half of all cycles (some 2000 of a wave for a head's chunk; the matrix unit a tenth), at two waves a SIMD with 37
+// registers spilled.  It writes 377 MB and reads 367 or more where inputs and outputs are 235: the rest are states, their gradients (a
+// head's goes to memory and back at every chunk), and db and dc of the blocks of heads.
 // ---------------------------------------------------------------------------
 template <typename T, int NT, bool WHOLE> struct BwdLds {
   static constexpr int SL = NT < 4 ? NT : 4, NS = 16 * SL;  // state tiles of a slice, which goes through LDS at once
@@ -1383,7 +1385,8 @@ SelPlan sel_plan(bool bf16, int64_t B, int64_t L, int64_t H, int64_t P, int64_t 
   p.HV = (int)(H * p.PB);
   p.HG = (int)(H / G * p.PB);
   p.HF = p.NT > 4 ? 2 : 4;
-  // row blocks of a group that a backward work-group has: more sum more of db and dc in registers and read b and c less often, fewer
+  // (HF and HR are by one size, a large call's; fewer were not measured where work-groups are fewer than CUs.)
+  // Row blocks of a group that a backward work-group has: more sum more of db and dc in registers and read b and c less often, fewer
   // keep more work-groups (8 x 8192, 8 heads of 64 x 64, bf16, a training step: 2, 4 and 8 took 521, 487 and 577 us).
   // The workspace counts the states of as many.
   p.HR = p.HG < SEL_BWD_HEADS ? p.HG : SEL_BWD_HEADS;

@@ -1763,7 +1763,8 @@ def _selective_inputs(x, dt, b, c, gamma, dt_bias, skip, dims):
 
 
 def selective_scan_workspace(act_dtype, B, L, H, P, G, N, device, backward=True):
-    """A workspace of the selective scan's calls of these sizes on one stream; ``backward`` False: of the forward alone."""
+    """A workspace of the selective scan's calls of these sizes on one stream (smaller ones may need a larger one); ``backward``
+    False: of the forward alone."""
     n = max(int(_lib.lib().resonator_selective_scan_workspace_bytes(k, _DT[act_dtype], B, L, H, P, G, N))
             for k in ((0, 1) if backward else (0,)))
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
@@ -1791,7 +1792,8 @@ def resonator_selective_scan_fwd(x, dt, b, c, gamma, dt_bias=None, skip=None, h0
     h0 [B, H, P, N] float32; ``lengths`` [B] int32: row b has its first lengths[b] steps (y is 0 behind them, the state
     stays, and what the inputs hold there does not matter).  Returns y; with ``return_state`` also the last state
     (written to ``h_out`` where given, which may be h0 itself); with ``save`` also what resonator_selective_scan_bwd
-    starts from.  ``ws``: a selective_scan_workspace, else one is made for the call."""
+    starts from.  ``ws``: a selective_scan_workspace, else one is made for the call.  A step's value that is not finite makes the
+    other steps of its 64 not finite too, earlier ones among them."""
     done = (_NATIVE or _native()).selective_scan_fwd(x, dt, b, c, gamma, dt_bias, skip, h0, lengths, return_state, save, out, ws,
                                                      h_out)
     if done is not None:
